@@ -329,6 +329,115 @@ int sjd_attention(int batch, int window, int n_heads, int n_kv_heads, int head_d
                   void *cuda_stream);
 
 /*
+ * A cache in 8 bits for serving (the paper has none): a pool of pages of SJD_KV_PAGE positions, all layers of a position range in one
+ * page, shared by sequences through a table of pages.  An entry is an e4m3 number times 2^e, one exponent e for each SJD_POOL_BLOCK
+ * positions of a head's keys or values (e is read as the nearest of -100 .. 100).  The sjd_pool functions write, read and manage it:
+ * sjd_pool_reserve gives a sequence the pages it is about to write, sjd_pool_append writes a window's keys and values (and applies the
+ * rotary positions), sjd_pool_attention attends them, sjd_pool_fork lets sequences share the pages of a common prompt (of an image's
+ * conditional streams, say), sjd_pool_free and sjd_pool_compact take pages back.  Everything is enqueued on the stream; nothing is
+ * decided on the host, so that all of it can be captured into a graph.
+ *   - What a kernel finds wrong with device data is reported in *status: a negative sjd_status is left there (the first one stays) until
+ *     the caller clears it.  Zero it once at the start.  What is at fault is left out (see the functions), nothing is read or written out
+ *     of range.  While *status is not 0, sjd_pool_reserve, _fork, _free and _compact change nothing.
+ *   - refs[page] counts the table entries that hold the page; a page with 0 is free.  Free pages are given lowest index first.
+ *   - Two calls that write the same pool, or of which one writes what the other reads, have to be ordered by the caller.
+ */
+#define SJD_POOL_BLOCK 16
+#define SJD_POOL_MAX_LIST 1024
+typedef struct {
+  void *pages;     /* device, e4m3 [n_pages][n_layers][K|V][n_kv_heads][SJD_KV_PAGE][head_dim], starts on 16 bytes    */
+  int8_t *exps;    /* device, [n_pages][n_layers][K|V][n_kv_heads][SJD_KV_PAGE / SJD_POOL_BLOCK], starts on 4 bytes   */
+  int32_t *table;  /* device, [n_seqs][pages_per_seq]: page of positions 64 i .. 64 i + 63 of a sequence, -1: none    */
+  int32_t *refs;   /* device, [n_pages]                                                                               */
+  int32_t *status; /* device, one word                                                                                */
+  int32_t n_pages, n_seqs, pages_per_seq, n_layers, n_kv_heads, head_dim; /* head_dim 64 or 128                       */
+} sjd_pool;
+
+/*
+ * Rotary positions with one to three axes (time, height and width of images and video; one axis: text).  A head has head_dim / 2
+ * pairs (i, i + head_dim / 2); axis a owns pairs[a] of them, sum(pairs) = head_dim / 2.  Pair i turns by the angle
+ * position[axis of i] * theta^(-2 f / rot), where
+ *   interleaved = 0: the pairs of an axis are neighbours (first those of axis 0);  1: pairs go round the axes, one each, an axis that has
+ *                    all of its pairs is passed over;
+ *   per_axis = 0: f = i, rot = head_dim;  1: f = number of the pair within its axis, rot = 2 pairs[axis] (each axis has all frequencies).
+ */
+typedef struct {
+  int32_t n_axes;
+  int32_t pairs[3];
+  int32_t interleaved, per_axis;
+  double theta; /* > 0 */
+} sjd_rope;
+
+/*
+ * Rotary step and append.  Row m = b * window + k of q [.][n_heads][head_dim], k and v [.][n_kv_heads][head_dim] (dtype SJD_F32 or
+ * SJD_BF16; rows are *_stride elements apart, even, and start on 8 resp. 4 bytes) is position in_pos[m] of sequence seqs[b] (null: b).
+ * The active rows of a sequence come first and are consecutive positions; the others have in_pos -1 and are left out.  k and q are
+ * rotated (rope null: neither is) by axis_pos [.][n_axes] (null: every axis by in_pos), cosine and sine in 64 bits rounded to 32, and
+ * products and sums in 32; q goes to q_out (q null: no queries; q_out may be q), k and v to layer `layer` of the pool.
+ * A block of 16 positions that gets new rows takes, for each head's keys and values, the smallest exponent that holds its rows
+ * up to the last new one in +-448 (0 if all are zero), and every entry is its value rounded to the nearest e4m3 number, ties to even; rows
+ * of the block before the new ones keep the value that they stood for, rows behind are left as they were and mean nothing.  So a window
+ * that is rolled back and written again leaves no trace but in entries that its exponent had rounded away.  Infinite and NaN
+ * entries are stored as NaN and do not count for the exponent.  The pages that are written must be the sequence's own (sjd_pool_reserve).
+ * status: BAD_ARG for positions that are not as above or have no page (the block is left out), seqs out of range or twice the same.
+ * Errors: BAD_ARG, UNSUPPORTED (head_dim, dtype), CUDA.
+ */
+int sjd_pool_append(const sjd_pool *pool, int layer, int batch, int window, int n_heads, int dtype, const void *q, int64_t q_stride,
+                    const void *k, int64_t k_stride, const void *v, int64_t v_stride, const int32_t *seqs, const int32_t *in_pos,
+                    const sjd_rope *rope, const int32_t *axis_pos, void *q_out, int64_t q_out_stride, void *cuda_stream);
+
+/*
+ * Attention over the pool: query row m = b * window + k (any window), at position in_pos[m] of sequence seqs[b] (null: b), sees the keys
+ * j <= in_pos[m]; with sliding > 0 of these only j > in_pos[m] - sliding and, as sinks, j < sinks:
+ *     out[m][h] = softmax_j(scale q[m][h] . K[j][h / (n_heads / n_kv_heads)]) V[j][...]      (scale 0: 1 / sqrt(head_dim))
+ * in_pos -1: a row that sees nothing, its output is zero.  q and out of dtype (fp32: about fp32 accuracy), rows *_stride elements apart,
+ * strides multiples of 4, starting on 16 (fp32) or 8 (bf16) bytes; out may not overlap q.  What rows behind a sequence or masked places
+ * hold (NaN included) does not matter; a visible NaN shows.  status: BAD_ARG for seqs or positions out of range (rows that see nothing)
+ * and for visible positions without a page (keys that are left out); DEVICE_TIMEOUT if a bounded wait ran out.
+ * ws: device scratch of sjd_pool_attention_workspace_bytes(...) bytes, 256-byte aligned, which the caller zeroes once; every call leaves
+ * it ready for the next one.  One call at a time on a workspace (captured graphs that may run at the same time have their own).
+ * Errors: BAD_ARG, UNSUPPORTED (head_dim, dtype, a device other than sm_100's), CAPACITY (ws too small), CUDA.
+ */
+size_t sjd_pool_attention_workspace_bytes(const sjd_pool *pool, int window, int n_heads);
+int sjd_pool_attention(const sjd_pool *pool, int layer, int batch, int window, int n_heads, int dtype, const void *q, int64_t q_stride,
+                       const int32_t *seqs, const int32_t *in_pos, int sliding, int sinks, float scale, void *out, int64_t out_stride,
+                       void *ws, size_t ws_bytes, void *cuda_stream);
+
+/*
+ * Pages for positions begin[i] .. end[i] - 1 of sequence seqs[i], i = 0 .. n - 1 (device int32 arrays, n <= SJD_POOL_MAX_LIST): absent
+ * pages are given; a page that other table entries hold as well is replaced by a page of its own, with a copy of its contents where
+ * positions before begin[i] lie in it, except that the last holder keeps it.  Claims count in the order of i, then of positions.
+ * Afterwards those positions may be written.  status: CAPACITY if there are too few free pages, BAD_ARG for sequences or positions out
+ * of range, or a sequence twice in the list; the call then changes nothing.
+ * ws: device scratch of sjd_pool_workspace_bytes(pool) bytes, 256-byte aligned, contents without meaning between calls.
+ * Errors: BAD_ARG, CAPACITY (ws too small, n too large), CUDA.
+ */
+size_t sjd_pool_workspace_bytes(const sjd_pool *pool);
+int sjd_pool_reserve(const sjd_pool *pool, int n, const int32_t *seqs, const int32_t *begin, const int32_t *end, void *ws,
+                     size_t ws_bytes, void *cuda_stream);
+
+/*
+ * Sequence dst[i] (which has to be empty) shares the pages of the first len[i] positions of sequence src[i].  No page is copied: see
+ * sjd_pool_reserve.  One source may have several children in a call.  status: BAD_ARG for sequences or lengths out of range, missing
+ * pages of a source, a dst that is not empty, is twice in the list or is also a source; the call then changes nothing.
+ * Errors: BAD_ARG, CAPACITY (n too large), CUDA.
+ */
+int sjd_pool_fork(const sjd_pool *pool, int n, const int32_t *src, const int32_t *dst, const int32_t *len, void *cuda_stream);
+
+/*
+ * Sequence seqs[i] gives back its pages behind the one of its first keep[i] positions (keep 0: all).  status: BAD_ARG for
+ * sequences out of range or twice in the list, negative keep; the call then changes nothing.
+ * Errors: BAD_ARG, CAPACITY (n too large), CUDA.
+ */
+int sjd_pool_free(const sjd_pool *pool, int n, const int32_t *seqs, const int32_t *keep, void *cuda_stream);
+
+/*
+ * Moves pages so that the pages in use are 0 .. count - 1: the pages in use from index count on move, in order, to the free indices
+ * below it; the tables follow.  ws: as sjd_pool_reserve.  Errors: BAD_ARG, CAPACITY (ws too small), CUDA.
+ */
+int sjd_pool_compact(const sjd_pool *pool, void *ws, size_t ws_bytes, void *cuda_stream);
+
+/*
  * Which kernels the steps of a pre-filled context run (the forward pass of Sec. 4.1 Step 2 has two
  * implementations: the tensor-core pipeline for bf16 models whose projection widths are multiples
  * of 128 with inner sizes that are multiples of 64, and generic FMA kernels, roughly 50 times slower

@@ -30,7 +30,10 @@ EXPORTS = ["sjd_workspace_bytes", "sjd_init", "sjd_prefill", "sjd_step", "sjd_ge
            "sjd_verify_workspace_bytes", "sjd_verify", "sjd_last_device_status", "sjd_last_cuda_error",
            "sjd_destroy", "sjd_strerror", "sjd_launch_count", "sjd_trace", "sjd_trace_read", "sjd_verify_static",
            "sjd_gemm_workspace_bytes", "sjd_gemm", "sjd_attention_workspace_bytes", "sjd_attention", "sjd_get_info",
-           "sjd_prefill_ragged", "sjd_get_tokens"]
+           "sjd_prefill_ragged", "sjd_get_tokens", "sjd_pool_append", "sjd_pool_attention_workspace_bytes",
+           "sjd_pool_attention", "sjd_pool_workspace_bytes", "sjd_pool_reserve", "sjd_pool_fork", "sjd_pool_free",
+           "sjd_pool_compact"]
+SJD_KV_PAGE, SJD_POOL_BLOCK, SJD_POOL_MAX_LIST = 64, 16, 1024
 
 
 class SJDError(RuntimeError):
@@ -73,6 +76,16 @@ class sjd_step_out(C.Structure):
 class sjd_info(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("tensor_core_projections", "tensor_core_attention", "step_graph",
                                          "rows_per_step")]
+
+
+class sjd_pool(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("pages", "exps", "table", "refs", "status")] + \
+               [(n, C.c_int32) for n in ("n_pages", "n_seqs", "pages_per_seq", "n_layers", "n_kv_heads", "head_dim")]
+
+
+class sjd_rope(C.Structure):
+    _fields_ = [("n_axes", C.c_int32), ("pairs", C.c_int32 * 3), ("interleaved", C.c_int32), ("per_axis", C.c_int32),
+                ("theta", C.c_double)]
 
 
 _lib = None
@@ -127,6 +140,25 @@ def lib():
     L.sjd_attention_workspace_bytes.argtypes = [C.c_int, C.c_int, C.c_int, C.c_int]
     L.sjd_attention.restype = C.c_int
     L.sjd_attention.argtypes = [C.c_int] * 6 + [C.c_void_p] * 5 + [C.c_size_t, C.c_void_p]
+    _pool, _i64 = C.POINTER(sjd_pool), C.c_int64
+    L.sjd_pool_append.restype = C.c_int
+    L.sjd_pool_append.argtypes = [_pool] + [C.c_int] * 5 + [C.c_void_p, _i64] * 3 + \
+        [C.c_void_p, C.c_void_p, C.POINTER(sjd_rope), C.c_void_p, C.c_void_p, _i64, C.c_void_p]
+    L.sjd_pool_attention_workspace_bytes.restype = C.c_size_t
+    L.sjd_pool_attention_workspace_bytes.argtypes = [_pool, C.c_int, C.c_int]
+    L.sjd_pool_attention.restype = C.c_int
+    L.sjd_pool_attention.argtypes = [_pool] + [C.c_int] * 5 + [C.c_void_p, _i64, C.c_void_p, C.c_void_p, C.c_int, C.c_int,
+                                                               C.c_float, C.c_void_p, _i64, C.c_void_p, C.c_size_t, C.c_void_p]
+    L.sjd_pool_workspace_bytes.restype = C.c_size_t
+    L.sjd_pool_workspace_bytes.argtypes = [_pool]
+    L.sjd_pool_reserve.restype = C.c_int
+    L.sjd_pool_reserve.argtypes = [_pool, C.c_int] + [C.c_void_p] * 4 + [C.c_size_t, C.c_void_p]
+    L.sjd_pool_fork.restype = C.c_int
+    L.sjd_pool_fork.argtypes = [_pool, C.c_int] + [C.c_void_p] * 4
+    L.sjd_pool_free.restype = C.c_int
+    L.sjd_pool_free.argtypes = [_pool, C.c_int] + [C.c_void_p] * 3
+    L.sjd_pool_compact.restype = C.c_int
+    L.sjd_pool_compact.argtypes = [_pool, C.c_void_p, C.c_size_t, C.c_void_p]
     L.sjd_get_info.restype = C.c_int
     L.sjd_get_info.argtypes = [C.c_void_p, C.POINTER(sjd_info)]
     L.sjd_last_device_status.restype = C.c_int
@@ -259,6 +291,171 @@ def sjd_attention(q, kv_cache, in_pos, window, n_kv_heads, out=None, ws=None):
     _check(lib().sjd_attention(b, window, h, n_kv_heads, hd, max_seq, _ptr(q), _ptr(kv_cache), _ptr(in_pos), _ptr(out),
                                _ptr(ws), nbytes, _stream()), "sjd_attention")
     return out, ws[:4].view(torch.int32)
+
+
+class CachePool:
+    """A paged cache in 8 bits (see sjd_pool in include/sjd.h) on borrowed torch tensors of one cuda device:
+
+      pages  float8_e4m3fn [n_pages][n_layers][2][n_kv_heads][64][head_dim]    exps  int8 [n_pages][n_layers][2][n_kv_heads][4]
+      table  int32 [n_seqs][pages_per_seq], -1: none                           refs  int32 [n_pages], table entries per page
+
+    `status` (int32 [1], zero at the start) keeps the first fault that a kernel found until `clear()`; `ws` and the workspaces
+    of attention() are the pool's own, so that calls on one pool follow one another (one stream, or ordered by the caller)."""
+
+    def __init__(self, pages, exps, table, refs):
+        n_pages, n_layers, two, n_kv_heads, rows, head_dim = pages.shape
+        want = (n_pages, n_layers, 2, n_kv_heads, SJD_KV_PAGE // SJD_POOL_BLOCK)
+        if two != 2 or rows != SJD_KV_PAGE or tuple(exps.shape) != want or tuple(refs.shape) != (n_pages,) or table.dim() != 2:
+            raise ValueError("shapes of a pool do not fit together")
+        for x, dt in ((pages, torch.float8_e4m3fn), (exps, torch.int8), (table, torch.int32), (refs, torch.int32)):
+            if x.dtype != dt or not x.is_contiguous() or x.device != pages.device:
+                raise ValueError("a pool's tensors are contiguous, on one device, of types e4m3, int8, int32 and int32")
+        self.pages, self.exps, self.table, self.refs = pages, exps, table, refs
+        self.device = pages.device
+        self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self.c = sjd_pool(pages.data_ptr(), exps.data_ptr(), table.data_ptr(), refs.data_ptr(), self.status.data_ptr(), n_pages,
+                          table.shape[0], table.shape[1], n_layers, n_kv_heads, head_dim)
+        self.ws_bytes = int(lib().sjd_pool_workspace_bytes(C.byref(self.c)))
+        if self.ws_bytes == 0:
+            raise SJDError(SJD_ERR_UNSUPPORTED, "sjd_pool_workspace_bytes")
+        self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.device)
+        self._attention_ws = torch.zeros(0, dtype=torch.uint8, device=self.device)
+
+    @classmethod
+    def empty(cls, n_pages, n_seqs, pages_per_seq, n_layers, n_kv_heads, head_dim, device="cuda"):
+        """A pool of its own tensors, no page in use."""
+        return cls(torch.zeros(n_pages, n_layers, 2, n_kv_heads, SJD_KV_PAGE, head_dim, dtype=torch.float8_e4m3fn, device=device),
+                   torch.zeros(n_pages, n_layers, 2, n_kv_heads, SJD_KV_PAGE // SJD_POOL_BLOCK, dtype=torch.int8, device=device),
+                   torch.full((n_seqs, pages_per_seq), -1, dtype=torch.int32, device=device),
+                   torch.zeros(n_pages, dtype=torch.int32, device=device))
+
+    def attention_ws(self, window: int, n_heads: int):
+        nbytes = int(lib().sjd_pool_attention_workspace_bytes(C.byref(self.c), window, n_heads))
+        if nbytes == 0:
+            raise SJDError(SJD_ERR_BAD_ARG, "sjd_pool_attention_workspace_bytes")
+        if self._attention_ws.numel() < nbytes:   # (zeroed once; every call leaves it ready for the next)
+            self._attention_ws = torch.zeros(nbytes, dtype=torch.uint8, device=self.device)
+        return self._attention_ws
+
+    def fault(self) -> int:
+        """The first fault that a kernel found since the start or clear() (an SJD_ERR_* value, 0: none).  Synchronises."""
+        return int(self.status.item())
+
+    def clear(self):
+        self.status.zero_()
+
+
+def make_rope_cfg(pairs, theta=10000.0, interleaved=False, per_axis=False) -> sjd_rope:
+    """pairs: pairs of each axis, one to three of them (they add up to head_dim / 2)."""
+    pairs = [int(x) for x in pairs]
+    if not 1 <= len(pairs) <= 3:
+        raise ValueError("one to three axes")
+    return sjd_rope(len(pairs), (C.c_int32 * 3)(*(pairs + [0] * (3 - len(pairs)))), int(bool(interleaved)), int(bool(per_axis)),
+                    float(theta))
+
+
+def _pool_rows(x, heads, pool, rows, where):
+    """Row stride of x [rows][heads][head_dim], whose rows may be parts of longer ones."""
+    hd = pool.c.head_dim
+    if x.dim() != 3 or tuple(x.shape) != (rows, heads, hd) or x.stride(2) != 1 or (heads > 1 and x.stride(1) != hd):
+        raise ValueError("%s: a tensor [%d][%d][%d] whose rows are contiguous" % (where, rows, heads, hd))
+    if x.device != pool.device:
+        raise ValueError("%s: on another device than the pool" % where)
+    return x.stride(0) if rows > 1 else max(x.stride(0), heads * hd)
+
+
+def _ints(x, n, pool, where):
+    if x is not None and (x.dtype != torch.int32 or not x.is_contiguous() or x.numel() != n or x.device != pool.device):
+        raise ValueError("%s: %d contiguous int32 entries on the pool's device" % (where, n))
+    return _ptr(x)
+
+
+def _pool_dtype(x, where):
+    if x.dtype not in (torch.float32, torch.bfloat16):
+        raise SJDError(SJD_ERR_UNSUPPORTED, where)
+    return SJD_F32 if x.dtype == torch.float32 else SJD_BF16
+
+
+def sjd_pool_append(pool: CachePool, layer: int, k, v, in_pos, window: int, q=None, q_out=None, rope: sjd_rope | None = None,
+                    axis_pos=None, seqs=None):
+    """Rotates q and k, appends k and v to the pool; returns the rotated q (q_out, which may be q; a new tensor if not given).
+    q [B*W][H][hd], k, v [B*W][KVh][hd] of one type, float32 or bfloat16, possibly parts of one matrix; in_pos int32 [B*W];
+    axis_pos int32 [B*W][n_axes]; seqs int32 [B] or None (sequence b is row b of the table)."""
+    m = in_pos.numel()
+    dtype = _pool_dtype(k, "sjd_pool_append")
+    if m % window != 0 or v.dtype != k.dtype or (q is not None and q.dtype != k.dtype):
+        raise ValueError("sjd_pool_append: whole windows, and q, k, v of one type")
+    kvh = pool.c.n_kv_heads
+    heads, qs, outs = 0, 0, 0
+    if q is not None:
+        heads = q.shape[1]
+        qs = _pool_rows(q, heads, pool, m, "q")
+        if q_out is None:
+            q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        if q_out.dtype != q.dtype:
+            raise ValueError("q_out: of q's type")
+        outs = _pool_rows(q_out, heads, pool, m, "q_out")
+    if axis_pos is not None and rope is None:
+        raise ValueError("axis_pos without rope")
+    with torch.cuda.device(pool.device):
+        _check(lib().sjd_pool_append(C.byref(pool.c), layer, m // window, window, heads, dtype, _ptr(q), qs, _ptr(k),
+                                     _pool_rows(k, kvh, pool, m, "k"), _ptr(v), _pool_rows(v, kvh, pool, m, "v"),
+                                     _ints(seqs, m // window, pool, "seqs"), _ints(in_pos, m, pool, "in_pos"),
+                                     C.byref(rope) if rope is not None else None,
+                                     _ints(axis_pos, m * (rope.n_axes if rope is not None else 0), pool, "axis_pos"), _ptr(q_out), outs,
+                                     _stream()), "sjd_pool_append")
+    return q_out
+
+
+def sjd_pool_attention(pool: CachePool, layer: int, q, in_pos, window: int, sliding=0, sinks=0, scale=0.0, out=None, ws=None, seqs=None):
+    """Attention of q [B*W][H][hd] (float32 or bfloat16) at positions in_pos over the pool; out of q's type.  ws: a zeroed workspace of
+    its own for calls that may run at the same time as others on the pool (default: the pool's)."""
+    m, heads = in_pos.numel(), q.shape[1]
+    dtype = _pool_dtype(q, "sjd_pool_attention")
+    if m % window != 0:
+        raise ValueError("sjd_pool_attention: whole windows")
+    if out is None:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    if out.dtype != q.dtype:
+        raise ValueError("out: of q's type")
+    with torch.cuda.device(pool.device):
+        if ws is None:
+            ws = pool.attention_ws(window, heads)
+        _check(lib().sjd_pool_attention(C.byref(pool.c), layer, m // window, window, heads, dtype, _ptr(q),
+                                        _pool_rows(q, heads, pool, m, "q"), _ints(seqs, m // window, pool, "seqs"),
+                                        _ints(in_pos, m, pool, "in_pos"), sliding, sinks, scale, _ptr(out),
+                                        _pool_rows(out, heads, pool, m, "out"), _ptr(ws), ws.numel(), _stream()), "sjd_pool_attention")
+    return out
+
+
+def sjd_pool_reserve(pool: CachePool, seqs, begin, end):
+    """Own pages for positions begin[i] .. end[i] - 1 of sequence seqs[i] (int32 cuda tensors)."""
+    n = seqs.numel()
+    with torch.cuda.device(pool.device):
+        _check(lib().sjd_pool_reserve(C.byref(pool.c), n, _ints(seqs, n, pool, "seqs"), _ints(begin, n, pool, "begin"),
+                                      _ints(end, n, pool, "end"), _ptr(pool.ws), pool.ws_bytes, _stream()), "sjd_pool_reserve")
+
+
+def sjd_pool_fork(pool: CachePool, src, dst, length):
+    """The empty sequence dst[i] shares the pages of the first length[i] positions of src[i] (int32 cuda tensors)."""
+    n = src.numel()
+    with torch.cuda.device(pool.device):
+        _check(lib().sjd_pool_fork(C.byref(pool.c), n, _ints(src, n, pool, "src"), _ints(dst, n, pool, "dst"),
+                                   _ints(length, n, pool, "length"), _stream()), "sjd_pool_fork")
+
+
+def sjd_pool_free(pool: CachePool, seqs, keep):
+    """Sequence seqs[i] gives back the pages behind its first keep[i] positions (int32 cuda tensors)."""
+    n = seqs.numel()
+    with torch.cuda.device(pool.device):
+        _check(lib().sjd_pool_free(C.byref(pool.c), n, _ints(seqs, n, pool, "seqs"), _ints(keep, n, pool, "keep"), _stream()),
+               "sjd_pool_free")
+
+
+def sjd_pool_compact(pool: CachePool):
+    """Moves pages so that those in use are the first ones of the pool."""
+    with torch.cuda.device(pool.device):
+        _check(lib().sjd_pool_compact(C.byref(pool.c), _ptr(pool.ws), pool.ws_bytes, _stream()), "sjd_pool_compact")
 
 
 class Context:

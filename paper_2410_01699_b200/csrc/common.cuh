@@ -409,4 +409,18 @@ int launch_attention_tc(const TensorMap &kv_map, int plane0, KvLayout kv, const 
                          float *out, HiLoOut hilo, int *status, int M, RowSegs segs, int n_heads, int n_kv_heads,
                          int head_dim, int splits, bool clear_status, cudaStream_t stream);
 
+// ---- 8-bit paged cache (pool.cu, pool_append.cu, pool_attention.cu)
+constexpr int kPoolBlock = SJD_POOL_BLOCK;
+constexpr int kPoolBlocks = KV_PAGE / SJD_POOL_BLOCK;
+int check_pool(const sjd_pool *p, bool with_refs);   // host-side checks of the fields
+// bytes of entries / of exponents of one page, all layers
+inline size_t pool_page_bytes(const sjd_pool &p) { return (size_t)p.n_layers * 2 * p.n_kv_heads * KV_PAGE * p.head_dim; }
+inline size_t pool_page_exps(const sjd_pool &p) { return (size_t)p.n_layers * 2 * p.n_kv_heads * kPoolBlocks; }
+#ifdef __CUDACC__
+__device__ __forceinline__ void pool_fault(int32_t *status, int code) { atomicCAS(status, 0, code); }
+// 2^e of a stored exponent
+__device__ __forceinline__ int pool_exp(int e) { return min(max(e, -100), 100); }
+__device__ __forceinline__ float two_to(int e) { return __int_as_float((e + 127) << 23); }   // -126 <= e <= 127
+#endif
+
 }  // namespace sjd
