@@ -1,29 +1,27 @@
 // Attention of window queries over the 8-bit paged cache, with an optional sliding window and sinks.
 //
-// Keys and values stay in 8 bits up to the tensor cores: mma.sync m16n8k32 multiplies e4m3 by e4m3 into 32 bits.  Queries and
-// probabilities are e4m3 numbers as well, but several of them: x = x1 + x2 (+ 2^-8 (x3 + x4)), x1 = e4m3(x), x2 = e4m3(x - x1) and
-// so on, each plane with its own product into the same sums.  The difference of a plane is exact, so n planes leave 2^-4n of an
-// entry at most (and about 2^-5.3n on average): two for bf16 queries, whose eight bits they hold exactly, four for fp32.  The products are exact in 32 bits.
-// (Rates measured here: e4m3 3850 products a clock and SM, f16 1016: two planes of each operand cost half of one f16 product and no
-// conversion of the cache, four as much as one.)
+// Keys and values stay in 8 bits up to the registers of the warp that multiplies them, where they become fp16 (which holds every e4m3
+// number) for mma.sync m16n8k16.  bf16 queries are fp16 after a power of two that brings a row's largest entry to 2^7 .. 2^8 (what that
+// leaves out is below 2^-32 of it), fp32 queries and their weights are two fp16 numbers, the second what the first leaves (2^-22).
+// (mma.sync takes e4m3 as well, but on this device it then converts both operands for every product: 700 products a clock and SM where
+// operands change, against 1016 with fp16.)
 //
 // Rows are (window row, query head of the kv head's group): all heads of a group share the keys that are read.
-//   S [16 rows x 8 keys]   = Q K^T           a key's 16-byte pieces are the columns that a thread's four words of the product take
-//   O [16 rows x 8 dims]  += P V             values of 4 keys x 4 dims are transposed in registers (8 byte permutes)
+//   S [16 rows x 8 keys]   = Q K^T           a word of a key is what a thread holds of one step of 16 dims
+//   O [16 rows x 8 dims]  += P V             values of 2 keys x 4 dims are paired by byte permutes
 // The order of dims in the first product and of keys in the second is free as long as both operands use the same; it is chosen so that
 // the 16-byte loads of both meet no bank twice (see key_of).
 //
 // Exponents: with s the score (in log2), e_K in its factor and e_V added to it, w = 2^(s + e_V - top) is the weight of a value's e4m3
-// number, top the largest s + e_V of the row in the tile, so that weights and products stay near 1 whatever the exponents of the
-// blocks; the sum of the softmax takes w 2^-e_V, which stays within 2^+-100 of the top as well.  Each tile's product is added to
-// the row's output under the running maximum.
+// number, top the largest s + e_V of the row so far, so that weights and products stay near 1 whatever the exponents of the
+// blocks; the sum of the softmax takes w 2^-e_V, which stays within 2^+-100 of the top as well.
 //
 // A CTA has eight warps that work and one that fetches.  A tile is 32 keys (TMA, K and V of one page half); RG warps share a tile's keys
 // (16 rows each), 8 / RG tiles are in work at a time, each with its own running maximum, and are joined at the end of a unit through
 // shared memory.  A unit is (sequence, tile of rows, kv head).  The tiles of all units are one line that is cut into as many equal
 // ranges as there are SMs (one CTA each): sequences of any lengths keep all SMs busy to the end, and a long one is spread over
 // many.  A unit that is cut is joined by the last of its CTAs to arrive (in the order of its ranges: results do not hang on who that is).
-// Bound: bytes of K and V; from 64 rows of bf16 (32 of fp32) on the tensor cores.
+// Bound: bytes of K and V up to 32 rows (fp32: 16), the tensor cores' fp16 rate beyond.
 #include "tcgen05.cuh"
 
 namespace sjd {
@@ -36,6 +34,10 @@ constexpr int kMaxEntries = 1024;    // (sequence, tile of rows) pairs of a call
 constexpr int kMaxSlots = 24;
 constexpr int kMaxCtas = 160;
 constexpr int kSmem = 232448;
+// Weights are 2^kUp at the row's maximum so far, which is renewed when a score passes it by more than kSlack: fp16 holds what is
+// between 2^15 and 2^-24, 2^-37 of the maximum's weight.
+constexpr int kUp = 13;
+constexpr float kSlack = 2.0f;
 
 struct PoolAttnParams {
   sjd_pool pool;
@@ -59,28 +61,17 @@ struct Entry {   // (sequence, tile of rows)
 
 __device__ __forceinline__ int key_of(int c) { return c ^ ((c & 1) << 2); }   // key of column c of 8
 
-__device__ __forceinline__ void mma_e4m3(float *c, const uint32_t *a, uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void mma_f16(float *c, const uint32_t *a, uint32_t b0, uint32_t b1) {
   asm volatile(
-      "mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ uint32_t e4m3_of_floats(float a, float b) {   // a in the low byte
-  uint16_t r;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(b), "f"(a));
-  return r;
+// two e4m3 numbers of a word (exact: fp16 holds all of them)
+__device__ __forceinline__ void halves_of_e4m3(uint32_t w, uint32_t &lo, uint32_t &hi) {
+  asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(lo), "=r"(hi) : "r"(w));
 }
-__device__ __forceinline__ uint32_t e4m3_of_halves(uint32_t h) {
-  uint16_t r;
-  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(h));
-  return r;
-}
-__device__ __forceinline__ uint32_t halves_of_e4m3(uint32_t v) {
-  uint32_t h;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)v));
-  return h;
-}
-__device__ __forceinline__ uint32_t halves_of_floats(float a, float b) {
+__device__ __forceinline__ uint32_t halves_of_floats(float a, float b) {   // a in the low half
   uint32_t h;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(h) : "f"(b), "f"(a));
   return h;
@@ -90,15 +81,14 @@ __device__ __forceinline__ float2 floats_of_halves(uint32_t h) {
   asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %2;\n\tcvt.f32.f16 %0, lo;\n\tcvt.f32.f16 %1, hi;\n\t}" : "=f"(f.x), "=f"(f.y) : "r"(h));
   return f;
 }
-__device__ __forceinline__ uint32_t sub_halves(uint32_t a, uint32_t b) {
-  uint32_t r;
-  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
-}
-__device__ __forceinline__ uint32_t fma_halves(uint32_t a, uint32_t b, uint32_t c) {
-  uint32_t r;
-  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
-  return r;
+// a, b as fp16 planes: the number and, of two, what is left of it
+template <int PL>
+__device__ __forceinline__ void split_halves(float a, float b, uint32_t *planes) {
+  planes[0] = halves_of_floats(a, b);
+  if constexpr (PL == 2) {
+    const float2 f = floats_of_halves(planes[0]);
+    planes[1] = halves_of_floats(a - f.x, b - f.y);
+  }
 }
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
@@ -117,23 +107,6 @@ __device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap *map, in
 }
 __device__ __forceinline__ void work_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kWorkWarps * 32) : "memory"); }
 __device__ __forceinline__ bool has_nan(uint32_t bytes) { return (((bytes & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) != 0; }
-
-// weights of two keys as e4m3 planes: planes[i] gets a 16-bit pair
-template <int PL>
-__device__ __forceinline__ void weight_planes(float a, float b, uint32_t *planes) {
-  const uint32_t h = halves_of_floats(a, b);
-  planes[0] = e4m3_of_halves(h);
-  uint32_t rest = sub_halves(h, halves_of_e4m3(planes[0]));   // exact: what is left of eleven bits
-  planes[1] = e4m3_of_halves(rest);
-  if constexpr (PL == 4) {
-    const float2 f = floats_of_halves(h);
-    rest = sub_halves(rest, halves_of_e4m3(planes[1]));
-    const uint32_t fine = halves_of_floats((a - f.x) * 256.0f, (b - f.y) * 256.0f);
-    rest = fma_halves(rest, 0x5C005C00u, fine);               // 256 rest + fine
-    planes[2] = e4m3_of_halves(rest);
-    planes[3] = e4m3_of_halves(sub_halves(rest, halves_of_e4m3(planes[2])));
-  }
-}
 
 template <typename T> __device__ __forceinline__ void load16(const T *p, float *x);   // 16 entries
 template <> __device__ __forceinline__ void load16<float>(const float *p, float *x) {
@@ -172,9 +145,9 @@ struct AttnShared {
 // T: float or bf16 queries and outputs; RG: warps of 16 rows that share a tile
 template <typename T, int HD, int RG>
 __global__ void __launch_bounds__(kThreads, 1) pool_attention_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ PoolAttnParams p) {
-  constexpr int PL = sizeof(T) == 4 ? 4 : 2;   // planes
+  constexpr int PL = sizeof(T) == 4 ? 2 : 1;   // planes
   constexpr int KG = kWorkWarps / RG;          // tiles in work at a time
-  constexpr int KS = HD / 32;                  // steps of the first product
+  constexpr int KS = HD / 16;                  // steps of the first product
   constexpr int NT = HD / 8;                   // column tiles of the second
   constexpr int BOX = kTile * HD;              // bytes of K or V of a tile
   constexpr int ROWS = 16 * RG;
@@ -302,11 +275,10 @@ __global__ void __launch_bounds__(kThreads, 1) pool_attention_kernel(const __gri
     return u;
   };
 
-  // 384 x 168 registers at the launch: 128 x 24 + 256 x 240
-  if (warp >= kWorkWarps) asm volatile("setmaxnreg.dec.sync.aligned.u32 24;");
-  else asm volatile("setmaxnreg.inc.sync.aligned.u32 240;");
-  if (warp > kWorkWarps) return;
-  if (warp == kWorkWarps) {
+  if (warp >= kWorkWarps) {
+    // 384 x 168 registers at the launch: 128 x 40 + 256 x 232
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    if (warp > kWorkWarps) return;
     // ------------------------------------------------------------------ fetching: tiles in order into the ring
     int slot = 0;
     uint32_t phase = 1;
@@ -372,6 +344,7 @@ __global__ void __launch_bounds__(kThreads, 1) pool_attention_kernel(const __gri
   }
 
   // -------------------------------------------------------------------- working warps
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
   const int kg = warp / RG, rg = warp % RG;
   const int g = lane >> 2, t4 = lane & 3;
   const T *qp = (const T *)p.q;
@@ -433,20 +406,11 @@ __global__ void __launch_bounds__(kThreads, 1) pool_attention_kernel(const __gri
       const float up = two_to(max(e, -126));
       factor[j] = p.scale * two_to(-max(e, -126));
 #pragma unroll
-      for (int i = 0; i < HD / 4; i += 2) {
-        float a = x[i] * up, c = x[i + 1] * up;
-        // word i / 4 of the row's words of this thread: step i / 8, half i / 4 % 2
-        const int s = i / 8, w = (i / 4 % 2) * 2 + j, sh16 = (i % 4) * 8;
+      for (int i = 0; i < HD / 4; i += 2) {   // step i / 4 of the product: its words j (k = 2 t4, ..) and j + 2 (k = 2 t4 + 8, ..)
+        uint32_t w[PL];
+        split_halves<PL>(x[i] * up, x[i + 1] * up, w);
 #pragma unroll
-        for (int l = 0; l < PL; ++l) {
-          if (l == 2) a *= 256.0f, c *= 256.0f;
-          const uint32_t v = e4m3_of_floats(a, c);
-          if (i % 4 == 0) qa[l][s][w] = v;
-          else qa[l][s][w] |= v << sh16;
-          const float2 f = floats_of_halves(halves_of_e4m3(v));
-          a -= f.x;
-          c -= f.y;
-        }
+        for (int l = 0; l < PL; ++l) qa[l][i / 4][i % 4 + j] = w[l];
       }
     }
     int lo = min(pos[0] >= 0 ? pos[0] : 0x7FFFFFFF, pos[1] >= 0 ? pos[1] : 0x7FFFFFFF), hi = max(pos[0], pos[1]);
@@ -498,19 +462,17 @@ __global__ void __launch_bounds__(kThreads, 1) pool_attention_kernel(const __gri
             }
           }
 #pragma unroll
-          for (int l = PL - 1; l >= 0; --l) {
+          for (int c = 0; c < HD / 64; ++c)
 #pragma unroll
-            for (int c = 0; c < HD / 64; ++c) {
+            for (int w = 0; w < 4; ++w)
 #pragma unroll
-              for (int i = 0; i < 4; ++i) mma_e4m3(s[i], qa[l][2 * c], kb[i][c].x, kb[i][c].y);
+              for (int i = 0; i < 4; ++i) {
+                const uint32_t word = w == 0 ? kb[i][c].x : w == 1 ? kb[i][c].y : w == 2 ? kb[i][c].z : kb[i][c].w;
+                uint32_t b0, b1;
+                halves_of_e4m3(word, b0, b1);
 #pragma unroll
-              for (int i = 0; i < 4; ++i) mma_e4m3(s[i], qa[l][2 * c + 1], kb[i][c].z, kb[i][c].w);
-            }
-            if (l == 2) {
-#pragma unroll
-              for (int i = 0; i < 4; ++i) s[i][0] *= 0x1p-8f, s[i][1] *= 0x1p-8f, s[i][2] *= 0x1p-8f, s[i][3] *= 0x1p-8f;
-            }
-          }
+                for (int l = PL - 1; l >= 0; --l) mma_f16(s[i], qa[l][4 * c + w], b0, b1);
+              }
         }
         float top[2] = {-INFINITY, -INFINITY};
         int ev[2];
@@ -541,58 +503,63 @@ __global__ void __launch_bounds__(kThreads, 1) pool_attention_kernel(const __gri
           top[0] = fmaxf(top[0], fmaxf(s[i][0], s[i][1]));
           top[1] = fmaxf(top[1], fmaxf(s[i][2], s[i][3]));
         }
-        float decay[2], grow[2], root[2];
+        bool renew = false, far = false;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], 1));
           top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], 2));
-          const float now = fmaxf(run[j], top[j]), ref = now > -INFINITY ? now : 0.0f;
-          // (roots first: a maximum may move by 200 with the values' exponents, and the sum by as much the other way)
-          const float d = exp2_fast(0.5f * (run[j] - ref)), u = exp2_fast(0.5f * (top[j] - ref));
-          total[j] = total[j] * d * d;
-          root[j] = u;
-          decay[j] = d * d;
-          grow[j] = u * u;
-          run[j] = now;
-          top[j] = (top[j] > -INFINITY ? top[j] : 0.0f) - 8.0f;   // weights of up to 2^8
+          renew |= top[j] > run[j] + kSlack;
+          far |= top[j] > -INFINITY && run[j] - top[j] > 64.0f;
+        }
+        if (__any_sync(0xffffffffu, renew)) {
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            if (!(top[j] > run[j])) continue;
+            // (by way of the root: with the values' exponents a maximum may move by 200, and the sum by as much the other way)
+            const float d = exp2_fast(0.5f * (run[j] - top[j]));
+            total[j] = total[j] * d * d;
+            const float decay = d * d;
+#pragma unroll
+            for (int i = 0; i < NT; ++i) o[i][2 * j] *= decay, o[i][2 * j + 1] *= decay;
+            run[j] = top[j];
+          }
         }
         // ---- weights, and their sum without the values' exponents
-        uint32_t pa[PL][4];
+        uint32_t pa[2][PL][4];
+        float ref[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) ref[j] = run[j] > -INFINITY ? run[j] : 0.0f;
         {
           float sum[2] = {0.0f, 0.0f};
 #pragma unroll
           for (int blk = 0; blk < 2; ++blk) {
-            const float back = two_to(-ev[blk] - 8);
+            const float back = two_to(-ev[blk] - kUp);
             float part[2] = {0.0f, 0.0f};
 #pragma unroll
-            for (int i = 2 * blk; i < 2 * blk + 2; ++i)
+            for (int i = 0; i < 2; ++i)
 #pragma unroll
               for (int j = 0; j < 2; ++j) {
-                const float a = exp2_fast(s[i][2 * j] - top[j]), c = exp2_fast(s[i][2 * j + 1] - top[j]);
+                const float a = exp2_fast(s[2 * blk + i][2 * j] - ref[j] + kUp), c = exp2_fast(s[2 * blk + i][2 * j + 1] - ref[j] + kUp);
                 part[j] += a + c;
                 uint32_t w[PL];
-                weight_planes<PL>(a, c, w);
-                // keys 0 .. 15 of the second product's steps are blocks' first words: word 2 blk + j, low half for even i
+                split_halves<PL>(a, c, w);
 #pragma unroll
-                for (int l = 0; l < PL; ++l) {
-                  if ((i & 1) == 0) pa[l][2 * blk + j] = w[l];
-                  else pa[l][2 * blk + j] |= w[l] << 16;
-                }
+                for (int l = 0; l < PL; ++l) pa[blk][l][2 * i + j] = w[l];
               }
             sum[0] = fmaf(part[0], back, sum[0]);
             sum[1] = fmaf(part[1], back, sum[1]);
           }
-          if (abs(ev[0] - ev[1]) > 64) {   // rare: weights of the smaller exponent may have left the range on the way
+          // rare: values' exponents that differ so much that weights, but not the sum's terms, have left the range
+          if (__any_sync(0xffffffffu, far) || abs(ev[0] - ev[1]) > 64) {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
               sum[j] = 0.0f;
 #pragma unroll
-              for (int i = 0; i < 4; ++i)
-                sum[j] += exp2_fast(s[i][2 * j] - ev[i >> 1] - (top[j] + 8.0f)) + exp2_fast(s[i][2 * j + 1] - ev[i >> 1] - (top[j] + 8.0f));
+              for (int i = 0; i < 4; ++i) sum[j] += exp2_fast(s[i][2 * j] - ev[i >> 1] - ref[j]) + exp2_fast(s[i][2 * j + 1] - ev[i >> 1] - ref[j]);
             }
           }
-          total[0] += sum[0] * root[0] * root[0];
-          total[1] += sum[1] * root[1] * root[1];
+          total[0] += sum[0];
+          total[1] += sum[1];
         }
         // ---- values: this thread's eight keys (four for each half of the product's step), CW dims of each
         uint32_t vb[8][CW / 4];
@@ -628,34 +595,22 @@ __global__ void __launch_bounds__(kThreads, 1) pool_attention_kernel(const __gri
           }
         }
 #pragma unroll
-        for (int c = 0; c < CW / 4; ++c) {
-          // bytes of four keys x four dims -> a word of four keys for each dim
-          uint32_t w[2][4];
+        for (int blk = 0; blk < 2; ++blk)
 #pragma unroll
-          for (int hf = 0; hf < 2; ++hf) {
-            const uint32_t k0 = vb[4 * hf][c], k1 = vb[4 * hf + 1][c], k2 = vb[4 * hf + 2][c], k3 = vb[4 * hf + 3][c];
-            const uint32_t a = __byte_perm(k0, k1, 0x5140), d = __byte_perm(k2, k3, 0x5140);
-            const uint32_t x = __byte_perm(k0, k1, 0x7362), y = __byte_perm(k2, k3, 0x7362);
-            w[hf][0] = __byte_perm(a, d, 0x5410);
-            w[hf][1] = __byte_perm(a, d, 0x7632);
-            w[hf][2] = __byte_perm(x, y, 0x5410);
-            w[hf][3] = __byte_perm(x, y, 0x7632);
+          for (int c = 0; c < CW / 4; ++c) {
+            // bytes of two keys x four dims -> pairs of keys for each dim
+            uint32_t b0[4], b1[4];
+            const uint32_t *v = &vb[4 * blk][c];
+            constexpr int W = CW / 4;
+            halves_of_e4m3(__byte_perm(v[0], v[W], 0x5140), b0[0], b0[1]);
+            halves_of_e4m3(__byte_perm(v[0], v[W], 0x7362), b0[2], b0[3]);
+            halves_of_e4m3(__byte_perm(v[2 * W], v[3 * W], 0x5140), b1[0], b1[1]);
+            halves_of_e4m3(__byte_perm(v[2 * W], v[3 * W], 0x7362), b1[2], b1[3]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int l = PL - 1; l >= 0; --l) mma_f16(o[4 * c + i], pa[blk][l], b0[i], b1[i]);
           }
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int l = PL - 1; l >= 0; --l) {
-              mma_e4m3(acc, pa[l], w[0][i], w[1][i]);
-              if (l == 2) acc[0] *= 0x1p-8f, acc[1] *= 0x1p-8f, acc[2] *= 0x1p-8f, acc[3] *= 0x1p-8f;
-            }
-            float *to = o[4 * c + i];
-            to[0] = fmaf(acc[0], grow[0], to[0] * decay[0]);
-            to[1] = fmaf(acc[1], grow[0], to[1] * decay[0]);
-            to[2] = fmaf(acc[2], grow[1], to[2] * decay[1]);
-            to[3] = fmaf(acc[3], grow[1], to[3] * decay[1]);
-          }
-        }
         if (odd) {   // rare: a row that sees a NaN gets it
 #pragma unroll 1
           for (int key = 0; key < kTile; ++key) {
@@ -740,7 +695,7 @@ __global__ void __launch_bounds__(kThreads, 1) pool_attention_kernel(const __gri
     auto store_row = [&](int r, int at, float4 v, float sum) {
       const int row = rt * ROWS + r;
       const int k = row / p.group;
-      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum * 0x1p-8f;   // (weights carry 2^8, their sum does not)
+      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum * two_to(-kUp);   // (weights carry 2^kUp, their sum does not)
       const bool live = (unsigned)p.in_pos[(long)b * p.window + k] < (unsigned)seq_keys && sum != 0.0f;   // (a NaN among the scores makes the sum NaN)
       v = live ? make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
       store4(outp + ((long)b * p.window + k) * p.out_stride + ((long)u.kvh * p.group + row % p.group) * HD + at * 4, v);
