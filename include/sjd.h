@@ -394,8 +394,8 @@ int sjd_pool_append(const sjd_pool *pool, int layer, int batch, int window, int 
  * strides multiples of 4, starting on 16 (fp32) or 8 (bf16) bytes; out may not overlap q.  What rows behind a sequence or masked places
  * hold (NaN included) does not matter; a visible NaN shows.  status: BAD_ARG for seqs or positions out of range (rows that see nothing)
  * and for visible positions without a page (keys that are left out); DEVICE_TIMEOUT if a bounded wait ran out.
- * ws: device scratch of sjd_pool_attention_workspace_bytes(...) bytes, 256-byte aligned, which the caller zeroes once; every call leaves
- * it ready for the next one.  One call at a time on a workspace (captured graphs that may run at the same time have their own).
+ * ws: device scratch of sjd_pool_attention_workspace_bytes(...) bytes, 256-byte aligned, contents without meaning between calls; one
+ * call at a time on a workspace (captured graphs that may run at the same time have their own).
  * Errors: BAD_ARG, UNSUPPORTED (head_dim, dtype, a device other than sm_100's), CAPACITY (ws too small), CUDA.
  */
 size_t sjd_pool_attention_workspace_bytes(const sjd_pool *pool, int window, int n_heads);

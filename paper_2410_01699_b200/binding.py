@@ -319,7 +319,7 @@ class CachePool:
         if self.ws_bytes == 0:
             raise SJDError(SJD_ERR_UNSUPPORTED, "sjd_pool_workspace_bytes")
         self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.device)
-        self._attention_ws = torch.zeros(0, dtype=torch.uint8, device=self.device)
+        self._attention_ws = torch.empty(0, dtype=torch.uint8, device=self.device)
 
     @classmethod
     def empty(cls, n_pages, n_seqs, pages_per_seq, n_layers, n_kv_heads, head_dim, device="cuda"):
@@ -333,8 +333,8 @@ class CachePool:
         nbytes = int(lib().sjd_pool_attention_workspace_bytes(C.byref(self.c), window, n_heads))
         if nbytes == 0:
             raise SJDError(SJD_ERR_BAD_ARG, "sjd_pool_attention_workspace_bytes")
-        if self._attention_ws.numel() < nbytes:   # (zeroed once; every call leaves it ready for the next)
-            self._attention_ws = torch.zeros(nbytes, dtype=torch.uint8, device=self.device)
+        if self._attention_ws.numel() < nbytes:
+            self._attention_ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         return self._attention_ws
 
     def fault(self) -> int:
@@ -408,7 +408,7 @@ def sjd_pool_append(pool: CachePool, layer: int, k, v, in_pos, window: int, q=No
 
 
 def sjd_pool_attention(pool: CachePool, layer: int, q, in_pos, window: int, sliding=0, sinks=0, scale=0.0, out=None, ws=None, seqs=None):
-    """Attention of q [B*W][H][hd] (float32 or bfloat16) at positions in_pos over the pool; out of q's type.  ws: a zeroed workspace of
+    """Attention of q [B*W][H][hd] (float32 or bfloat16) at positions in_pos over the pool; out of q's type.  ws: a workspace of
     its own for calls that may run at the same time as others on the pool (default: the pool's)."""
     m, heads = in_pos.numel(), q.shape[1]
     dtype = _pool_dtype(q, "sjd_pool_attention")

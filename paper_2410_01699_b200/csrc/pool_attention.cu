@@ -1,43 +1,42 @@
 // Attention of window queries over the 8-bit paged cache, with an optional sliding window and sinks.
 //
-// Keys and values stay in 8 bits up to the registers of the warp that multiplies them, where they become fp16 (which holds every e4m3
-// number) for mma.sync m16n8k16.  bf16 queries are fp16 after a power of two that brings a row's largest entry to 2^7 .. 2^8 (what that
-// leaves out is below 2^-32 of it), fp32 queries and their weights are two fp16 numbers, the second what the first leaves (2^-22).
-// (mma.sync takes e4m3 as well, but on this device it then converts both operands for every product: 700 products a clock and SM where
-// operands change, against 1016 with fp16.)
+// Keys and values stay in 8 bits: tcgen05 multiplies e4m3 by e4m3 (kind::f8f6f4, products exact, sums in 32 bits), K and V as TMA left them.
+// Keys are the rows of both products and the queries their columns, because few queries meet many keys:
+//   S^T [128 keys x NC]  =  K [128 keys x HD] . Q^T          O^T [HD x NC]  =  V^T [HD x 128 keys] . P
+// Queries and weights are e4m3 numbers too, but several of them: x = x1 + 2^-4 x2 (+ 2^-8 x3 + 2^-12 x4), x1 = e4m3(x), x2 = e4m3(16 (x - x1))
+// and so on.  The planes are columns of the same product, added when they are read from tensor memory.  n planes leave 2^-4n of a
+// number at most (half a step of e4m3 is 2^-4 of it) and about 2^-5.3n on average: two for bf16 queries, whose eight bits they hold
+// exactly, four for fp32.  (mma.sync has e4m3 as well, but here it converts both operands for every product: 700 products a clock and SM.
+// With conversions in registers and fp16 products: 8 x 32 rows x 4009 keys of 32 heads, fp32, 130 us, 32 tokens of up to 4224 keys 63.)
 //
-// Rows are (window row, query head of the kv head's group): all heads of a group share the keys that are read.
-//   S [16 rows x 8 keys]   = Q K^T           a word of a key is what a thread holds of one step of 16 dims
-//   O [16 rows x 8 dims]  += P V             values of 2 keys x 4 dims are paired by byte permutes
-// The order of dims in the first product and of keys in the second is free as long as both operands use the same; it is chosen so that
-// the 16-byte loads of both meet no bank twice (see key_of).
+// Columns are rows of a window times the query heads of the kv head's group: all heads of a group share the keys that are read.  RP of
+// them make a unit's tile of rows; a unit is (sequence, tile of rows, kv head).  The key tiles of all units are one line that is cut into
+// as many equal ranges as CTAs are resident, so that sequences of any lengths keep all SMs busy to the end and a long one is
+// spread over many.  A second launch joins the parts of units that are cut, in the order of the ranges.  (By the last of a unit's
+// CTAs to arrive, which a counter tells: 6 us between its last tile and the first part that it may read, and a lone CTA reads the 33
+// parts of 12 rows of a long sequence in 17.)
 //
-// Exponents: with s the score (in log2), e_K in its factor and e_V added to it, w = 2^(s + e_V - top) is the weight of a value's e4m3
-// number, top the largest s + e_V of the row so far, so that weights and products stay near 1 whatever the exponents of the
-// blocks; the sum of the softmax takes w 2^-e_V, which stays within 2^+-100 of the top as well.
+// A thread of the four softmax warps (eight with 64 columns of rows) is a key of the tile.  With s the score (in log2), e_K in its
+// factor and e_V added to it, w = 2^(s + e_V - top + 8) is the weight of the value's e4m3 numbers, top the largest s + e_V of the row in this
+// tile: weights fill the range of e4m3 whatever stands in other tiles (under one reference for all, the weights of 10^5 keys that share
+// a tenth of the mass beside one that has the rest would be zero) and whatever the exponents of the blocks are.  The sum of the softmax takes
+// w 2^-e_V.  The same threads, then a dim each, add the tile's O^T to their registers under the running maximum.
 //
-// A CTA has eight warps that work and one that fetches.  A tile is 32 keys (TMA, K and V of one page half); RG warps share a tile's keys
-// (16 rows each), 8 / RG tiles are in work at a time, each with its own running maximum, and are joined at the end of a unit through
-// shared memory.  A unit is (sequence, tile of rows, kv head).  The tiles of all units are one line that is cut into as many equal
-// ranges as there are SMs (one CTA each): sequences of any lengths keep all SMs busy to the end, and a long one is spread over
-// many.  A unit that is cut is joined by the last of its CTAs to arrive (in the order of its ranges: results do not hang on who that is).
-// Bound: bytes of K and V up to 32 rows (fp32: 16), the tensor cores' fp16 rate beyond.
+// Bound: bytes of K and V up to about 32 rows; beyond, the issue slots of the softmax (some 13 instructions for an entry of
+// S^T with bf16, 23 with fp32).  Two CTAs per SM (one with 64 rows), each with a ring of tiles: 96 to 160 KB of copies in flight.
 #include "tcgen05.cuh"
 
 namespace sjd {
 namespace {
 
-constexpr int kTile = 32;            // keys
-constexpr int kWorkWarps = 8;
-constexpr int kThreads = (kWorkWarps + 4) * 32;   // the working warps, and a warpgroup of which one warp fetches
-constexpr int kMaxEntries = 1024;    // (sequence, tile of rows) pairs of a call whose tiles are cut into equal ranges
-constexpr int kMaxSlots = 24;
-constexpr int kMaxCtas = 160;
-constexpr int kSmem = 232448;
-// Weights are 2^kUp at the row's maximum so far, which is renewed when a score passes it by more than kSlack: fp16 holds what is
-// between 2^15 and 2^-24, 2^-37 of the maximum's weight.
-constexpr int kUp = 13;
-constexpr float kSlack = 2.0f;
+constexpr int kTile = 128;           // keys
+constexpr int kMaxEntries = 512;     // (sequence, tile of rows) pairs of a call whose tiles are cut into equal ranges
+constexpr int kMaxSlots = 8;
+constexpr int kMeta = 16;            // tiles that the fetching warp may be ahead: more than the ring holds
+constexpr int kMaxCtas = 320;
+constexpr int kMinTiles = 2;        // of a range
+constexpr int kWholeTiles = 4;      // units of up to so many tiles are not cut where they are few
+constexpr int kUp = 8;               // the largest weight of a row in a tile is 2^kUp (e4m3 ends at 448)
 
 struct PoolAttnParams {
   sjd_pool pool;
@@ -48,10 +47,17 @@ struct PoolAttnParams {
   long q_stride, out_stride;
   const int32_t *seqs, *in_pos;
   void *out;
-  int *tickets;                 // [kMaxCtas], zero between calls
-  float *parts;                 // [2 kMaxCtas][16 RG rows][head_dim], then (top, sum) of each
+  int4 *cuts;                   // [kMaxCtas]: (sequence, tile of rows, kv head, CTAs) of the unit that begins in a CTA's range and goes on behind it
+  float2 *stats;                // [2 kMaxCtas][RP]: (top, sum) of the rows of the CTAs' parts of cut units
+  float *parts;                 // [2 kMaxCtas][RP][head_dim]: their sums
   int n_entries, cut, slots;    // cut: ranges of tiles; else a CTA per unit
 };
+
+// With 16 columns a thread, the softmax of an SM has 16 warps (8 with 16 rows): the time of a tile is a chain of latencies, and it takes
+// that many to fill the issue slots.
+__host__ __device__ constexpr int groups_of(int rp) { return rp <= 16 ? 1 : rp / 16; }
+__host__ __device__ constexpr int ctas_of(int rp) { return rp == 64 ? 1 : 2; }
+__host__ __device__ constexpr int threads_of(int rp) { return groups_of(rp) * 128 + 64; }
 
 struct Entry {   // (sequence, tile of rows)
   int before;    // tiles of one kv head in the entries before
@@ -59,19 +65,49 @@ struct Entry {   // (sequence, tile of rows)
   int sink;      // tiles before it
 };
 
-__device__ __forceinline__ int key_of(int c) { return c ^ ((c & 1) << 2); }   // key of column c of 8
+struct Meta {    // of a tile that is being fetched
+  int key0;
+  int k_exp[2], v_exp[2];   // exponents of its two pages' blocks
+  int pages;                // bit j: page j is there
+};
 
-__device__ __forceinline__ void mma_f16(float *c, const uint32_t *a, uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+template <int RP>
+struct PoolAttnShared {
+  uint64_t full[kMaxSlots], empty[kMaxSlots];
+  uint64_t meta_full[kMeta];
+  uint64_t q_ready, s_full, s_free, p_full, o_full;
+  uint32_t tmem_base;
+  int failed, wide[4][2], exp_range[4][2][4], n_nan, lo, hi;
+  Meta meta[kMeta];
+  alignas(16) float red[4][RP];   // (these are read and written four at a time)
+  alignas(16) float ref[RP];
+  alignas(16) float fac[RP];
+  alignas(16) float alpha[2][RP];
+  alignas(16) float beta[2][RP];
+  float alpha_root[2][RP], beta_root[2][RP], inv[RP];
+  int pos[RP];
+  long out_at[RP];             // first entry of a row in out
+  int nan_key[kTile];
+  uint32_t nan_dims[kTile][4];
+  Entry entry[kMaxEntries + 1];
+};
+
+__device__ __forceinline__ uint32_t e4m3_of_floats(float a, float b) {   // a in the low byte
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(b), "f"(a));
+  return r;
 }
-// two e4m3 numbers of a word (exact: fp16 holds all of them)
-__device__ __forceinline__ void halves_of_e4m3(uint32_t w, uint32_t &lo, uint32_t &hi) {
-  asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(lo), "=r"(hi) : "r"(w));
+__device__ __forceinline__ uint32_t e4m3_of_halves(uint32_t h) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(h));
+  return r;
 }
-__device__ __forceinline__ uint32_t halves_of_floats(float a, float b) {   // a in the low half
+__device__ __forceinline__ uint32_t halves_of_e4m3(uint32_t v) {
+  uint32_t h;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)v));
+  return h;
+}
+__device__ __forceinline__ uint32_t halves_of_floats(float a, float b) {
   uint32_t h;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(h) : "f"(b), "f"(a));
   return h;
@@ -81,91 +117,159 @@ __device__ __forceinline__ float2 floats_of_halves(uint32_t h) {
   asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %2;\n\tcvt.f32.f16 %0, lo;\n\tcvt.f32.f16 %1, hi;\n\t}" : "=f"(f.x), "=f"(f.y) : "r"(h));
   return f;
 }
-// a, b as fp16 planes: the number and, of two, what is left of it
-template <int PL>
-__device__ __forceinline__ void split_halves(float a, float b, uint32_t *planes) {
-  planes[0] = halves_of_floats(a, b);
-  if constexpr (PL == 2) {
-    const float2 f = floats_of_halves(planes[0]);
-    planes[1] = halves_of_floats(a - f.x, b - f.y);
-  }
+// 16 (a - b) of halves, exact where b is a's e4m3 number
+__device__ __forceinline__ uint32_t rest_of_halves(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("{\n\t.reg .b32 d;\n\tsub.rn.f16x2 d, %1, %2;\n\tmul.rn.f16x2 %0, d, %3;\n\t}" : "=r"(r) : "r"(a), "r"(b), "r"(0x4C004C00u));
+  return r;
+}
+__device__ __forceinline__ uint32_t add_halves(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("add.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
 }
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+__device__ __forceinline__ float max_of_warp(float x) {   // (a NaN is no maximum)
+  float y;
+  asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
+  return y;
+}
 __device__ __forceinline__ void arrive(uint64_t *bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
-__device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap *map, int row, int plane, int page, uint64_t *bar) {
+__device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap *map, int plane, int page, uint64_t *bar) {
   asm volatile(
       "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes"
-      " [%0], [%1, {%2, %3, %4, %5}], [%6];"
-      ::"r"(dst), "l"(map), "r"(0), "r"(row), "r"(plane), "r"(page), "r"(smem_u32(bar))
+      " [%0], [%1, {%2, %2, %3, %4}], [%5];"
+      ::"r"(dst), "l"(map), "r"(0), "r"(plane), "r"(page), "r"(smem_u32(bar))
       : "memory");
 }
-__device__ __forceinline__ void work_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kWorkWarps * 32) : "memory"); }
+__device__ __forceinline__ void mma_e4m3(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, bool accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.u32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"((uint32_t)accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_ld8_issue(uint32_t taddr, uint32_t *r) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr));
+}
+template <int N>
+__device__ __forceinline__ void tmem_ld_issue(uint32_t taddr, uint32_t *r) {
+  if constexpr (N == 8) tmem_ld8_issue(taddr, r);
+  else tmem_ld16_issue(taddr, r);
+}
 __device__ __forceinline__ bool has_nan(uint32_t bytes) { return (((bytes & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) != 0; }
 
-template <typename T> __device__ __forceinline__ void load16(const T *p, float *x);   // 16 entries
-template <> __device__ __forceinline__ void load16<float>(const float *p, float *x) {
+// sums of N values over the lanes: value i in the lanes whose number ends in i
+template <int N>
+__device__ __forceinline__ float lanes_sum(float *v) {
+  const int lane = threadIdx.x & 31;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float4 v = *reinterpret_cast<const float4 *>(p + 4 * i);
-    x[4 * i] = v.x, x[4 * i + 1] = v.y, x[4 * i + 2] = v.z, x[4 * i + 3] = v.w;
+  for (int o = 16; o >= N; o >>= 1)
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+#pragma unroll
+  for (int o = N / 2 < 16 ? N / 2 : 16; o > 0; o >>= 1)
+#pragma unroll
+    for (int j = 0; j < N / 2; ++j) {
+      if (j >= o) break;
+      const float send = lane & o ? v[j] : v[j + o], keep = lane & o ? v[j + o] : v[j];
+      v[j] = keep + __shfl_xor_sync(0xffffffffu, send, o);
+    }
+  return v[0];
+}
+
+// weights of two rows as e4m3 planes: planes[i] gets a 16-bit pair
+template <int PL>
+__device__ __forceinline__ void weight_planes(float a, float b, uint32_t *planes) {
+  const uint32_t h = halves_of_floats(a, b);
+  planes[0] = e4m3_of_halves(h);
+  uint32_t rest = rest_of_halves(h, halves_of_e4m3(planes[0]));
+  planes[1] = e4m3_of_halves(rest);
+  if constexpr (PL == 4) {
+    const float2 f = floats_of_halves(h);
+    // what is left of the eleven bits of h, and what h left of the weight
+    rest = rest_of_halves(rest, halves_of_e4m3(planes[1]));
+    rest = add_halves(rest, halves_of_floats((a - f.x) * 256.0f, (b - f.y) * 256.0f));
+    planes[2] = e4m3_of_halves(rest);
+    planes[3] = e4m3_of_halves(rest_of_halves(rest, halves_of_e4m3(planes[2])));
   }
 }
-template <> __device__ __forceinline__ void load16<__nv_bfloat16>(const __nv_bfloat16 *p, float *x) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint2 v = *reinterpret_cast<const uint2 *>(p + 4 * i);
-    x[4 * i] = __uint_as_float(v.x << 16), x[4 * i + 1] = __uint_as_float(v.x & 0xFFFF0000u);
-    x[4 * i + 2] = __uint_as_float(v.y << 16), x[4 * i + 3] = __uint_as_float(v.y & 0xFFFF0000u);
-  }
+
+template <typename T> __device__ __forceinline__ float4 load4(const T *p);
+template <> __device__ __forceinline__ float4 load4<float>(const float *p) { return *reinterpret_cast<const float4 *>(p); }
+template <> __device__ __forceinline__ float4 load4<__nv_bfloat16>(const __nv_bfloat16 *p) {
+  const uint2 v = *reinterpret_cast<const uint2 *>(p);
+  return make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xFFFF0000u), __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xFFFF0000u));
 }
 __device__ __forceinline__ void store4(float *p, float4 v) { *reinterpret_cast<float4 *>(p) = v; }
 __device__ __forceinline__ void store4(__nv_bfloat16 *p, float4 v) {
   const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
   *reinterpret_cast<uint2 *>(p) = make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
 }
+__device__ __forceinline__ void store1(float *p, float v) { *p = v; }
+__device__ __forceinline__ void store1(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
 
-template <int HD>
-struct AttnShared {
-  uint64_t full[kMaxSlots], empty[kMaxSlots];
-  int key0[kMaxSlots];                 // first key of the tile in a slot, -1: it has no page
-  int k_exp[kMaxSlots], v_exp[kMaxSlots];   // exponents of the page's four blocks
-  float top[kWorkWarps][16], sum[kWorkWarps][16];
-  float factor[kWorkWarps][16];
-  int scan[32];
-  int failed, last;
-  Entry entry[kMaxEntries + 1];
-};
+// Shared-memory matrix descriptor of rows of BYTES (32, 64 or 128) under the swizzle of that width, 8 rows a group; lbo: bytes between
+// columns of that width (MN-major operands wider than 128 bytes; 0: the second one is the first again).
+template <int BYTES>
+__device__ __forceinline__ uint64_t operand(uint32_t lbo) {
+  return (uint64_t)(lbo >> 4) << 16 | (uint64_t)(8 * BYTES >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)(BYTES == 128 ? 2 : BYTES == 64 ? 4 : 6) << 61;
+}
+// byte `col` of row `row` under that swizzle
+template <int BYTES>
+__device__ __forceinline__ uint32_t swizzled(uint32_t row, uint32_t col) {
+  return row * BYTES + (BYTES == 128 ? col ^ (row & 7) << 4 : BYTES == 64 ? col ^ (row >> 1 & 3) << 4 : col ^ (row >> 2 & 1) << 4);
+}
 
-// T: float or bf16 queries and outputs; RG: warps of 16 rows that share a tile
-template <typename T, int HD, int RG>
-__global__ void __launch_bounds__(kThreads, 1) pool_attention_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ PoolAttnParams p) {
-  constexpr int PL = sizeof(T) == 4 ? 2 : 1;   // planes
-  constexpr int KG = kWorkWarps / RG;          // tiles in work at a time
-  constexpr int KS = HD / 16;                  // steps of the first product
-  constexpr int NT = HD / 8;                   // column tiles of the second
-  constexpr int BOX = kTile * HD;              // bytes of K or V of a tile
-  constexpr int ROWS = 16 * RG;
-  constexpr int CW = HD / 8;                   // bytes of a value row that a thread takes
+// T: float or bf16 queries and outputs; RP: rows of a unit's tile
+template <typename T, int HD, int RP>
+__global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
+    pool_attention_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ PoolAttnParams p) {
+  constexpr int PL = sizeof(T) == 4 ? 4 : 2;   // planes
+  constexpr int CG = groups_of(RP);            // groups of four softmax warps, each with its columns
+  constexpr int NQ = RP / CG;                  // columns of a thread
+  constexpr int NC = PL * RP;                  // columns of the products
+  constexpr int PB = NC < 128 ? NC : 128;      // bytes of a row of P
+  constexpr int WORK = 4 * CG, WORK_T = WORK * 32, ALL_T = WORK_T + 64;
+  constexpr int TILE = kTile * HD, BOX = TILE / 2;
+  constexpr int LD = PL == 4 ? 8 : 16;         // columns of a load from tensor memory (of all planes: 32 registers)
+  constexpr int T_COLS = 2 * NC < 32 ? 32 : 2 * NC;
   extern __shared__ __align__(1024) uint8_t smem[];
-  uint8_t *ring = smem;                                                            // [slots][K | V]
-  float *join = reinterpret_cast<float *>(ring + p.slots * 2 * BOX);               // [8 warps][16][HD]
-  AttnShared<HD> &sh = *reinterpret_cast<AttnShared<HD> *>(join + kWorkWarps * 16 * HD);
+  uint8_t *ring = smem;                                   // [slots][128 keys][HD]
+  uint8_t *Ps = ring + p.slots * TILE;                    // [NC / PB][128 keys][PB]
+  uint8_t *Qs = Ps + kTile * NC;                          // [NC][HD]
+  PoolAttnShared<RP> &sh = *reinterpret_cast<PoolAttnShared<RP> *>(Qs + NC * HD);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int kv_heads = p.pool.n_kv_heads, seq_keys = p.pool.pages_per_seq * KV_PAGE;
 
+  pdl_trigger();   // (the joining launch waits for the end of this one)
+  if (tid < kMeta) mbar_init(&sh.meta_full[tid], 1);
   if (tid < p.slots) {
     mbar_init(&sh.full[tid], 1);
-    mbar_init(&sh.empty[tid], RG);
+    mbar_init(&sh.empty[tid], 1);
+  }
+  if (tid == 0) {
+    mbar_init(&sh.q_ready, WORK);
+    mbar_init(&sh.s_full, 1);
+    mbar_init(&sh.s_free, WORK);
+    mbar_init(&sh.p_full, WORK);
+    mbar_init(&sh.o_full, 1);
+    sh.failed = 0;
+    sh.n_nan = 0;
+  }
+  if (warp == 0) {
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
-  if (tid == 0) sh.failed = 0;
 
   // ---- tiles of every entry (a row that is out of range sees nothing)
   auto position = [&](int b, int k) {
@@ -192,18 +296,18 @@ __global__ void __launch_bounds__(kThreads, 1) pool_attention_kernel(const __gri
   };
   {
     // a group of lanes per entry, as many as it has positions
-    const int span = min(p.window, (ROWS - 1) / p.group + 2);
+    const int span = min(p.window, (RP - 1) / p.group + 2);
     int lanes = 1;
     while (lanes < 32 && lanes < span) lanes <<= 1;
-    const int per_pass = kThreads / lanes, mine = tid / lanes, l = tid % lanes;
+    const int per_pass = ALL_T / lanes, mine = tid / lanes, l = tid % lanes;
     for (int e0 = 0; e0 < n_entries; e0 += per_pass) {
       const int e = e0 + mine;
       int lo = 0x7FFFFFFF, hi = -1;
-      if (e < n_entries) {
+      if (mine < per_pass && e < n_entries) {
         int b, rt;
         entry_at(e, &b, &rt);
-        const int r1 = min(p.rows, (rt + 1) * ROWS);
-        for (int k = rt * ROWS / p.group + l; k <= (r1 - 1) / p.group; k += lanes) {
+        const int r1 = min(p.rows, (rt + 1) * RP);
+        for (int k = rt * RP / p.group + l; k <= (r1 - 1) / p.group; k += lanes) {
           const int at = position(b, k);
           if (at >= 0) {
             lo = min(lo, at);
@@ -215,7 +319,7 @@ __global__ void __launch_bounds__(kThreads, 1) pool_attention_kernel(const __gri
         lo = min(lo, __shfl_xor_sync(0xffffffffu, lo, o));
         hi = max(hi, __shfl_xor_sync(0xffffffffu, hi, o));
       }
-      if (e < n_entries && l == 0) {
+      if (mine < per_pass && e < n_entries && l == 0) {
         Entry n;
         n.low = p.sliding > 0 && hi >= 0 ? max(0, lo - p.sliding + 1) / kTile : 0;
         n.sink = min(n.low, (min(p.sinks, seq_keys) + kTile - 1) / kTile);
@@ -243,15 +347,21 @@ __global__ void __launch_bounds__(kThreads, 1) pool_attention_kernel(const __gri
     }
     if (lane == 31) sh.entry[n_entries].before = x;
   }
+  if (warp == WORK + 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem_base)), "r"(T_COLS) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
   __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = sh.tmem_base;
   const long all = (long)sh.entry[n_entries].before * (p.cut ? kv_heads : 1);
-  // a range has enough tiles for all warps of a CTA
   long chunk = all;
   if (p.cut) {
     chunk = (all + gridDim.x - 1) / gridDim.x;
-    chunk = chunk < 2 * KG ? 2 * KG : chunk;
+    chunk = chunk < kMinTiles ? kMinTiles : chunk;
   }
-  const long t_begin = p.cut ? blockIdx.x * chunk : 0, t_end = min(all, t_begin + chunk);
+  const long t_begin = p.cut ? min(all, blockIdx.x * chunk) : 0, t_end = min(all, t_begin + chunk);
 
   // unit of a tile: its entry, kv head, first tile
   struct Unit {
@@ -274,20 +384,25 @@ __global__ void __launch_bounds__(kThreads, 1) pool_attention_kernel(const __gri
     u.first = t - (in - (long)h * u.n);
     return u;
   };
+  auto fail = [&]() {
+    if (lane == 0) {
+      *(volatile int *)&sh.failed = 1;
+      pool_fault(p.pool.status, SJD_ERR_DEVICE_TIMEOUT);
+    }
+  };
+  // Operands go through the ring in the order in which they are multiplied: K of a unit's first tile, then K of the next tile
+  // and V of the one before, and V of the last tile.
 
-  if (warp >= kWorkWarps) {
-    // 384 x 168 registers at the launch: 128 x 40 + 256 x 232
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
-    if (warp > kWorkWarps) return;
-    // ------------------------------------------------------------------ fetching: tiles in order into the ring
-    int slot = 0;
+  if (warp == WORK) {
+    // ------------------------------------------------------------------ fetching
+    int slot = 0, meta = 0;
     uint32_t phase = 1;
     long issued = 0;
     bool ok = true;
-    int n_key0 = -1, n_page = -1, n_kexp = 0, n_vexp = 0, n_plane = 0;
+    int n_key0 = 0, n_page[2] = {-1, -1}, n_ke[2] = {0, 0}, n_ve[2] = {0, 0}, n_head = 0, n_last = 0;
     auto look_up = [&](long t) {   // what lane `lane` knows of tile t + lane
-      n_key0 = n_page = -1;
-      n_kexp = n_vexp = n_plane = 0;
+      n_page[0] = n_page[1] = -1;
+      n_last = 0;
       if (t + lane >= t_end) return;
       const Unit u = unit_of(t + lane);
       const int i = (int)(t + lane - u.first);
@@ -295,458 +410,614 @@ __global__ void __launch_bounds__(kThreads, 1) pool_attention_kernel(const __gri
       int b, rt;
       entry_at(u.e, &b, &rt);
       n_key0 = (i < en.sink ? i : en.low + i - en.sink) * kTile;
+      n_head = u.kvh;
+      n_last = i == u.n - 1 || t + lane == t_end - 1;
       const int seq = p.seqs ? p.seqs[b] : b;
-      n_page = p.pool.table[(long)seq * p.pool.pages_per_seq + n_key0 / KV_PAGE];
-      if (n_page < 0 || n_page >= p.pool.n_pages) {
-        pool_fault(p.pool.status, SJD_ERR_BAD_ARG);
-        n_page = -1;
-        return;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int at = n_key0 / KV_PAGE + j;
+        if (at >= p.pool.pages_per_seq) continue;
+        // (the second page of the last tile may be behind the sequence)
+        const int page = p.pool.table[(long)seq * p.pool.pages_per_seq + at];
+        n_page[j] = page < 0 || page >= p.pool.n_pages ? -1 : page;
       }
-      n_plane = u.kvh;
-      const long at = ((long)n_page * p.pool.n_layers + p.layer) * 2 * kv_heads + u.kvh;
-      n_kexp = *reinterpret_cast<const int *>(p.pool.exps + at * kPoolBlocks);
-      n_vexp = *reinterpret_cast<const int *>(p.pool.exps + (at + kv_heads) * kPoolBlocks);
     };
-    if (t_begin < t_end) look_up(t_begin);
-    for (long t0 = t_begin; t0 < t_end && ok; t0 += 32) {
-      const int key0 = n_key0, page = n_page, kexp = n_kexp, vexp = n_vexp, plane = n_plane;
-      if (t0 + 32 < t_end) look_up(t0 + 32);
-      const int n = (int)min(32L, t_end - t0);
-      for (int i = 0; i < n; ++i) {
-        const int key = __shfl_sync(0xffffffffu, key0, i), pg = __shfl_sync(0xffffffffu, page, i), pl = __shfl_sync(0xffffffffu, plane, i);
-        const int ke = __shfl_sync(0xffffffffu, kexp, i), ve = __shfl_sync(0xffffffffu, vexp, i);
-        if (issued >= p.slots && !warp_wait(&sh.empty[slot], phase)) { ok = false; break; }
-        if (elect_one()) {
-          sh.key0[slot] = pg < 0 ? -1 : key;
-          sh.k_exp[slot] = ke;
-          sh.v_exp[slot] = ve;
-          const uint32_t dst = smem_u32(ring) + slot * 2 * BOX;
-          if (pg < 0) {
-            arrive(&sh.full[slot]);
-          } else {
-            mbar_expect_tx(&sh.full[slot], 2 * BOX);
-            tma_box(dst, &map, key % KV_PAGE, pl, pg, &sh.full[slot]);
-            tma_box(dst + BOX, &map, key % KV_PAGE, kv_heads + pl, pg, &sh.full[slot]);
-          }
-        }
-        __syncwarp();
-        ++issued;
-        if (++slot == p.slots) { slot = 0; phase ^= 1u; }
+    auto look_up_exps = [&]() {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        n_ke[j] = n_ve[j] = 0;
+        if (n_page[j] < 0) continue;
+        const long at = ((long)n_page[j] * p.pool.n_layers + p.layer) * 2 * kv_heads + n_head;
+        n_ke[j] = *reinterpret_cast<const int *>(p.pool.exps + at * kPoolBlocks);
+        n_ve[j] = *reinterpret_cast<const int *>(p.pool.exps + (at + kv_heads) * kPoolBlocks);
       }
-    }
-    if (!ok && lane == 0) {
-      *(volatile int *)&sh.failed = 1;
-      pool_fault(p.pool.status, SJD_ERR_DEVICE_TIMEOUT);
-    }
-    // leave no copy in flight
-    for (long j = issued > p.slots ? issued - p.slots : 0; j < issued; ++j) warp_wait(&sh.full[j % p.slots], (uint32_t)((j / p.slots) & 1));
-    return;
-  }
-
-  // -------------------------------------------------------------------- working warps
-  asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
-  const int kg = warp / RG, rg = warp % RG;
-  const int g = lane >> 2, t4 = lane & 3;
-  const T *qp = (const T *)p.q;
-  T *outp = (T *)p.out;
-  long mine = t_begin + kg;   // this warp's next tile, its slot in the ring and the parity of the slot's round
-  int slot = kg;
-  uint32_t phase = 0;
-  bool ok = true;
-  // rows without a tile are in no range: the CTAs share them (an entry whose rows see nothing has no tiles)
-  if (p.cut || all == 0) {
-    for (int e = p.cut ? blockIdx.x : 0; e < n_entries; e += gridDim.x) {
-      if (sh.entry[e + 1].before != sh.entry[e].before) continue;
-      int b, rt;
-      entry_at(e, &b, &rt);
-      const int r1 = min(p.rows, (rt + 1) * ROWS);
-      for (int i = tid; i < (r1 - rt * ROWS) * (HD / 4); i += kWorkWarps * 32) {
-        const int r = rt * ROWS + i / (HD / 4), dim = i % (HD / 4) * 4;
-        for (int h = p.cut ? 0 : unit0 % kv_heads; h < (p.cut ? kv_heads : unit0 % kv_heads + 1); ++h)
-          store4(outp + ((long)b * p.window + r / p.group) * p.out_stride + ((long)h * p.group + r % p.group) * HD + dim, make_float4(0.0f, 0.0f, 0.0f, 0.0f));
-      }
-    }
-  }
-
-  for (long t = t_begin; t < t_end;) {
-    const Unit u = unit_of(t);
-    const long u_end = u.first + u.n, end = min(t_end, u_end);
-    int b, rt;
-    entry_at(u.e, &b, &rt);
-    // ---- this thread's rows: g and g + 8 of its warp's 16
-    int pos[2];
-    float factor[2];
-    uint32_t qa[PL][KS][4];
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int r = rt * ROWS + rg * 16 + g + 8 * j;
-      const bool have = r < p.rows;
-      pos[j] = -1;
-      float x[HD / 4];
-#pragma unroll
-      for (int i = 0; i < HD / 4; ++i) x[i] = 0.0f;
-      if (have) {
-        const int k = r / p.group, h = u.kvh * p.group + r % p.group;
-        pos[j] = position(b, k);
-        const T *src = qp + ((long)b * p.window + k) * p.q_stride + (long)h * HD;
-#pragma unroll
-        for (int c = 0; c < HD / 64; ++c) load16<T>(src + 16 * (t4 + 4 * c), x + 16 * c);
-      }
-      float top = 0.0f;
-#pragma unroll
-      for (int i = 0; i < HD / 4; ++i) {
-        if (fabsf(x[i]) == INFINITY) x[i] = __int_as_float(0x7FFFFFFF);   // (e4m3 has no infinity: its row is NaN, as it would be)
-        top = fmaxf(top, fabsf(x[i]));
-      }
-      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-      // a power of two that brings the largest entry to 128 .. 256
-      int e = top > 0.0f ? 7 - (int)((__float_as_uint(top) >> 23) - 127) : 0;
-      e = min(e, 126);   // (entries below 2^-119 lose places)
-      const float up = two_to(max(e, -126));
-      factor[j] = p.scale * two_to(-max(e, -126));
-#pragma unroll
-      for (int i = 0; i < HD / 4; i += 2) {   // step i / 4 of the product: its words j (k = 2 t4, ..) and j + 2 (k = 2 t4 + 8, ..)
-        uint32_t w[PL];
-        split_halves<PL>(x[i] * up, x[i + 1] * up, w);
-#pragma unroll
-        for (int l = 0; l < PL; ++l) qa[l][i / 4][i % 4 + j] = w[l];
-      }
-    }
-    int lo = min(pos[0] >= 0 ? pos[0] : 0x7FFFFFFF, pos[1] >= 0 ? pos[1] : 0x7FFFFFFF), hi = max(pos[0], pos[1]);
-    lo = __reduce_min_sync(0xffffffffu, lo);
-    hi = __reduce_max_sync(0xffffffffu, hi);
-    const int sliding = p.sliding > 0 ? p.sliding : 0x7FFFFFFF;
-    // keys above `from` are in the window of every row, those up to `until` in none's
-    const int from = hi - sliding, until = lo == 0x7FFFFFFF ? 0x7FFFFFFF : lo - sliding;
-
-    float o[NT][4], run[2] = {-INFINITY, -INFINITY}, total[2] = {0.0f, 0.0f};
-#pragma unroll
-    for (int i = 0; i < NT; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.0f;
-
-    auto next = [&]() {
-      mine += KG;
-      slot += KG;
-      if (slot >= p.slots) { slot -= p.slots; phase ^= 1u; }
     };
-    for (; mine < end; next()) {
-      ok = ok && !*(volatile int *)&sh.failed;
-      if (ok && !warp_wait(&sh.full[slot], phase)) {
-        ok = false;
-        if (lane == 0) {
-          *(volatile int *)&sh.failed = 1;
-          pool_fault(p.pool.status, SJD_ERR_DEVICE_TIMEOUT);
-        }
-      }
-      if (!ok) continue;
-      const int key0 = sh.key0[slot];
-      const bool seen = key0 >= 0 && key0 <= hi && (key0 + kTile - 1 > until || key0 < p.sinks);
-      if (seen) {
-        const bool whole = key0 + kTile - 1 <= lo && (key0 > from || key0 + kTile <= p.sinks);
-        const uint8_t *ks = ring + slot * 2 * BOX, *vs = ks + BOX;
-        const int half = key0 % KV_PAGE / kTile * 16;   // the tile's two blocks of the page's four
-        const int kw = sh.k_exp[slot] >> half, vw = sh.v_exp[slot] >> half;
-        // ---- scores
-        float s[4][4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.0f;
-        {
-          uint4 kb[4][HD / 64];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int key = i * 8 + key_of(g);
-#pragma unroll
-            for (int c = 0; c < HD / 64; ++c) {
-              const int piece = HD == 128 ? (t4 + 4 * c) ^ (key & 7) : t4 ^ (key >> 1 & 3);
-              kb[i][c] = *reinterpret_cast<const uint4 *>(ks + key * HD + piece * 16);
-            }
-          }
-#pragma unroll
-          for (int c = 0; c < HD / 64; ++c)
-#pragma unroll
-            for (int w = 0; w < 4; ++w)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const uint32_t word = w == 0 ? kb[i][c].x : w == 1 ? kb[i][c].y : w == 2 ? kb[i][c].z : kb[i][c].w;
-                uint32_t b0, b1;
-                halves_of_e4m3(word, b0, b1);
-#pragma unroll
-                for (int l = PL - 1; l >= 0; --l) mma_f16(s[i], qa[l][4 * c + w], b0, b1);
-              }
-        }
-        float top[2] = {-INFINITY, -INFINITY};
-        int ev[2];
-#pragma unroll
-        for (int blk = 0; blk < 2; ++blk) {
-          const float k2 = two_to(pool_exp((int8_t)(kw >> (8 * blk))));
-          ev[blk] = pool_exp((int8_t)(vw >> (8 * blk)));
-          const float f0 = factor[0] * k2, f1 = factor[1] * k2, add = (float)ev[blk];
-#pragma unroll
-          for (int i = 2 * blk; i < 2 * blk + 2; ++i) {
-            s[i][0] = fmaf(s[i][0], f0, add);
-            s[i][1] = fmaf(s[i][1], f0, add);
-            s[i][2] = fmaf(s[i][2], f1, add);
-            s[i][3] = fmaf(s[i][3], f1, add);
-          }
-        }
-        if (!whole) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              const int key = key0 + i * 8 + key_of(2 * t4 + (c & 1)), at = pos[c >> 1];
-              if (!(key <= at && (key > at - sliding || key < p.sinks))) s[i][c] = -INFINITY;
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          top[0] = fmaxf(top[0], fmaxf(s[i][0], s[i][1]));
-          top[1] = fmaxf(top[1], fmaxf(s[i][2], s[i][3]));
-        }
-        bool renew = false, far = false;
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], 1));
-          top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], 2));
-          renew |= top[j] > run[j] + kSlack;
-          far |= top[j] > -INFINITY && run[j] - top[j] > 64.0f;
-        }
-        if (__any_sync(0xffffffffu, renew)) {
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            if (!(top[j] > run[j])) continue;
-            // (by way of the root: with the values' exponents a maximum may move by 200, and the sum by as much the other way)
-            const float d = exp2_fast(0.5f * (run[j] - top[j]));
-            total[j] = total[j] * d * d;
-            const float decay = d * d;
-#pragma unroll
-            for (int i = 0; i < NT; ++i) o[i][2 * j] *= decay, o[i][2 * j + 1] *= decay;
-            run[j] = top[j];
-          }
-        }
-        // ---- weights, and their sum without the values' exponents
-        uint32_t pa[2][PL][4];
-        float ref[2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) ref[j] = run[j] > -INFINITY ? run[j] : 0.0f;
-        {
-          float sum[2] = {0.0f, 0.0f};
-#pragma unroll
-          for (int blk = 0; blk < 2; ++blk) {
-            const float back = two_to(-ev[blk] - kUp);
-            float part[2] = {0.0f, 0.0f};
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-              for (int j = 0; j < 2; ++j) {
-                const float a = exp2_fast(s[2 * blk + i][2 * j] - ref[j] + kUp), c = exp2_fast(s[2 * blk + i][2 * j + 1] - ref[j] + kUp);
-                part[j] += a + c;
-                uint32_t w[PL];
-                split_halves<PL>(a, c, w);
-#pragma unroll
-                for (int l = 0; l < PL; ++l) pa[blk][l][2 * i + j] = w[l];
-              }
-            sum[0] = fmaf(part[0], back, sum[0]);
-            sum[1] = fmaf(part[1], back, sum[1]);
-          }
-          // rare: values' exponents that differ so much that weights, but not the sum's terms, have left the range
-          if (__any_sync(0xffffffffu, far) || abs(ev[0] - ev[1]) > 64) {
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              sum[j] = 0.0f;
-#pragma unroll
-              for (int i = 0; i < 4; ++i) sum[j] += exp2_fast(s[i][2 * j] - ev[i >> 1] - ref[j]) + exp2_fast(s[i][2 * j + 1] - ev[i >> 1] - ref[j]);
-            }
-          }
-          total[0] += sum[0];
-          total[1] += sum[1];
-        }
-        // ---- values: this thread's eight keys (four for each half of the product's step), CW dims of each
-        uint32_t vb[8][CW / 4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            const int key = i * 8 + key_of(2 * t4 + c);
-            uint32_t *to = vb[2 * i + c];
-            if constexpr (HD == 128) {
-              const uint4 v = *reinterpret_cast<const uint4 *>(vs + key * HD + ((g ^ (key & 7)) << 4));
-              to[0] = v.x, to[1] = v.y, to[2] = v.z, to[3] = v.w;
-            } else {
-              const uint2 v = *reinterpret_cast<const uint2 *>(vs + key * HD + (((g >> 1) ^ (key >> 1 & 3)) << 4) + (g & 1) * 8);
-              to[0] = v.x, to[1] = v.y;
-            }
-          }
-        bool odd = false;
-        if (!whole) {   // some row does not see some key: what stands there must not reach it, a NaN times a weight of zero would
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-#pragma unroll
-            for (int c = 0; c < CW / 4; ++c) odd |= has_nan(vb[i][c]);
-          odd = __any_sync(0xffffffffu, odd);
-          if (odd) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-#pragma unroll
-              for (int c = 0; c < CW / 4; ++c) {
-                const uint32_t n = ((vb[i][c] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;   // the top bit of every NaN byte
-                vb[i][c] &= ~((n >> 7) * 0xFFu);
-              }
-          }
-        }
-#pragma unroll
-        for (int blk = 0; blk < 2; ++blk)
-#pragma unroll
-          for (int c = 0; c < CW / 4; ++c) {
-            // bytes of two keys x four dims -> pairs of keys for each dim
-            uint32_t b0[4], b1[4];
-            const uint32_t *v = &vb[4 * blk][c];
-            constexpr int W = CW / 4;
-            halves_of_e4m3(__byte_perm(v[0], v[W], 0x5140), b0[0], b0[1]);
-            halves_of_e4m3(__byte_perm(v[0], v[W], 0x7362), b0[2], b0[3]);
-            halves_of_e4m3(__byte_perm(v[2 * W], v[3 * W], 0x5140), b1[0], b1[1]);
-            halves_of_e4m3(__byte_perm(v[2 * W], v[3 * W], 0x7362), b1[2], b1[3]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-              for (int l = PL - 1; l >= 0; --l) mma_f16(o[4 * c + i], pa[blk][l], b0[i], b1[i]);
-          }
-        if (odd) {   // rare: a row that sees a NaN gets it
-#pragma unroll 1
-          for (int key = 0; key < kTile; ++key) {
-            bool sees[2];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) sees[j] = key0 + key <= pos[j] && (key0 + key > pos[j] - sliding || key0 + key < p.sinks);
-#pragma unroll
-            for (int i = 0; i < NT; ++i)
-#pragma unroll
-              for (int c = 0; c < 2; ++c) {
-                const int dim = (2 * t4 + c) * CW + i;
-                const int piece = HD == 128 ? (dim >> 4) ^ (key & 7) : (dim >> 4) ^ (key >> 1 & 3);
-                if ((vs[key * HD + piece * 16 + (dim & 15)] & 0x7F) == 0x7F) {
-                  if (sees[0]) o[i][c] = __int_as_float(0x7FFFFFFF);
-                  if (sees[1]) o[i][2 + c] = __int_as_float(0x7FFFFFFF);
-                }
-              }
-          }
+    auto fetch = [&](int plane, int page0, int page1) {
+      if (issued >= p.slots && !warp_wait(&sh.empty[slot], phase)) { ok = false; return; }
+      if (elect_one()) {
+        const uint32_t dst = smem_u32(ring) + slot * TILE;
+        if (page0 < 0 && page1 < 0) {
+          arrive(&sh.full[slot]);
+        } else {
+          mbar_expect_tx(&sh.full[slot], (page0 >= 0 ? BOX : 0) + (page1 >= 0 ? BOX : 0));
+          if (page0 >= 0) tma_box(dst, &map, plane, page0, &sh.full[slot]);
+          if (page1 >= 0) tma_box(dst + BOX, &map, plane, page1, &sh.full[slot]);
         }
       }
       __syncwarp();
-      if (lane == 0) arrive(&sh.empty[slot]);
+      ++issued;
+      if (++slot == p.slots) { slot = 0; phase ^= 1u; }
+    };
+    int v_plane = 0, v_page0 = -1, v_page1 = -1;
+    bool v_open = false;   // V of the tile before is to be fetched behind this K
+    if (t_begin < t_end) look_up(t_begin);
+    for (long t0 = t_begin; t0 < t_end && ok; t0 += 32) {
+      look_up_exps();
+      Meta m;
+      m.key0 = n_key0;
+      m.k_exp[0] = n_ke[0], m.k_exp[1] = n_ke[1], m.v_exp[0] = n_ve[0], m.v_exp[1] = n_ve[1];
+      m.pages = (n_page[0] >= 0 ? 1 : 0) | (n_page[1] >= 0 ? 2 : 0);
+      const int pg0 = n_page[0], pg1 = n_page[1], head = n_head, last = n_last;
+      if (t0 + 32 < t_end) look_up(t0 + 32);
+      const int n = (int)min(32L, t_end - t0);
+      int told = 0;   // tiles of these 32 whose lanes have written what they know: not before the copies that there is room for are under way
+      auto tell = [&](int upto) {
+        if (lane >= told && lane < upto) {
+          const int at = (meta + lane) % kMeta;
+          sh.meta[at] = m;
+          arrive(&sh.meta_full[at]);
+        }
+        __syncwarp();
+        told = upto;
+      };
+      for (int i = 0; i < n && ok; ++i) {
+        const int page0 = __shfl_sync(0xffffffffu, pg0, i), page1 = __shfl_sync(0xffffffffu, pg1, i), h = __shfl_sync(0xffffffffu, head, i);
+        if (issued + 3 > p.slots) tell(i + 1);   // (a copy of this round may have to wait)
+        fetch(h, page0, page1);
+        if (v_open && ok) fetch(v_plane, v_page0, v_page1);
+        v_plane = kv_heads + h;
+        v_page0 = page0;
+        v_page1 = page1;
+        v_open = true;
+        if (__shfl_sync(0xffffffffu, last, i) && ok) {
+          fetch(v_plane, v_page0, v_page1);
+          v_open = false;
+        }
+      }
+      tell(n);
+      meta = (meta + n) % kMeta;
+    }
+    if (!ok) fail();
+    // leave no copy in flight
+    for (long j = issued > p.slots ? issued - p.slots : 0; j < issued; ++j) warp_wait(&sh.full[j % p.slots], (uint32_t)((j / p.slots) & 1));
+  } else if (warp == WORK + 1) {
+    // ------------------------------------------------------------------ issuing the products
+    constexpr uint32_t idesc = (1u << 4) | (uint32_t)(NC >> 3) << 17 | (uint32_t)(128 >> 4) << 24;   // e4m3 both, sums in 32 bits
+    constexpr uint32_t idesc_v = idesc | 1u << 15 | 1u << 16;                                       // both operands MN-major
+    const uint64_t desc_k = operand<HD>(16), desc_v = operand<HD>(HD == 64 ? 0 : 16), desc_p = operand<PB>(NC > 128 ? kTile * 128 : 16);
+    const uint32_t ring0 = smem_u32(ring), q_at = smem_u32(Qs), p_at = smem_u32(Ps);
+    int slot = 0;
+    uint32_t phase = 0, q_ph = 0, sfree_ph = 0, p_ph = 0;
+    bool ok = true, first_s = true;
+    auto next = [&]() {
+      __syncwarp();
+      if (++slot == p.slots) { slot = 0; phase ^= 1u; }
+    };
+    auto scores = [&](bool first) {
+      ok = ok && !*(volatile int *)&sh.failed && warp_wait(&sh.full[slot], phase);
+      if (ok && first) {
+        ok = warp_wait(&sh.q_ready, q_ph);
+        q_ph ^= 1u;
+      }
+      if (ok && !first_s) {
+        ok = warp_wait(&sh.s_free, sfree_ph);
+        sfree_ph ^= 1u;
+      }
+      first_s = false;
+      if (!ok) return;
+      tc_fence_after();
+      if (elect_one()) {
+        const uint64_t a = desc_k | (uint64_t)((ring0 + slot * TILE) >> 4), b = desc_k | (uint64_t)(q_at >> 4);
+#pragma unroll
+        for (int k = 0; k < HD / 32; ++k) mma_e4m3(tmem, a + k * 2, b + k * 2, idesc, k > 0);
+        umma_commit(&sh.empty[slot]);
+        umma_commit(&sh.s_full);
+      }
+      next();
+    };
+    auto values = [&]() {
+      ok = ok && !*(volatile int *)&sh.failed && warp_wait_both(&sh.full[slot], phase, &sh.p_full, p_ph);
+      p_ph ^= 1u;
+      if (!ok) return;
+      tc_fence_after();
+      if (elect_one()) {
+        const uint64_t a = desc_v | (uint64_t)((ring0 + slot * TILE) >> 4), b = desc_p | (uint64_t)(p_at >> 4);
+#pragma unroll
+        for (int k = 0; k < kTile / 32; ++k) mma_e4m3(tmem + NC, a + k * (32 * HD >> 4), b + k * (32 * PB >> 4), idesc_v, k > 0);
+        umma_commit(&sh.empty[slot]);
+        umma_commit(&sh.o_full);
+      }
+      next();
+    };
+    for (long t = t_begin; t < t_end && ok;) {
+      const Unit u = unit_of(t);
+      const int n = (int)(min(t_end, u.first + u.n) - t);
+      scores(true);
+      for (int i = 1; i < n && ok; ++i) {
+        scores(false);
+        if (ok) values();
+      }
+      if (ok) values();
+      t += n;
+    }
+    if (!ok) fail();
+  } else {
+    // ------------------------------------------------------------------ softmax warps: thread = key of the tile, then dim of the output
+    const int w = warp & 3, cg = warp >> 2, c0 = cg * NQ, key_t = w * 32 + lane;
+    const uint32_t t_s = tmem + ((uint32_t)(w * 32) << 16) + c0, t_o = t_s + NC;
+    const T *qp = (const T *)p.q;
+    T *outp = (T *)p.out;
+    uint32_t s_ph = 0, o_ph = 0, v_use = 0;   // v_use: ring slots of the units before
+    int meta = 0;
+    uint32_t meta_ph = 0;
+    bool ok = true;
+    auto sync = [&]() { asm volatile("bar.sync 1, %0;" ::"n"(WORK_T) : "memory"); };
+    auto group_sync = [&]() { asm volatile("bar.sync %0, 128;" ::"r"(2 + cg) : "memory"); };
+    const int gt = tid & 127;            // thread of its group
+    if (p.cut && tid == 0) {
+      int4 c = make_int4(0, 0, 0, 0);
+      if (t_begin < t_end && t_end < all) {
+        const Unit u = unit_of(t_end - 1);
+        if (u.first >= t_begin && u.first + u.n > t_end) {
+          entry_at(u.e, &c.x, &c.y);
+          c.z = u.kvh;
+          c.w = (int)((u.first + u.n - 1) / chunk) - (int)blockIdx.x + 1;
+        }
+      }
+      p.cuts[blockIdx.x] = c;
+    }
+    // rows without a tile are in no range: the CTAs share them (an entry whose rows see nothing has no tiles)
+    if (p.cut || all == 0) {
+      for (int e = p.cut ? blockIdx.x : 0; e < n_entries; e += gridDim.x) {
+        if (sh.entry[e + 1].before != sh.entry[e].before) continue;
+        int b, rt;
+        entry_at(e, &b, &rt);
+        const int r1 = min(p.rows, (rt + 1) * RP), h0 = p.cut ? 0 : unit0 % kv_heads, h1 = p.cut ? kv_heads : h0 + 1;
+        for (int r = rt * RP; r < r1; ++r)
+          for (int h = h0; h < h1; ++h)
+            for (int i = tid; i < HD; i += WORK_T)
+              store1(outp + ((long)b * p.window + r / p.group) * p.out_stride + ((long)h * p.group + r % p.group) * HD + i, 0.0f);
+      }
     }
 
-    t = end;
-    // ---- join the warps that share rows
+    for (long t = t_begin; t < t_end;) {
+      const Unit u = unit_of(t);
+      const long u_end = u.first + u.n, end = min(t_end, u_end);
+      const int n = (int)(end - t);
+      int b, rt;
+      entry_at(u.e, &b, &rt);
+      {
+        // ---- queries: a power of two brings a row's largest entry to 128 .. 256, then its planes; a row is HD / 4 lanes
+        constexpr int LANES = HD / 4, PER = 32 / LANES, N = (RP + WORK * PER - 1) / (WORK * PER);
+        const int sub = lane / LANES, d = lane % LANES * 4;
+        float4 x[N];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      total[j] += __shfl_xor_sync(0xffffffffu, total[j], 1);
-      total[j] += __shfl_xor_sync(0xffffffffu, total[j], 2);
-    }
-    work_sync();   // (the unit before has been read)
-    if (t4 == 0) {
-      sh.top[warp][g] = run[0];
-      sh.top[warp][g + 8] = run[1];
-      sh.sum[warp][g] = total[0];
-      sh.sum[warp][g + 8] = total[1];
-    }
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int row = g + 8 * j;
-      float *dst = join + (warp * 16 + row) * HD;
-#pragma unroll
-      for (int c = 0; c < 2; ++c)
-#pragma unroll
-        for (int i = 0; i < NT; i += 4) {
-          const int at = ((2 * t4 + c) * CW + i) / 4;   // of HD / 4 groups of four
-          const int where = HD == 128 ? at ^ (at >> 3 & 3) ^ ((row & 1) << 2) : at ^ (at >> 2 & 3) ^ ((row & 1) << 2);
-          *reinterpret_cast<float4 *>(dst + where * 4) = make_float4(o[i][2 * j + c], o[i + 1][2 * j + c], o[i + 2][2 * j + c], o[i + 3][2 * j + c]);
+        for (int i = 0; i < N; ++i) {
+          const int r = rt * RP + (i * WORK + warp) * PER + sub;
+          x[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          if (r < min(p.rows, (rt + 1) * RP))
+            x[i] = load4<T>(qp + ((long)b * p.window + r / p.group) * p.q_stride + ((long)u.kvh * p.group + r % p.group) * HD + d);
         }
-    }
-    work_sync();
-    if (tid < ROWS) {   // factor of every warp's part of row tid; the row's maximum and sum in place of warp (row group)'s
-      const int w0 = tid / 16, r = tid % 16;
-      float best = -INFINITY;
-      for (int i = 0; i < KG; ++i) best = fmaxf(best, sh.top[i * RG + w0][r]);
-      const float ref = best > -INFINITY ? best : 0.0f;
-      float sum = 0.0f;
-      for (int i = 0; i < KG; ++i) {
-        const float f = exp2_fast(0.5f * (sh.top[i * RG + w0][r] - ref));
-        sh.factor[i * RG + w0][r] = f * f;
-        sum += sh.sum[i * RG + w0][r] * f * f;
-      }
-      sh.top[w0][r] = best;
-      sh.sum[w0][r] = sum;
-    }
-    work_sync();
-    const bool cut = u.first < t_begin || u_end > t_end;
-    const int c0 = cut ? (int)(u.first / chunk) : 0, c1 = cut ? (int)((u_end - 1) / chunk) : 0;
-    auto joined = [&](int r, int at) {   // group `at` of four dims of row r
-      float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-      const int w0 = r / 16, row = r % 16;
-      const int where = HD == 128 ? at ^ (at >> 3 & 3) ^ ((row & 1) << 2) : at ^ (at >> 2 & 3) ^ ((row & 1) << 2);
+        int my_pos = -1;
+        if (tid < RP && rt * RP + tid < p.rows) my_pos = position(b, (rt * RP + tid) / p.group);
+        sync();   // (what the unit before left in shared memory has been read)
+        if (tid < RP) {
+          const int r = rt * RP + tid;
+          sh.pos[tid] = my_pos;
+          sh.out_at[tid] = ((long)b * p.window + r / p.group) * p.out_stride + ((long)u.kvh * p.group + r % p.group) * HD;
+        }
 #pragma unroll
-      for (int i = 0; i < KG; ++i) {
-        const float f = sh.factor[i * RG + w0][row];
-        const float4 x = *reinterpret_cast<const float4 *>(join + ((i * RG + w0) * 16 + row) * HD + where * 4);
-        v.x = fmaf(x.x, f, v.x), v.y = fmaf(x.y, f, v.y), v.z = fmaf(x.z, f, v.z), v.w = fmaf(x.w, f, v.w);
-      }
-      return v;
-    };
-    auto store_row = [&](int r, int at, float4 v, float sum) {
-      const int row = rt * ROWS + r;
-      const int k = row / p.group;
-      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum * two_to(-kUp);   // (weights carry 2^kUp, their sum does not)
-      const bool live = (unsigned)p.in_pos[(long)b * p.window + k] < (unsigned)seq_keys && sum != 0.0f;   // (a NaN among the scores makes the sum NaN)
-      v = live ? make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-      store4(outp + ((long)b * p.window + k) * p.out_stride + ((long)u.kvh * p.group + row % p.group) * HD + at * 4, v);
-    };
-    const int rows_here = min(ROWS, p.rows - rt * ROWS);
-    constexpr int G4 = HD / 4;
-    if (!cut) {
-      for (int i = tid; i < rows_here * G4; i += kWorkWarps * 32) store_row(i / G4, i % G4, joined(i / G4, i % G4), sh.sum[i / G4 / 16][i / G4 % 16]);
-    } else {
-      // this CTA's part: slot 0 of a unit that began before its range, slot 1 of one that goes on behind it
-      constexpr long PART = (long)ROWS * HD;
-      float *stats = p.parts + 2L * kMaxCtas * PART;
-      const int my = 2 * blockIdx.x + (u.first < t_begin ? 0 : 1);
-      for (int i = tid; i < rows_here * G4; i += kWorkWarps * 32) __stcg(reinterpret_cast<float4 *>(p.parts + my * PART) + i, joined(i / G4, i % G4));
-      if (tid < rows_here) __stcg(reinterpret_cast<float2 *>(stats) + my * ROWS + tid, make_float2(sh.top[tid / 16][tid % 16], sh.sum[tid / 16][tid % 16]));
-      __threadfence();
-      work_sync();
-      if (tid == 0) sh.last = atomicAdd(&p.tickets[c0], 1) == c1 - c0;
-      work_sync();
-      if (sh.last) {
-        __threadfence();
-        for (int i = tid; i < rows_here * G4; i += kWorkWarps * 32) {
-          const int r = i / G4;
-          float best = -INFINITY, sum = 0.0f;
-          float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-          for (int c = c0; c <= c1; ++c) {
-            const int from_slot = 2 * c + (c == c0 ? 1 : 0);
-            const float2 ms = __ldcg(reinterpret_cast<const float2 *>(stats) + from_slot * ROWS + r);
-            const float4 x = __ldcg(reinterpret_cast<const float4 *>(p.parts + from_slot * PART) + i);
-            const float now = fmaxf(best, ms.x), ref = now > -INFINITY ? now : 0.0f;
-            const float k2 = exp2_fast(0.5f * (best - ref)), t2 = exp2_fast(0.5f * (ms.x - ref)), keep = k2 * k2, take = t2 * t2;
-            best = now;
-            sum = sum * k2 * k2 + ms.y * t2 * t2;
-            v.x = v.x * keep + x.x * take, v.y = v.y * keep + x.y * take, v.z = v.z * keep + x.z * take, v.w = v.w * keep + x.w * take;
+        for (int i = 0; i < N; ++i) {
+          const int r = (i * WORK + warp) * PER + sub;
+          float v[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+          float top = 0.0f;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            if (fabsf(v[j]) == INFINITY) v[j] = __int_as_float(0x7FFFFFFF);   // (e4m3 has no infinity: its row is NaN, as it would be)
+            top = fmaxf(top, fabsf(v[j]));
           }
-          store_row(r, i % G4, v, sum);
+#pragma unroll
+          for (int o = LANES / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+          int e = top > 0.0f ? 7 - (int)((__float_as_uint(top) >> 23) - 127) : 0;
+          e = max(min(e, 126), -126);   // (entries below 2^-119 lose places)
+          const float up = two_to(e);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[j] *= up;
+          if (r < RP) {
+            if (d == 0) sh.fac[r] = p.scale * two_to(-e);
+#pragma unroll
+            for (int l = 0; l < PL; ++l) {
+              const uint32_t a = e4m3_of_floats(v[0], v[1]), c = e4m3_of_floats(v[2], v[3]);
+              *reinterpret_cast<uint32_t *>(Qs + swizzled<HD>(l * RP + r, d)) = a | c << 16;
+              const float2 fa = floats_of_halves(halves_of_e4m3(a)), fc = floats_of_halves(halves_of_e4m3(c));
+              v[0] = (v[0] - fa.x) * 16.0f, v[1] = (v[1] - fa.y) * 16.0f, v[2] = (v[2] - fc.x) * 16.0f, v[3] = (v[3] - fc.y) * 16.0f;
+            }
+          }
         }
-        if (tid == 0) p.tickets[c0] = 0;
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        sync();
+        if (warp == 0) {   // smallest and largest position of the tile's rows
+          int lo = 0x7FFFFFFF, hi = -1;
+#pragma unroll
+          for (int i = 0; i < (RP + 31) / 32; ++i) {
+            const int at = lane + 32 * i < RP ? sh.pos[lane + 32 * i] : -1;
+            if (at >= 0) lo = min(lo, at);
+            hi = max(hi, at);
+          }
+          lo = __reduce_min_sync(0xffffffffu, lo);
+          hi = __reduce_max_sync(0xffffffffu, hi);
+          if (lane == 0) sh.lo = lo, sh.hi = hi;
+        }
+        sync();
+        if (lane == 0) arrive(&sh.q_ready);
+      }
+      const int lo = sh.lo, hi = sh.hi;
+      const int sliding = p.sliding > 0 ? p.sliding : 0x7FFFFFFF;
+      const int from = hi - sliding;      // keys above are in the window of every row
+      auto sees = [&](int key, int at) { return key <= at && (key > at - sliding || key < p.sinks); };
+
+      float o[NQ], l_acc[NQ];
+#pragma unroll
+      for (int i = 0; i < NQ; ++i) o[i] = l_acc[i] = 0.0f;
+      float my_run = -INFINITY;   // thread i < NQ of a group: the running maximum of its row
+
+      auto add_values = [&](int par) {   // O^T of a tile to this thread's dim, under the maximum after that tile
+        tc_fence_after();
+        if (w * 32 < HD) {
+#pragma unroll
+          for (int c = 0; c < NQ / LD; ++c) {
+            uint32_t x[PL][LD];
+#pragma unroll
+            for (int l = 0; l < PL; ++l) tmem_ld_issue<LD>(t_o + l * RP + c * LD, x[l]);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < LD; i += 4) {
+              const float4 a4 = *reinterpret_cast<const float4 *>(&sh.alpha[par][c0 + c * LD + i]), b4 = *reinterpret_cast<const float4 *>(&sh.beta[par][c0 + c * LD + i]);
+              const float al[4] = {a4.x, a4.y, a4.z, a4.w}, be[4] = {b4.x, b4.y, b4.z, b4.w};
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                float v = __uint_as_float(x[PL - 1][i + j]);
+#pragma unroll
+                for (int l = PL - 2; l >= 0; --l) v = fmaf(v, 0.0625f, __uint_as_float(x[l][i + j]));
+                o[c * LD + i + j] = fmaf(v, be[j], o[c * LD + i + j] * al[j]);
+              }
+            }
+          }
+        }
+        tc_fence_before();
+      };
+      auto add_nans = [&]() {   // rare: entries that are NaN where only some rows see their key
+        const int many = min(sh.n_nan, kTile);
+        for (int i = 0; i < many; ++i) {
+          if (w * 32 >= HD || !(sh.nan_dims[i][w] >> lane & 1u)) continue;
+#pragma unroll
+          for (int q = 0; q < NQ; ++q)
+            if (sees(sh.nan_key[i], sh.pos[c0 + q])) o[q] = __int_as_float(0x7FFFFFFF);
+        }
+      };
+
+      for (int i = 0; i < n; ++i) {
+        const int par = i & 1;
+        ok = ok && !*(volatile int *)&sh.failed;
+        if (ok && !(warp_wait(&sh.meta_full[meta], meta_ph) && warp_wait(&sh.s_full, s_ph))) {
+          ok = false;
+          fail();
+        }
+        const Meta &m = sh.meta[meta];   // (not written again before this tile is done)
+        if (++meta == kMeta) { meta = 0; meta_ph ^= 1u; }
+        s_ph ^= 1u;
+        tc_fence_after();
+        // ---- scores
+        const int key = m.key0 + key_t, half = key_t >> 6;
+        const int ev = pool_exp((int8_t)(m.v_exp[half] >> (8 * (key_t >> 4 & 3))));
+        const float k2 = two_to(pool_exp((int8_t)(m.k_exp[half] >> (8 * (key_t >> 4 & 3))))), add = (float)ev;
+        const bool whole = m.pages == 3 && m.key0 + kTile - 1 <= lo && (m.key0 > from || m.key0 + kTile <= p.sinks);
+        float s[NQ];
+#pragma unroll
+        for (int c = 0; c < NQ / LD; ++c) {
+          uint32_t x[PL][LD];
+#pragma unroll
+          for (int l = 0; l < PL; ++l) tmem_ld_issue<LD>(t_s + l * RP + c * LD, x[l]);
+          tmem_ld_wait();
+#pragma unroll
+          for (int j = 0; j < LD; j += 4) {
+            const float4 f4 = *reinterpret_cast<const float4 *>(&sh.fac[c0 + c * LD + j]);
+            const float f[4] = {f4.x, f4.y, f4.z, f4.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              float v = __uint_as_float(x[PL - 1][j + k]);
+#pragma unroll
+              for (int l = PL - 2; l >= 0; --l) v = fmaf(v, 0.0625f, __uint_as_float(x[l][j + k]));
+              s[c * LD + j + k] = fmaf(v * k2, f[k], add);
+            }
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) arrive(&sh.s_free);
+        if (!whole) {
+          const bool there = m.pages >> half & 1;
+          bool missed = false;
+#pragma unroll
+          for (int q = 0; q < NQ; ++q) {
+            const bool in = sees(key, sh.pos[c0 + q]);
+            missed |= in && !there;
+            if (!in || !there) s[q] = -INFINITY;
+          }
+          if (missed) pool_fault(p.pool.status, SJD_ERR_BAD_ARG);   // (no page where some row sees a key)
+        }
+        // ---- the tile's maximum of every row
+#pragma unroll
+        for (int q = 0; q < NQ; q += 4) {
+          float4 v;
+          v.x = max_of_warp(s[q]), v.y = max_of_warp(s[q + 1]), v.z = max_of_warp(s[q + 2]), v.w = max_of_warp(s[q + 3]);
+          if (lane == 0) *reinterpret_cast<float4 *>(&sh.red[w][c0 + q]) = v;
+        }
+        // exponents that differ so much that weights, but not the terms of the sum, may leave the range
+        {
+          const int e_min = __reduce_min_sync(0xffffffffu, ev), e_max = __reduce_max_sync(0xffffffffu, ev);
+          if (lane == 0) sh.exp_range[cg][par][w] = e_max << 16 | (e_min & 0xFFFF);
+          if (gt == 0) sh.wide[cg][par] = 0;
+        }
+        group_sync();
+        if (gt < NQ) {
+          const int r = c0 + gt;
+          const float mx = fmaxf(fmaxf(sh.red[0][r], sh.red[1][r]), fmaxf(sh.red[2][r], sh.red[3][r]));
+          const float now = fmaxf(my_run, mx), at = now > -INFINITY ? now : 0.0f;
+          // (by way of the roots: with the values' exponents a maximum may move by 200, and the sum by as much the other way)
+          const float a = exp2_fast(0.5f * (my_run - at)), c = exp2_fast(0.5f * (mx - at));
+          sh.ref[r] = (mx > -INFINITY ? mx : 0.0f) - (float)kUp;
+          sh.alpha[par][r] = a * a;
+          sh.beta[par][r] = c * c;
+          sh.alpha_root[par][r] = a;
+          sh.beta_root[par][r] = c;
+          if ((my_run > -INFINITY && my_run - at < -64.0f) || (mx > -INFINITY && mx - at < -64.0f)) sh.wide[cg][par] = 1;
+          my_run = now;
+          if (gt == 0) {
+            int e_min = 127, e_max = -128;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              e_max = max(e_max, sh.exp_range[cg][par][j] >> 16);
+              e_min = min(e_min, (int)(int16_t)sh.exp_range[cg][par][j]);
+            }
+            if (e_max - e_min > 64) sh.wide[cg][par] = 1;
+          }
+        }
+        group_sync();
+        // ---- weights and their sum without the values' exponents
+        uint32_t pk[PL][NQ / 4];
+        const float back = two_to(-ev - kUp);   // (the sum goes without 2^kUp)
+        const bool wide = sh.wide[cg][par] != 0;
+        if (wide) {
+#pragma unroll
+          for (int q = 0; q < NQ; ++q) {
+            const float ar = sh.alpha_root[par][c0 + q], br = sh.beta_root[par][c0 + q];
+            l_acc[q] = l_acc[q] * ar * ar + exp2_fast(s[q] - add - sh.ref[c0 + q] - (float)kUp) * br * br;
+          }
+        }
+#pragma unroll
+        for (int q = 0; q < NQ; q += 4) {
+          const float4 r = *reinterpret_cast<const float4 *>(&sh.ref[c0 + q]);
+          s[q] = exp2_fast(s[q] - r.x), s[q + 1] = exp2_fast(s[q + 1] - r.y), s[q + 2] = exp2_fast(s[q + 2] - r.z), s[q + 3] = exp2_fast(s[q + 3] - r.w);
+        }
+        if (!wide) {
+#pragma unroll
+          for (int q = 0; q < NQ; q += 4) {
+            const float4 a = *reinterpret_cast<const float4 *>(&sh.alpha[par][c0 + q]), c = *reinterpret_cast<const float4 *>(&sh.beta[par][c0 + q]);
+            l_acc[q] = fmaf(s[q] * back, c.x, l_acc[q] * a.x);
+            l_acc[q + 1] = fmaf(s[q + 1] * back, c.y, l_acc[q + 1] * a.y);
+            l_acc[q + 2] = fmaf(s[q + 2] * back, c.z, l_acc[q + 2] * a.z);
+            l_acc[q + 3] = fmaf(s[q + 3] * back, c.w, l_acc[q + 3] * a.w);
+          }
+        }
+#pragma unroll
+        for (int q = 0; q < NQ; q += 4) {
+          uint32_t lo2[PL], hi2[PL];
+          weight_planes<PL>(s[q], s[q + 1], lo2);
+          weight_planes<PL>(s[q + 2], s[q + 3], hi2);
+#pragma unroll
+          for (int l = 0; l < PL; ++l) pk[l][q / 4] = lo2[l] | hi2[l] << 16;
+        }
+        // ---- the tile before is multiplied: its O^T is there, and P may be written
+        if (i > 0) {
+          if (ok && !warp_wait(&sh.o_full, o_ph)) {
+            ok = false;
+            fail();
+          }
+          o_ph ^= 1u;
+        }
+#pragma unroll
+        for (int l = 0; l < PL; ++l) {
+          constexpr int STEP = NQ < 16 ? NQ : 16;
+#pragma unroll
+          for (int q = 0; q < NQ; q += STEP) {
+            const uint32_t col = l * RP + c0 + q;
+            uint8_t *dst = Ps + (col / 128) * (kTile * 128) + swizzled<PB>(key_t, col % 128);
+            if constexpr (STEP == 16) *reinterpret_cast<uint4 *>(dst) = make_uint4(pk[l][q / 4], pk[l][q / 4 + 1], pk[l][q / 4 + 2], pk[l][q / 4 + 3]);
+            else *reinterpret_cast<uint2 *>(dst) = make_uint2(pk[l][q / 4], pk[l][q / 4 + 1]);
+          }
+        }
+        if (i > 0) {
+          add_values(par ^ 1);
+          if (sh.n_nan > 0) add_nans();   // (of the tile before)
+        }
+        if (!whole) {
+          // A key that some row does not see must not reach it: a weight of zero times NaN would.  NaN entries become zero, and
+          // the rows that see them get their NaN afterwards.
+          sync();   // (what the tile before left in the list has been read)
+          if (tid == 0) sh.n_nan = 0;
+          sync();
+          if (cg == 0) {
+            const uint32_t use = v_use + (i < n - 1 ? 2 * i + 2 : 2 * n - 1);
+            if (ok && !warp_wait(&sh.full[use % p.slots], use / p.slots & 1)) {
+              ok = false;
+              fail();
+            }
+            uint8_t *v = ring + (use % p.slots) * TILE;
+            uint32_t dims[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int c = 0; c < HD / 16; ++c) {
+              uint4 *at = reinterpret_cast<uint4 *>(v + swizzled<HD>(key_t, c * 16));
+              uint4 x = *at;
+              uint32_t *xs = reinterpret_cast<uint32_t *>(&x);
+              if (has_nan(x.x) || has_nan(x.y) || has_nan(x.z) || has_nan(x.w)) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                  const uint32_t nan = ((xs[j] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;   // the top bit of every NaN byte
+                  xs[j] &= ~((nan >> 7) * 0xFFu);
+                  dims[c >> 1] |= ((nan >> 7 & 1u) | (nan >> 14 & 2u) | (nan >> 21 & 4u) | (nan >> 28 & 8u)) << ((c & 1) * 16 + j * 4);
+                }
+                *at = x;
+              }
+            }
+            if ((dims[0] | dims[1] | dims[2] | dims[3]) != 0 && key <= hi && (m.pages >> half & 1)) {
+              const int at = atomicAdd(&sh.n_nan, 1);
+              sh.nan_key[at] = key;
+#pragma unroll
+              for (int j = 0; j < 4; ++j) sh.nan_dims[at][j] = dims[j];
+            }
+          }
+          sync();
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) arrive(&sh.p_full);
+      }
+      v_use += 2 * n;
+      t = end;
+
+      // ---- sums over the keys, while the last tile is multiplied
+      {
+        const float v = lanes_sum<NQ>(l_acc);
+        if (lane < NQ) sh.red[w][c0 + lane] = v;
+      }
+      group_sync();
+      const bool cut = u.first < t_begin || u_end > t_end;
+      const int rows_here = min(RP, p.rows - rt * RP), dim = w * 32 + lane;
+      constexpr long PART = (long)RP * HD;
+      // this CTA's part of a cut unit: slot 0 of a unit that began before its range, slot 1 of one that goes on behind it
+      const int my = 2 * blockIdx.x + (u.first < t_begin ? 0 : 1);
+      if (gt < NQ) {
+        const int r = c0 + gt;
+        const float sum = (sh.red[0][r] + sh.red[1][r]) + (sh.red[2][r] + sh.red[3][r]);
+        sh.inv[r] = sh.pos[r] >= 0 && sum != 0.0f ? two_to(-kUp) / sum : 0.0f;   // (a NaN among the scores makes the sum NaN)
+        if (cut) p.stats[my * RP + r] = make_float2(my_run, sum);
+      }
+      if (ok && !warp_wait(&sh.o_full, o_ph)) {
+        ok = false;
+        fail();
+      }
+      o_ph ^= 1u;
+      add_values(n - 1 & 1);
+      if (sh.n_nan > 0) add_nans();
+      sync();
+      if (tid == 0) sh.n_nan = 0;
+      if (w * 32 < HD) {
+        if (!cut) {
+#pragma unroll
+          for (int q = 0; q < NQ; ++q) {
+            const float inv = sh.inv[c0 + q];
+            if (c0 + q < rows_here) store1(outp + sh.out_at[c0 + q] + dim, inv == 0.0f ? 0.0f : o[q] * inv);
+          }
+        } else {
+#pragma unroll
+          for (int q = 0; q < NQ; ++q)
+            if (c0 + q < rows_here) p.parts[my * PART + (c0 + q) * HD + dim] = o[q];
+        }
       }
     }
   }
+
+  tc_fence_before();
+  __syncthreads();
+  if (warp == WORK + 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(T_COLS) : "memory");
+  }
 }
 
-// the layer's pages as boxes of 32 rows of a plane
+// Joins the parts of the unit that begins in range blockIdx.x and is cut: a warp per row.
+constexpr int kJoinWarps = 8;
+template <typename T, int HD>
+__global__ void __launch_bounds__(kJoinWarps * 32) pool_attention_join_kernel(const __grid_constant__ PoolAttnParams p, int RP) {
+  pdl_wait();
+  const int4 c = p.cuts[blockIdx.x];
+  const int lane = threadIdx.x & 31, r = blockIdx.y * kJoinWarps + (threadIdx.x >> 5), row = c.y * RP + r;
+  if (c.w < 2 || r >= RP || row >= p.rows) return;
+  auto slot_of = [&](int i) { return 2 * ((int)blockIdx.x + i) + (i == 0 ? 1 : 0); };
+  const int k = row / p.group, at = p.in_pos[(long)c.x * p.window + k];
+  float best = -INFINITY, sum = 0.0f;
+  float2 ms = make_float2(-INFINITY, 0.0f);
+  for (int i = lane; i < c.w; i += 32) {
+    ms = p.stats[slot_of(i) * RP + r];
+    best = fmaxf(best, ms.x);
+  }
+  best = warp_max(best);
+  if (best == -INFINITY) best = 0.0f;
+  constexpr int D = HD / 32, U = 8;
+  float acc[D];
+#pragma unroll
+  for (int d = 0; d < D; ++d) acc[d] = 0.0f;
+  for (int base = 0; base < c.w; base += 32) {
+    const int n = min(32, c.w - base);
+    float f = 0.0f;
+    if (lane < n) {
+      if (c.w > 32) ms = p.stats[slot_of(base + lane) * RP + r];
+      f = exp2_fast(0.5f * (ms.x - best));   // (its root: see the sums' range)
+      sum += ms.y * f * f;
+      f *= f;
+    }
+    for (int i = 0; i < n; i += U) {
+      float x[U][D];
+#pragma unroll
+      for (int j = 0; j < U; ++j) {
+        const float *src = p.parts + ((long)slot_of(base + min(i + j, n - 1)) * RP + r) * HD + lane * D;
+        if constexpr (D == 4) {
+          const float4 v = *reinterpret_cast<const float4 *>(src);
+          x[j][0] = v.x, x[j][1] = v.y, x[j][2] = v.z, x[j][3] = v.w;
+        } else {
+          const float2 v = *reinterpret_cast<const float2 *>(src);
+          x[j][0] = v.x, x[j][1] = v.y;
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < U; ++j) {
+        const float w = __shfl_sync(0xffffffffu, f, i + j < n ? i + j : 0);
+        if (i + j < n) {
+#pragma unroll
+          for (int d = 0; d < D; ++d) acc[d] = fmaf(x[j][d], w, acc[d]);
+        }
+      }
+    }
+  }
+  sum = warp_sum(sum);
+  const bool live = (unsigned)at < (unsigned)(p.pool.pages_per_seq * KV_PAGE) && sum != 0.0f;
+  const float inv = live ? two_to(-kUp) / sum : 0.0f;
+  T *dst = (T *)p.out + ((long)c.x * p.window + k) * p.out_stride + ((long)c.z * p.group + row % p.group) * HD + lane * D;
+#pragma unroll
+  for (int d = 0; d < D; ++d) acc[d] = live ? acc[d] * inv : 0.0f;
+  if constexpr (D == 4) store4(dst, make_float4(acc[0], acc[1], acc[2], acc[3]));
+  else store1(dst, acc[0]), store1(dst + 1, acc[1]);
+}
+
+// the layer's pages as boxes of 64 rows of a plane
 int make_pool_map(TensorMap *out, const sjd_pool &p, int layer) {
   EncodeTiledFn fn = encode_fn();
   if (!fn) return SJD_ERR_UNSUPPORTED;
   const cuuint64_t plane = (cuuint64_t)KV_PAGE * p.head_dim, planes = 2ull * p.n_kv_heads;
   cuuint64_t dims[4] = {(cuuint64_t)p.head_dim, (cuuint64_t)KV_PAGE, planes, (cuuint64_t)p.n_pages};
   cuuint64_t strides[3] = {(cuuint64_t)p.head_dim, plane, plane * planes * p.n_layers};
-  cuuint32_t box[4] = {(cuuint32_t)p.head_dim, (cuuint32_t)kTile, 1, 1};
+  cuuint32_t box[4] = {(cuuint32_t)p.head_dim, (cuuint32_t)KV_PAGE, 1, 1};
   cuuint32_t estr[4] = {1, 1, 1, 1};
   const CUresult r = fn(reinterpret_cast<CUtensorMap *>(out), CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, (uint8_t *)p.pages + plane * planes * layer,
                         dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
@@ -755,8 +1026,14 @@ int make_pool_map(TensorMap *out, const sjd_pool &p, int layer) {
   return r == CUDA_SUCCESS ? SJD_OK : SJD_ERR_UNSUPPORTED;
 }
 
-int row_groups(int rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : rows <= 64 ? 4 : 8; }
-size_t parts_bytes(int rg, int hd) { return 2ull * kMaxCtas * 16 * rg * (hd + 2) * 4; }
+// rows of a unit's tile
+int tile_rows(int64_t rows, int dtype) {
+  const int least = dtype == SJD_F32 ? 8 : 16;
+  return rows <= least ? least : rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+}
+constexpr size_t kCutBytes = kMaxCtas * sizeof(int4);
+size_t stat_bytes(int rp) { return 2ull * kMaxCtas * rp * sizeof(float2); }
+size_t parts_bytes(int rp, int hd) { return 2ull * kMaxCtas * rp * hd * sizeof(float); }
 
 }  // namespace
 }  // namespace sjd
@@ -765,8 +1042,8 @@ using namespace sjd;
 
 extern "C" size_t sjd_pool_attention_workspace_bytes(const sjd_pool *pool, int window, int n_heads) {
   if (check_pool(pool, false) != SJD_OK || window < 1 || n_heads < 1 || n_heads % pool->n_kv_heads != 0) return 0;
-  const int64_t rows = (int64_t)window * (n_heads / pool->n_kv_heads);
-  return 1024 + parts_bytes(row_groups(rows > 128 ? 128 : (int)rows), pool->head_dim);
+  const int rp = tile_rows((int64_t)window * (n_heads / pool->n_kv_heads), SJD_BF16);
+  return kCutBytes + stat_bytes(rp) + parts_bytes(rp, pool->head_dim);
 }
 
 extern "C" int sjd_pool_attention(const sjd_pool *pool, int layer, int batch, int window, int n_heads, int dtype, const void *q,
@@ -792,7 +1069,7 @@ extern "C" int sjd_pool_attention(const sjd_pool *pool, int layer, int batch, in
   TensorMap map;
   rc = make_pool_map(&map, *pool, layer);
   if (rc != SJD_OK) return rc;
-  const int rg = row_groups(rows > 128 ? 128 : (int)rows), hd = pool->head_dim;
+  const int rp = tile_rows(rows, dtype), hd = pool->head_dim;
   PoolAttnParams p;
   memset(&p, 0, sizeof(p));
   p.pool = *pool;
@@ -802,7 +1079,7 @@ extern "C" int sjd_pool_attention(const sjd_pool *pool, int layer, int batch, in
   p.n_heads = n_heads;
   p.group = group;
   p.rows = (int)rows;
-  p.row_tiles = (int)((rows + 16 * rg - 1) / (16 * rg));
+  p.row_tiles = (int)((rows + rp - 1) / rp);
   p.sliding = sliding;
   p.sinks = sliding > 0 ? sinks : 0;
   p.scale = (scale > 0.0f ? scale : 1.0f / sqrtf((float)hd)) * 1.4426950408889634f;
@@ -812,30 +1089,45 @@ extern "C" int sjd_pool_attention(const sjd_pool *pool, int layer, int batch, in
   p.seqs = seqs;
   p.in_pos = in_pos;
   p.out = out;
-  p.tickets = (int *)ws;
-  p.parts = (float *)((char *)ws + 1024);
+  p.cuts = (int4 *)ws;
+  p.stats = (float2 *)((char *)ws + kCutBytes);
+  p.parts = (float *)((char *)ws + kCutBytes + stat_bytes(rp));
   const int64_t entries = (int64_t)batch * p.row_tiles, units = entries * pool->n_kv_heads;
   if (units > 0x7FFFFFFF) return SJD_ERR_CAPACITY;
-  // Equal ranges, unless the CTAs would have to look at too many positions to find them: then there are units enough
-  p.cut = entries <= kMaxEntries && (int64_t)batch * window <= 8192;
+  // A CTA per unit where units are short and few (the joining launch costs more than it could win: 2 us), or where the CTAs would have
+  // to look at too many positions to find equal ranges (then there are units enough); else equal ranges.
+  int64_t most = ((int64_t)pool->pages_per_seq * KV_PAGE + kTile - 1) / kTile;   // tiles of a unit
+  if (sliding > 0) {
+    const int64_t in = ((int64_t)sliding + window + kTile - 2) / kTile + 1 + ((int64_t)sinks + kTile - 1) / kTile;
+    most = most < in ? most : in;
+  }
+  p.cut = entries <= kMaxEntries && (int64_t)batch * window <= 8192 && (most > kWholeTiles || units > 2 * sms);
   p.n_entries = (int)entries;
-  const int box = kTile * hd, fixed = kWorkWarps * 16 * hd * 4 + (int)sizeof(AttnShared<128>);
-  p.slots = (kSmem - 1024 - fixed) / (2 * box);
-  p.slots = p.slots > kMaxSlots ? kMaxSlots : p.slots;
-  const size_t smem = (size_t)fixed + (size_t)p.slots * 2 * box;
-  const unsigned grid = p.cut ? (unsigned)(sms < kMaxCtas ? sms : kMaxCtas) : (unsigned)units;
   const CUtensorMap &m = reinterpret_cast<const CUtensorMap &>(map);
-  auto launch = [&](auto kernel) -> int {
-    const int r = allow_smem(kernel, smem);   // (the size follows from the kernel's head_dim)
+  auto launch = [&](auto kernel, auto join, int RP, int PL, size_t shared) -> int {
+    const int per_sm = ctas_of(RP), tile = kTile * hd, fixed = PL * RP * (kTile + hd) + (int)shared;
+    p.slots = (232448 / per_sm - 1024 - fixed) / tile;   // (1 KB of an SM's shared memory goes to every CTA)
+    p.slots = p.slots > kMaxSlots ? kMaxSlots : p.slots;
+    const size_t smem = (size_t)fixed + (size_t)p.slots * tile;
+    const int r = allow_smem(kernel, smem);   // (the size follows from the kernel's types and sizes)
     if (r != SJD_OK) return r;
-    SJD_CUDA(launch_kernel(kernel, dim3(grid), dim3(kThreads), smem, (cudaStream_t)cuda_stream, m, p));
+    const int ctas = sms * per_sm < kMaxCtas ? sms * per_sm : kMaxCtas;
+    SJD_CUDA(launch_kernel(kernel, dim3(p.cut ? (unsigned)ctas : (unsigned)units), dim3(threads_of(RP)), smem, (cudaStream_t)cuda_stream, m, p));
+    SJD_CHECK_LAUNCH();
+    if (!p.cut) return SJD_OK;
+    g_pdl = true;   // (waits for the launch before it itself)
+    const cudaError_t e = launch_kernel(join, dim3((unsigned)ctas, (unsigned)((RP + kJoinWarps - 1) / kJoinWarps)), dim3(kJoinWarps * 32), 0,
+                                        (cudaStream_t)cuda_stream, p, RP);
+    g_pdl = false;
+    SJD_CUDA(e);
     SJD_CHECK_LAUNCH();
     return SJD_OK;
   };
-#define SJD_PICK(T, HD) \
-  (rg == 1 ? launch(pool_attention_kernel<T, HD, 1>) : rg == 2 ? launch(pool_attention_kernel<T, HD, 2>) \
-   : rg == 4 ? launch(pool_attention_kernel<T, HD, 4>) : launch(pool_attention_kernel<T, HD, 8>))
-  if (dtype == SJD_F32) return hd == 128 ? SJD_PICK(float, 128) : SJD_PICK(float, 64);
-  return hd == 128 ? SJD_PICK(__nv_bfloat16, 128) : SJD_PICK(__nv_bfloat16, 64);
+#define SJD_PICK(T, PL, HD, RP) launch(pool_attention_kernel<T, HD, RP>, pool_attention_join_kernel<T, HD>, RP, PL, sizeof(PoolAttnShared<RP>))
+#define SJD_PICK_ROWS(T, PL, RP) (hd == 128 ? SJD_PICK(T, PL, 128, RP) : SJD_PICK(T, PL, 64, RP))
+  if (dtype == SJD_F32)
+    return rp == 8 ? SJD_PICK_ROWS(float, 4, 8) : rp == 16 ? SJD_PICK_ROWS(float, 4, 16) : rp == 32 ? SJD_PICK_ROWS(float, 4, 32) : SJD_PICK_ROWS(float, 4, 64);
+  return rp == 16 ? SJD_PICK_ROWS(__nv_bfloat16, 2, 16) : rp == 32 ? SJD_PICK_ROWS(__nv_bfloat16, 2, 32) : SJD_PICK_ROWS(__nv_bfloat16, 2, 64);
 #undef SJD_PICK
+#undef SJD_PICK_ROWS
 }

@@ -56,17 +56,19 @@ def _filled(lens, n_layers, kvh, hd, seed, spare=3, per_seq=None, exps=(-8, -5),
 
 # ------------------------------------------------------------------------------------------------------------ attention
 def _bound(dtype, want):
-    """Most that an output may be off.  A weight is one fp16 number (bf16 calls), half a step being 2^-11 of it, or two (fp32): 2^-22.  The
-    row's maximum so far weighs 2^13 to 2^15 and the smallest step of fp16 is 2^-24: half of it is 2^-38 of the maximum's weight (fp32
-    calls: the same, under the first number's).  A query's entry is exact (bf16) or off by 2^-22 of it (fp32), and by 2^-32 of the row's
-    largest, which is 2^7 to 2^8; a score has about 32 fp32 additions (2^-24 of their magnitudes each) and counts twice, in the numerator
-    and in the sum.  Sums over the keys: two roundings a step of 16 keys, up to 200 steps of a warp and the merges, 2^-15.  The output's own
+    """Most that an output may be off.  A weight's planes leave 2^-8 (bf16: two) or 2^-16 (fp32: four) of it, half a step of e4m3 being
+    2^-4 of a number; its conversion to fp16 before leaves 2^-11 (bf16; with fp32 the planes hold that rest too).  The largest weight of a
+    row in a tile of 128 keys is 2^8 and the smallest step of e4m3 2^-9, under the last plane's factor (2^-4, fp32 2^-12): half of it is 2^-22
+    resp. 2^-30 of that weight.  A query's planes leave 2^-16 of an entry (fp32; bf16: nothing) and the same floors of the row's
+    largest; a score has about 20 fp32 additions (2^-24 of their magnitudes each) and counts twice, in the numerator and in the sum.  Sums
+    over the keys: a tile's products and two roundings a tile, up to 800 tiles of a sequence and the merges, 2^-15.  The output's own
     rounding: half a step."""
     out, mass, floor, reach, flat = want
-    two = dtype == "f32"
-    score = flat * 2.0 ** -32 + reach * ((2.0 ** -22 if two else 0.0) + 2.0 ** -19)
-    return 1.02 * (((2.0 ** -22 if two else 2.0 ** -11) + 2 * score[..., None] + 2.0 ** -15) * mass + floor * 2.0 ** -38) \
-        + (2.0 ** -24 if two else 2.0 ** -8) * np.abs(out) + 1e-35
+    two = dtype == "bf16"
+    low = 2.0 ** -22 if two else 2.0 ** -30
+    score = flat * low + reach * (2.0 ** -19 if two else 2.0 ** -16 + 2.0 ** -19)
+    weight = 2.0 ** -8 + 2.0 ** -11 if two else 2.0 ** -16
+    return 1.02 * ((weight + 2 * score[..., None] + 2.0 ** -15) * mass + floor * low) + (2.0 ** -8 if two else 2.0 ** -24) * np.abs(out) + 1e-35
 
 
 def _check_attention(pool, q, in_pos, window, dtype, sliding=0, sinks=0, scale=0.0, seqs=None, layer=0, out=None, ref=None):
@@ -85,7 +87,7 @@ def _check_attention(pool, q, in_pos, window, dtype, sliding=0, sinks=0, scale=0
         if p < 0:
             assert (got[m] == 0).all()
     norm = np.linalg.norm(want)
-    if norm > 0:   # (without the second fp16 number fp32 calls would be off by about 2^-13)
+    if norm > 0:   # (a plane less would leave about 2^-5 resp. 2^-16 of the weights, and 2^-4 resp. 2^-12 of every query's entries)
         assert np.linalg.norm(got - want) / norm <= (2.0 ** -8 if dtype == "bf16" else 2.0 ** -18)
     return out
 
