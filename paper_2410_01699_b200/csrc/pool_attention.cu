@@ -3,9 +3,9 @@
 // Keys and values stay in 8 bits: tcgen05 multiplies e4m3 by e4m3 (kind::f8f6f4, products exact, sums in 32 bits), K and V as TMA left them.
 // Keys are the rows of both products and the queries their columns, because few queries meet many keys:
 //   S^T [128 keys x NC]  =  K [128 keys x HD] . Q^T          O^T [HD x NC]  =  V^T [HD x 128 keys] . P
-// Queries and weights are e4m3 numbers too, but several of them: x = x1 + 2^-4 x2 (+ 2^-8 x3 + 2^-12 x4), x1 = e4m3(x), x2 = e4m3(16 (x - x1))
-// and so on.  The planes are columns of the same product, added when they are read from tensor memory.  n planes leave 2^-4n of a
-// number at most (half a step of e4m3 is 2^-4 of it) and about 2^-5.3n on average: two for bf16 queries, whose eight bits they hold
+// Queries and weights are e4m3 numbers too, but several of them: x = x1 + x2 (+ 2^-8 (x3 + x4)), x1 = e4m3(x), x2 = e4m3(x - x1),
+// x3 = e4m3(256 (x - x1 - x2)) and so on.  The planes are columns of one product, added when they are read from tensor memory (as more
+// products into the same columns they read K and V once more each: 8 x 32 rows 108 -> 113 us).  n planes leave 2^-4n of a number at most (half a step of e4m3 is 2^-4 of it) and about 2^-5.3n on average: two for bf16 queries, whose eight bits they hold
 // exactly, four for fp32.  (mma.sync has e4m3 as well, but here it converts both operands for every product: 700 products a clock and SM.
 // With conversions in registers and fp16 products: 8 x 32 rows x 4009 keys of 32 heads, fp32, 130 us, 32 tokens of up to 4224 keys 63.)
 //
@@ -41,6 +41,7 @@ constexpr int kUp = 8;               // the largest weight of a row in a tile is
 struct PoolAttnParams {
   sjd_pool pool;
   int layer, batch, window, n_heads, group, rows, row_tiles;   // rows: window * group
+  unsigned group_inv;           // 2^32 / group, rounded up: exact for the few rows beside a tile's first
   int sliding, sinks;
   float scale;                  // times log2(e)
   const void *q;
@@ -68,7 +69,7 @@ struct Entry {   // (sequence, tile of rows)
 struct Meta {    // of a tile that is being fetched
   int key0;
   int k_exp[2], v_exp[2];   // exponents of its two pages' blocks
-  int pages;                // bit j: page j is there
+  int pages;                // bit j: page j is there; bit 2: values' exponents of them more than 64 apart
 };
 
 template <int RP>
@@ -77,35 +78,36 @@ struct PoolAttnShared {
   uint64_t meta_full[kMeta];
   uint64_t q_ready, s_full, s_free, p_full, o_full;
   uint32_t tmem_base;
-  int failed, wide[4][2], exp_range[4][2][4], n_nan, lo, hi;
+  int failed, wide[4][2], n_nan;
   Meta meta[kMeta];
   alignas(16) float red[4][RP];   // (these are read and written four at a time)
-  alignas(16) float ref[RP];
-  alignas(16) float fac[RP];
+  alignas(16) float up[RP];       // kUp - the tile's maximum
+  alignas(16) float fac[2][RP];   // of this unit and the next (as pos and out_at)
   alignas(16) float alpha[2][RP];
   alignas(16) float beta[2][RP];
   float alpha_root[2][RP], beta_root[2][RP], inv[RP];
-  int pos[RP];
-  long out_at[RP];             // first entry of a row in out
+  int pos[2][RP];
+  long out_at[2][RP];          // first entry of a row in out
   int nan_key[kTile];
   uint32_t nan_dims[kTile][4];
   Entry entry[kMaxEntries + 1];
 };
 
-__device__ __forceinline__ uint32_t e4m3_of_floats(float a, float b) {   // a in the low byte
-  uint16_t r;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(b), "f"(a));
+__device__ __forceinline__ uint32_t e4m3_of_floats(const float *v) {   // four, the first one in the low byte
+  uint32_t r;
+  asm("{\n\t.reg .b16 x, y;\n\tcvt.rn.satfinite.e4m3x2.f32 x, %2, %1;\n\tcvt.rn.satfinite.e4m3x2.f32 y, %4, %3;\n\tmov.b32 %0, {x, y};\n\t}"
+      : "=r"(r)
+      : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]));
   return r;
 }
-__device__ __forceinline__ uint32_t e4m3_of_halves(uint32_t h) {
-  uint16_t r;
-  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(h));
+// four numbers in a word, from and to two pairs of fp16
+__device__ __forceinline__ uint32_t e4m3_of_halves(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("{\n\t.reg .b16 x, y;\n\tcvt.rn.satfinite.e4m3x2.f16x2 x, %1;\n\tcvt.rn.satfinite.e4m3x2.f16x2 y, %2;\n\tmov.b32 %0, {x, y};\n\t}" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
-__device__ __forceinline__ uint32_t halves_of_e4m3(uint32_t v) {
-  uint32_t h;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)v));
-  return h;
+__device__ __forceinline__ void halves_of_e4m3(uint32_t v, uint32_t &a, uint32_t &b) {
+  asm("{\n\t.reg .b16 x, y;\n\tmov.b32 {x, y}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, x;\n\tcvt.rn.f16x2.e4m3x2 %1, y;\n\t}" : "=r"(a), "=r"(b) : "r"(v));
 }
 __device__ __forceinline__ uint32_t halves_of_floats(float a, float b) {
   uint32_t h;
@@ -117,16 +119,37 @@ __device__ __forceinline__ float2 floats_of_halves(uint32_t h) {
   asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %2;\n\tcvt.f32.f16 %0, lo;\n\tcvt.f32.f16 %1, hi;\n\t}" : "=f"(f.x), "=f"(f.y) : "r"(h));
   return f;
 }
-// 16 (a - b) of halves, exact where b is a's e4m3 number
-__device__ __forceinline__ uint32_t rest_of_halves(uint32_t a, uint32_t b) {
+__device__ __forceinline__ uint32_t sub_halves(uint32_t a, uint32_t b) {
   uint32_t r;
-  asm("{\n\t.reg .b32 d;\n\tsub.rn.f16x2 d, %1, %2;\n\tmul.rn.f16x2 %0, d, %3;\n\t}" : "=r"(r) : "r"(a), "r"(b), "r"(0x4C004C00u));
+  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
-__device__ __forceinline__ uint32_t add_halves(uint32_t a, uint32_t b) {
+__device__ __forceinline__ uint32_t fma_halves(uint32_t a, uint32_t b, uint32_t c) {
   uint32_t r;
-  asm("add.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
   return r;
+}
+// two fp32 operations an instruction
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\tfma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
 }
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
@@ -187,20 +210,25 @@ __device__ __forceinline__ float lanes_sum(float *v) {
   return v[0];
 }
 
-// weights of two rows as e4m3 planes: planes[i] gets a 16-bit pair
+// weights of four rows as e4m3 planes, a word each
 template <int PL>
-__device__ __forceinline__ void weight_planes(float a, float b, uint32_t *planes) {
-  const uint32_t h = halves_of_floats(a, b);
-  planes[0] = e4m3_of_halves(h);
-  uint32_t rest = rest_of_halves(h, halves_of_e4m3(planes[0]));
-  planes[1] = e4m3_of_halves(rest);
+__device__ __forceinline__ void weight_planes(float2 v, float2 w, uint32_t *planes) {
+  const uint32_t h0 = halves_of_floats(v.x, v.y), h1 = halves_of_floats(w.x, w.y);
+  uint32_t a, b;
+  planes[0] = e4m3_of_halves(h0, h1);
+  halves_of_e4m3(planes[0], a, b);
+  uint32_t r0 = sub_halves(h0, a), r1 = sub_halves(h1, b);   // (exact)
+  planes[1] = e4m3_of_halves(r0, r1);
   if constexpr (PL == 4) {
-    const float2 f = floats_of_halves(h);
-    // what is left of the eleven bits of h, and what h left of the weight
-    rest = rest_of_halves(rest, halves_of_e4m3(planes[1]));
-    rest = add_halves(rest, halves_of_floats((a - f.x) * 256.0f, (b - f.y) * 256.0f));
-    planes[2] = e4m3_of_halves(rest);
-    planes[3] = e4m3_of_halves(rest_of_halves(rest, halves_of_e4m3(planes[2])));
+    // what is left of the eleven bits of h, and what h left of the weight, times 256
+    halves_of_e4m3(planes[1], a, b);
+    r0 = sub_halves(r0, a), r1 = sub_halves(r1, b);
+    const float2 k = make_float2(256.0f, 256.0f), n = make_float2(-256.0f, -256.0f);
+    const float2 f0 = fma2(floats_of_halves(h0), n, mul2(v, k)), f1 = fma2(floats_of_halves(h1), n, mul2(w, k));
+    r0 = fma_halves(r0, 0x5C005C00u, halves_of_floats(f0.x, f0.y)), r1 = fma_halves(r1, 0x5C005C00u, halves_of_floats(f1.x, f1.y));
+    planes[2] = e4m3_of_halves(r0, r1);
+    halves_of_e4m3(planes[2], a, b);
+    planes[3] = e4m3_of_halves(sub_halves(r0, a), sub_halves(r1, b));
   }
 }
 
@@ -218,11 +246,12 @@ __device__ __forceinline__ void store4(__nv_bfloat16 *p, float4 v) {
 __device__ __forceinline__ void store1(float *p, float v) { *p = v; }
 __device__ __forceinline__ void store1(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
 
-// Shared-memory matrix descriptor of rows of BYTES (32, 64 or 128) under the swizzle of that width, 8 rows a group; lbo: bytes between
-// columns of that width (MN-major operands wider than 128 bytes; 0: the second one is the first again).
+// Shared-memory matrix descriptor of rows of BYTES (32, 64 or 128) under the swizzle of that width, 8 rows a group;
+// lbo: bytes between columns of that width (MN-major operands that are wider; 0: the second one is the first again).
 template <int BYTES>
 __device__ __forceinline__ uint64_t operand(uint32_t lbo) {
-  return (uint64_t)(lbo >> 4) << 16 | (uint64_t)(8 * BYTES >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)(BYTES == 128 ? 2 : BYTES == 64 ? 4 : 6) << 61;
+  return (uint64_t)(lbo >> 4) << 16 | (uint64_t)(8 * BYTES >> 4) << 32 | (uint64_t)1 << 46 |
+         (uint64_t)(BYTES == 128 ? 2 : BYTES == 64 ? 4 : 6) << 61;
 }
 // byte `col` of row `row` under that swizzle
 template <int BYTES>
@@ -239,9 +268,9 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
   constexpr int NQ = RP / CG;                  // columns of a thread
   constexpr int NC = PL * RP;                  // columns of the products
   constexpr int PB = NC < 128 ? NC : 128;      // bytes of a row of P
+  constexpr int LD = 8;                        // columns of a load from tensor memory
   constexpr int WORK = 4 * CG, WORK_T = WORK * 32, ALL_T = WORK_T + 64;
   constexpr int TILE = kTile * HD, BOX = TILE / 2;
-  constexpr int LD = PL == 4 ? 8 : 16;         // columns of a load from tensor memory (of all planes: 32 registers)
   constexpr int T_COLS = 2 * NC < 32 ? 32 : 2 * NC;
   extern __shared__ __align__(1024) uint8_t smem[];
   uint8_t *ring = smem;                                   // [slots][128 keys][HD]
@@ -355,33 +384,32 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = sh.tmem_base;
-  const long all = (long)sh.entry[n_entries].before * (p.cut ? kv_heads : 1);
-  long chunk = all;
+  const int all = sh.entry[n_entries].before * (p.cut ? kv_heads : 1);
+  int chunk = all;
   if (p.cut) {
-    chunk = (all + gridDim.x - 1) / gridDim.x;
+    chunk = (all + (int)gridDim.x - 1) / (int)gridDim.x;
     chunk = chunk < kMinTiles ? kMinTiles : chunk;
   }
-  const long t_begin = p.cut ? min(all, blockIdx.x * chunk) : 0, t_end = min(all, t_begin + chunk);
+  const int t_begin = p.cut ? (int)min((long)all, (long)blockIdx.x * chunk) : 0, t_end = min(all, t_begin + chunk);
 
   // unit of a tile: its entry, kv head, first tile
   struct Unit {
-    int e, kvh, n;      // n: its tiles
-    long first;
+    int e, b, rt, kvh, n, first;      // n: its tiles
   };
-  auto unit_of = [&](long t) {
+  auto unit_of = [&](int t) {
     Unit u;
     int lo = 0, hi = n_entries - 1;
     const int heads = p.cut ? kv_heads : 1;
     while (lo < hi) {   // last entry that begins at t or before
       const int mid = (lo + hi + 1) >> 1;
-      if ((long)sh.entry[mid].before * heads <= t) lo = mid; else hi = mid - 1;
+      if (sh.entry[mid].before * heads <= t) lo = mid; else hi = mid - 1;
     }
     u.e = lo;
     u.n = sh.entry[lo + 1].before - sh.entry[lo].before;
-    const long in = t - (long)sh.entry[lo].before * heads;
-    const int h = (int)(in / u.n);
+    const int in = t - sh.entry[lo].before * heads, h = in / u.n;
     u.kvh = p.cut ? h : unit0 % kv_heads;
-    u.first = t - (in - (long)h * u.n);
+    u.first = t - (in - h * u.n);
+    entry_at(lo, &u.b, &u.rt);
     return u;
   };
   auto fail = [&]() {
@@ -397,22 +425,20 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
     // ------------------------------------------------------------------ fetching
     int slot = 0, meta = 0;
     uint32_t phase = 1;
-    long issued = 0;
+    int issued = 0;
     bool ok = true;
     int n_key0 = 0, n_page[2] = {-1, -1}, n_ke[2] = {0, 0}, n_ve[2] = {0, 0}, n_head = 0, n_last = 0;
-    auto look_up = [&](long t) {   // what lane `lane` knows of tile t + lane
+    auto look_up = [&](int t) {   // what lane `lane` knows of tile t + lane
       n_page[0] = n_page[1] = -1;
       n_last = 0;
       if (t + lane >= t_end) return;
       const Unit u = unit_of(t + lane);
-      const int i = (int)(t + lane - u.first);
+      const int i = t + lane - u.first;
       const Entry en = sh.entry[u.e];
-      int b, rt;
-      entry_at(u.e, &b, &rt);
       n_key0 = (i < en.sink ? i : en.low + i - en.sink) * kTile;
       n_head = u.kvh;
       n_last = i == u.n - 1 || t + lane == t_end - 1;
-      const int seq = p.seqs ? p.seqs[b] : b;
+      const int seq = p.seqs ? p.seqs[u.b] : u.b;
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const int at = n_key0 / KV_PAGE + j;
@@ -451,15 +477,25 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
     int v_plane = 0, v_page0 = -1, v_page1 = -1;
     bool v_open = false;   // V of the tile before is to be fetched behind this K
     if (t_begin < t_end) look_up(t_begin);
-    for (long t0 = t_begin; t0 < t_end && ok; t0 += 32) {
+    for (int t0 = t_begin; t0 < t_end && ok; t0 += 32) {
       look_up_exps();
       Meta m;
       m.key0 = n_key0;
       m.k_exp[0] = n_ke[0], m.k_exp[1] = n_ke[1], m.v_exp[0] = n_ve[0], m.v_exp[1] = n_ve[1];
       m.pages = (n_page[0] >= 0 ? 1 : 0) | (n_page[1] >= 0 ? 2 : 0);
+      {
+        int e_min = 127, e_max = -128;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int e = pool_exp((int8_t)(m.v_exp[j >> 2] >> (8 * (j & 3))));
+          e_min = min(e_min, e);
+          e_max = max(e_max, e);
+        }
+        if (e_max - e_min > 64) m.pages |= 4;
+      }
       const int pg0 = n_page[0], pg1 = n_page[1], head = n_head, last = n_last;
       if (t0 + 32 < t_end) look_up(t0 + 32);
-      const int n = (int)min(32L, t_end - t0);
+      const int n = min(32, t_end - t0);
       int told = 0;   // tiles of these 32 whose lanes have written what they know: not before the copies that there is room for are under way
       auto tell = [&](int upto) {
         if (lane >= told && lane < upto) {
@@ -489,7 +525,7 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
     }
     if (!ok) fail();
     // leave no copy in flight
-    for (long j = issued > p.slots ? issued - p.slots : 0; j < issued; ++j) warp_wait(&sh.full[j % p.slots], (uint32_t)((j / p.slots) & 1));
+    for (int j = issued > p.slots ? issued - p.slots : 0; j < issued; ++j) warp_wait(&sh.full[j % p.slots], (uint32_t)((j / p.slots) & 1));
   } else if (warp == WORK + 1) {
     // ------------------------------------------------------------------ issuing the products
     constexpr uint32_t idesc = (1u << 4) | (uint32_t)(NC >> 3) << 17 | (uint32_t)(128 >> 4) << 24;   // e4m3 both, sums in 32 bits
@@ -539,9 +575,9 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
       }
       next();
     };
-    for (long t = t_begin; t < t_end && ok;) {
+    for (int t = t_begin; t < t_end && ok;) {
       const Unit u = unit_of(t);
-      const int n = (int)(min(t_end, u.first + u.n) - t);
+      const int n = min(t_end, u.first + u.n) - t;
       scores(true);
       for (int i = 1; i < n && ok; ++i) {
         scores(false);
@@ -564,14 +600,100 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
     auto sync = [&]() { asm volatile("bar.sync 1, %0;" ::"n"(WORK_T) : "memory"); };
     auto group_sync = [&]() { asm volatile("bar.sync %0, 128;" ::"r"(2 + cg) : "memory"); };
     const int gt = tid & 127;            // thread of its group
+    // ---- queries of a unit: a power of two brings a row's largest entry to 128 .. 256, then its planes; a row is HD / 4 lanes
+    constexpr int LANES = HD / 4, PER = 32 / LANES, N = (RP + WORK * PER - 1) / (WORK * PER);
+    const int q_sub = lane / LANES, q_dim = lane % LANES * 4;
+    float4 qx[N];
+    int q_pos = -1;
+    // window row and head of row j of a unit's tile
+    struct Rows {
+      int left, k, rem;    // rows that there are; window row and head of its first one
+    };
+    auto rows_of = [&](const Unit &u) {
+      const int r = u.rt * RP, k = r / p.group;
+      return Rows{min(RP, p.rows - r), k, r - k * p.group};
+    };
+    auto place = [&](const Unit &u, const Rows &rw, int j, long stride) {   // first entry of the row in q or out
+      const int x = rw.rem + j, dk = p.group == 1 ? x : __umulhi(x, p.group_inv);
+      return ((long)u.b * p.window + rw.k + dk) * stride + ((long)u.kvh * p.group + x - dk * p.group) * HD;
+    };
+    auto load_queries = [&](const Unit &u) {
+      const Rows rw = rows_of(u);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int j = (i * WORK + warp) * PER + q_sub;
+        qx[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (j < rw.left) qx[i] = load4<T>(qp + place(u, rw, j, p.q_stride) + q_dim);
+      }
+      q_pos = -1;
+      if (tid < rw.left) {
+        const int x = rw.rem + tid;
+        q_pos = position(u.b, rw.k + (p.group == 1 ? x : (int)__umulhi(x, p.group_inv)));
+      }
+    };
+    // (a load behind the copies that are under way takes about 3 us)
+    auto prefetch_queries = [&](const Unit &u) {
+      const Rows rw = rows_of(u);
+      constexpr int LINES = HD * (int)sizeof(T) / 128;
+      for (int i = tid; i < rw.left * LINES; i += WORK_T)
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(qp + place(u, rw, i / LINES, p.q_stride) + i % LINES * (128 / (int)sizeof(T))));
+    };
+    auto publish_queries = [&](const Unit &u, int up) {
+      if (tid < RP) {
+        sh.pos[up][tid] = q_pos;
+        sh.out_at[up][tid] = place(u, rows_of(u), tid, p.out_stride);
+      }
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int r = (i * WORK + warp) * PER + q_sub;
+        float v[4] = {qx[i].x, qx[i].y, qx[i].z, qx[i].w};
+        float top = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if (fabsf(v[j]) == INFINITY) v[j] = __int_as_float(0x7FFFFFFF);   // (e4m3 has no infinity: its row is NaN, as it would be)
+          top = fmaxf(top, fabsf(v[j]));
+        }
+#pragma unroll
+        for (int o = LANES / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        int e = top > 0.0f ? 7 - (int)((__float_as_uint(top) >> 23) - 127) : 0;
+        e = max(min(e, 126), -126);   // (entries below 2^-119 lose places)
+        const float up2 = two_to(e);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] *= up2;
+        if (r < RP) {
+          if (q_dim == 0) sh.fac[up][r] = p.scale * two_to(-e);
+#pragma unroll
+          for (int l = 0; l < PL; ++l) {
+            if (l == 2) v[0] *= 256.0f, v[1] *= 256.0f, v[2] *= 256.0f, v[3] *= 256.0f;
+            const uint32_t four = e4m3_of_floats(v);
+            *reinterpret_cast<uint32_t *>(Qs + swizzled<HD>(l * RP + r, q_dim)) = four;
+            uint32_t ha, hc;
+            halves_of_e4m3(four, ha, hc);
+            const float2 fa = floats_of_halves(ha), fc = floats_of_halves(hc);
+            v[0] -= fa.x, v[1] -= fa.y, v[2] -= fc.x, v[3] -= fc.y;
+          }
+        }
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) arrive(&sh.q_ready);
+    };
+
+    int up = 0;
+    if (t_begin < t_end) {
+      const Unit u = unit_of(t_begin);
+      load_queries(u);
+      publish_queries(u, 0);
+    }
     if (p.cut && tid == 0) {
       int4 c = make_int4(0, 0, 0, 0);
       if (t_begin < t_end && t_end < all) {
         const Unit u = unit_of(t_end - 1);
         if (u.first >= t_begin && u.first + u.n > t_end) {
-          entry_at(u.e, &c.x, &c.y);
+          c.x = u.b;
+          c.y = u.rt;
           c.z = u.kvh;
-          c.w = (int)((u.first + u.n - 1) / chunk) - (int)blockIdx.x + 1;
+          c.w = (u.first + u.n - 1) / chunk - (int)blockIdx.x + 1;
         }
       }
       p.cuts[blockIdx.x] = c;
@@ -589,109 +711,64 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
               store1(outp + ((long)b * p.window + r / p.group) * p.out_stride + ((long)h * p.group + r % p.group) * HD + i, 0.0f);
       }
     }
-
-    for (long t = t_begin; t < t_end;) {
+    for (int t = t_begin; t < t_end; up ^= 1) {
       const Unit u = unit_of(t);
-      const long u_end = u.first + u.n, end = min(t_end, u_end);
-      const int n = (int)(end - t);
-      int b, rt;
-      entry_at(u.e, &b, &rt);
-      {
-        // ---- queries: a power of two brings a row's largest entry to 128 .. 256, then its planes; a row is HD / 4 lanes
-        constexpr int LANES = HD / 4, PER = 32 / LANES, N = (RP + WORK * PER - 1) / (WORK * PER);
-        const int sub = lane / LANES, d = lane % LANES * 4;
-        float4 x[N];
+      const int u_end = u.first + u.n, end = min(t_end, u_end);
+      const int n = end - t;
+      if (end < t_end) prefetch_queries(unit_of(end));
+      sync();   // (every row's position is there; what the unit before left in shared memory has been read)
+      int lo = 0x7FFFFFFF, hi = -1;   // smallest and largest position of the tile's rows
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const int r = rt * RP + (i * WORK + warp) * PER + sub;
-          x[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-          if (r < min(p.rows, (rt + 1) * RP))
-            x[i] = load4<T>(qp + ((long)b * p.window + r / p.group) * p.q_stride + ((long)u.kvh * p.group + r % p.group) * HD + d);
-        }
-        int my_pos = -1;
-        if (tid < RP && rt * RP + tid < p.rows) my_pos = position(b, (rt * RP + tid) / p.group);
-        sync();   // (what the unit before left in shared memory has been read)
-        if (tid < RP) {
-          const int r = rt * RP + tid;
-          sh.pos[tid] = my_pos;
-          sh.out_at[tid] = ((long)b * p.window + r / p.group) * p.out_stride + ((long)u.kvh * p.group + r % p.group) * HD;
-        }
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const int r = (i * WORK + warp) * PER + sub;
-          float v[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-          float top = 0.0f;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            if (fabsf(v[j]) == INFINITY) v[j] = __int_as_float(0x7FFFFFFF);   // (e4m3 has no infinity: its row is NaN, as it would be)
-            top = fmaxf(top, fabsf(v[j]));
-          }
-#pragma unroll
-          for (int o = LANES / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-          int e = top > 0.0f ? 7 - (int)((__float_as_uint(top) >> 23) - 127) : 0;
-          e = max(min(e, 126), -126);   // (entries below 2^-119 lose places)
-          const float up = two_to(e);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) v[j] *= up;
-          if (r < RP) {
-            if (d == 0) sh.fac[r] = p.scale * two_to(-e);
-#pragma unroll
-            for (int l = 0; l < PL; ++l) {
-              const uint32_t a = e4m3_of_floats(v[0], v[1]), c = e4m3_of_floats(v[2], v[3]);
-              *reinterpret_cast<uint32_t *>(Qs + swizzled<HD>(l * RP + r, d)) = a | c << 16;
-              const float2 fa = floats_of_halves(halves_of_e4m3(a)), fc = floats_of_halves(halves_of_e4m3(c));
-              v[0] = (v[0] - fa.x) * 16.0f, v[1] = (v[1] - fa.y) * 16.0f, v[2] = (v[2] - fc.x) * 16.0f, v[3] = (v[3] - fc.y) * 16.0f;
-            }
-          }
-        }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        sync();
-        if (warp == 0) {   // smallest and largest position of the tile's rows
-          int lo = 0x7FFFFFFF, hi = -1;
-#pragma unroll
-          for (int i = 0; i < (RP + 31) / 32; ++i) {
-            const int at = lane + 32 * i < RP ? sh.pos[lane + 32 * i] : -1;
-            if (at >= 0) lo = min(lo, at);
-            hi = max(hi, at);
-          }
-          lo = __reduce_min_sync(0xffffffffu, lo);
-          hi = __reduce_max_sync(0xffffffffu, hi);
-          if (lane == 0) sh.lo = lo, sh.hi = hi;
-        }
-        sync();
-        if (lane == 0) arrive(&sh.q_ready);
+      for (int i = 0; i < (RP + 31) / 32; ++i) {
+        const int at = lane + 32 * i < RP ? sh.pos[up][lane + 32 * i] : -1;
+        if (at >= 0) lo = min(lo, at);
+        hi = max(hi, at);
       }
-      const int lo = sh.lo, hi = sh.hi;
+      lo = __reduce_min_sync(0xffffffffu, lo);
+      hi = __reduce_max_sync(0xffffffffu, hi);
       const int sliding = p.sliding > 0 ? p.sliding : 0x7FFFFFFF;
       const int from = hi - sliding;      // keys above are in the window of every row
       auto sees = [&](int key, int at) { return key <= at && (key > at - sliding || key < p.sinks); };
 
-      float o[NQ], l_acc[NQ];
+      float2 o[NQ / 2], l_acc[NQ / 2];
 #pragma unroll
-      for (int i = 0; i < NQ; ++i) o[i] = l_acc[i] = 0.0f;
+      for (int i = 0; i < NQ / 2; ++i) o[i] = l_acc[i] = make_float2(0.0f, 0.0f);
       float my_run = -INFINITY;   // thread i < NQ of a group: the running maximum of its row
 
+      auto pair_of = [&](const float *a, int q) { return *reinterpret_cast<const float2 *>(a + c0 + q); };
+      auto four_of = [&](const float *a, int q) { return *reinterpret_cast<const float4 *>(a + c0 + q); };
+      // columns of a product, its planes added (the fine ones first: 16 registers of loads at a time)
+      auto load_columns = [&](uint32_t from_col, float2 *v) {
+#pragma unroll
+        for (int c = 0; c < NQ; c += LD) {
+          float2 fine[LD / 2];
+#pragma unroll
+          for (int l = PL - 2; l >= 0; l -= 2) {
+            uint32_t x[2][LD];
+            tmem_ld_issue<LD>(from_col + l * RP + c, x[0]);
+            tmem_ld_issue<LD>(from_col + (l + 1) * RP + c, x[1]);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < LD / 2; ++i) {
+              float2 sum = add2(make_float2(__uint_as_float(x[0][2 * i]), __uint_as_float(x[0][2 * i + 1])),
+                                make_float2(__uint_as_float(x[1][2 * i]), __uint_as_float(x[1][2 * i + 1])));
+              if (PL == 4 && l == 0) sum = fma2(fine[i], make_float2(0x1p-8f, 0x1p-8f), sum);
+              if (l > 0) fine[i] = sum;
+              else v[c / 2 + i] = sum;
+            }
+          }
+        }
+      };
       auto add_values = [&](int par) {   // O^T of a tile to this thread's dim, under the maximum after that tile
         tc_fence_after();
         if (w * 32 < HD) {
+          float2 v[NQ / 2];
+          load_columns(t_o, v);
 #pragma unroll
-          for (int c = 0; c < NQ / LD; ++c) {
-            uint32_t x[PL][LD];
-#pragma unroll
-            for (int l = 0; l < PL; ++l) tmem_ld_issue<LD>(t_o + l * RP + c * LD, x[l]);
-            tmem_ld_wait();
-#pragma unroll
-            for (int i = 0; i < LD; i += 4) {
-              const float4 a4 = *reinterpret_cast<const float4 *>(&sh.alpha[par][c0 + c * LD + i]), b4 = *reinterpret_cast<const float4 *>(&sh.beta[par][c0 + c * LD + i]);
-              const float al[4] = {a4.x, a4.y, a4.z, a4.w}, be[4] = {b4.x, b4.y, b4.z, b4.w};
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                float v = __uint_as_float(x[PL - 1][i + j]);
-#pragma unroll
-                for (int l = PL - 2; l >= 0; --l) v = fmaf(v, 0.0625f, __uint_as_float(x[l][i + j]));
-                o[c * LD + i + j] = fmaf(v, be[j], o[c * LD + i + j] * al[j]);
-              }
-            }
+          for (int i = 0; i < NQ / 2; i += 2) {
+            const float4 a = four_of(sh.alpha[par], 2 * i), c = four_of(sh.beta[par], 2 * i);
+            o[i] = fma2(v[i], make_float2(c.x, c.y), mul2(o[i], make_float2(a.x, a.y)));
+            o[i + 1] = fma2(v[i + 1], make_float2(c.z, c.w), mul2(o[i + 1], make_float2(a.z, a.w)));
           }
         }
         tc_fence_before();
@@ -701,8 +778,10 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
         for (int i = 0; i < many; ++i) {
           if (w * 32 >= HD || !(sh.nan_dims[i][w] >> lane & 1u)) continue;
 #pragma unroll
-          for (int q = 0; q < NQ; ++q)
-            if (sees(sh.nan_key[i], sh.pos[c0 + q])) o[q] = __int_as_float(0x7FFFFFFF);
+          for (int q = 0; q < NQ / 2; ++q) {
+            if (sees(sh.nan_key[i], sh.pos[up][c0 + 2 * q])) o[q].x = __int_as_float(0x7FFFFFFF);
+            if (sees(sh.nan_key[i], sh.pos[up][c0 + 2 * q + 1])) o[q].y = __int_as_float(0x7FFFFFFF);
+          }
         }
       };
 
@@ -721,38 +800,27 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
         const int key = m.key0 + key_t, half = key_t >> 6;
         const int ev = pool_exp((int8_t)(m.v_exp[half] >> (8 * (key_t >> 4 & 3))));
         const float k2 = two_to(pool_exp((int8_t)(m.k_exp[half] >> (8 * (key_t >> 4 & 3))))), add = (float)ev;
-        const bool whole = m.pages == 3 && m.key0 + kTile - 1 <= lo && (m.key0 > from || m.key0 + kTile <= p.sinks);
-        float s[NQ];
-#pragma unroll
-        for (int c = 0; c < NQ / LD; ++c) {
-          uint32_t x[PL][LD];
-#pragma unroll
-          for (int l = 0; l < PL; ++l) tmem_ld_issue<LD>(t_s + l * RP + c * LD, x[l]);
-          tmem_ld_wait();
-#pragma unroll
-          for (int j = 0; j < LD; j += 4) {
-            const float4 f4 = *reinterpret_cast<const float4 *>(&sh.fac[c0 + c * LD + j]);
-            const float f[4] = {f4.x, f4.y, f4.z, f4.w};
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              float v = __uint_as_float(x[PL - 1][j + k]);
-#pragma unroll
-              for (int l = PL - 2; l >= 0; --l) v = fmaf(v, 0.0625f, __uint_as_float(x[l][j + k]));
-              s[c * LD + j + k] = fmaf(v * k2, f[k], add);
-            }
-          }
-        }
+        const bool whole = (m.pages & 3) == 3 && m.key0 + kTile - 1 <= lo && (m.key0 > from || m.key0 + kTile <= p.sinks);
+        float2 s[NQ / 2];
+        load_columns(t_s, s);
         tc_fence_before();
         __syncwarp();
         if (lane == 0) arrive(&sh.s_free);
+#pragma unroll
+        for (int q = 0; q < NQ / 2; q += 2) {
+          const float4 f = four_of(sh.fac[up], 2 * q);
+          s[q] = fma2(s[q], mul2(make_float2(f.x, f.y), make_float2(k2, k2)), make_float2(add, add));
+          s[q + 1] = fma2(s[q + 1], mul2(make_float2(f.z, f.w), make_float2(k2, k2)), make_float2(add, add));
+        }
         if (!whole) {
           const bool there = m.pages >> half & 1;
           bool missed = false;
 #pragma unroll
-          for (int q = 0; q < NQ; ++q) {
-            const bool in = sees(key, sh.pos[c0 + q]);
-            missed |= in && !there;
-            if (!in || !there) s[q] = -INFINITY;
+          for (int q = 0; q < NQ / 2; ++q) {
+            const bool in0 = sees(key, sh.pos[up][c0 + 2 * q]), in1 = sees(key, sh.pos[up][c0 + 2 * q + 1]);
+            missed |= (in0 || in1) && !there;
+            if (!in0 || !there) s[q].x = -INFINITY;
+            if (!in1 || !there) s[q].y = -INFINITY;
           }
           if (missed) pool_fault(p.pool.status, SJD_ERR_BAD_ARG);   // (no page where some row sees a key)
         }
@@ -760,15 +828,10 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
 #pragma unroll
         for (int q = 0; q < NQ; q += 4) {
           float4 v;
-          v.x = max_of_warp(s[q]), v.y = max_of_warp(s[q + 1]), v.z = max_of_warp(s[q + 2]), v.w = max_of_warp(s[q + 3]);
+          v.x = max_of_warp(s[q / 2].x), v.y = max_of_warp(s[q / 2].y), v.z = max_of_warp(s[q / 2 + 1].x), v.w = max_of_warp(s[q / 2 + 1].y);
           if (lane == 0) *reinterpret_cast<float4 *>(&sh.red[w][c0 + q]) = v;
         }
-        // exponents that differ so much that weights, but not the terms of the sum, may leave the range
-        {
-          const int e_min = __reduce_min_sync(0xffffffffu, ev), e_max = __reduce_max_sync(0xffffffffu, ev);
-          if (lane == 0) sh.exp_range[cg][par][w] = e_max << 16 | (e_min & 0xFFFF);
-          if (gt == 0) sh.wide[cg][par] = 0;
-        }
+        if (gt == 0) sh.wide[cg][par] = m.pages & 4;   // exponents that differ so much that weights, but not the sum's terms, may leave the range
         group_sync();
         if (gt < NQ) {
           const int r = c0 + gt;
@@ -776,22 +839,13 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
           const float now = fmaxf(my_run, mx), at = now > -INFINITY ? now : 0.0f;
           // (by way of the roots: with the values' exponents a maximum may move by 200, and the sum by as much the other way)
           const float a = exp2_fast(0.5f * (my_run - at)), c = exp2_fast(0.5f * (mx - at));
-          sh.ref[r] = (mx > -INFINITY ? mx : 0.0f) - (float)kUp;
+          sh.up[r] = (float)kUp - (mx > -INFINITY ? mx : 0.0f);
           sh.alpha[par][r] = a * a;
           sh.beta[par][r] = c * c;
           sh.alpha_root[par][r] = a;
           sh.beta_root[par][r] = c;
           if ((my_run > -INFINITY && my_run - at < -64.0f) || (mx > -INFINITY && mx - at < -64.0f)) sh.wide[cg][par] = 1;
           my_run = now;
-          if (gt == 0) {
-            int e_min = 127, e_max = -128;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              e_max = max(e_max, sh.exp_range[cg][par][j] >> 16);
-              e_min = min(e_min, (int)(int16_t)sh.exp_range[cg][par][j]);
-            }
-            if (e_max - e_min > 64) sh.wide[cg][par] = 1;
-          }
         }
         group_sync();
         // ---- weights and their sum without the values' exponents
@@ -800,33 +854,36 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
         const bool wide = sh.wide[cg][par] != 0;
         if (wide) {
 #pragma unroll
-          for (int q = 0; q < NQ; ++q) {
-            const float ar = sh.alpha_root[par][c0 + q], br = sh.beta_root[par][c0 + q];
-            l_acc[q] = l_acc[q] * ar * ar + exp2_fast(s[q] - add - sh.ref[c0 + q] - (float)kUp) * br * br;
+          for (int q = 0; q < NQ / 2; ++q) {
+            const float2 ar = pair_of(sh.alpha_root[par], 2 * q), br = pair_of(sh.beta_root[par], 2 * q), r = pair_of(sh.up, 2 * q);
+            l_acc[q].x = l_acc[q].x * ar.x * ar.x + exp2_fast(s[q].x - add + r.x - (float)kUp) * br.x * br.x;
+            l_acc[q].y = l_acc[q].y * ar.y * ar.y + exp2_fast(s[q].y - add + r.y - (float)kUp) * br.y * br.y;
           }
         }
 #pragma unroll
-        for (int q = 0; q < NQ; q += 4) {
-          const float4 r = *reinterpret_cast<const float4 *>(&sh.ref[c0 + q]);
-          s[q] = exp2_fast(s[q] - r.x), s[q + 1] = exp2_fast(s[q + 1] - r.y), s[q + 2] = exp2_fast(s[q + 2] - r.z), s[q + 3] = exp2_fast(s[q + 3] - r.w);
+        for (int q = 0; q < NQ / 2; q += 2) {
+          const float4 r = four_of(sh.up, 2 * q);
+          s[q] = add2(s[q], make_float2(r.x, r.y));
+          s[q + 1] = add2(s[q + 1], make_float2(r.z, r.w));
+          s[q].x = exp2_fast(s[q].x);
+          s[q].y = exp2_fast(s[q].y);
+          s[q + 1].x = exp2_fast(s[q + 1].x);
+          s[q + 1].y = exp2_fast(s[q + 1].y);
         }
         if (!wide) {
 #pragma unroll
-          for (int q = 0; q < NQ; q += 4) {
-            const float4 a = *reinterpret_cast<const float4 *>(&sh.alpha[par][c0 + q]), c = *reinterpret_cast<const float4 *>(&sh.beta[par][c0 + q]);
-            l_acc[q] = fmaf(s[q] * back, c.x, l_acc[q] * a.x);
-            l_acc[q + 1] = fmaf(s[q + 1] * back, c.y, l_acc[q + 1] * a.y);
-            l_acc[q + 2] = fmaf(s[q + 2] * back, c.z, l_acc[q + 2] * a.z);
-            l_acc[q + 3] = fmaf(s[q + 3] * back, c.w, l_acc[q + 3] * a.w);
+          for (int q = 0; q < NQ / 2; q += 2) {
+            const float4 a = four_of(sh.alpha[par], 2 * q), c = four_of(sh.beta[par], 2 * q);
+            l_acc[q] = fma2(mul2(s[q], make_float2(back, back)), make_float2(c.x, c.y), mul2(l_acc[q], make_float2(a.x, a.y)));
+            l_acc[q + 1] = fma2(mul2(s[q + 1], make_float2(back, back)), make_float2(c.z, c.w), mul2(l_acc[q + 1], make_float2(a.z, a.w)));
           }
         }
 #pragma unroll
         for (int q = 0; q < NQ; q += 4) {
-          uint32_t lo2[PL], hi2[PL];
-          weight_planes<PL>(s[q], s[q + 1], lo2);
-          weight_planes<PL>(s[q + 2], s[q + 3], hi2);
+          uint32_t four[PL];
+          weight_planes<PL>(s[q / 2], s[q / 2 + 1], four);
 #pragma unroll
-          for (int l = 0; l < PL; ++l) pk[l][q / 4] = lo2[l] | hi2[l] << 16;
+          for (int l = 0; l < PL; ++l) pk[l][q / 4] = four[l];
         }
         // ---- the tile before is multiplied: its O^T is there, and P may be written
         if (i > 0) {
@@ -838,14 +895,10 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
         }
 #pragma unroll
         for (int l = 0; l < PL; ++l) {
-          constexpr int STEP = NQ < 16 ? NQ : 16;
-#pragma unroll
-          for (int q = 0; q < NQ; q += STEP) {
-            const uint32_t col = l * RP + c0 + q;
-            uint8_t *dst = Ps + (col / 128) * (kTile * 128) + swizzled<PB>(key_t, col % 128);
-            if constexpr (STEP == 16) *reinterpret_cast<uint4 *>(dst) = make_uint4(pk[l][q / 4], pk[l][q / 4 + 1], pk[l][q / 4 + 2], pk[l][q / 4 + 3]);
-            else *reinterpret_cast<uint2 *>(dst) = make_uint2(pk[l][q / 4], pk[l][q / 4 + 1]);
-          }
+          const uint32_t col = l * RP + c0;
+          uint8_t *dst = Ps + (col / 128) * (kTile * 128) + swizzled<PB>(key_t, col % 128);
+          if constexpr (NQ == 16) *reinterpret_cast<uint4 *>(dst) = make_uint4(pk[l][0], pk[l][1], pk[l][2], pk[l][3]);
+          else *reinterpret_cast<uint2 *>(dst) = make_uint2(pk[l][0], pk[l][1]);
         }
         if (i > 0) {
           add_values(par ^ 1);
@@ -895,24 +948,29 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
       }
       v_use += 2 * n;
       t = end;
-
-      // ---- sums over the keys, while the last tile is multiplied
+      // ---- the next unit's queries, and this one's sums over the keys, while the last tile is multiplied
+      const Unit next = unit_of(t < t_end ? t : t_end - 1);
+      if (t < t_end) load_queries(next);
       {
-        const float v = lanes_sum<NQ>(l_acc);
-        if (lane < NQ) sh.red[w][c0 + lane] = v;
+        float v[NQ];
+#pragma unroll
+        for (int q = 0; q < NQ / 2; ++q) v[2 * q] = l_acc[q].x, v[2 * q + 1] = l_acc[q].y;
+        const float l = lanes_sum<NQ>(v);
+        if (lane < NQ) sh.red[w][c0 + lane] = l;
       }
       group_sync();
       const bool cut = u.first < t_begin || u_end > t_end;
-      const int rows_here = min(RP, p.rows - rt * RP), dim = w * 32 + lane;
+      const int rows_here = min(RP, p.rows - u.rt * RP), dim = w * 32 + lane;
       constexpr long PART = (long)RP * HD;
       // this CTA's part of a cut unit: slot 0 of a unit that began before its range, slot 1 of one that goes on behind it
       const int my = 2 * blockIdx.x + (u.first < t_begin ? 0 : 1);
       if (gt < NQ) {
         const int r = c0 + gt;
         const float sum = (sh.red[0][r] + sh.red[1][r]) + (sh.red[2][r] + sh.red[3][r]);
-        sh.inv[r] = sh.pos[r] >= 0 && sum != 0.0f ? two_to(-kUp) / sum : 0.0f;   // (a NaN among the scores makes the sum NaN)
+        sh.inv[r] = sh.pos[up][r] >= 0 && sum != 0.0f ? two_to(-kUp) / sum : 0.0f;   // (a NaN among the scores makes the sum NaN)
         if (cut) p.stats[my * RP + r] = make_float2(my_run, sum);
       }
+      if (t < t_end) publish_queries(next, up ^ 1);   // (all scores of this unit have been waited for)
       if (ok && !warp_wait(&sh.o_full, o_ph)) {
         ok = false;
         fail();
@@ -923,16 +981,16 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
       sync();
       if (tid == 0) sh.n_nan = 0;
       if (w * 32 < HD) {
-        if (!cut) {
 #pragma unroll
-          for (int q = 0; q < NQ; ++q) {
+        for (int q = 0; q < NQ; ++q) {
+          const float v = q & 1 ? o[q / 2].y : o[q / 2].x;
+          if (c0 + q >= rows_here) break;
+          if (cut) {
+            p.parts[my * PART + (c0 + q) * HD + dim] = v;
+          } else {
             const float inv = sh.inv[c0 + q];
-            if (c0 + q < rows_here) store1(outp + sh.out_at[c0 + q] + dim, inv == 0.0f ? 0.0f : o[q] * inv);
+            store1(outp + sh.out_at[up][c0 + q] + dim, inv == 0.0f ? 0.0f : v * inv);
           }
-        } else {
-#pragma unroll
-          for (int q = 0; q < NQ; ++q)
-            if (c0 + q < rows_here) p.parts[my * PART + (c0 + q) * HD + dim] = o[q];
         }
       }
     }
@@ -946,13 +1004,14 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
   }
 }
 
-// Joins the parts of the unit that begins in range blockIdx.x and is cut: a warp per row.
-constexpr int kJoinWarps = 8;
+// Joins the parts of the unit that begins in range blockIdx.x and is cut: a warp per row, sixteen parts' loads in flight together.
+constexpr int kJoinRows = 8;
 template <typename T, int HD>
-__global__ void __launch_bounds__(kJoinWarps * 32) pool_attention_join_kernel(const __grid_constant__ PoolAttnParams p, int RP) {
+__global__ void __launch_bounds__(kJoinRows * 32) pool_attention_join_kernel(const __grid_constant__ PoolAttnParams p, int RP) {
+  constexpr int D = HD / 32, U = 16;
   pdl_wait();
   const int4 c = p.cuts[blockIdx.x];
-  const int lane = threadIdx.x & 31, r = blockIdx.y * kJoinWarps + (threadIdx.x >> 5), row = c.y * RP + r;
+  const int lane = threadIdx.x & 31, r = blockIdx.y * kJoinRows + (threadIdx.x >> 5), row = c.y * RP + r;
   if (c.w < 2 || r >= RP || row >= p.rows) return;
   auto slot_of = [&](int i) { return 2 * ((int)blockIdx.x + i) + (i == 0 ? 1 : 0); };
   const int k = row / p.group, at = p.in_pos[(long)c.x * p.window + k];
@@ -964,7 +1023,6 @@ __global__ void __launch_bounds__(kJoinWarps * 32) pool_attention_join_kernel(co
   }
   best = warp_max(best);
   if (best == -INFINITY) best = 0.0f;
-  constexpr int D = HD / 32, U = 8;
   float acc[D];
 #pragma unroll
   for (int d = 0; d < D; ++d) acc[d] = 0.0f;
@@ -973,7 +1031,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) pool_attention_join_kernel(co
     float f = 0.0f;
     if (lane < n) {
       if (c.w > 32) ms = p.stats[slot_of(base + lane) * RP + r];
-      f = exp2_fast(0.5f * (ms.x - best));   // (its root: see the sums' range)
+      f = exp2_fast(0.5f * (ms.x - best));   // (a root: see the range of the sums)
       sum += ms.y * f * f;
       f *= f;
     }
@@ -981,7 +1039,8 @@ __global__ void __launch_bounds__(kJoinWarps * 32) pool_attention_join_kernel(co
       float x[U][D];
 #pragma unroll
       for (int j = 0; j < U; ++j) {
-        const float *src = p.parts + ((long)slot_of(base + min(i + j, n - 1)) * RP + r) * HD + lane * D;
+        if (i + j >= n) break;
+        const float *src = p.parts + ((long)slot_of(base + i + j) * RP + r) * HD + lane * D;
         if constexpr (D == 4) {
           const float4 v = *reinterpret_cast<const float4 *>(src);
           x[j][0] = v.x, x[j][1] = v.y, x[j][2] = v.z, x[j][3] = v.w;
@@ -992,18 +1051,17 @@ __global__ void __launch_bounds__(kJoinWarps * 32) pool_attention_join_kernel(co
       }
 #pragma unroll
       for (int j = 0; j < U; ++j) {
-        const float w = __shfl_sync(0xffffffffu, f, i + j < n ? i + j : 0);
-        if (i + j < n) {
+        if (i + j >= n) break;
+        const float w = __shfl_sync(0xffffffffu, f, i + j);
 #pragma unroll
-          for (int d = 0; d < D; ++d) acc[d] = fmaf(x[j][d], w, acc[d]);
-        }
+        for (int d = 0; d < D; ++d) acc[d] = fmaf(x[j][d], w, acc[d]);
       }
     }
   }
   sum = warp_sum(sum);
   const bool live = (unsigned)at < (unsigned)(p.pool.pages_per_seq * KV_PAGE) && sum != 0.0f;
   const float inv = live ? two_to(-kUp) / sum : 0.0f;
-  T *dst = (T *)p.out + ((long)c.x * p.window + k) * p.out_stride + ((long)c.z * p.group + row % p.group) * HD + lane * D;
+  T *dst = (T *)p.out + ((long)c.x * p.window + k) * p.out_stride + ((long)c.z * p.group + row - k * p.group) * HD + lane * D;
 #pragma unroll
   for (int d = 0; d < D; ++d) acc[d] = live ? acc[d] * inv : 0.0f;
   if constexpr (D == 4) store4(dst, make_float4(acc[0], acc[1], acc[2], acc[3]));
@@ -1078,6 +1136,7 @@ extern "C" int sjd_pool_attention(const sjd_pool *pool, int layer, int batch, in
   p.window = window;
   p.n_heads = n_heads;
   p.group = group;
+  p.group_inv = (unsigned)((0x100000000ull + group - 1) / group);   // (not used with 1)
   p.rows = (int)rows;
   p.row_tiles = (int)((rows + rp - 1) / rp);
   p.sliding = sliding;
@@ -1101,7 +1160,8 @@ extern "C" int sjd_pool_attention(const sjd_pool *pool, int layer, int batch, in
     const int64_t in = ((int64_t)sliding + window + kTile - 2) / kTile + 1 + ((int64_t)sinks + kTile - 1) / kTile;
     most = most < in ? most : in;
   }
-  p.cut = entries <= kMaxEntries && (int64_t)batch * window <= 8192 && (most > kWholeTiles || units > 2 * sms);
+  p.cut = entries <= kMaxEntries && (int64_t)batch * window <= 8192 && (most > kWholeTiles || units > 2 * sms) &&
+          units * most < 1 << 30;   // (tiles are counted in 32 bits)
   p.n_entries = (int)entries;
   const CUtensorMap &m = reinterpret_cast<const CUtensorMap &>(map);
   auto launch = [&](auto kernel, auto join, int RP, int PL, size_t shared) -> int {
@@ -1116,7 +1176,7 @@ extern "C" int sjd_pool_attention(const sjd_pool *pool, int layer, int batch, in
     SJD_CHECK_LAUNCH();
     if (!p.cut) return SJD_OK;
     g_pdl = true;   // (waits for the launch before it itself)
-    const cudaError_t e = launch_kernel(join, dim3((unsigned)ctas, (unsigned)((RP + kJoinWarps - 1) / kJoinWarps)), dim3(kJoinWarps * 32), 0,
+    const cudaError_t e = launch_kernel(join, dim3((unsigned)ctas, (unsigned)((RP + kJoinRows - 1) / kJoinRows)), dim3(kJoinRows * 32), 0,
                                         (cudaStream_t)cuda_stream, p, RP);
     g_pdl = false;
     SJD_CUDA(e);

@@ -58,14 +58,14 @@ def _filled(lens, n_layers, kvh, hd, seed, spare=3, per_seq=None, exps=(-8, -5),
 def _bound(dtype, want):
     """Most that an output may be off.  A weight's planes leave 2^-8 (bf16: two) or 2^-16 (fp32: four) of it, half a step of e4m3 being
     2^-4 of a number; its conversion to fp16 before leaves 2^-11 (bf16; with fp32 the planes hold that rest too).  The largest weight of a
-    row in a tile of 128 keys is 2^8 and the smallest step of e4m3 2^-9, under the last plane's factor (2^-4, fp32 2^-12): half of it is 2^-22
-    resp. 2^-30 of that weight.  A query's planes leave 2^-16 of an entry (fp32; bf16: nothing) and the same floors of the row's
+    row in a tile of 128 keys is 2^8 and the smallest step of e4m3 2^-9 (fp32: under the factor 2^-8 of the third and fourth plane): half of
+    it is 2^-18 resp. 2^-26 of that weight.  A query's planes leave 2^-16 of an entry (fp32; bf16: nothing) and the same floors of the row's
     largest; a score has about 20 fp32 additions (2^-24 of their magnitudes each) and counts twice, in the numerator and in the sum.  Sums
     over the keys: a tile's products and two roundings a tile, up to 800 tiles of a sequence and the merges, 2^-15.  The output's own
     rounding: half a step."""
     out, mass, floor, reach, flat = want
     two = dtype == "bf16"
-    low = 2.0 ** -22 if two else 2.0 ** -30
+    low = 2.0 ** -18 if two else 2.0 ** -26
     score = flat * low + reach * (2.0 ** -19 if two else 2.0 ** -16 + 2.0 ** -19)
     weight = 2.0 ** -8 + 2.0 ** -11 if two else 2.0 ** -16
     return 1.02 * ((weight + 2 * score[..., None] + 2.0 ** -15) * mass + floor * low) + (2.0 ** -8 if two else 2.0 ** -24) * np.abs(out) + 1e-35
