@@ -370,7 +370,7 @@ typedef struct {
 
 /*
  * Rotary step and append.  Row m = b * window + k of q [.][n_heads][head_dim], k and v [.][n_kv_heads][head_dim] (dtype SJD_F32 or
- * SJD_BF16; rows are *_stride elements apart, even, and start on 8 resp. 4 bytes) is position in_pos[m] of sequence seqs[b] (null: b).
+ * SJD_BF16; rows are *_stride elements apart, a multiple of 4, and start on 16 resp. 8 bytes) is position in_pos[m] of sequence seqs[b] (null: b).
  * The active rows of a sequence come first and are consecutive positions; the others have in_pos -1 and are left out.  k and q are
  * rotated (rope null: neither is) by axis_pos [.][n_axes] (null: every axis by in_pos), cosine and sine in 64 bits rounded to 32, and
  * products and sums in 32; q goes to q_out (q null: no queries; q_out may be q), k and v to layer `layer` of the pool.

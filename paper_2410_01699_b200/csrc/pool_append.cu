@@ -3,7 +3,8 @@
 // A block of threads owns a block of 16 positions of a sequence and some heads, a warp one head (of the queries, keys or values) at a time:
 // it loads the head's rows, rotates them, reduces the largest entry, and stores 16 x head_dim bytes under one power-of-two scale.  Rows that
 // were in the block before are read, scaled to what they stand for, and take part; nothing outside the block's rows up to the last
-// new one is touched, so no two warps meet.  A lane holds pairs (i, i + head_dim / 2) of all rows, so that the rotation needs no exchange.
+// new one is touched, so no two warps meet.  A lane holds four pairs (i, i + head_dim / 2) of half of the rows (64: a quarter), so that the rotation
+// needs no exchange.
 //   (a, b) -> (a c - b s, b c + a s), angle = position * theta^(-2 f / rot)
 // Angles are products in 64 bits (a position of 10^6 times a frequency in 32 bits is off by 0.06), their cosine and sine are rounded to
 // 32 bits once and shared by the heads of a block of threads through shared memory.  Products and sums are single 32-bit operations
@@ -33,29 +34,38 @@ struct AppendParams {
   uint8_t axis[64];
 };
 
-// two neighbouring entries as floats
-template <typename T> struct Pair;
-template <> struct Pair<float> {
-  typedef float2 raw;
-  static __device__ __forceinline__ float2 get(raw r) { return r; }
-  static __device__ __forceinline__ raw put(float a, float b) { return make_float2(a, b); }
+// four neighbouring entries as floats
+template <typename T> struct Four;
+template <> struct Four<float> {
+  typedef float4 raw;
+  static __device__ __forceinline__ float4 get(raw r) { return r; }
+  static __device__ __forceinline__ raw put(float4 v) { return v; }
 };
-template <> struct Pair<__nv_bfloat16> {
-  typedef __nv_bfloat162 raw;
-  static __device__ __forceinline__ float2 get(raw r) { return __bfloat1622float2(r); }
-  static __device__ __forceinline__ raw put(float a, float b) { return __floats2bfloat162_rn(a, b); }
+template <> struct Four<__nv_bfloat16> {
+  typedef uint2 raw;
+  static __device__ __forceinline__ float4 get(raw r) {
+    return make_float4(__uint_as_float(r.x << 16), __uint_as_float(r.x & 0xFFFF0000u), __uint_as_float(r.y << 16), __uint_as_float(r.y & 0xFFFF0000u));
+  }
+  static __device__ __forceinline__ raw put(float4 v) {
+    const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
+    return make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
+  }
 };
 
-__device__ __forceinline__ uint16_t to_e4m3x2(float a, float b) {   // a in the low byte; NaN stays NaN, the rest saturates
-  uint16_t r;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(b), "f"(a));
+// four e4m3 numbers of a word, the first in the low byte; NaN stays NaN, the rest saturates
+__device__ __forceinline__ uint32_t to_e4m3(float4 v) {
+  uint32_t r;
+  asm("{\n\t.reg .b16 a, b;\n\tcvt.rn.satfinite.e4m3x2.f32 a, %2, %1;\n\tcvt.rn.satfinite.e4m3x2.f32 b, %4, %3;\n\tmov.b32 %0, {a, b};\n\t}"
+      : "=r"(r)
+      : "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w));
   return r;
 }
-__device__ __forceinline__ float2 from_e4m3x2(uint16_t v) {
-  uint32_t h;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(v));
-  float2 f;
-  asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %2;\n\tcvt.f32.f16 %0, lo;\n\tcvt.f32.f16 %1, hi;\n\t}" : "=f"(f.x), "=f"(f.y) : "r"(h));
+__device__ __forceinline__ float4 from_e4m3(uint32_t v) {
+  float4 f;
+  asm("{\n\t.reg .b16 a, b, c, d;\n\t.reg .b32 x, y;\n\tmov.b32 {a, b}, %4;\n\tcvt.rn.f16x2.e4m3x2 x, a;\n\tcvt.rn.f16x2.e4m3x2 y, b;\n\t"
+      "mov.b32 {a, b}, x;\n\tmov.b32 {c, d}, y;\n\tcvt.f32.f16 %0, a;\n\tcvt.f32.f16 %1, b;\n\tcvt.f32.f16 %2, c;\n\tcvt.f32.f16 %3, d;\n\t}"
+      : "=f"(f.x), "=f"(f.y), "=f"(f.z), "=f"(f.w)
+      : "r"(v));
   return f;
 }
 __device__ __forceinline__ float finite_abs(float x) {
@@ -64,16 +74,20 @@ __device__ __forceinline__ float finite_abs(float x) {
 }
 __device__ __forceinline__ float scaled(float x, float s) { return fabsf(x) < INFINITY ? x * s : __int_as_float(0x7FFFFFFF); }
 
+__device__ __forceinline__ float4 scaled(float4 v, float s) { return make_float4(scaled(v.x, s), scaled(v.y, s), scaled(v.z, s), scaled(v.w, s)); }
+__device__ __forceinline__ float finite_abs(float4 v) { return fmaxf(fmaxf(finite_abs(v.x), finite_abs(v.y)), fmaxf(finite_abs(v.z), finite_abs(v.w))); }
+
 template <typename T, int HD>
-__global__ void __launch_bounds__(kAppendThreads) pool_append_kernel(const AppendParams p) {
+__global__ void __launch_bounds__(kAppendThreads, 2) pool_append_kernel(const __grid_constant__ AppendParams p) {
   constexpr int HALF = HD / 2;
-  constexpr int LANES = HD / 4;              // lanes of a row: two pairs each
+  constexpr int LANES = HD / 8;              // lanes of a row: four pairs each
   constexpr int STEP = 32 / LANES;           // rows a warp works on at once
   constexpr int N = kPoolBlock / STEP;       // rows of a lane
-  __shared__ float2 turn[kPoolBlock][HALF];
+  __shared__ alignas(16) float cosine[kPoolBlock][HALF], sine[kPoolBlock][HALF];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int b = blockIdx.x / p.blocks_per_seq, j = blockIdx.x - b * p.blocks_per_seq;
   const int32_t *pos = p.in_pos + (long)b * p.window;
+  const int seq = p.seqs ? p.seqs[b] : b;
   const int start = pos[0];
   if (start >= p.pool.pages_per_seq * KV_PAGE) {   // (at most 2^26: the sums below stay in 32 bits)
     if (tid == 0) pool_fault(p.pool.status, SJD_ERR_BAD_ARG);
@@ -83,26 +97,20 @@ __global__ void __launch_bounds__(kAppendThreads) pool_append_kernel(const Appen
   // rows of the window in this block: k0 .. k1 - 1, of which the first n_new are active
   const int k0 = start < 0 ? j * kPoolBlock : max(0, base - start), k1 = min(p.window, start < 0 ? k0 + kPoolBlock : base + kPoolBlock - start);
   if (k0 >= k1) return;
-  bool bad = false;
+  bool bad = seq < 0 || seq >= p.pool.n_seqs;
+  int page = -1;
+  if (!bad && start >= 0 && base < p.pool.pages_per_seq * KV_PAGE) page = p.pool.table[(long)seq * p.pool.pages_per_seq + base / KV_PAGE];
   int active = 0;
   if (tid < k1 - k0) {
     const int at = pos[k0 + tid];
     active = at >= 0;
-    bad = at < -1 || (active && (start < 0 || at != start + k0 + tid));
+    bad |= at < -1 || (active && (start < 0 || at != start + k0 + tid));
     if (active && k0 + tid > 0 && pos[k0 + tid - 1] < 0) bad = true;   // a hole before an active row
   }
-  int seq = p.seqs ? p.seqs[b] : b;
-  if (seq < 0 || seq >= p.pool.n_seqs) bad = true;
   for (int i = tid; p.seqs && i < p.batch; i += kAppendThreads) bad |= i != b && p.seqs[i] == seq;
   const int n_new = __syncthreads_count(active);
-  if (n_new > 0 && (long)base + kPoolBlock > (long)p.pool.pages_per_seq * KV_PAGE) bad = true;
-  bad = __syncthreads_or(bad);
-  int page = -1;
-  if (!bad && n_new > 0) {
-    page = p.pool.table[(long)seq * p.pool.pages_per_seq + base / KV_PAGE];
-    bad = page < 0 || page >= p.pool.n_pages;
-  }
-  if (bad) {
+  bad |= n_new > 0 && (page < 0 || page >= p.pool.n_pages);
+  if (__syncthreads_or(bad)) {
     if (tid == 0) pool_fault(p.pool.status, SJD_ERR_BAD_ARG);
     return;
   }
@@ -110,108 +118,110 @@ __global__ void __launch_bounds__(kAppendThreads) pool_append_kernel(const Appen
   const long m0 = (long)b * p.window + k0;      // first new row
   const int row0 = start + k0 - base;           // its place in the block; rows before it are kept
 
+  typedef typename Four<T>::raw raw;
+  const int sub = lane / LANES, d = (lane % LANES) * 4;   // lane's row of a step, its first pair
   const int h_begin = blockIdx.y * p.heads_per_block, h_all = p.n_heads + 2 * p.pool.n_kv_heads;
   const int h_end = min(h_all, h_begin + p.heads_per_block);
+  raw ra[N], rb[N];   // new rows as they are loaded
+  auto load = [&](int h) {
+    const bool is_q = h < p.n_heads, is_k = !is_q && h < p.n_heads + p.pool.n_kv_heads;
+    const int kh = is_q ? h : is_k ? h - p.n_heads : h - p.n_heads - p.pool.n_kv_heads;
+    const long stride = is_q ? p.q_stride : is_k ? p.k_stride : p.v_stride;
+    const T *src = (const T *)(is_q ? p.q : is_k ? p.k : p.v) + (m0 - row0) * stride + (long)kh * HD + d;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int r = i * STEP + sub;
+      if (r >= row0 && r < row0 + n_new) {
+        ra[i] = *reinterpret_cast<const raw *>(src + r * stride);
+        rb[i] = *reinterpret_cast<const raw *>(src + r * stride + HALF);
+      }
+    }
+  };
+  int h = h_begin + warp;
+  if (h < h_end) load(h);   // (under way while the angles are computed)
   if (p.rotate && h_begin < p.n_heads + p.pool.n_kv_heads) {
     for (int i = tid; i < n_new * HALF; i += kAppendThreads) {
       const int r = i / HALF, f = i % HALF;
       const int at = p.axis_pos ? p.axis_pos[(m0 + r) * p.n_axes + p.axis[f]] : start + k0 + r;
       double s, c;
       sincospi((double)at * p.turns[f], &s, &c);
-      turn[r][f] = make_float2((float)c, (float)s);
+      cosine[row0 + r][f] = (float)c;
+      sine[row0 + r][f] = (float)s;
     }
     __syncthreads();
   }
 
-  typedef typename Pair<T>::raw raw;
-  const int sub = lane / LANES, d = (lane % LANES) * 2;   // lane's row of a step, its first pair
-  for (int h = h_begin + warp; h < h_end; h += kAppendWarps) {
+  for (; h < h_end; h += kAppendWarps) {
     const bool is_q = h < p.n_heads, is_k = !is_q && h < p.n_heads + p.pool.n_kv_heads;
     const int kh = is_q ? h : is_k ? h - p.n_heads : h - p.n_heads - p.pool.n_kv_heads;
-    const long stride = is_q ? p.q_stride : is_k ? p.k_stride : p.v_stride;
-    const T *src = (const T *)(is_q ? p.q : is_k ? p.k : p.v) + m0 * stride + (long)kh * HD + d;
-    raw ra[N], rb[N];
+    float4 a[N], c[N];   // rows of the block: new ones, and with keys and values those that stay
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int r = i * STEP + sub;
-      if (r < n_new) {
-        ra[i] = *reinterpret_cast<const raw *>(src + r * stride);
-        rb[i] = *reinterpret_cast<const raw *>(src + r * stride + HALF);
-      }
-    }
-    float2 a[N], c[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int r = i * STEP + sub;
-      a[i] = c[i] = make_float2(0.0f, 0.0f);
-      if (r >= n_new) continue;
-      const float2 x = Pair<T>::get(ra[i]), y = Pair<T>::get(rb[i]);
+      a[i] = c[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      if (r < row0 || r >= row0 + n_new) continue;
+      const float4 x = Four<T>::get(ra[i]), y = Four<T>::get(rb[i]);
+      a[i] = x;
+      c[i] = y;
       if (p.rotate && (is_q || is_k)) {
-        const float2 t0 = turn[r][d], t1 = turn[r][d + 1];
-        a[i].x = __fsub_rn(__fmul_rn(x.x, t0.x), __fmul_rn(y.x, t0.y));
-        a[i].y = __fsub_rn(__fmul_rn(x.y, t1.x), __fmul_rn(y.y, t1.y));
-        c[i].x = __fadd_rn(__fmul_rn(y.x, t0.x), __fmul_rn(x.x, t0.y));
-        c[i].y = __fadd_rn(__fmul_rn(y.y, t1.x), __fmul_rn(x.y, t1.y));
-      } else {
-        a[i] = x;
-        c[i] = y;
+        const float4 cs = *reinterpret_cast<const float4 *>(&cosine[r][d]), sn = *reinterpret_cast<const float4 *>(&sine[r][d]);
+        a[i].x = __fsub_rn(__fmul_rn(x.x, cs.x), __fmul_rn(y.x, sn.x));
+        a[i].y = __fsub_rn(__fmul_rn(x.y, cs.y), __fmul_rn(y.y, sn.y));
+        a[i].z = __fsub_rn(__fmul_rn(x.z, cs.z), __fmul_rn(y.z, sn.z));
+        a[i].w = __fsub_rn(__fmul_rn(x.w, cs.w), __fmul_rn(y.w, sn.w));
+        c[i].x = __fadd_rn(__fmul_rn(y.x, cs.x), __fmul_rn(x.x, sn.x));
+        c[i].y = __fadd_rn(__fmul_rn(y.y, cs.y), __fmul_rn(x.y, sn.y));
+        c[i].z = __fadd_rn(__fmul_rn(y.z, cs.z), __fmul_rn(x.z, sn.z));
+        c[i].w = __fadd_rn(__fmul_rn(y.w, cs.w), __fmul_rn(x.w, sn.w));
       }
     }
     if (is_q) {
-      T *dst = (T *)p.q_out + m0 * p.out_stride + (long)kh * HD + d;
+      T *dst = (T *)p.q_out + (m0 - row0) * p.out_stride + (long)kh * HD + d;
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const int r = i * STEP + sub;
-        if (r >= n_new) continue;
-        *reinterpret_cast<raw *>(dst + r * p.out_stride) = Pair<T>::put(a[i].x, a[i].y);
-        *reinterpret_cast<raw *>(dst + r * p.out_stride + HALF) = Pair<T>::put(c[i].x, c[i].y);
+        if (r < row0 || r >= row0 + n_new) continue;
+        *reinterpret_cast<raw *>(dst + r * p.out_stride) = Four<T>::put(a[i]);
+        *reinterpret_cast<raw *>(dst + r * p.out_stride + HALF) = Four<T>::put(c[i]);
       }
-      continue;
-    }
-    const long plane = (((long)page * p.pool.n_layers + p.layer) * 2 + (is_k ? 0 : 1)) * p.pool.n_kv_heads + kh;
-    uint8_t *bytes = (uint8_t *)p.pool.pages + (plane * KV_PAGE + base % KV_PAGE) * HD + d;
-    int8_t *exp_at = p.pool.exps + plane * kPoolBlocks + base % KV_PAGE / kPoolBlock;
-    // rows that stay: at most 15, only in the window's first block
-    float2 ka[N], kc[N];
-    float top = 0.0f;
-    if (row0 > 0) {
-      const float s = two_to(pool_exp(*exp_at));
+    } else {
+      const long plane = (((long)page * p.pool.n_layers + p.layer) * 2 + (is_k ? 0 : 1)) * p.pool.n_kv_heads + kh;
+      uint8_t *bytes = (uint8_t *)p.pool.pages + (plane * KV_PAGE + base % KV_PAGE) * HD + d;
+      int8_t *exp_at = p.pool.exps + plane * kPoolBlocks + base % KV_PAGE / kPoolBlock;
+      if (row0 > 0) {   // rows that stay: at most 15, only in the window's first block
+        const float s = two_to(pool_exp(*exp_at));
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const int r = i * STEP + sub;
+          if (r >= row0) continue;
+          a[i] = from_e4m3(*reinterpret_cast<const uint32_t *>(bytes + r * HD));
+          c[i] = from_e4m3(*reinterpret_cast<const uint32_t *>(bytes + r * HD + HALF));
+          a[i].x *= s, a[i].y *= s, a[i].z *= s, a[i].w *= s;
+          c[i].x *= s, c[i].y *= s, c[i].z *= s, c[i].w *= s;
+        }
+        __syncwarp();   // (every lane has read the exponent)
+      }
+      float top = 0.0f;
+#pragma unroll
+      for (int i = 0; i < N; ++i) top = fmaxf(top, fmaxf(finite_abs(a[i]), finite_abs(c[i])));
+      top = warp_max(top);
+      // top = f 2^e, 1/2 <= f < 1: the smallest power of two that brings it to 448 = 7/8 2^9 at most
+      int e = 0;
+      if (top > 0.0f) {
+        const float f = frexpf(top, &e);
+        e = pool_exp(e - 9 + (f > 0.875f));
+      }
+      const float inv = two_to(-e);
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const int r = i * STEP + sub;
-        ka[i] = kc[i] = make_float2(0.0f, 0.0f);
-        if (r >= row0) continue;
-        ka[i] = from_e4m3x2(*reinterpret_cast<const uint16_t *>(bytes + r * HD));
-        kc[i] = from_e4m3x2(*reinterpret_cast<const uint16_t *>(bytes + r * HD + HALF));
-        ka[i].x *= s, ka[i].y *= s, kc[i].x *= s, kc[i].y *= s;
-        top = fmaxf(top, fmaxf(fmaxf(finite_abs(ka[i].x), finite_abs(ka[i].y)), fmaxf(finite_abs(kc[i].x), finite_abs(kc[i].y))));
+        if (r >= row0 + n_new) continue;
+        *reinterpret_cast<uint32_t *>(bytes + r * HD) = to_e4m3(scaled(a[i], inv));
+        *reinterpret_cast<uint32_t *>(bytes + r * HD + HALF) = to_e4m3(scaled(c[i], inv));
       }
+      if (lane == 0) *exp_at = (int8_t)e;
     }
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      top = fmaxf(top, fmaxf(fmaxf(finite_abs(a[i].x), finite_abs(a[i].y)), fmaxf(finite_abs(c[i].x), finite_abs(c[i].y))));
-    top = warp_max(top);
-    // top = f 2^e, 1/2 <= f < 1: the smallest power of two that brings it to 448 = 7/8 2^9 at most
-    int e = 0;
-    if (top > 0.0f) {
-      const float f = frexpf(top, &e);
-      e = pool_exp(e - 9 + (f > 0.875f));
-    }
-    const float inv = two_to(-e);
-    auto put = [&](int r, float2 x, float2 y) {
-      *reinterpret_cast<uint16_t *>(bytes + r * HD) = to_e4m3x2(scaled(x.x, inv), scaled(x.y, inv));
-      *reinterpret_cast<uint16_t *>(bytes + r * HD + HALF) = to_e4m3x2(scaled(y.x, inv), scaled(y.y, inv));
-    };
-    if (row0 > 0) {
-      __syncwarp();   // (every lane has read the exponent)
-#pragma unroll
-      for (int i = 0; i < N; ++i)
-        if (i * STEP + sub < row0) put(i * STEP + sub, ka[i], kc[i]);
-    }
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (i * STEP + sub < n_new) put(row0 + i * STEP + sub, a[i], c[i]);
-    if (lane == 0) *exp_at = (int8_t)e;
+    if (h + kAppendWarps < h_end) load(h + kAppendWarps);
   }
 }
 
@@ -233,8 +243,8 @@ extern "C" int sjd_pool_append(const sjd_pool *pool, int layer, int batch, int w
   const int hd = pool->head_dim;
   const int64_t kv_row = (int64_t)pool->n_kv_heads * hd, q_row = q ? (int64_t)n_heads * hd : 0;
   if (k_stride < kv_row || v_stride < kv_row || (q && (q_stride < q_row || q_out_stride < q_row))) return SJD_ERR_BAD_ARG;
-  if (((k_stride | v_stride) & 1) || (q && ((q_stride | q_out_stride) & 1))) return SJD_ERR_BAD_ARG;
-  const uintptr_t align = dtype == SJD_F32 ? 7 : 3;
+  if (((k_stride | v_stride) & 3) || (q && ((q_stride | q_out_stride) & 3))) return SJD_ERR_BAD_ARG;
+  const uintptr_t align = dtype == SJD_F32 ? 15 : 7;
   if ((((uintptr_t)k | (uintptr_t)v | (q ? (uintptr_t)q | (uintptr_t)q_out : 0)) & align) != 0) return SJD_ERR_BAD_ARG;
   AppendParams p;
   memset(&p, 0, sizeof(p));

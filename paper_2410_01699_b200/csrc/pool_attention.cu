@@ -34,7 +34,8 @@ constexpr int kMaxEntries = 512;     // (sequence, tile of rows) pairs of a call
 constexpr int kMaxSlots = 8;
 constexpr int kMeta = 16;            // tiles that the fetching warp may be ahead: more than the ring holds
 constexpr int kMaxCtas = 320;
-constexpr int kMinTiles = 2;        // of a range
+constexpr int kUnitCost = 3;        // what a unit's begin and end take, in tiles
+constexpr int kMinTiles = 5;        // of a range, with that
 constexpr int kWholeTiles = 4;      // units of up to so many tiles are not cut where they are few
 constexpr int kUp = 8;               // the largest weight of a row in a tile is 2^kUp (e4m3 ends at 448)
 
@@ -61,7 +62,7 @@ __host__ __device__ constexpr int ctas_of(int rp) { return rp == 64 ? 1 : 2; }
 __host__ __device__ constexpr int threads_of(int rp) { return groups_of(rp) * 128 + 64; }
 
 struct Entry {   // (sequence, tile of rows)
-  int before;    // tiles of one kv head in the entries before
+  int before;    // cost of one kv head in the entries before: their tiles, and kUnitCost for each
   int low;       // first tile of the sliding part
   int sink;      // tiles before it
 };
@@ -310,7 +311,7 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
     }
     return at;
   };
-  const int n_entries = p.cut ? p.n_entries : 1;
+  const int n_entries = p.cut ? p.n_entries : 1, unit_cost = p.cut ? kUnitCost : 0;
   const int unit0 = p.cut ? 0 : blockIdx.x;
   // (entry numbers: sequence by sequence; without ranges the units with the most keys, the last rows of a window, start first)
   auto entry_at = [&](int e, int *b, int *rt) {
@@ -352,7 +353,7 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
         Entry n;
         n.low = p.sliding > 0 && hi >= 0 ? max(0, lo - p.sliding + 1) / kTile : 0;
         n.sink = min(n.low, (min(p.sinks, seq_keys) + kTile - 1) / kTile);
-        n.before = hi < 0 ? 0 : hi / kTile + 1 - n.low + n.sink;   // (its own tiles so far)
+        n.before = hi < 0 ? 0 : hi / kTile + 1 - n.low + n.sink + unit_cost;   // (its own so far)
         sh.entry[e] = n;
       }
     }
@@ -392,9 +393,9 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
   }
   const int t_begin = p.cut ? (int)min((long)all, (long)blockIdx.x * chunk) : 0, t_end = min(all, t_begin + chunk);
 
-  // unit of a tile: its entry, kv head, first tile
+  // Places on the line: kUnitCost of a unit, then its tiles.  Unit of a place:
   struct Unit {
-    int e, b, rt, kvh, n, first;      // n: its tiles
+    int e, b, rt, kvh, n, first;      // n: its tiles; first: the place of the first one
   };
   auto unit_of = [&](int t) {
     Unit u;
@@ -405,10 +406,10 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
       if (sh.entry[mid].before * heads <= t) lo = mid; else hi = mid - 1;
     }
     u.e = lo;
-    u.n = sh.entry[lo + 1].before - sh.entry[lo].before;
-    const int in = t - sh.entry[lo].before * heads, h = in / u.n;
+    const int len = sh.entry[lo + 1].before - sh.entry[lo].before, in = t - sh.entry[lo].before * heads, h = in / len;
+    u.n = len - unit_cost;
     u.kvh = p.cut ? h : unit0 % kv_heads;
-    u.first = t - (in - h * u.n);
+    u.first = t - (in - h * len) + unit_cost;
     entry_at(lo, &u.b, &u.rt);
     return u;
   };
@@ -427,13 +428,15 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
     uint32_t phase = 1;
     int issued = 0;
     bool ok = true;
-    int n_key0 = 0, n_page[2] = {-1, -1}, n_ke[2] = {0, 0}, n_ve[2] = {0, 0}, n_head = 0, n_last = 0;
+    int n_key0 = 0, n_page[2] = {-1, -1}, n_ke[2] = {0, 0}, n_ve[2] = {0, 0}, n_head = 0, n_last = 0, n_tile = 0;
     auto look_up = [&](int t) {   // what lane `lane` knows of tile t + lane
       n_page[0] = n_page[1] = -1;
-      n_last = 0;
+      n_last = n_tile = 0;
       if (t + lane >= t_end) return;
       const Unit u = unit_of(t + lane);
       const int i = t + lane - u.first;
+      if (i < 0) return;   // (no tile)
+      n_tile = 1;
       const Entry en = sh.entry[u.e];
       n_key0 = (i < en.sink ? i : en.low + i - en.sink) * kTile;
       n_head = u.kvh;
@@ -494,20 +497,23 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
         if (e_max - e_min > 64) m.pages |= 4;
       }
       const int pg0 = n_page[0], pg1 = n_page[1], head = n_head, last = n_last;
-      if (t0 + 32 < t_end) look_up(t0 + 32);
-      const int n = min(32, t_end - t0);
+      const unsigned tiles = __ballot_sync(0xffffffffu, n_tile);
+      const int rank = n_tile ? __popc(tiles & ((1u << lane) - 1)) : 32, n = __popc(tiles);
       int told = 0;   // tiles of these 32 whose lanes have written what they know: not before the copies that there is room for are under way
       auto tell = [&](int upto) {
-        if (lane >= told && lane < upto) {
-          const int at = (meta + lane) % kMeta;
+        if (rank >= told && rank < upto) {
+          const int at = (meta + rank) % kMeta;
           sh.meta[at] = m;
           arrive(&sh.meta_full[at]);
         }
         __syncwarp();
         told = upto;
       };
-      for (int i = 0; i < n && ok; ++i) {
-        const int page0 = __shfl_sync(0xffffffffu, pg0, i), page1 = __shfl_sync(0xffffffffu, pg1, i), h = __shfl_sync(0xffffffffu, head, i);
+      unsigned todo = tiles;
+      if (t0 + 32 < t_end) look_up(t0 + 32);
+      for (int i = 0; i < n && ok; ++i, todo &= todo - 1) {
+        const int from = __ffs(todo) - 1;
+        const int page0 = __shfl_sync(0xffffffffu, pg0, from), page1 = __shfl_sync(0xffffffffu, pg1, from), h = __shfl_sync(0xffffffffu, head, from);
         if (issued + 3 > p.slots) tell(i + 1);   // (a copy of this round may have to wait)
         fetch(h, page0, page1);
         if (v_open && ok) fetch(v_plane, v_page0, v_page1);
@@ -515,7 +521,7 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
         v_page0 = page0;
         v_page1 = page1;
         v_open = true;
-        if (__shfl_sync(0xffffffffu, last, i) && ok) {
+        if (__shfl_sync(0xffffffffu, last, from) && ok) {
           fetch(v_plane, v_page0, v_page1);
           v_open = false;
         }
@@ -577,6 +583,8 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
     };
     for (int t = t_begin; t < t_end && ok;) {
       const Unit u = unit_of(t);
+      t = max(t, u.first);
+      if (t >= t_end) break;
       const int n = min(t_end, u.first + u.n) - t;
       scores(true);
       for (int i = 1; i < n && ok; ++i) {
@@ -680,20 +688,24 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
     };
 
     int up = 0;
+    int t_first = t_end;
     if (t_begin < t_end) {
       const Unit u = unit_of(t_begin);
-      load_queries(u);
-      publish_queries(u, 0);
+      t_first = max(t_begin, u.first);
+      if (t_first < t_end) {
+        load_queries(u);
+        publish_queries(u, 0);
+      }
     }
     if (p.cut && tid == 0) {
       int4 c = make_int4(0, 0, 0, 0);
       if (t_begin < t_end && t_end < all) {
-        const Unit u = unit_of(t_end - 1);
-        if (u.first >= t_begin && u.first + u.n > t_end) {
-          c.x = u.b;
-          c.y = u.rt;
-          c.z = u.kvh;
-          c.w = (u.first + u.n - 1) / chunk - (int)blockIdx.x + 1;
+        const Unit l = unit_of(t_end - 1);
+        if (l.first >= t_begin && l.first < t_end && l.first + l.n > t_end) {
+          c.x = l.b;
+          c.y = l.rt;
+          c.z = l.kvh;
+          c.w = (l.first + l.n - 1) / chunk - (int)blockIdx.x + 1;
         }
       }
       p.cuts[blockIdx.x] = c;
@@ -711,7 +723,7 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
               store1(outp + ((long)b * p.window + r / p.group) * p.out_stride + ((long)h * p.group + r % p.group) * HD + i, 0.0f);
       }
     }
-    for (int t = t_begin; t < t_end; up ^= 1) {
+    for (int t = t_first; t < t_end; up ^= 1) {
       const Unit u = unit_of(t);
       const int u_end = u.first + u.n, end = min(t_end, u_end);
       const int n = end - t;
@@ -947,10 +959,10 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
         if (lane == 0) arrive(&sh.p_full);
       }
       v_use += 2 * n;
-      t = end;
       // ---- the next unit's queries, and this one's sums over the keys, while the last tile is multiplied
-      const Unit next = unit_of(t < t_end ? t : t_end - 1);
-      if (t < t_end) load_queries(next);
+      const Unit next = unit_of(end < t_end ? end : end - 1);
+      const bool more = end < t_end && next.first < t_end;
+      if (more) load_queries(next);
       {
         float v[NQ];
 #pragma unroll
@@ -970,7 +982,7 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
         sh.inv[r] = sh.pos[up][r] >= 0 && sum != 0.0f ? two_to(-kUp) / sum : 0.0f;   // (a NaN among the scores makes the sum NaN)
         if (cut) p.stats[my * RP + r] = make_float2(my_run, sum);
       }
-      if (t < t_end) publish_queries(next, up ^ 1);   // (all scores of this unit have been waited for)
+      if (more) publish_queries(next, up ^ 1);   // (all scores of this unit have been waited for)
       if (ok && !warp_wait(&sh.o_full, o_ph)) {
         ok = false;
         fail();
@@ -993,6 +1005,7 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
           }
         }
       }
+      t = more ? next.first : t_end;
     }
   }
 
@@ -1161,7 +1174,7 @@ extern "C" int sjd_pool_attention(const sjd_pool *pool, int layer, int batch, in
     most = most < in ? most : in;
   }
   p.cut = entries <= kMaxEntries && (int64_t)batch * window <= 8192 && (most > kWholeTiles || units > 2 * sms) &&
-          units * most < 1 << 30;   // (tiles are counted in 32 bits)
+          units * (most + kUnitCost) < 1 << 30;   // (places are counted in 32 bits)
   p.n_entries = (int)entries;
   const CUtensorMap &m = reinterpret_cast<const CUtensorMap &>(map);
   auto launch = [&](auto kernel, auto join, int RP, int PL, size_t shared) -> int {
