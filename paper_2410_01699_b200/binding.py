@@ -311,15 +311,18 @@ class CachePool:
             if x.dtype != dt or not x.is_contiguous() or x.device != pages.device:
                 raise ValueError("a pool's tensors are contiguous, on one device, of types e4m3, int8, int32 and int32")
         self.pages, self.exps, self.table, self.refs = pages, exps, table, refs
-        self.device = pages.device
+        self.device, self.index = pages.device, pages.get_device()   # (-1: on the host, where nothing can be launched)
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
         self.c = sjd_pool(pages.data_ptr(), exps.data_ptr(), table.data_ptr(), refs.data_ptr(), self.status.data_ptr(), n_pages,
                           table.shape[0], table.shape[1], n_layers, n_kv_heads, head_dim)
-        self.ws_bytes = int(lib().sjd_pool_workspace_bytes(C.byref(self.c)))
+        self.n_kv_heads, self.head_dim = n_kv_heads, head_dim
+        self.ref = C.byref(self.c)
+        self.ws_bytes = int(lib().sjd_pool_workspace_bytes(self.ref))
         if self.ws_bytes == 0:
             raise SJDError(SJD_ERR_UNSUPPORTED, "sjd_pool_workspace_bytes")
         self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.device)
-        self._attention_ws = torch.empty(0, dtype=torch.uint8, device=self.device)
+        self.ws_at = self.ws.data_ptr()
+        self._attention_ws = None
 
     @classmethod
     def empty(cls, n_pages, n_seqs, pages_per_seq, n_layers, n_kv_heads, head_dim, device="cuda"):
@@ -329,11 +332,10 @@ class CachePool:
                    torch.full((n_seqs, pages_per_seq), -1, dtype=torch.int32, device=device),
                    torch.zeros(n_pages, dtype=torch.int32, device=device))
 
-    def attention_ws(self, window: int, n_heads: int):
-        nbytes = int(lib().sjd_pool_attention_workspace_bytes(C.byref(self.c), window, n_heads))
-        if nbytes == 0:
-            raise SJDError(SJD_ERR_BAD_ARG, "sjd_pool_attention_workspace_bytes")
-        if self._attention_ws.numel() < nbytes:
+    def attention_ws(self):
+        """The pool's workspace for attention calls, large enough for all of them (a captured graph keeps its address)."""
+        if self._attention_ws is None:
+            nbytes = int(lib().sjd_pool_attention_workspace_bytes(self.ref, 64, self.n_kv_heads))   # (tiles have at most 64 rows)
             self._attention_ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         return self._attention_ws
 
@@ -354,26 +356,50 @@ def make_rope_cfg(pairs, theta=10000.0, interleaved=False, per_axis=False) -> sj
                     float(theta))
 
 
+# These calls are made once or more a layer and can be shorter on the device than in here: pointers go as plain integers, the device is
+# switched only where it is another one than the current, and the stream is asked for without making an object of it.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+def _pool_call(pool, where, function, *args):
+    """function(pool, *args, stream) on the pool's device and its current stream."""
+    index = pool.index
+    if index < 0:
+        raise ValueError("%s: a pool on the host" % where)
+    if torch.cuda.current_device() == index:
+        status = function(pool.ref, *args, _raw_stream(index))
+    else:
+        with torch.cuda.device(index):
+            status = function(pool.ref, *args, _raw_stream(index))
+    if status != SJD_OK:
+        raise SJDError(status, where)
+
+
 def _pool_rows(x, heads, pool, rows, where):
     """Row stride of x [rows][heads][head_dim], whose rows may be parts of longer ones."""
-    hd = pool.c.head_dim
-    if x.dim() != 3 or tuple(x.shape) != (rows, heads, hd) or x.stride(2) != 1 or (heads > 1 and x.stride(1) != hd):
+    hd, stride = pool.head_dim, x.stride()
+    if x.shape != (rows, heads, hd) or stride[2] != 1 or (heads > 1 and stride[1] != hd):
         raise ValueError("%s: a tensor [%d][%d][%d] whose rows are contiguous" % (where, rows, heads, hd))
-    if x.device != pool.device:
+    if x.get_device() != pool.index:
         raise ValueError("%s: on another device than the pool" % where)
-    return x.stride(0) if rows > 1 else max(x.stride(0), heads * hd)
+    return stride[0] if rows > 1 else max(stride[0], heads * hd)
 
 
 def _ints(x, n, pool, where):
-    if x is not None and (x.dtype != torch.int32 or not x.is_contiguous() or x.numel() != n or x.device != pool.device):
+    """Address of n int32 entries on the pool's device; None for None."""
+    if x is None:
+        return None
+    if x.dtype is not torch.int32 or x.numel() != n or not x.is_contiguous() or x.get_device() != pool.index:
         raise ValueError("%s: %d contiguous int32 entries on the pool's device" % (where, n))
-    return _ptr(x)
+    return x.data_ptr()
 
 
 def _pool_dtype(x, where):
-    if x.dtype not in (torch.float32, torch.bfloat16):
-        raise SJDError(SJD_ERR_UNSUPPORTED, where)
-    return SJD_F32 if x.dtype == torch.float32 else SJD_BF16
+    if x.dtype is torch.float32:
+        return SJD_F32
+    if x.dtype is torch.bfloat16:
+        return SJD_BF16
+    raise SJDError(SJD_ERR_UNSUPPORTED, where)
 
 
 def sjd_pool_append(pool: CachePool, layer: int, k, v, in_pos, window: int, q=None, q_out=None, rope: sjd_rope | None = None,
@@ -381,29 +407,25 @@ def sjd_pool_append(pool: CachePool, layer: int, k, v, in_pos, window: int, q=No
     """Rotates q and k, appends k and v to the pool; returns the rotated q (q_out, which may be q; a new tensor if not given).
     q [B*W][H][hd], k, v [B*W][KVh][hd] of one type, float32 or bfloat16, possibly parts of one matrix; in_pos int32 [B*W];
     axis_pos int32 [B*W][n_axes]; seqs int32 [B] or None (sequence b is row b of the table)."""
-    m = in_pos.numel()
+    m, kvh = in_pos.numel(), pool.n_kv_heads
     dtype = _pool_dtype(k, "sjd_pool_append")
     if m % window != 0 or v.dtype != k.dtype or (q is not None and q.dtype != k.dtype):
         raise ValueError("sjd_pool_append: whole windows, and q, k, v of one type")
-    kvh = pool.c.n_kv_heads
-    heads, qs, outs = 0, 0, 0
+    heads, q_at, q_stride, out_at, out_stride = 0, None, 0, None, 0
     if q is not None:
         heads = q.shape[1]
-        qs = _pool_rows(q, heads, pool, m, "q")
+        q_at, q_stride = q.data_ptr(), _pool_rows(q, heads, pool, m, "q")
         if q_out is None:
             q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
         if q_out.dtype != q.dtype:
             raise ValueError("q_out: of q's type")
-        outs = _pool_rows(q_out, heads, pool, m, "q_out")
+        out_at, out_stride = q_out.data_ptr(), _pool_rows(q_out, heads, pool, m, "q_out")
     if axis_pos is not None and rope is None:
         raise ValueError("axis_pos without rope")
-    with torch.cuda.device(pool.device):
-        _check(lib().sjd_pool_append(C.byref(pool.c), layer, m // window, window, heads, dtype, _ptr(q), qs, _ptr(k),
-                                     _pool_rows(k, kvh, pool, m, "k"), _ptr(v), _pool_rows(v, kvh, pool, m, "v"),
-                                     _ints(seqs, m // window, pool, "seqs"), _ints(in_pos, m, pool, "in_pos"),
-                                     C.byref(rope) if rope is not None else None,
-                                     _ints(axis_pos, m * (rope.n_axes if rope is not None else 0), pool, "axis_pos"), _ptr(q_out), outs,
-                                     _stream()), "sjd_pool_append")
+    _pool_call(pool, "sjd_pool_append", lib().sjd_pool_append, layer, m // window, window, heads, dtype, q_at, q_stride, k.data_ptr(),
+               _pool_rows(k, kvh, pool, m, "k"), v.data_ptr(), _pool_rows(v, kvh, pool, m, "v"), _ints(seqs, m // window, pool, "seqs"),
+               _ints(in_pos, m, pool, "in_pos"), C.byref(rope) if rope is not None else None,
+               _ints(axis_pos, m * (rope.n_axes if rope is not None else 0), pool, "axis_pos"), out_at, out_stride)
     return q_out
 
 
@@ -418,44 +440,39 @@ def sjd_pool_attention(pool: CachePool, layer: int, q, in_pos, window: int, slid
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
     if out.dtype != q.dtype:
         raise ValueError("out: of q's type")
-    with torch.cuda.device(pool.device):
-        if ws is None:
-            ws = pool.attention_ws(window, heads)
-        _check(lib().sjd_pool_attention(C.byref(pool.c), layer, m // window, window, heads, dtype, _ptr(q),
-                                        _pool_rows(q, heads, pool, m, "q"), _ints(seqs, m // window, pool, "seqs"),
-                                        _ints(in_pos, m, pool, "in_pos"), sliding, sinks, scale, _ptr(out),
-                                        _pool_rows(out, heads, pool, m, "out"), _ptr(ws), ws.numel(), _stream()), "sjd_pool_attention")
+    if ws is None:
+        ws = pool.attention_ws()
+    elif ws.get_device() != pool.index or not ws.is_contiguous():
+        raise ValueError("ws: contiguous, on the pool's device")
+    _pool_call(pool, "sjd_pool_attention", lib().sjd_pool_attention, layer, m // window, window, heads, dtype, q.data_ptr(),
+               _pool_rows(q, heads, pool, m, "q"), _ints(seqs, m // window, pool, "seqs"), _ints(in_pos, m, pool, "in_pos"), sliding, sinks,
+               scale, out.data_ptr(), _pool_rows(out, heads, pool, m, "out"), ws.data_ptr(), ws.nbytes)
     return out
 
 
 def sjd_pool_reserve(pool: CachePool, seqs, begin, end):
     """Own pages for positions begin[i] .. end[i] - 1 of sequence seqs[i] (int32 cuda tensors)."""
     n = seqs.numel()
-    with torch.cuda.device(pool.device):
-        _check(lib().sjd_pool_reserve(C.byref(pool.c), n, _ints(seqs, n, pool, "seqs"), _ints(begin, n, pool, "begin"),
-                                      _ints(end, n, pool, "end"), _ptr(pool.ws), pool.ws_bytes, _stream()), "sjd_pool_reserve")
+    _pool_call(pool, "sjd_pool_reserve", lib().sjd_pool_reserve, n, _ints(seqs, n, pool, "seqs"), _ints(begin, n, pool, "begin"),
+               _ints(end, n, pool, "end"), pool.ws_at, pool.ws_bytes)
 
 
 def sjd_pool_fork(pool: CachePool, src, dst, length):
     """The empty sequence dst[i] shares the pages of the first length[i] positions of src[i] (int32 cuda tensors)."""
     n = src.numel()
-    with torch.cuda.device(pool.device):
-        _check(lib().sjd_pool_fork(C.byref(pool.c), n, _ints(src, n, pool, "src"), _ints(dst, n, pool, "dst"),
-                                   _ints(length, n, pool, "length"), _stream()), "sjd_pool_fork")
+    _pool_call(pool, "sjd_pool_fork", lib().sjd_pool_fork, n, _ints(src, n, pool, "src"), _ints(dst, n, pool, "dst"),
+               _ints(length, n, pool, "length"))
 
 
 def sjd_pool_free(pool: CachePool, seqs, keep):
     """Sequence seqs[i] gives back the pages behind its first keep[i] positions (int32 cuda tensors)."""
     n = seqs.numel()
-    with torch.cuda.device(pool.device):
-        _check(lib().sjd_pool_free(C.byref(pool.c), n, _ints(seqs, n, pool, "seqs"), _ints(keep, n, pool, "keep"), _stream()),
-               "sjd_pool_free")
+    _pool_call(pool, "sjd_pool_free", lib().sjd_pool_free, n, _ints(seqs, n, pool, "seqs"), _ints(keep, n, pool, "keep"))
 
 
 def sjd_pool_compact(pool: CachePool):
     """Moves pages so that those in use are the first ones of the pool."""
-    with torch.cuda.device(pool.device):
-        _check(lib().sjd_pool_compact(C.byref(pool.c), _ptr(pool.ws), pool.ws_bytes, _stream()), "sjd_pool_compact")
+    _pool_call(pool, "sjd_pool_compact", lib().sjd_pool_compact, pool.ws_at, pool.ws_bytes)
 
 
 class Context:

@@ -13,6 +13,9 @@ namespace {
 constexpr int kPlanThreads = 1024;
 constexpr int kCopyThreads = 256;
 constexpr int kListMax = SJD_POOL_MAX_LIST;
+// One block does what takes it less than a launch more would: copies of 128 KB (8 rounds of 16 KB), tables of 16384 entries (16 rounds).
+constexpr size_t kCopyHere = 128 << 10;
+constexpr int kForkHere = 16384;
 
 // device scratch of a call: counts, then int32 lists of n_pages each
 constexpr int kLists = 6;
@@ -77,7 +80,7 @@ __device__ bool list_bad(const int32_t *seqs, int n, int n_seqs, uint32_t *seen)
 // A claim is (list entry, page of its range); claims are numbered entry by entry.
 __global__ void __launch_bounds__(kPlanThreads) reserve_plan_kernel(sjd_pool p, int n, const int32_t *__restrict__ seqs,
                                                                     const int32_t *__restrict__ begin, const int32_t *__restrict__ end,
-                                                                    PlanScratch ps) {
+                                                                    PlanScratch ps, size_t page_bytes, size_t page_exps, int copy_here) {
   extern __shared__ uint32_t seen[];
   __shared__ int warp_sums[32];
   __shared__ int first[kListMax + 1];   // number of the first claim of every list entry
@@ -233,6 +236,17 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_plan_kernel(sjd_pool p, 
     if (ps.old[i] >= 0) atomicSub(&p.refs[ps.old[i]], 1);
   }
   if (tid == 0) *ps.count = copies;
+  if (copy_here) {   // few bytes: a launch less
+    for (int i = 0; i < copies; ++i) {
+      const uint4 *src = reinterpret_cast<const uint4 *>((const char *)p.pages + (size_t)ps.src[i] * page_bytes);
+      uint4 *dst = reinterpret_cast<uint4 *>((char *)p.pages + (size_t)ps.dst[i] * page_bytes);
+#pragma unroll 4
+      for (size_t j = tid; j < page_bytes / 16; j += kPlanThreads) dst[j] = src[j];
+      const int32_t *es = reinterpret_cast<const int32_t *>(p.exps + (size_t)ps.src[i] * page_exps);
+      int32_t *ed = reinterpret_cast<int32_t *>(p.exps + (size_t)ps.dst[i] * page_exps);
+      for (int j = tid; j < (int)(page_exps / 4); j += kPlanThreads) ed[j] = es[j];
+    }
+  }
 }
 
 // pages src[i] -> dst[i], i < *count, in pieces of 16 KB (all of a thread's loads in flight before its stores); REMAP: tables first
@@ -368,6 +382,42 @@ __global__ void __launch_bounds__(kCopyThreads) fork_kernel(sjd_pool p, const in
   }
 }
 
+// the same in one block, for lists and tables of few entries
+__global__ void __launch_bounds__(kPlanThreads) fork_one_kernel(sjd_pool p, int n, const int32_t *__restrict__ src,
+                                                                const int32_t *__restrict__ dst, const int32_t *__restrict__ len) {
+  extern __shared__ uint32_t seen[];
+  pdl_trigger();
+  pdl_wait();
+  bool bad = *(volatile int32_t *)p.status != 0;
+  if (__syncthreads_or(bad)) return;
+  bad = list_bad(dst, n, p.n_seqs, seen);
+  for (int i = threadIdx.x; !bad && i < n; i += kPlanThreads) {
+    const int s = src[i], l = len[i];
+    bad = s < 0 || s >= p.n_seqs || l < 0 || l > (long)p.pages_per_seq * KV_PAGE || (seen[s >> 5] >> (s & 31) & 1u);
+  }
+  bad = __syncthreads_or(bad) != 0;
+  const int all = n * p.pages_per_seq;
+  if (!bad) {
+    for (int x = threadIdx.x; x < all; x += kPlanThreads) {
+      const int i = x / p.pages_per_seq, j = x - i * p.pages_per_seq;
+      const int from = j * KV_PAGE < len[i] ? p.table[(size_t)src[i] * p.pages_per_seq + j] : 0;
+      bad |= p.table[(size_t)dst[i] * p.pages_per_seq + j] != -1 || from < 0 || from >= p.n_pages;
+    }
+    bad = __syncthreads_or(bad) != 0;
+  }
+  if (bad) {
+    if (threadIdx.x == 0) pool_fault(p.status, SJD_ERR_BAD_ARG);
+    return;
+  }
+  for (int x = threadIdx.x; x < all; x += kPlanThreads) {
+    const int i = x / p.pages_per_seq, j = x - i * p.pages_per_seq;
+    if (j * KV_PAGE >= len[i]) continue;
+    const int page = p.table[(size_t)src[i] * p.pages_per_seq + j];
+    p.table[(size_t)dst[i] * p.pages_per_seq + j] = page;
+    atomicAdd(&p.refs[page], 1);
+  }
+}
+
 // a block for each sequence; every block sees from the list alone whether the call is refused
 __global__ void __launch_bounds__(kCopyThreads) free_kernel(sjd_pool p, int n, const int32_t *__restrict__ seqs, const int32_t *__restrict__ keep) {
   extern __shared__ uint32_t seen[];
@@ -447,8 +497,11 @@ extern "C" int sjd_pool_reserve(const sjd_pool *pool, int n, const int32_t *seqs
   const PlanScratch ps = scratch_of(ws, pool->n_pages);
   cudaStream_t stream = (cudaStream_t)cuda_stream;
   PdlScope pdl;
-  SJD_CUDA(launch_kernel(reserve_plan_kernel, dim3(1), dim3(kPlanThreads), seen_bytes(*pool), stream, *pool, n, seqs, begin, end, ps));
+  const int copy_here = (size_t)n * pool_page_bytes(*pool) <= kCopyHere;
+  SJD_CUDA(launch_kernel(reserve_plan_kernel, dim3(1), dim3(kPlanThreads), seen_bytes(*pool), stream, *pool, n, seqs, begin, end, ps,
+                         pool_page_bytes(*pool), pool_page_exps(*pool), copy_here));
   SJD_CHECK_LAUNCH();
+  if (copy_here) return SJD_OK;
   return launch_copies<false>(*pool, ps, n, stream);   // (only the page in which an entry begins can have positions before it)
 }
 
@@ -460,6 +513,11 @@ extern "C" int sjd_pool_fork(const sjd_pool *pool, int n, const int32_t *src, co
   if (n == 0) return SJD_OK;
   cudaStream_t stream = (cudaStream_t)cuda_stream;
   PdlScope pdl;
+  if ((int64_t)n * pool->pages_per_seq <= kForkHere) {
+    SJD_CUDA(launch_kernel(fork_one_kernel, dim3(1), dim3(kPlanThreads), seen_bytes(*pool), stream, *pool, n, src, dst, len));
+    SJD_CHECK_LAUNCH();
+    return SJD_OK;
+  }
   SJD_CUDA(launch_kernel(fork_check_kernel, dim3(n), dim3(kCopyThreads), seen_bytes(*pool), stream, *pool, n, src, dst, len));
   SJD_CHECK_LAUNCH();
   SJD_CUDA(launch_kernel(fork_kernel, dim3(n), dim3(kCopyThreads), 0, stream, *pool, src, dst, len));

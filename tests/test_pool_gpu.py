@@ -305,7 +305,7 @@ def test_calls_of_two_streams_and_graphs():
     pos = _i32(_window_pos(lens, 4))
     want = B.sjd_pool_attention(pool, 0, q, pos, 4)
     torch.cuda.synchronize()
-    ws = [torch.zeros_like(pool.attention_ws(4, 4)) for _ in range(2)]
+    ws = [torch.empty_like(pool.attention_ws()) for _ in range(2)]
     outs = [torch.empty_like(q) for _ in range(2)]
     streams = [torch.cuda.Stream() for _ in range(2)]
     graphs = []
@@ -531,6 +531,19 @@ def test_a_long_list_in_a_large_pool():
     _same(pool, ref, entries=False)
     B.sjd_pool_compact(pool)
     ref.compact()
+    _same(pool, ref, entries=False)
+    empty = [s for s in range(3000) if (ref.table[s] == -1).all()][:450]
+    length = rng.integers(0, 129, len(empty)).tolist()
+    src = [300 + i % 700 for i in range(len(empty))]
+    length = [n if (ref.table[s, :-(-n // 64)] >= 0).all() else 0 for s, n in zip(src, length)]
+    assert len(empty) * 40 > 16384 and sum(length) > 0       # (a block for every child)
+    B.sjd_pool_fork(pool, _i32(src), _i32(empty), _i32(length))
+    ref.fork(src, empty, length)
+    assert pool.fault() == 0
+    _same(pool, ref, entries=False)
+    taken = next(i for i, n in enumerate(length) if n > 0)
+    B.sjd_pool_fork(pool, _i32(src), _i32(empty[:taken] + [empty[taken]] + empty[taken + 1:]), _i32(length))     # one is not empty
+    assert pool.fault() == B.SJD_ERR_BAD_ARG
     _same(pool, ref, entries=False)
 
 
