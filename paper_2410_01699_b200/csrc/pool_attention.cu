@@ -34,8 +34,8 @@ constexpr int kMaxEntries = 512;     // (sequence, tile of rows) pairs of a call
 constexpr int kMaxSlots = 8;
 constexpr int kMeta = 16;            // tiles that the fetching warp may be ahead: more than the ring holds
 constexpr int kMaxCtas = 320;
-constexpr int kUnitCost = 3;        // what a unit's begin and end take, in tiles
-constexpr int kMinTiles = 5;        // of a range, with that
+constexpr int kUnitCost = 2;        // what a unit's begin and end take, in tiles
+constexpr int kMinTiles = 4;        // of a range, with that
 constexpr int kWholeTiles = 4;      // units of up to so many tiles are not cut where they are few
 constexpr int kUp = 8;               // the largest weight of a row in a tile is 2^kUp (e4m3 ends at 448)
 
@@ -79,14 +79,15 @@ struct PoolAttnShared {
   uint64_t meta_full[kMeta];
   uint64_t q_ready, s_full, s_free, p_full, o_full;
   uint32_t tmem_base;
-  int failed, wide[4][2], n_nan;
+  int failed, n_nan;
   Meta meta[kMeta];
-  alignas(16) float red[4][RP];   // (these are read and written four at a time)
-  alignas(16) float up[RP];       // kUp - the tile's maximum
-  alignas(16) float fac[2][RP];   // of this unit and the next (as pos and out_at)
-  alignas(16) float alpha[2][RP];
-  alignas(16) float beta[2][RP];
-  float alpha_root[2][RP], beta_root[2][RP], inv[RP];
+  alignas(16) float red[2][4][RP];   // (these are read and written four at a time)
+  alignas(16) float fac[2][RP];      // of this unit and the next (as pos and out_at)
+  // what a tile changes, a copy for every warp: kUp - the tile's maximum; factors of the sums so far and of the tile; their logarithms
+  struct Change {
+    alignas(16) float up[RP < 16 ? RP : 16], alpha[2][RP < 16 ? RP : 16], beta[2][RP < 16 ? RP : 16], old_by[RP < 16 ? RP : 16], new_by[RP < 16 ? RP : 16];
+  } change[groups_of(RP) * 4];
+  float inv[RP];
   int pos[2][RP];
   long out_at[2][RP];          // first entry of a row in out
   int nan_key[kTile];
@@ -745,10 +746,10 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
       float2 o[NQ / 2], l_acc[NQ / 2];
 #pragma unroll
       for (int i = 0; i < NQ / 2; ++i) o[i] = l_acc[i] = make_float2(0.0f, 0.0f);
-      float my_run = -INFINITY;   // thread i < NQ of a group: the running maximum of its row
+      float my_run = -INFINITY;   // lane i < NQ: the running maximum of the warp's row i
 
-      auto pair_of = [&](const float *a, int q) { return *reinterpret_cast<const float2 *>(a + c0 + q); };
-      auto four_of = [&](const float *a, int q) { return *reinterpret_cast<const float4 *>(a + c0 + q); };
+      auto &change = sh.change[warp];
+      auto four_of = [&](const float *a, int q) { return *reinterpret_cast<const float4 *>(a + q); };
       // columns of a product, its planes added (the fine ones first: 16 registers of loads at a time)
       auto load_columns = [&](uint32_t from_col, float2 *v) {
 #pragma unroll
@@ -778,7 +779,7 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
           load_columns(t_o, v);
 #pragma unroll
           for (int i = 0; i < NQ / 2; i += 2) {
-            const float4 a = four_of(sh.alpha[par], 2 * i), c = four_of(sh.beta[par], 2 * i);
+            const float4 a = four_of(change.alpha[par], 2 * i), c = four_of(change.beta[par], 2 * i);
             o[i] = fma2(v[i], make_float2(c.x, c.y), mul2(o[i], make_float2(a.x, a.y)));
             o[i + 1] = fma2(v[i + 1], make_float2(c.z, c.w), mul2(o[i + 1], make_float2(a.z, a.w)));
           }
@@ -820,7 +821,7 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
         if (lane == 0) arrive(&sh.s_free);
 #pragma unroll
         for (int q = 0; q < NQ / 2; q += 2) {
-          const float4 f = four_of(sh.fac[up], 2 * q);
+          const float4 f = four_of(sh.fac[up] + c0, 2 * q);
           s[q] = fma2(s[q], mul2(make_float2(f.x, f.y), make_float2(k2, k2)), make_float2(add, add));
           s[q + 1] = fma2(s[q + 1], mul2(make_float2(f.z, f.w), make_float2(k2, k2)), make_float2(add, add));
         }
@@ -841,40 +842,41 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
         for (int q = 0; q < NQ; q += 4) {
           float4 v;
           v.x = max_of_warp(s[q / 2].x), v.y = max_of_warp(s[q / 2].y), v.z = max_of_warp(s[q / 2 + 1].x), v.w = max_of_warp(s[q / 2 + 1].y);
-          if (lane == 0) *reinterpret_cast<float4 *>(&sh.red[w][c0 + q]) = v;
+          if (lane == 0) *reinterpret_cast<float4 *>(&sh.red[par][w][c0 + q]) = v;
         }
-        if (gt == 0) sh.wide[cg][par] = m.pages & 4;   // exponents that differ so much that weights, but not the sum's terms, may leave the range
         group_sync();
-        if (gt < NQ) {
-          const int r = c0 + gt;
-          const float mx = fmaxf(fmaxf(sh.red[0][r], sh.red[1][r]), fmaxf(sh.red[2][r], sh.red[3][r]));
-          const float now = fmaxf(my_run, mx), at = now > -INFINITY ? now : 0.0f;
-          // (by way of the roots: with the values' exponents a maximum may move by 200, and the sum by as much the other way)
-          const float a = exp2_fast(0.5f * (my_run - at)), c = exp2_fast(0.5f * (mx - at));
-          sh.up[r] = (float)kUp - (mx > -INFINITY ? mx : 0.0f);
-          sh.alpha[par][r] = a * a;
-          sh.beta[par][r] = c * c;
-          sh.alpha_root[par][r] = a;
-          sh.beta_root[par][r] = c;
-          if ((my_run > -INFINITY && my_run - at < -64.0f) || (mx > -INFINITY && mx - at < -64.0f)) sh.wide[cg][par] = 1;
+        // (every warp for itself: one for all would take a second barrier)
+        bool wide = (m.pages & 4) != 0;   // exponents that differ so much that weights, but not the sum's terms, may leave the range
+        if (lane < NQ) {
+          const int r = c0 + lane;
+          const float mx = fmaxf(fmaxf(sh.red[par][0][r], sh.red[par][1][r]), fmaxf(sh.red[par][2][r], sh.red[par][3][r]));
+          const float now = fmaxf(my_run, mx), at = now > -INFINITY ? now : 0.0f, da = my_run - at, db = mx - at;
+          change.up[lane] = (float)kUp - (mx > -INFINITY ? mx : 0.0f);
+          change.alpha[par][lane] = exp2_fast(da);
+          change.beta[par][lane] = exp2_fast(db);
+          change.old_by[lane] = da;
+          change.new_by[lane] = db;
+          wide |= (my_run > -INFINITY && da < -64.0f) || (mx > -INFINITY && db < -64.0f);
           my_run = now;
         }
-        group_sync();
+        wide = __any_sync(0xffffffffu, wide);
+        __syncwarp();
         // ---- weights and their sum without the values' exponents
         uint32_t pk[PL][NQ / 4];
         const float back = two_to(-ev - kUp);   // (the sum goes without 2^kUp)
-        const bool wide = sh.wide[cg][par] != 0;
         if (wide) {
 #pragma unroll
           for (int q = 0; q < NQ / 2; ++q) {
-            const float2 ar = pair_of(sh.alpha_root[par], 2 * q), br = pair_of(sh.beta_root[par], 2 * q), r = pair_of(sh.up, 2 * q);
-            l_acc[q].x = l_acc[q].x * ar.x * ar.x + exp2_fast(s[q].x - add + r.x - (float)kUp) * br.x * br.x;
-            l_acc[q].y = l_acc[q].y * ar.y * ar.y + exp2_fast(s[q].y - add + r.y - (float)kUp) * br.y * br.y;
+            // (in two steps: with the values' exponents a maximum may move by 200, and the sum by as much the other way)
+            const float a0 = exp2_fast(0.5f * change.old_by[2 * q]), a1 = exp2_fast(0.5f * change.old_by[2 * q + 1]);
+            const float b0 = exp2_fast(0.5f * change.new_by[2 * q]), b1 = exp2_fast(0.5f * change.new_by[2 * q + 1]);
+            l_acc[q].x = l_acc[q].x * a0 * a0 + exp2_fast(s[q].x - add + change.up[2 * q] - (float)kUp) * b0 * b0;
+            l_acc[q].y = l_acc[q].y * a1 * a1 + exp2_fast(s[q].y - add + change.up[2 * q + 1] - (float)kUp) * b1 * b1;
           }
         }
 #pragma unroll
         for (int q = 0; q < NQ / 2; q += 2) {
-          const float4 r = four_of(sh.up, 2 * q);
+          const float4 r = four_of(change.up, 2 * q);
           s[q] = add2(s[q], make_float2(r.x, r.y));
           s[q + 1] = add2(s[q + 1], make_float2(r.z, r.w));
           s[q].x = exp2_fast(s[q].x);
@@ -885,7 +887,7 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
         if (!wide) {
 #pragma unroll
           for (int q = 0; q < NQ / 2; q += 2) {
-            const float4 a = four_of(sh.alpha[par], 2 * q), c = four_of(sh.beta[par], 2 * q);
+            const float4 a = four_of(change.alpha[par], 2 * q), c = four_of(change.beta[par], 2 * q);
             l_acc[q] = fma2(mul2(s[q], make_float2(back, back)), make_float2(c.x, c.y), mul2(l_acc[q], make_float2(a.x, a.y)));
             l_acc[q + 1] = fma2(mul2(s[q + 1], make_float2(back, back)), make_float2(c.z, c.w), mul2(l_acc[q + 1], make_float2(a.z, a.w)));
           }
@@ -968,7 +970,7 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
 #pragma unroll
         for (int q = 0; q < NQ / 2; ++q) v[2 * q] = l_acc[q].x, v[2 * q + 1] = l_acc[q].y;
         const float l = lanes_sum<NQ>(v);
-        if (lane < NQ) sh.red[w][c0 + lane] = l;
+        if (lane < NQ) sh.red[n & 1][w][c0 + lane] = l;   // (not the last tile's: a warp may still read that)
       }
       group_sync();
       const bool cut = u.first < t_begin || u_end > t_end;
@@ -978,7 +980,7 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
       const int my = 2 * blockIdx.x + (u.first < t_begin ? 0 : 1);
       if (gt < NQ) {
         const int r = c0 + gt;
-        const float sum = (sh.red[0][r] + sh.red[1][r]) + (sh.red[2][r] + sh.red[3][r]);
+        const float sum = (sh.red[n & 1][0][r] + sh.red[n & 1][1][r]) + (sh.red[n & 1][2][r] + sh.red[n & 1][3][r]);
         sh.inv[r] = sh.pos[up][r] >= 0 && sum != 0.0f ? two_to(-kUp) / sum : 0.0f;   // (a NaN among the scores makes the sum NaN)
         if (cut) p.stats[my * RP + r] = make_float2(my_run, sum);
       }
