@@ -5,7 +5,8 @@
 //   S^T [128 keys x NC]  =  K [128 keys x HD] . Q^T          O^T [HD x NC]  =  V^T [HD x 128 keys] . P
 // Queries and weights are e4m3 numbers too, but several of them: x = x1 + x2 (+ 2^-8 (x3 + x4)), x1 = e4m3(x), x2 = e4m3(x - x1),
 // x3 = e4m3(256 (x - x1 - x2)) and so on.  The planes are columns of one product, added when they are read from tensor memory (as more
-// products into the same columns they read K and V once more each: 8 x 32 rows 108 -> 113 us).  n planes leave 2^-4n of a number at most (half a step of e4m3 is 2^-4 of it) and about 2^-5.3n on average: two for bf16 queries, whose eight bits they hold
+// products into the same columns they read K and V once more each: 8 x 32 rows 108 -> 113 us).  n planes leave 2^-4n of a number at
+// most (half a step of e4m3 is 2^-4 of it) and about 2^-5.3n on average: two for bf16 queries, whose eight bits they hold
 // exactly, four for fp32.  (mma.sync has e4m3 as well, but here it converts both operands for every product: 700 products a clock and SM.
 // With conversions in registers and fp16 products: 8 x 32 rows x 4009 keys of 32 heads, fp32, 130 us, 32 tokens of up to 4224 keys 63.)
 //
@@ -16,14 +17,19 @@
 // CTAs to arrive, which a counter tells: 6 us between its last tile and the first part that it may read, and a lone CTA reads the 33
 // parts of 12 rows of a long sequence in 17.)
 //
-// A thread of the four softmax warps (eight with 64 columns of rows) is a key of the tile.  With s the score (in log2), e_K in its
+// A thread of the softmax warps is a key of the tile, with up to 16 of the rows.  With s the score (in log2), e_K in its
 // factor and e_V added to it, w = 2^(s + e_V - top + 8) is the weight of the value's e4m3 numbers, top the largest s + e_V of the row in this
 // tile: weights fill the range of e4m3 whatever stands in other tiles (under one reference for all, the weights of 10^5 keys that share
 // a tenth of the mass beside one that has the rest would be zero) and whatever the exponents of the blocks are.  The sum of the softmax takes
 // w 2^-e_V.  The same threads, then a dim each, add the tile's O^T to their registers under the running maximum.
 //
-// Bound: bytes of K and V up to about 32 rows; beyond, the issue slots of the softmax (some 13 instructions for an entry of
-// S^T with bf16, 23 with fp32).  Two CTAs per SM (one with 64 rows), each with a ring of tiles: 96 to 160 KB of copies in flight.
+// Bound: bytes of K and V up to 16 rows (in a long run 7.1 TB/s; 32 tokens of up to 4224 keys, 32 heads on 8, bf16, 210 MB, 50 us, of which
+// some 18 are the start, the units' ends and the joining launch; 3 tokens of 100,003 keys, 205 MB, 54 us); beyond, the
+// issue slots of the softmax: with 32 rows and bf16 some 47 instructions for an entry of S^T and its share of O^T (8 x 32 rows of up
+// to 4009 keys of 32 heads, fp32, 271 MB, 106 us; 2 x 64 rows of such heads, bf16, 46 us).  Two CTAs per SM (one with 64 rows),
+// each with a ring of tiles: 96 to 160 KB of copies in flight.  What few tiles need stands behind one branch and is short, for the
+// instructions fetched with the common path (NaN entries of V found by a first look of the keys' threads alone, their words mended
+// one at a time: 32 tokens 51.5 -> 50 us, 100,003 keys 57.5 -> 54, though 2 x 64 rows 45 -> 46).
 #include "tcgen05.cuh"
 
 namespace sjd {
@@ -607,6 +613,15 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
     uint32_t meta_ph = 0;
     bool ok = true;
     auto sync = [&]() { asm volatile("bar.sync 1, %0;" ::"n"(WORK_T) : "memory"); };
+    auto any = [&](bool pred) {   // of all softmax threads
+      uint32_t r;
+      asm volatile(
+          "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 q, %1, 0;\n\tbar.red.or.pred p, 1, %2, q;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+          : "=r"(r)
+          : "r"((uint32_t)pred), "n"(WORK_T)
+          : "memory");
+      return r != 0;
+    };
     auto group_sync = [&]() { asm volatile("bar.sync %0, 128;" ::"r"(2 + cg) : "memory"); };
     const int gt = tid & 127;            // thread of its group
     // ---- queries of a unit: a power of two brings a row's largest entry to 128 .. 256, then its planes; a row is HD / 4 lanes
@@ -746,6 +761,7 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
       float2 o[NQ / 2], l_acc[NQ / 2];
 #pragma unroll
       for (int i = 0; i < NQ / 2; ++i) o[i] = l_acc[i] = make_float2(0.0f, 0.0f);
+      bool nans = false;          // the last tile had NaN entries among keys that not all rows see
       float my_run = -INFINITY;   // lane i < NQ: the running maximum of the warp's row i
 
       auto &change = sh.change[warp];
@@ -854,8 +870,7 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
           change.up[lane] = (float)kUp - (mx > -INFINITY ? mx : 0.0f);
           change.alpha[par][lane] = exp2_fast(da);
           change.beta[par][lane] = exp2_fast(db);
-          change.old_by[lane] = da;
-          change.new_by[lane] = db;
+          change.old_by[lane] = da, change.new_by[lane] = db;
           wide |= (my_run > -INFINITY && da < -64.0f) || (mx > -INFINITY && db < -64.0f);
           my_run = now;
         }
@@ -916,45 +931,50 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
         }
         if (i > 0) {
           add_values(par ^ 1);
-          if (sh.n_nan > 0) add_nans();   // (of the tile before)
+          if (nans) add_nans();   // (of the tile before)
         }
         if (!whole) {
           // A key that some row does not see must not reach it: a weight of zero times NaN would.  NaN entries become zero, and
           // the rows that see them get their NaN afterwards.
-          sync();   // (what the tile before left in the list has been read)
-          if (tid == 0) sh.n_nan = 0;
-          sync();
+          bool found = false;
+          uint8_t *v = nullptr;
           if (cg == 0) {
             const uint32_t use = v_use + (i < n - 1 ? 2 * i + 2 : 2 * n - 1);
             if (ok && !warp_wait(&sh.full[use % p.slots], use / p.slots & 1)) {
               ok = false;
               fail();
             }
-            uint8_t *v = ring + (use % p.slots) * TILE;
-            uint32_t dims[4] = {0u, 0u, 0u, 0u};
+            v = ring + (use % p.slots) * TILE;
 #pragma unroll
             for (int c = 0; c < HD / 16; ++c) {
-              uint4 *at = reinterpret_cast<uint4 *>(v + swizzled<HD>(key_t, c * 16));
-              uint4 x = *at;
-              uint32_t *xs = reinterpret_cast<uint32_t *>(&x);
-              if (has_nan(x.x) || has_nan(x.y) || has_nan(x.z) || has_nan(x.w)) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                  const uint32_t nan = ((xs[j] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;   // the top bit of every NaN byte
-                  xs[j] &= ~((nan >> 7) * 0xFFu);
-                  dims[c >> 1] |= ((nan >> 7 & 1u) | (nan >> 14 & 2u) | (nan >> 21 & 4u) | (nan >> 28 & 8u)) << ((c & 1) * 16 + j * 4);
-                }
-                *at = x;
-              }
-            }
-            if ((dims[0] | dims[1] | dims[2] | dims[3]) != 0 && key <= hi && (m.pages >> half & 1)) {
-              const int at = atomicAdd(&sh.n_nan, 1);
-              sh.nan_key[at] = key;
-#pragma unroll
-              for (int j = 0; j < 4; ++j) sh.nan_dims[at][j] = dims[j];
+              const uint4 x = *reinterpret_cast<const uint4 *>(v + swizzled<HD>(key_t, c * 16));
+              found |= has_nan(x.x) || has_nan(x.y) || has_nan(x.z) || has_nan(x.w);
             }
           }
-          sync();
+          nans = any(found);
+          if (__builtin_expect(nans, 0)) {
+            if (tid == 0) sh.n_nan = 0;
+            sync();
+            if (found) {
+              uint32_t dims[4] = {0u, 0u, 0u, 0u};
+#pragma unroll 1
+              for (int c = 0; c < HD / 4; ++c) {
+                uint32_t *at = reinterpret_cast<uint32_t *>(v + swizzled<HD>(key_t, c * 4));
+                const uint32_t x = *at, nan = ((x & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;   // the top bit of every NaN byte
+                *at = x & ~((nan >> 7) * 0xFFu);
+                dims[c >> 3] |= ((nan >> 7 & 1u) | (nan >> 14 & 2u) | (nan >> 21 & 4u) | (nan >> 28 & 8u)) << ((c & 7) * 4);
+              }
+              if (key <= hi && (m.pages >> half & 1)) {
+                const int at = atomicAdd(&sh.n_nan, 1);
+                sh.nan_key[at] = key;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sh.nan_dims[at][j] = dims[j];
+              }
+            }
+            sync();
+          }
+        } else {
+          nans = false;
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
@@ -991,9 +1011,8 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
       }
       o_ph ^= 1u;
       add_values(n - 1 & 1);
-      if (sh.n_nan > 0) add_nans();
+      if (nans) add_nans();
       sync();
-      if (tid == 0) sh.n_nan = 0;
       if (w * 32 < HD) {
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
