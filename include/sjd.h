@@ -396,7 +396,8 @@ int sjd_pool_append(const sjd_pool *pool, int layer, int batch, int window, int 
  * and for visible positions without a page (keys that are left out); DEVICE_TIMEOUT if a bounded wait ran out.
  * ws: device scratch of sjd_pool_attention_workspace_bytes(...) bytes, 256-byte aligned, contents without meaning between calls; one
  * call at a time on a workspace (captured graphs that may run at the same time have their own).
- * Errors: BAD_ARG, UNSUPPORTED (head_dim, dtype, a device other than sm_100's), CAPACITY (ws too small), CUDA.
+ * Errors: BAD_ARG, UNSUPPORTED (head_dim, dtype, a device other than sm_100's), CAPACITY (ws too small, more than 32768 query heads on
+ * a kv head), CUDA.
  */
 size_t sjd_pool_attention_workspace_bytes(const sjd_pool *pool, int window, int n_heads);
 int sjd_pool_attention(const sjd_pool *pool, int layer, int batch, int window, int n_heads, int dtype, const void *q, int64_t q_stride,

@@ -382,7 +382,7 @@ def _pool_rows(x, heads, pool, rows, where):
         raise ValueError("%s: a tensor [%d][%d][%d] whose rows are contiguous" % (where, rows, heads, hd))
     if x.get_device() != pool.index:
         raise ValueError("%s: on another device than the pool" % where)
-    return stride[0] if rows > 1 else max(stride[0], heads * hd)
+    return stride[0] if rows > 1 else heads * hd
 
 
 def _ints(x, n, pool, where):
@@ -409,7 +409,7 @@ def sjd_pool_append(pool: CachePool, layer: int, k, v, in_pos, window: int, q=No
     axis_pos int32 [B*W][n_axes]; seqs int32 [B] or None (sequence b is row b of the table)."""
     m, kvh = in_pos.numel(), pool.n_kv_heads
     dtype = _pool_dtype(k, "sjd_pool_append")
-    if m % window != 0 or v.dtype != k.dtype or (q is not None and q.dtype != k.dtype):
+    if window < 1 or m % window != 0 or v.dtype != k.dtype or (q is not None and q.dtype != k.dtype):
         raise ValueError("sjd_pool_append: whole windows, and q, k, v of one type")
     heads, q_at, q_stride, out_at, out_stride = 0, None, 0, None, 0
     if q is not None:
@@ -434,7 +434,7 @@ def sjd_pool_attention(pool: CachePool, layer: int, q, in_pos, window: int, slid
     its own for calls that may run at the same time as others on the pool (default: the pool's)."""
     m, heads = in_pos.numel(), q.shape[1]
     dtype = _pool_dtype(q, "sjd_pool_attention")
-    if m % window != 0:
+    if window < 1 or m % window != 0:
         raise ValueError("sjd_pool_attention: whole windows")
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)

@@ -43,6 +43,7 @@ constexpr int kMaxCtas = 320;
 constexpr int kUnitCost = 2;        // what a unit's begin and end take, in tiles
 constexpr int kMinTiles = 4;        // of a range, with that
 constexpr int kWholeTiles = 4;      // units of up to so many tiles are not cut where they are few
+constexpr int kMaxGroup = 32768;     // query heads of a kv head
 constexpr int kUp = 8;               // the largest weight of a row in a tile is 2^kUp (e4m3 ends at 448)
 
 struct PoolAttnParams {
@@ -1151,7 +1152,8 @@ extern "C" int sjd_pool_attention(const sjd_pool *pool, int layer, int batch, in
   if ((((uintptr_t)q | (uintptr_t)out) & (dtype == SJD_F32 ? 15 : 7)) != 0 || ((uintptr_t)ws & 255u) != 0) return SJD_ERR_BAD_ARG;
   const int group = n_heads / pool->n_kv_heads;
   const int64_t rows = (int64_t)window * group;
-  if ((int64_t)batch * window > 0x7FFFFFFF || rows > 0x7FFFFFFF) return SJD_ERR_CAPACITY;
+  // (kMaxGroup: up to there products with group_inv are quotients by the group)
+  if (group > kMaxGroup || (int64_t)batch * window > 0x7FFFFFFF || rows > 0x7FFFFFFF) return SJD_ERR_CAPACITY;
   if (ws_bytes < sjd_pool_attention_workspace_bytes(pool, window, n_heads)) return SJD_ERR_CAPACITY;
   int dev = 0, cc_major = 0, sms = 0;
   SJD_CUDA(cudaGetDevice(&dev));

@@ -85,7 +85,7 @@ def test_append_refuses(kw, status):
     (dict(q=None), -1), (dict(in_pos=None), -1), (dict(out=None), -1), (dict(ws=None), -1), (dict(ws=FAKE + 128), -1),
     (dict(qs=252), -1), (dict(qs=258), -1), (dict(outs=258), -1), (dict(q=FAKE + 8), -1), (dict(dtype=1, out=FAKE + 4), -1),
     (dict(sliding=-1), -1), (dict(sinks=-1), -1), (dict(scale=-1.0), -1), (dict(scale=math.nan), -1), (dict(scale=math.inf), -1),
-    (dict(ws_bytes=1024), -2), (dict(batch=1 << 20, window=1 << 20), -2)])
+    (dict(ws_bytes=1024), -2), (dict(batch=1 << 20, window=1 << 20), -2), (dict(heads=2 * 32769, qs=2 * 32769 * 64, outs=2 * 32769 * 64), -2)])
 def test_attention_refuses(kw, status):
     assert _attention(**kw) == status
 
@@ -132,6 +132,13 @@ def test_wrapper_refuses_tensors_that_do_not_fit():
         with pytest.raises(ValueError):
             with torch.device("cpu"):
                 B.sjd_pool_append(pool, 0, **{**dict(in_pos=pos, window=2), **kw})
+    for window in (0, -2):
+        with pytest.raises(ValueError):
+            B.sjd_pool_append(pool, 0, k, k, pos, window)
+        with pytest.raises(ValueError):
+            B.sjd_pool_attention(pool, 0, k, pos, window)
+    # one row alone has no stride that matters
+    assert B._pool_rows(torch.zeros(3, 131)[:1, :128].view(1, 2, 64), 2, pool, 1, "k") == 128
     with pytest.raises(B.SJDError):
         B.sjd_pool_append(pool, 0, k.half(), k.half(), pos, 2)
     with pytest.raises(B.SJDError):
