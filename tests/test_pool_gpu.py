@@ -217,6 +217,26 @@ def test_a_nan_shows_where_it_is_seen_and_nowhere_else():
             assert pool.fault() == 0
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("window,heads", [(2, 2), (12, 4), (24, 8)])
+def test_nans_at_both_ends_of_sliding_windows(dtype, window, heads):
+    """Values that are NaN wherever only some rows see them, in the tiles of many sequences and heads, one after another."""
+    lens, sliding, sinks = [300 + 37 * i for i in range(40)], 190, 70
+    pool = _filled(lens, 1, 2, 128, 51)
+    rng, raw, table = np.random.default_rng(52), pool.pages.view(torch.uint8), pool.table.cpu().numpy()
+    for b, n in enumerate(lens):
+        for key in [n - 1, n - window, n - sliding, n - sliding - window + 1, sinks - 1, sinks, n // 2]:
+            raw[table[b, key // 64], 0, 1, rng.integers(2), key % 64, rng.integers(128)] = int(rng.choice([0x7F, 0xFF]))
+    pos = _window_pos(lens, window)
+    q = _queries(len(lens) * window, heads, 128, dtype, 53)
+    got = B.sjd_pool_attention(pool, 0, q, _i32(pos), window, sliding=sliding, sinks=sinks).float().cpu().numpy()
+    exact = _oracle(pool).attention(0, q.float().cpu().numpy(), range(len(lens)), pos, window, sliding, sinks, 0.0)
+    assert pool.fault() == 0 and np.isnan(exact[0]).any() and not np.isnan(exact[0]).all()
+    assert np.array_equal(np.isnan(got), np.isnan(exact[0]))
+    fine = ~np.isnan(exact[0])
+    assert (np.abs(got - exact[0]) <= _bound(dtype, exact))[fine].all()
+
+
 def test_queries_that_are_not_finite_or_zero():
     pool = _filled((80,), 1, 1, 64, 14)
     q = _queries(4, 2, 64, "f32", 10)
