@@ -4,7 +4,9 @@
 // the claims and of the free pages' indices alone, so results do not hang on the order in which threads run: a prefix count numbers the
 // claims that need a page and another one the free pages, and number i gets number i.
 // Bound: the copies (a page's bytes read and written once each) at the rate of a device copy; without copies the launches (one block that
-// plans, which the copying launch overlaps as far as its own start).
+// plans, which the copying launch overlaps as far as its own start).  Compaction that moves 320 pages of 4.2 MB (2.69 GB read and written):
+// 475 us, 5.7 TB/s.  Sixteen children of a prompt, fork, reserve with 16 copies of 4.2 MB (134 MB) and free: 24.5 us.  Two
+// children in a pool of one small layer, fork, reserve and free: 12.4 us, three launches.
 #include "common.cuh"
 
 namespace sjd {
@@ -14,6 +16,7 @@ constexpr int kPlanThreads = 1024;
 constexpr int kCopyThreads = 256;
 constexpr int kListMax = SJD_POOL_MAX_LIST;
 // One block does what takes it less than a launch more would: copies of 128 KB (8 rounds of 16 KB), tables of 16384 entries (16 rounds).
+// Fork, reserve and free of two children of a small prompt (32 KB to copy): 12.4 us so, 13.6 with the launches that larger ones take.
 constexpr size_t kCopyHere = 128 << 10;
 constexpr int kForkHere = 16384;
 
