@@ -23,11 +23,11 @@
 // a tenth of the mass beside one that has the rest would be zero) and whatever the exponents of the blocks are.  The sum of the softmax takes
 // w 2^-e_V.  The same threads, then a dim each, add the tile's O^T to their registers under the running maximum.
 //
-// Bound: bytes of K and V up to 16 rows (in a long run 7.1 TB/s; 32 tokens of up to 4224 keys, 32 heads on 8, bf16, 210 MB, 50 us, of which
-// some 18 are the start, the units' ends and the joining launch; 3 tokens of 100,003 keys, 205 MB, 54 us); beyond, the softmax between
+// Bound: bytes of K and V up to 16 rows (in a long run 7.1 TB/s; 32 tokens of up to 4224 keys, 32 heads on 8, bf16, 210 MB, 49 us, of which
+// some 18 are the start, the units' ends and the joining launch; 3 tokens of 100,003 keys, 205 MB, 53 us); beyond, the softmax between
 // the products: a warp takes 770 instructions (bf16: 615) for 32 keys by 16 rows, four of them a scheduler fill 54 % of its issue slots, and
 // the rest are latencies of one tile's chain that the other warps do not cover (8 x 32 rows of 4009 keys of 32 heads, fp32, 271 MB,
-// 106 us, bf16 90; 2 x 64 rows, 32 heads on 8, bf16, 46 us).  Two CTAs per SM (one with 64 rows),
+// 106 us, bf16 90; 2 x 64 rows, 32 heads on 8, bf16, 45 us).  Two CTAs per SM (one with 64 rows),
 // each with a ring of tiles: 96 to 160 KB of copies in flight.  What few tiles need stands behind one branch and is short, for the
 // instructions fetched with the common path (NaN entries of V found by a first look of the keys' threads alone, their words mended
 // one at a time: 32 tokens 51.5 -> 50 us, 100,003 keys 57.5 -> 54, though 2 x 64 rows 45 -> 46).
@@ -41,7 +41,7 @@ constexpr int kMaxEntries = 512;     // (sequence, tile of rows) pairs of a call
 constexpr int kMaxSlots = 8;
 constexpr int kMeta = 16;            // tiles that the fetching warp may be ahead: more than the ring holds
 constexpr int kMaxCtas = 320;
-constexpr int kUnitCost = 2;        // what a unit's begin and end take, in tiles
+constexpr int kUnitCost = 3;        // what a unit's begin and end take, in tiles (41 calls of all kinds: with 1 7 % slower, 2 2.6, 4 0.5, 5 1.3)
 constexpr int kMinTiles = 4;        // of a range, with that
 constexpr int kWholeTiles = 4;      // units of up to so many tiles are not cut where they are few
 constexpr int kMaxGroup = 32768;     // query heads of a kv head
