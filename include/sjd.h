@@ -391,9 +391,11 @@ int sjd_pool_append(const sjd_pool *pool, int layer, int batch, int window, int 
  * j <= in_pos[m]; with sliding > 0 of these only j > in_pos[m] - sliding and, as sinks, j < sinks:
  *     out[m][h] = softmax_j(scale q[m][h] . K[j][h / (n_heads / n_kv_heads)]) V[j][...]      (scale 0: 1 / sqrt(head_dim))
  * in_pos -1: a row that sees nothing, its output is zero.  q and out of dtype (fp32: about fp32 accuracy), rows *_stride elements apart,
- * strides multiples of 4, starting on 16 (fp32) or 8 (bf16) bytes; out may not overlap q.  What rows behind a sequence or masked places
- * hold (NaN included) does not matter; a visible NaN shows.  status: BAD_ARG for seqs or positions out of range (rows that see nothing)
- * and for visible positions without a page (keys that are left out); DEVICE_TIMEOUT if a bounded wait ran out.
+ * strides multiples of 4, starting on 16 (fp32) or 8 (bf16) bytes; out may not overlap q.  Scores and sums are held in 32 bits; a weight is
+ * rounded by up to 1.13 x 2^-8 (bf16) or 2^-16 (fp32) of itself and 2^-13 resp. 2^-21 of the row's largest.  What rows behind a sequence or
+ * masked places hold (NaN included) does not matter, nor does the exponent that a masked row gave its block; a visible NaN shows.
+ * status: BAD_ARG for seqs or positions out of range (rows that see nothing) and for visible positions without a page (keys that are left
+ * out); DEVICE_TIMEOUT if a bounded wait ran out.
  * ws: device scratch of sjd_pool_attention_workspace_bytes(...) bytes, 256-byte aligned, contents without meaning between calls; one
  * call at a time on a workspace (captured graphs that may run at the same time have their own).
  * Errors: BAD_ARG, UNSUPPORTED (head_dim, dtype, a device other than sm_100's), CAPACITY (ws too small, more than 32768 query heads on

@@ -23,6 +23,16 @@
 // a tenth of the mass beside one that has the rest would be zero) and whatever the exponents of the blocks are.  The sum of the softmax takes
 // w 2^-e_V.  The same threads, then a dim each, add the tile's O^T to their registers under the running maximum.
 //
+// A block's exponent is set by its largest entry, which the row need not see (a later row of the window, one before a sliding window).  With
+// one reference for exponents far apart, the weights of all other blocks would lose their places to it.  So a tile is worked on in
+// parts, as tiles of their own, each with the blocks whose exponents lie within kExpBand of the largest one that is left, and the keys of
+// the others masked.  Half of the smallest step of a weight is then at most 2^(kExpBand - 18) (four planes: -26) of the row's largest weight,
+// whatever rows that it does not see hold.  Computed for one reference, a hidden value 2^d times the others: error of an output (norm), fp32
+// 4.2e-7 with d = 0, 4.8e-7 with 4, 7.1e-7 with 5, 1.2e-6 with 6, 5e-6 with 8, 5.5e-5 with 12 (bf16 before its rounding 6e-4, 6.5e-4, 6.5e-4,
+// 7e-4, 1.3e-3, 1.4e-2).  Five, so that first tokens with values of an eighth stand beside blocks that differ by four.  Nearly all tiles have one
+// part, which costs nothing but the code (32 tokens 50.8 -> 51.2 us a call of the binding, 8 x 32 rows 108.9 -> 110.6, 100,003 keys 51.4 ->
+// 53.4, others as before); two parts in every tile 2.7 to 2.9 times the call, for masked tiles take longer than whole ones.
+//
 // Bound: bytes of K and V up to 16 rows (in a long run 7.1 TB/s; 32 tokens of up to 4224 keys, 32 heads on 8, bf16, 210 MB, 49 us, of which
 // some 18 are the start, the units' ends and the joining launch; 3 tokens of 100,003 keys, 205 MB, 53 us); beyond, the softmax between
 // the products: a warp takes 770 instructions (bf16: 615) for 32 keys by 16 rows, four of them a scheduler fill 54 % of its issue slots, and
@@ -46,6 +56,9 @@ constexpr int kMinTiles = 4;        // of a range, with that
 constexpr int kWholeTiles = 4;      // units of up to so many tiles are not cut where they are few
 constexpr int kMaxGroup = 32768;     // query heads of a kv head
 constexpr int kUp = 8;               // the largest weight of a row in a tile is 2^kUp (e4m3 ends at 448)
+constexpr int kExpBand = 5;          // exponents of values that are weighed together: see the comment above
+constexpr int kBlocksAt = 8, kMoreAt = 16;   // in Meta::pages
+constexpr int kMaxParts = 1 << 22;           // 8 of a tile, 2^19 tiles of a sequence: an end where waits have run out
 
 struct PoolAttnParams {
   sjd_pool pool;
@@ -72,13 +85,15 @@ __host__ __device__ constexpr int threads_of(int rp) { return groups_of(rp) * 12
 struct Entry {   // (sequence, tile of rows)
   int before;    // cost of one kv head in the entries before: their tiles, and kUnitCost for each
   int low;       // first tile of the sliding part
-  int sink;      // tiles before it
+  uint32_t sink : 24;   // tiles before it
+  uint32_t top : 8;     // block of the last tile with the largest position
 };
 
 struct Meta {    // of a tile that is being fetched
   int key0;
   int k_exp[2], v_exp[2];   // exponents of its two pages' blocks
-  int pages;                // bit j: page j is there; bit 2: values' exponents of them more than 64 apart
+  int pages;                // bit j: page j is there; bit 2: the tile has one part; from kBlocksAt on: blocks of this part; from kMoreAt on: how many
+                            // parts follow beside the tiles
 };
 
 template <int RP>
@@ -291,7 +306,10 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
   const int kv_heads = p.pool.n_kv_heads, seq_keys = p.pool.pages_per_seq * KV_PAGE;
 
   pdl_trigger();   // (the joining launch waits for the end of this one)
-  if (tid < kMeta) mbar_init(&sh.meta_full[tid], 1);
+  if (tid < kMeta) {
+    mbar_init(&sh.meta_full[tid], 1);
+    sh.meta[tid].pages = 0;   // (what is read after a wait that ran out)
+  }
   if (tid < p.slots) {
     mbar_init(&sh.full[tid], 1);
     mbar_init(&sh.empty[tid], 1);
@@ -361,8 +379,10 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
       if (mine < per_pass && e < n_entries && l == 0) {
         Entry n;
         n.low = p.sliding > 0 && hi >= 0 ? max(0, lo - p.sliding + 1) / kTile : 0;
-        n.sink = min(n.low, (min(p.sinks, seq_keys) + kTile - 1) / kTile);
-        n.before = hi < 0 ? 0 : hi / kTile + 1 - n.low + n.sink + unit_cost;   // (its own so far)
+        const int sink = min(n.low, (min(p.sinks, seq_keys) + kTile - 1) / kTile);
+        n.sink = sink;
+        n.top = hi < 0 ? 0 : hi % kTile / kPoolBlock;
+        n.before = hi < 0 ? 0 : hi / kTile + 1 - n.low + sink + unit_cost;   // (its own so far)
         sh.entry[e] = n;
       }
     }
@@ -438,6 +458,7 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
     int issued = 0;
     bool ok = true;
     int n_key0 = 0, n_page[2] = {-1, -1}, n_ke[2] = {0, 0}, n_ve[2] = {0, 0}, n_head = 0, n_last = 0, n_tile = 0;
+    unsigned n_blocks = 0;   // blocks with positions that some row may see
     auto look_up = [&](int t) {   // what lane `lane` knows of tile t + lane
       n_page[0] = n_page[1] = -1;
       n_last = n_tile = 0;
@@ -447,7 +468,9 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
       if (i < 0) return;   // (no tile)
       n_tile = 1;
       const Entry en = sh.entry[u.e];
-      n_key0 = (i < en.sink ? i : en.low + i - en.sink) * kTile;
+      const int sink = (int)en.sink;
+      n_key0 = (i < sink ? i : en.low + i - sink) * kTile;
+      n_blocks = i == u.n - 1 ? (2u << en.top) - 1 : 0xFFu;   // (exponents behind the sequence may be anything)
       n_head = u.kvh;
       n_last = i == u.n - 1 || t + lane == t_end - 1;
       const int seq = p.seqs ? p.seqs[u.b] : u.b;
@@ -459,6 +482,8 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
         const int page = p.pool.table[(long)seq * p.pool.pages_per_seq + at];
         n_page[j] = page < 0 || page >= p.pool.n_pages ? -1 : page;
       }
+      if (n_page[0] < 0) n_blocks &= 0xF0u;
+      if (n_page[1] < 0) n_blocks &= 0x0Fu;
     };
     auto look_up_exps = [&]() {
 #pragma unroll
@@ -494,48 +519,115 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
       Meta m;
       m.key0 = n_key0;
       m.k_exp[0] = n_ke[0], m.k_exp[1] = n_ke[1], m.v_exp[0] = n_ve[0], m.v_exp[1] = n_ve[1];
-      m.pages = (n_page[0] >= 0 ? 1 : 0) | (n_page[1] >= 0 ? 2 : 0);
-      {
-        int e_min = 127, e_max = -128;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int e = pool_exp((int8_t)(m.v_exp[j >> 2] >> (8 * (j & 3))));
-          e_min = min(e_min, e);
-          e_max = max(e_max, e);
-        }
-        if (e_max - e_min > 64) m.pages |= 4;
-      }
+      const int there = (n_page[0] >= 0 ? 1 : 0) | (n_page[1] >= 0 ? 2 : 0);
+      m.pages = there | 4 | 0xFF << kBlocksAt;
       const int pg0 = n_page[0], pg1 = n_page[1], head = n_head, last = n_last;
-      const unsigned tiles = __ballot_sync(0xffffffffu, n_tile);
-      const int rank = n_tile ? __popc(tiles & ((1u << lane) - 1)) : 32, n = __popc(tiles);
-      int told = 0;   // tiles of these 32 whose lanes have written what they know: not before the copies that there is room for are under way
-      auto tell = [&](int upto) {
-        if (rank >= told && rank < upto) {
-          const int at = (meta + rank) % kMeta;
-          sh.meta[at] = m;
-          arrive(&sh.meta_full[at]);
-        }
-        __syncwarp();
-        told = upto;
+      const unsigned tiles = __ballot_sync(0xffffffffu, n_tile), below = (1u << lane) - 1;
+      // A unit's tiles among these are a run.  Parts of its tiles behind their first ones come after the run, as tiles of their own: they are rare,
+      // and their bytes in L2; and the first copies need not wait for the exponents.
+      const unsigned ends = __ballot_sync(0xffffffffu, n_tile && (last || tiles >> lane == 1u));
+      unsigned rest = n_tile ? n_blocks : 0;   // blocks of this lane's tile whose parts have not been told
+      int rank = n_tile ? __popc(tiles & below) : 0x7FFF, n = __popc(tiles);   // number of this lane's first part, of all parts
+      int more = 0, more_at = 0, follow = 0;   // this lane's parts behind the first, number of the first of them; with a run's end: of the run
+      bool known = false, multi = false;       // multi: some lane has more parts than one
+      int told = 0;   // parts of these 32 tiles whose lanes have written what they know: not before the copies that there is room for are under way
+      auto exp_of = [&](int b) { return pool_exp((int8_t)((b < 4 ? m.v_exp[0] : m.v_exp[1]) >> (8 * (b & 3)))); };
+      auto band = [&](unsigned of) {   // the blocks among these whose exponents of values are the largest one or up to kExpBand below it
+        int top = -128;
+        unsigned in = 0;
+#pragma unroll 1
+        for (int b = 0; b < 8; ++b) top = of >> b & 1u ? max(top, exp_of(b)) : top;
+#pragma unroll 1
+        for (int b = 0; b < 8; ++b) in |= exp_of(b) >= top - kExpBand ? 1u << b : 0u;
+        return of & in;
       };
-      unsigned todo = tiles;
       if (t0 + 32 < t_end) look_up(t0 + 32);
-      for (int i = 0; i < n && ok; ++i, todo &= todo - 1) {
-        const int from = __ffs(todo) - 1;
+      int done = 0, left = 0;            // parts so far; parts that a run's tiles have left
+      bool at_end = false, over = false; // at the end of a run, which is the end of its unit
+#pragma unroll 1
+      for (unsigned todo = tiles; (todo != 0 || left > 0) && ok;) {
+        int from = __ffs(todo) - 1;
+        const bool first = left == 0;
+        if (first) {
+          todo &= todo - 1;
+          at_end = ends >> from & 1u;
+        } else {
+          from = __ffs(__ballot_sync(0xffffffffu, done >= more_at && done < more_at + more)) - 1;
+          --left;
+        }
+        ++done;
+        const bool full = issued + 3 > p.slots;   // a copy of this round may have to wait
+        if (!known && (full || at_end)) {
+          known = true;
+          int e_min = 127, e_max = -128;
+#pragma unroll
+          for (int b = 0; b < 8; ++b) {
+            const int e = exp_of(b);
+            e_min = rest >> b & 1u ? min(e_min, e) : e_min;
+            e_max = rest >> b & 1u ? max(e_max, e) : e_max;
+          }
+          const bool far = e_max - e_min > kExpBand;   // (no block: not)
+          multi = __any_sync(0xffffffffu, far);
+          if (__builtin_expect(multi, 0)) {
+            if (far) {
+              const unsigned now = band(rest);
+              m.pages = there | (int)now << kBlocksAt;
+              rest &= ~now;
+#pragma unroll 1
+              for (unsigned r = rest; r != 0; ++more) r &= ~band(r);
+            }
+            int x = more;   // (sums up to this lane's)
+#pragma unroll 1
+            for (int o = 1; o < 32; o <<= 1) {
+              const int y = __shfl_up_sync(0xffffffffu, x, o);
+              if (lane >= o) x += y;
+            }
+            const unsigned ended = ends & below, end = ends & ~below;
+            const int before = __shfl_sync(0xffffffffu, x, ended ? 31 - __clz(ended) : 0), runs = ended ? before : 0;   // in the runs before
+            rank += runs;
+            more_at = __popc(tiles & ((end & -end) * 2 - 1)) + x - more;
+            follow = ends >> lane & 1u ? x - runs : 0;
+            m.pages |= follow << kMoreAt;
+            n += __shfl_sync(0xffffffffu, x, 31);
+          }
+        }
+        if (first && at_end) {
+          over = __shfl_sync(0xffffffffu, last, from);
+          left = __shfl_sync(0xffffffffu, follow, from);
+        }
+        if (full || (todo == 0 && left == 0)) {
+          auto write = [&](int i) {
+            const int at = (meta + i) % kMeta;
+            sh.meta[at] = m;
+            arrive(&sh.meta_full[at]);
+          };
+          if (rank >= told && rank < done) write(rank);
+          if (__builtin_expect(multi, 0)) {
+#pragma unroll 1
+            for (int i = max(more_at, told); i < min(more_at + more, done); ++i) {
+              const unsigned now = band(rest);
+              m.pages = there | (int)now << kBlocksAt;
+              rest &= ~now;
+              write(i);
+            }
+          }
+          __syncwarp();
+          told = done;
+        }
+        // K of this part, V of the one before, and V of a unit's last part
         const int page0 = __shfl_sync(0xffffffffu, pg0, from), page1 = __shfl_sync(0xffffffffu, pg1, from), h = __shfl_sync(0xffffffffu, head, from);
-        if (issued + 3 > p.slots) tell(i + 1);   // (a copy of this round may have to wait)
-        fetch(h, page0, page1);
-        if (v_open && ok) fetch(v_plane, v_page0, v_page1);
+        const bool flush = at_end && left == 0 && over;
+#pragma unroll 1
+        for (int o = 0; o < 3 && ok; ++o) {
+          if (o == 1 ? !v_open : o == 2 && !flush) continue;
+          const bool own = o != 1;
+          fetch(o == 0 ? h : own ? kv_heads + h : v_plane, own ? page0 : v_page0, own ? page1 : v_page1);
+        }
         v_plane = kv_heads + h;
         v_page0 = page0;
         v_page1 = page1;
-        v_open = true;
-        if (__shfl_sync(0xffffffffu, last, from) && ok) {
-          fetch(v_plane, v_page0, v_page1);
-          v_open = false;
-        }
+        v_open = !flush;
       }
-      tell(n);
       meta = (meta + n) % kMeta;
     }
     if (!ok) fail();
@@ -548,7 +640,8 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
     const uint64_t desc_k = operand<HD>(16), desc_v = operand<HD>(HD == 64 ? 0 : 16), desc_p = operand<PB>(NC > 128 ? kTile * 128 : 16);
     const uint32_t ring0 = smem_u32(ring), q_at = smem_u32(Qs), p_at = smem_u32(Ps);
     int slot = 0;
-    uint32_t phase = 0, q_ph = 0, sfree_ph = 0, p_ph = 0;
+    uint32_t phase = 0, q_ph = 0, sfree_ph = 0, p_ph = 0, meta_ph = 0;
+    int meta = 0;
     bool ok = true, first_s = true;
     auto next = [&]() {
       __syncwarp();
@@ -595,10 +688,15 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
       t = max(t, u.first);
       if (t >= t_end) break;
       const int n = min(t_end, u.first + u.n) - t;
-      scores(true);
-      for (int i = 1; i < n && ok; ++i) {
-        scores(false);
-        if (ok) values();
+      bool first = true;
+      for (int left = n; left > 0 && ok;) {
+        scores(first);
+        if (ok && !first) values();
+        first = false;
+        // (whether other parts of tiles follow)
+        ok = ok && warp_wait(&sh.meta_full[meta], meta_ph);
+        if (ok) left += (*(volatile int *)&sh.meta[meta].pages >> kMoreAt) - 1;
+        if (++meta == kMeta) { meta = 0; meta_ph ^= 1u; }
       }
       if (ok) values();
       t += n;
@@ -816,7 +914,8 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
         }
       };
 
-      for (int i = 0; i < n; ++i) {
+      int i = 0;
+      for (int until = n; i < until; ++i) {
         const int par = i & 1;
         ok = ok && !*(volatile int *)&sh.failed;
         if (ok && !(warp_wait(&sh.meta_full[meta], meta_ph) && warp_wait(&sh.s_full, s_ph))) {
@@ -825,13 +924,14 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
         }
         const Meta &m = sh.meta[meta];   // (not written again before this tile is done)
         if (++meta == kMeta) { meta = 0; meta_ph ^= 1u; }
+        until = min(until + (m.pages >> kMoreAt), kMaxParts);
         s_ph ^= 1u;
         tc_fence_after();
         // ---- scores
         const int key = m.key0 + key_t, half = key_t >> 6;
         const int ev = pool_exp((int8_t)(m.v_exp[half] >> (8 * (key_t >> 4 & 3))));
         const float k2 = two_to(pool_exp((int8_t)(m.k_exp[half] >> (8 * (key_t >> 4 & 3))))), add = (float)ev;
-        const bool whole = (m.pages & 3) == 3 && m.key0 + kTile - 1 <= lo && (m.key0 > from || m.key0 + kTile <= p.sinks);
+        const bool whole = (m.pages & 7) == 7 && m.key0 + kTile - 1 <= lo && (m.key0 > from || m.key0 + kTile <= p.sinks);
         float2 s[NQ / 2];
         load_columns(t_s, s);
         tc_fence_before();
@@ -844,14 +944,14 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
           s[q + 1] = fma2(s[q + 1], mul2(make_float2(f.z, f.w), make_float2(k2, k2)), make_float2(add, add));
         }
         if (!whole) {
-          const bool there = m.pages >> half & 1;
+          const bool there = m.pages >> half & 1, part = m.pages >> (kBlocksAt + (key_t >> 4)) & 1;
           bool missed = false;
 #pragma unroll
           for (int q = 0; q < NQ / 2; ++q) {
             const bool in0 = sees(key, sh.pos[up][c0 + 2 * q]), in1 = sees(key, sh.pos[up][c0 + 2 * q + 1]);
             missed |= (in0 || in1) && !there;
-            if (!in0 || !there) s[q].x = -INFINITY;
-            if (!in1 || !there) s[q].y = -INFINITY;
+            if (!in0 || !there || !part) s[q].x = -INFINITY;
+            if (!in1 || !there || !part) s[q].y = -INFINITY;
           }
           if (missed) pool_fault(p.pool.status, SJD_ERR_BAD_ARG);   // (no page where some row sees a key)
         }
@@ -864,7 +964,7 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
         }
         group_sync();
         // (every warp for itself: one for all would take a second barrier)
-        bool wide = (m.pages & 4) != 0;   // exponents that differ so much that weights, but not the sum's terms, may leave the range
+        bool wide = false;   // maxima that differ so much that weights, but not the sum's terms, may leave the range
         if (lane < NQ) {
           const int r = c0 + lane;
           const float mx = fmaxf(fmaxf(sh.red[par][0][r], sh.red[par][1][r]), fmaxf(sh.red[par][2][r], sh.red[par][3][r]));
@@ -941,7 +1041,7 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
           bool found = false;
           uint8_t *v = nullptr;
           if (cg == 0) {
-            const uint32_t use = v_use + (i < n - 1 ? 2 * i + 2 : 2 * n - 1);
+            const uint32_t use = v_use + (i + 1 < until ? 2 * i + 2 : 2 * i + 1);
             if (ok && !warp_wait(&sh.full[use % p.slots], use / p.slots & 1)) {
               ok = false;
               fail();
@@ -966,7 +1066,7 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
                 *at = x & ~((nan >> 7) * 0xFFu);
                 dims[c >> 3] |= ((nan >> 7 & 1u) | (nan >> 14 & 2u) | (nan >> 21 & 4u) | (nan >> 28 & 8u)) << ((c & 7) * 4);
               }
-              if (key <= hi && (m.pages >> half & 1)) {
+              if (key <= hi && (m.pages >> half & 1) && (m.pages >> (kBlocksAt + (key_t >> 4)) & 1)) {
                 const int at = atomicAdd(&sh.n_nan, 1);
                 sh.nan_key[at] = key;
 #pragma unroll
@@ -982,7 +1082,7 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
         __syncwarp();
         if (lane == 0) arrive(&sh.p_full);
       }
-      v_use += 2 * n;
+      v_use += 2 * i;
       // ---- the next unit's queries, and this one's sums over the keys, while the last tile is multiplied
       const Unit next = unit_of(end < t_end ? end : end - 1);
       const bool more = end < t_end && next.first < t_end;
@@ -992,7 +1092,7 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
 #pragma unroll
         for (int q = 0; q < NQ / 2; ++q) v[2 * q] = l_acc[q].x, v[2 * q + 1] = l_acc[q].y;
         const float l = lanes_sum<NQ>(v);
-        if (lane < NQ) sh.red[n & 1][w][c0 + lane] = l;   // (not the last tile's: a warp may still read that)
+        if (lane < NQ) sh.red[i & 1][w][c0 + lane] = l;   // (not the last tile's: a warp may still read that)
       }
       group_sync();
       const bool cut = u.first < t_begin || u_end > t_end;
@@ -1002,7 +1102,7 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
       const int my = 2 * blockIdx.x + (u.first < t_begin ? 0 : 1);
       if (gt < NQ) {
         const int r = c0 + gt;
-        const float sum = (sh.red[n & 1][0][r] + sh.red[n & 1][1][r]) + (sh.red[n & 1][2][r] + sh.red[n & 1][3][r]);
+        const float sum = (sh.red[i & 1][0][r] + sh.red[i & 1][1][r]) + (sh.red[i & 1][2][r] + sh.red[i & 1][3][r]);
         sh.inv[r] = sh.pos[up][r] >= 0 && sum != 0.0f ? two_to(-kUp) / sum : 0.0f;   // (a NaN among the scores makes the sum NaN)
         if (cut) p.stats[my * RP + r] = make_float2(my_run, sum);
       }
@@ -1012,7 +1112,7 @@ __global__ void __launch_bounds__(threads_of(RP), ctas_of(RP))
         fail();
       }
       o_ph ^= 1u;
-      add_values(n - 1 & 1);
+      add_values(i - 1 & 1);
       if (nans) add_nans();
       sync();
       if (w * 32 < HD) {

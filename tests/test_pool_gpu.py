@@ -175,6 +175,53 @@ def test_more_positions_than_ranges_are_cut_for():
         assert (np.abs(out[m].float().cpu().numpy() - want[0][0]) <= _bound("bf16", want)[0]).all()
 
 
+def _check_weights(dtype, got, exact, q, ref, in_pos, window, sliding, sinks):
+    """Entries against a bound in which no row counts that a query does not see, nor an exponent that such a row has set: keys are weighed
+    together with blocks of at most 2^5 times smaller exponents, so that half of the smallest step of a weight (_bound: 2^-18 resp. 2^-26 of
+    the largest weight times 2^e) is at most 2^-13 resp. 2^-21 of the row's largest weight on every visible |v_j|.  And the norm of every
+    head's output as in _check_attention."""
+    out, mass, _, reach, flat = exact
+    heads, kvh = q.shape[1], ref.pages.shape[3]
+    x, floor = q.float().cpu().numpy().astype(np.float64), np.zeros_like(out)
+    for m, at in enumerate(in_pos):
+        j = np.arange(at + 1)
+        seen = (sliding == 0) | (j > at - sliding) | (j < sinks)
+        for h in range(heads):
+            (k, ke), (v, ve) = (ref.entries(0, m // window, i, h * kvh // heads, at + 1) for i in range(2))
+            s = (k * ke)[seen] @ x[m, h] * x.shape[-1] ** -0.5
+            floor[m, h] = np.exp(s.max()) / np.exp(s).sum() * np.abs(v * ve)[seen].sum(0)
+    bound = _bound(dtype, (out, mass, np.zeros_like(out), reach, flat)) + 1.02 * 2.0 ** (-13 if dtype == "bf16" else -21) * floor
+    assert (np.abs(got - out) <= bound).all(), "worst %.3g of its bound" % (np.abs(got - out) / bound).max()
+    norms = np.linalg.norm(got - out, axis=-1) / np.linalg.norm(out, axis=-1)
+    assert norms.max() <= (2.0 ** -8 if dtype == "bf16" else 2.0 ** -18), "%s: %.3g" % (np.unravel_index(norms.argmax(), norms.shape), norms.max())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("factor", [2.0 ** 8, 2.0 ** 12, 2.0 ** 16])
+@pytest.mark.parametrize("window,heads,kvh,hd,sliding,sinks", [(4, 2, 2, 128, 0, 0), (12, 4, 2, 64, 0, 0), (24, 1, 1, 128, 0, 0), (40, 2, 1, 64, 0, 0),
+                                                             (1, 4, 2, 128, 100, 0), (4, 2, 1, 64, 90, 4), (33, 2, 1, 128, 120, 16)])
+def test_a_large_value_that_is_not_seen_takes_nothing_from_the_others(dtype, factor, window, heads, kvh, hd, sliding, sinks):
+    """Values of a window's last row, or of a row before a sliding window, that are up to 2^16 times the others' set the exponent of their
+    block, while the block's other rows are ordinary ones that a query sees beside those of the blocks around it."""
+    lens = (window + sliding + 75, window + 300)
+    pool = _filled(lens, 1, kvh, hd, 61)
+    pos = _window_pos(lens, window)
+    for b, n in enumerate(lens):
+        v = torch.randn(n, kvh, hd, generator=torch.Generator().manual_seed(62 + b))
+        # full: the window's last row, which its others do not see; sliding: the last row that no row of the window sees
+        v[n - window - sliding if sliding else n - 1] *= factor
+        B.sjd_pool_append(pool, 0, _rows(n, kvh, hd, "f32", 64 + b) * 0.01, v.cuda(), _i32(list(range(n))), n, seqs=_i32([b]))
+    q = _queries(2 * window, heads, hd, dtype, 66)
+    got = B.sjd_pool_attention(pool, 0, q, _i32(pos), window, sliding=sliding, sinks=sinks).float().cpu().numpy().astype(np.float64)
+    assert pool.fault() == 0
+    ref = _oracle(pool)
+    exact = ref.attention(0, q.float().cpu().numpy(), (0, 1), pos, window, sliding, sinks)
+    if not sliding:   # (without the rows that see the large value)
+        rows = [m for m in range(2 * window) if m % window != window - 1]
+        exact, got, q, pos, window = tuple(x[rows] for x in exact), got[rows], q[torch.tensor(rows)], [pos[m] for m in rows], window - 1
+    _check_weights(dtype, got, exact, q, ref, pos, window, sliding, sinks)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_exponents_of_any_size(dtype):
     """Values' exponents from end to end of their range within one sequence; keys' so that no score leaves fp32."""
@@ -192,6 +239,35 @@ def test_exponents_of_any_size(dtype):
     pool.exps[:, :, 1] = 5
     pool.exps[pool.table[:, 0].long(), :, 1, :, 0] = -30
     _check_attention(pool, _queries(2 * 8, 2, 64, dtype, 8, spread=4.0), _window_pos(lens, 8), 8, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("window,heads,kvh,hd,sliding,sinks", [(1, 4, 1, 128, 0, 0), (3, 8, 2, 64, 0, 0), (20, 2, 2, 128, 0, 0), (40, 2, 1, 64, 700, 70)])
+def test_tiles_in_several_parts(dtype, window, heads, kvh, hd, sliding, sinks):
+    """Exponents of values far apart in every tile, units that several blocks of threads share, the same again from a graph, and values that are
+    NaN where only some rows see them."""
+    lens = (5000, 1301, window)
+    pool = _filled(lens, 1, kvh, hd, 71, per_seq=80)
+    rng = np.random.default_rng(72)
+    pool.exps[:, :, 1] = torch.from_numpy(rng.integers(-15, 16, tuple(pool.exps[:, :, 1].shape)).astype(np.int8)).cuda()
+    pos, q = _window_pos(lens, window), _queries(3 * window, heads, hd, dtype, 73)
+    out = _check_attention(pool, q, pos, window, dtype, sliding, sinks)
+    at, again, g = _i32(pos), torch.empty_like(out), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        B.sjd_pool_attention(pool, 0, q, at, window, sliding=sliding, sinks=sinks, out=again)
+    for _ in range(3):
+        again.zero_()
+        g.replay()
+        assert torch.equal(again, out)
+    raw, table = pool.pages.view(torch.uint8), pool.table.cpu().numpy()
+    for b, n in enumerate(lens):
+        for key in [n - 1, n - window // 2 - 1] + ([n - sliding, n - sliding - window + 1, sinks - 1] if sliding and n > sliding + window else []):
+            raw[table[b, key // 64], 0, 1, rng.integers(kvh), key % 64, rng.integers(hd)] = int(rng.choice([0x7F, 0xFF]))
+    got = B.sjd_pool_attention(pool, 0, q, at, window, sliding=sliding, sinks=sinks).float().cpu().numpy()
+    exact = _oracle(pool).attention(0, q.float().cpu().numpy(), range(3), pos, window, sliding, sinks)
+    assert pool.fault() == 0 and np.isnan(exact[0]).any() and np.array_equal(np.isnan(got), np.isnan(exact[0]))
+    fine = ~np.isnan(exact[0])
+    assert (np.abs(got - exact[0]) <= _bound(dtype, exact))[fine].all()
 
 
 def test_a_nan_shows_where_it_is_seen_and_nowhere_else():
