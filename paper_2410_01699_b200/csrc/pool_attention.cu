@@ -41,19 +41,16 @@
 // each with a ring of tiles: 96 to 160 KB of copies in flight.  What few tiles need stands behind one branch and is short, for the
 // instructions fetched with the common path (NaN entries of V found by a first look of the keys' threads alone, their words mended
 // one at a time: 32 tokens 51.5 -> 50 us, 100,003 keys 57.5 -> 54, though 2 x 64 rows 45 -> 46).
+#include "pool_route.h"
 #include "tcgen05.cuh"
 
 namespace sjd {
 namespace {
 
-constexpr int kTile = 128;           // keys
-constexpr int kMaxEntries = 512;     // (sequence, tile of rows) pairs of a call whose tiles are cut into equal ranges
 constexpr int kMaxSlots = 8;
 constexpr int kMeta = 16;            // tiles that the fetching warp may be ahead: more than the ring holds
 constexpr int kMaxCtas = 320;
-constexpr int kUnitCost = 3;        // what a unit's begin and end take, in tiles (41 calls of all kinds: with 1 7 % slower, 2 2.6, 4 0.5, 5 1.3)
 constexpr int kMinTiles = 4;        // of a range, with that
-constexpr int kWholeTiles = 4;      // units of up to so many tiles are not cut where they are few
 constexpr int kMaxGroup = 32768;     // query heads of a kv head
 constexpr int kUp = 8;               // the largest weight of a row in a tile is 2^kUp (e4m3 ends at 448)
 constexpr int kExpBand = 5;          // exponents of values that are weighed together: see the comment above
@@ -1290,15 +1287,7 @@ extern "C" int sjd_pool_attention(const sjd_pool *pool, int layer, int batch, in
   p.parts = (float *)((char *)ws + kCutBytes + stat_bytes(rp));
   const int64_t entries = (int64_t)batch * p.row_tiles, units = entries * pool->n_kv_heads;
   if (units > 0x7FFFFFFF) return SJD_ERR_CAPACITY;
-  // A CTA per unit where units are short and few (the joining launch costs more than it could win: 2 us), or where the CTAs would have
-  // to look at too many positions to find equal ranges (then there are units enough); else equal ranges.
-  int64_t most = ((int64_t)pool->pages_per_seq * KV_PAGE + kTile - 1) / kTile;   // tiles of a unit
-  if (sliding > 0) {
-    const int64_t in = ((int64_t)sliding + window + kTile - 2) / kTile + 1 + ((int64_t)sinks + kTile - 1) / kTile;
-    most = most < in ? most : in;
-  }
-  p.cut = entries <= kMaxEntries && (int64_t)batch * window <= 8192 && (most > kWholeTiles || units > 2 * sms) &&
-          units * (most + kUnitCost) < 1 << 30;   // (places are counted in 32 bits)
+  p.cut = pool_equal_ranges(entries, pool->n_kv_heads, (int64_t)batch * window, pool->pages_per_seq, window, sliding, sinks, sms);
   p.n_entries = (int)entries;
   const CUtensorMap &m = reinterpret_cast<const CUtensorMap &>(map);
   auto launch = [&](auto kernel, auto join, int RP, int PL, size_t shared) -> int {

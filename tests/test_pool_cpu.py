@@ -2,6 +2,9 @@
 pins (e4m3 numbers against torch's, block exponents, page claims by hand)."""
 import ctypes as C
 import math
+import os
+import subprocess
+import tempfile
 
 import numpy as np
 import pytest
@@ -180,3 +183,34 @@ def test_claims_by_hand():
     for args in (([0, 0], [0, 0], [1, 1]), ([4], [0], [1]), ([0], [0], [193]), ([0, 2], [0, 0], [192, 192])):
         with pytest.raises(O.Refused):
             pool.reserve(*args)
+
+
+# ------------------------------------------------------------------------------------------------- how attention is shared out
+def _equal_ranges(calls):
+    """The library's rule (csrc/pool_route.h) for calls (entries, kv_heads, positions, pages_per_seq, window, sliding, sinks, sms)."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    with tempfile.TemporaryDirectory() as d:
+        src, exe = os.path.join(d, "route.cpp"), os.path.join(d, "route")
+        with open(src, "w") as f:
+            f.write('#include <cstdio>\n#include "pool_route.h"\nint main() {\n  long a[8];\n'
+                    '  while (std::scanf("%ld %ld %ld %ld %ld %ld %ld %ld", a, a + 1, a + 2, a + 3, a + 4, a + 5, a + 6, a + 7) == 8)\n'
+                    '    std::printf("%d\\n", (int)sjd::pool_equal_ranges(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7]));\n}\n')
+        subprocess.run(["g++", "-std=c++17", "-I" + os.path.join(root, "include"),
+                        "-I" + os.path.join(root, "paper_2410_01699_b200", "csrc"), src, "-o", exe], check=True)
+        text = "".join(" ".join(str(int(x)) for x in c) + "\n" for c in calls)
+        return [bool(int(x)) for x in subprocess.run([exe], input=text, capture_output=True, text=True, check=True).stdout.split()]
+
+
+def test_places_of_equal_ranges_stay_in_32_bits():
+    """Rows of a window at any positions: a unit can have all tiles of its table, a sliding window or not, and 3 more places."""
+    rng = np.random.default_rng(3)
+    calls = [(512, 8, 4096, 1 << 20, 8, 100, 0, 148), (4096 // 64, 64, 512, 1 << 20, 8, 1, 4, 148)]
+    for _ in range(2000):
+        entries, kv, window = rng.integers(1, 600), 1 << rng.integers(0, 12), rng.integers(1, 64)
+        calls.append((entries, kv, entries * window, 1 << rng.integers(0, 21), window, rng.choice([0, rng.integers(1, 2**31)]), rng.integers(0, 200), 148))
+    for c, cut in zip(calls, _equal_ranges(calls)):
+        tiles = c[0] * c[1] * (c[3] * 64 // 128 + 3)
+        assert not cut or tiles < 1 << 30, c
+    # one token of a short and of a long sequence, many of them, more than are looked at
+    assert _equal_ranges([(1, 2, 1, 4, 1, 0, 0, 148), (1, 8, 1, 1600, 1, 0, 0, 148), (32, 8, 32, 66, 1, 0, 0, 148), (4, 8, 4, 400, 1, 100, 4, 148),
+                          (513, 8, 513, 66, 1, 0, 0, 148)]) == [False, True, True, False, False]
