@@ -175,6 +175,46 @@ def test_more_positions_than_ranges_are_cut_for():
         assert (np.abs(out[m].float().cpu().numpy() - want[0][0]) <= _bound("bf16", want)[0]).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads,kvh,hd,sliding,sinks", [(2, 1, 128, 0, 0), (4, 2, 64, 0, 0), (4, 1, 128, 70, 3), (1, 1, 64, 300, 0)])
+def test_more_sequences_than_ranges_are_cut_for(dtype, heads, kvh, hd, sliding, sinks):
+    """513 sequences and more: a block of threads per unit, one of them with a long sequence."""
+    lens = [1 + 37 * i % 210 for i in range(519)] + [9000, 64]
+    pool = _filled(lens, 1, kvh, hd, 41)
+    _check_attention(pool, _queries(len(lens), heads, hd, dtype, 42), _window_pos(lens, 1), 1, dtype, sliding, sinks)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads,kvh,hd,sliding,sinks", [(2, 1, 128, 0, 0), (2, 2, 64, 100, 5)])
+def test_windows_of_more_positions_than_ranges_are_cut_for(dtype, heads, kvh, hd, sliding, sinks):
+    """8400 positions: windows of 60 rows, short and empty ones among them, and rows at any positions."""
+    window, lens = 60, [60 + 29 * i % 200 for i in range(139)] + [1500]
+    pool = _filled(lens, 1, kvh, hd, 43)
+    pos = _window_pos(lens, window, [window - 7 * i % 61 for i in range(139)] + [window])
+    rng = np.random.default_rng(44)
+    pos[-window:] = rng.integers(-1, lens[-1], window).tolist()
+    _check_attention(pool, _queries(len(lens) * window, heads, hd, dtype, 45), pos, window, dtype, sliding, sinks)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_nan_of_one_entry_stays_with_the_rows_and_the_entry_that_see_it(dtype, hd):
+    """Every head of a row that does not see a NaN is as without it, bit for bit; of the others only the entry."""
+    n, window = 100, 20
+    pool = _filled((n,), 1, 1, hd, 13)
+    q, pos = _queries(window, 2, hd, dtype, 9), _window_pos((n,), window)
+    clean = B.sjd_pool_attention(pool, 0, q, _i32(pos), window)
+    pool.pages.view(torch.uint8)[int(pool.table[0, 90 // 64]), 0, 1, 0, 90 % 64, 5] = 0xFF
+    got = B.sjd_pool_attention(pool, 0, q, _i32(pos), window)
+    assert pool.fault() == 0
+    for m in range(window):
+        bad = torch.isnan(got[m])
+        if pos[m] < 90:
+            assert torch.equal(got[m], clean[m])
+        else:
+            assert bad[:, 5].all() and int(bad.sum()) == 2 and torch.equal(got[m][~bad], clean[m][~bad])
+
+
 def _check_weights(dtype, got, exact, q, ref, in_pos, window, sliding, sinks):
     """Entries against a bound in which no row counts that a query does not see, nor an exponent that such a row has set: keys are weighed
     together with blocks of at most 2^5 times smaller exponents, so that half of the smallest step of a weight (_bound: 2^-18 resp. 2^-26 of
