@@ -396,6 +396,8 @@ int sjd_pool_append(const sjd_pool *pool, int layer, int batch, int window, int 
  * masked places hold (NaN included) does not matter, nor does the exponent that a masked row gave its block; a visible NaN shows.
  * status: BAD_ARG for seqs or positions out of range (rows that see nothing) and for visible positions without a page (keys that are left
  * out); DEVICE_TIMEOUT if a bounded wait ran out.
+ * Calls of up to 512 (sequence, 64 query rows of a kv head) pairs and 8192 rows share the keys out evenly over the device, whatever the sequences'
+ * lengths; larger ones do not cut a sequence, so that very long ones are better given in a call of their own.
  * ws: device scratch of sjd_pool_attention_workspace_bytes(...) bytes, 256-byte aligned, contents without meaning between calls; one
  * call at a time on a workspace (captured graphs that may run at the same time have their own).
  * Errors: BAD_ARG, UNSUPPORTED (head_dim, dtype, a device other than sm_100's), CAPACITY (ws too small, more than 32768 query heads on

@@ -12,7 +12,8 @@
 // Rounding: q to its own type, k and v to e4m3 (half a step is 2^-4 of an entry) under a scale that lets the largest entry reach
 // 224 to 448; the scale itself is exact.
 // Bound: bytes, one pass over q, k, v: 4224 rows of 32 + 2 x 8 heads, bf16, 95 MB, 23.1 us, 4.1 TB/s (the loads of a warp's next head
-// wait for the stores of the one before; issued earlier they cost registers that spill: 22.9, and fp32 45.7 -> 45.9); 8 windows of
+// wait for the stores of the one before; issued earlier they cost registers that spill: 22.9, and fp32, which spills 204 bytes with heads of
+// 128 as it is, 45.7 -> 45.9); 8 windows of
 // 32 rows of 32 + 2 x 32 heads, fp32, three axes, 18.9 MB, 9.4 us.  Two blocks a SM: one, which no register limit binds, takes 37.5 and 11.2.
 #include "common.cuh"
 

@@ -30,17 +30,19 @@
 // whatever rows that it does not see hold.  Computed for one reference, a hidden value 2^d times the others: error of an output (norm), fp32
 // 4.2e-7 with d = 0, 4.8e-7 with 4, 7.1e-7 with 5, 1.2e-6 with 6, 5e-6 with 8, 5.5e-5 with 12 (bf16 before its rounding 6e-4, 6.5e-4, 6.5e-4,
 // 7e-4, 1.3e-3, 1.4e-2).  Five, so that first tokens with values of an eighth stand beside blocks that differ by four.  Nearly all tiles have one
-// part, which costs nothing but the code (32 tokens 50.8 -> 51.2 us a call of the binding, 8 x 32 rows 108.9 -> 110.6, 100,003 keys 51.4 ->
-// 53.4, others as before); two parts in every tile 2.7 to 2.9 times the call, for masked tiles take longer than whole ones.
+// part, which costs nothing but the code (32 tokens 50.8 -> 51.2 us a call of the binding, 8 x 32 rows 108.9 -> 110.6, 100,003 keys 51.5 ->
+// 53, others as before); two parts in every tile 2.7 to 2.9 times the call, for masked tiles take longer than whole ones.
 //
-// Bound: bytes of K and V up to 16 rows (in a long run 7.1 TB/s; 32 tokens of up to 4224 keys, 32 heads on 8, bf16, 210 MB, 49 us, of which
-// some 18 are the start, the units' ends and the joining launch; 3 tokens of 100,003 keys, 205 MB, 53 us); beyond, the softmax between
+// Bound: bytes of K and V up to 16 rows (in a long run 7.1 TB/s; 32 tokens of up to 4224 keys, 32 heads on 8, bf16, 210 MB, 50 us, of which
+// some 18 are the start, the units' ends and the joining launch; 3 tokens of 100,003 keys, 205 MB, 54 us); beyond, the softmax between
 // the products: a warp takes 770 instructions (bf16: 615) for 32 keys by 16 rows, four of them a scheduler fill 54 % of its issue slots, and
 // the rest are latencies of one tile's chain that the other warps do not cover (8 x 32 rows of 4009 keys of 32 heads, fp32, 271 MB,
-// 106 us, bf16 90; 2 x 64 rows, 32 heads on 8, bf16, 45 us).  Two CTAs per SM (one with 64 rows),
-// each with a ring of tiles: 96 to 160 KB of copies in flight.  What few tiles need stands behind one branch and is short, for the
-// instructions fetched with the common path (NaN entries of V found by a first look of the keys' threads alone, their words mended
-// one at a time: 32 tokens 51.5 -> 50 us, 100,003 keys 57.5 -> 54, though 2 x 64 rows 45 -> 46).
+// 108 us, bf16 91; 2 x 64 rows, 32 heads on 8, bf16, 45 us; a prompt of 4224 rows, 32 heads on 8, bf16, 146 GFLOP, 786 us).  Two CTAs per SM
+// (one with 64 rows), each with a ring of tiles: 96 to 160 KB of copies in flight.  With 32 and 64 rows every warp has 96 registers, the
+// fetching and the issuing one too, and the softmax warps spill (64 dims 188 to 208 bytes, 128 dims 320 to 328).  What few tiles need stands
+// behind one branch and is short, and a copy is issued in one place, for the instructions fetched with the common path (NaN entries of V found
+// by a first look of the keys' threads alone, their words mended one at a time: 32 tokens 51.5 -> 50 us, 100,003 keys 57.5 -> 54, though
+// 2 x 64 rows 45 -> 46; copies issued in three places 54 and 60).
 #include "pool_route.h"
 #include "tcgen05.cuh"
 
