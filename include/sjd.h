@@ -329,6 +329,27 @@ int sjd_attention(int batch, int window, int n_heads, int n_kv_heads, int head_d
                   void *cuda_stream);
 
 /*
+ * What a decoder loop of a caller's own needs beside the pool: sjd_block_norm between two blocks, sjd_linear for the projections (bf16
+ * activations; sjd_gemm takes fp32 ones).  Both only enqueue a kernel on the stream, need no workspace and keep nothing between calls.
+ *
+ * sjd_block_norm: the norm after a block, its gate, the residual and the norm before the next block, for rows m of d entries:
+ *     t = y[m], or N(y[m]) * post_gain + post_bias;    t *= g,  g = gate[m / gate_rows] or (gate_tanh) tanh of it;
+ *     h_out[m] = h[m] + scale * t;    z[m] = N(h_out[m]) * pre_gain + pre_bias
+ *     N(x) = x / sqrt(mean(x^2) + eps)  (SJD_NORM_RMS);  the same of x - mean(x)  (SJD_NORM_LAYER)
+ * Null: post_gain (no norm after the block), either bias (0), gate (1), pre_gain with z (no norm after the residual), y with h_out (z is the
+ * norm of h; then no post_gain and no gate).  y, gains and biases [d], gate [.][d], z are of dtype, h and h_out of h_dtype, SJD_F32 or SJD_BF16
+ * each; rows are *_stride elements apart.  All arithmetic is in 32 bits, rounded once for each output; z is of h_out before it is rounded.
+ * h_out may be h and z may be y (same stride); no other overlap.  d <= 32768.  Where d and the strides are multiples of 8 and all
+ * addresses of 16 bytes, rows are read and written in vectors.  rows 0: nothing.
+ * Errors: BAD_ARG (also an address that is not a multiple of its type's size), UNSUPPORTED (types, kind, d), CUDA.
+ */
+typedef enum { SJD_NORM_RMS = 0, SJD_NORM_LAYER = 1 } sjd_norm_kind;
+int sjd_block_norm(int rows, int d, int kind, float eps, int dtype, int h_dtype, const void *h, int64_t h_stride, const void *y,
+                   int64_t y_stride, const void *post_gain, const void *post_bias, const void *gate, int gate_rows, int gate_tanh,
+                   float scale, void *h_out, int64_t h_out_stride, const void *pre_gain, const void *pre_bias, void *z, int64_t z_stride,
+                   void *cuda_stream);
+
+/*
  * A cache in 8 bits for serving (the paper has none): a pool of pages of SJD_KV_PAGE positions, all layers of a position range in one
  * page, shared by sequences through a table of pages.  An entry is an e4m3 number times 2^e, one exponent e for each SJD_POOL_BLOCK
  * positions of a head's keys or values (e is read as the nearest of -100 .. 100).  The sjd_pool functions write, read and manage it:

@@ -20,6 +20,7 @@ SJD_ERR_CUDA, SJD_ERR_DEVICE_TIMEOUT, SJD_ERR_STATE = -4, -5, -6
 SJD_F32, SJD_BF16 = 0, 1
 SJD_INIT_RANDOM, SJD_INIT_COPY_ABOVE, SJD_INIT_COPY_LEFT, SJD_INIT_RESAMPLE_LEFT, SJD_INIT_RESAMPLE_ABOVE = 0, 1, 2, 3, 4
 SJD_Q_ROW, SJD_Q_UNIFORM, SJD_Q_ONEHOT, SJD_Q_RING = 0, 1, 2, 3
+SJD_NORM_RMS, SJD_NORM_LAYER = 0, 1
 SJD_SCHEDULE_SJD, SJD_SCHEDULE_JACOBI, SJD_SCHEDULE_NO_REFINE = 0, 1, 2
 SJD_FLAG_NEAR_TIE_ACCEPT, SJD_FLAG_RESIDUAL_EMPTY, SJD_FLAG_NONFINITE, SJD_FLAG_DONE = 1, 4, 8, 16
 
@@ -32,7 +33,7 @@ EXPORTS = ["sjd_workspace_bytes", "sjd_init", "sjd_prefill", "sjd_step", "sjd_ge
            "sjd_gemm_workspace_bytes", "sjd_gemm", "sjd_attention_workspace_bytes", "sjd_attention", "sjd_get_info",
            "sjd_prefill_ragged", "sjd_get_tokens", "sjd_pool_append", "sjd_pool_attention_workspace_bytes",
            "sjd_pool_attention", "sjd_pool_workspace_bytes", "sjd_pool_reserve", "sjd_pool_fork", "sjd_pool_free",
-           "sjd_pool_compact"]
+           "sjd_pool_compact", "sjd_block_norm"]
 SJD_KV_PAGE, SJD_POOL_BLOCK, SJD_POOL_MAX_LIST = 64, 16, 1024
 
 
@@ -141,6 +142,10 @@ def lib():
     L.sjd_attention.restype = C.c_int
     L.sjd_attention.argtypes = [C.c_int] * 6 + [C.c_void_p] * 5 + [C.c_size_t, C.c_void_p]
     _pool, _i64 = C.POINTER(sjd_pool), C.c_int64
+    L.sjd_block_norm.restype = C.c_int
+    L.sjd_block_norm.argtypes = [C.c_int, C.c_int, C.c_int, C.c_float, C.c_int, C.c_int, C.c_void_p, _i64, C.c_void_p, _i64, C.c_void_p,
+                                 C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_float, C.c_void_p, _i64, C.c_void_p, C.c_void_p,
+                                 C.c_void_p, _i64, C.c_void_p]
     L.sjd_pool_append.restype = C.c_int
     L.sjd_pool_append.argtypes = [_pool] + [C.c_int] * 5 + [C.c_void_p, _i64] * 3 + \
         [C.c_void_p, C.c_void_p, C.POINTER(sjd_rope), C.c_void_p, C.c_void_p, _i64, C.c_void_p]
@@ -363,16 +368,78 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda in
 
 def _pool_call(pool, where, function, *args):
     """function(pool, *args, stream) on the pool's device and its current stream."""
-    index = pool.index
-    if index < 0:
+    if pool.index < 0:
         raise ValueError("%s: a pool on the host" % where)
+    _call_on(pool.index, where, function, pool.ref, *args)
+
+
+def _call_on(index, where, function, *args):
+    """function(*args, stream) on device `index` and its current stream."""
     if torch.cuda.current_device() == index:
-        status = function(pool.ref, *args, _raw_stream(index))
+        status = function(*args, _raw_stream(index))
     else:
         with torch.cuda.device(index):
-            status = function(pool.ref, *args, _raw_stream(index))
+            status = function(*args, _raw_stream(index))
     if status != SJD_OK:
         raise SJDError(status, where)
+
+
+def _rows(x, rows, d, like, where, dtype=None):
+    """(address, row stride) of x [rows][d] on the device of `like`, of `dtype` if that is given; entries of a row are contiguous."""
+    if x.dim() != 2 or x.shape[0] != rows or x.shape[1] != d or (x.stride(1) != 1 and d > 1) or (rows > 1 and x.stride(0) < d):
+        raise ValueError("%s: [%d][%d], entries of a row contiguous" % (where, rows, d))
+    _same_place(x, like, where, dtype)
+    return x.data_ptr(), x.stride(0) if rows > 1 else max(d, x.stride(0))
+
+
+def _vector(x, d, like, where):
+    """Address of d contiguous entries of `like`'s type and device; None for None."""
+    if x is None:
+        return None
+    if x.numel() != d or not x.is_contiguous():
+        raise ValueError("%s: %d contiguous entries" % (where, d))
+    _same_place(x, like, where, like.dtype)
+    return x.data_ptr()
+
+
+def _same_place(x, like, where, dtype):
+    if x.get_device() != like.get_device() or (dtype is not None and x.dtype is not dtype):
+        raise ValueError("%s: on the device of the other tensors, of their type" % where)
+
+
+def sjd_block_norm(h, y=None, post_gain=None, post_bias=None, gate=None, gate_tanh=False, scale=1.0, pre_gain=None, pre_bias=None,
+                   kind=SJD_NORM_RMS, eps=1e-5, h_out=None, z=None):
+    """(h + scale * gate * N(y), the norm of that): a block's output y [M][d], normed (post_gain) and gated, goes to the residual stream h
+    [M][d], and what the next block reads is its norm (pre_gain).  What is None is left out (see sjd_block_norm in include/sjd.h); without
+    y the norm of h alone.  gate [G][d], one row for each M / G rows; y, gains, biases, gate and z are of one type, h and h_out of one.
+    Returns (h_out, z), new tensors unless given; None for what is not asked for."""
+    if h.dim() != 2 or not h.is_cuda:
+        raise ValueError("sjd_block_norm: h [M][d] on a cuda device")
+    m, d = h.shape
+    kin = y if y is not None else pre_gain
+    if kin is None or (y is None and h_out is not None) or (pre_gain is None and z is not None):
+        raise ValueError("sjd_block_norm: y, pre_gain or both, and outputs of what is asked for")
+    dtype, h_dtype = _pool_dtype(kin, "sjd_block_norm"), _pool_dtype(h, "sjd_block_norm")
+    h_at, h_stride = _rows(h, m, d, h, "h")
+    y_at, y_stride, out_at, out_stride, z_at, z_stride, gate_at, gate_rows = None, 0, None, 0, None, 0, None, 0
+    if y is not None:
+        y_at, y_stride = _rows(y, m, d, h, "y")
+        if h_out is None:
+            h_out = torch.empty_like(h, memory_format=torch.contiguous_format)
+        out_at, out_stride = _rows(h_out, m, d, h, "h_out", h.dtype)
+    if pre_gain is not None:
+        _same_place(kin, h, "pre_gain", None)
+        if z is None:
+            z = torch.empty((m, d), dtype=kin.dtype, device=h.device)
+        z_at, z_stride = _rows(z, m, d, h, "z", kin.dtype)
+    if gate is not None:
+        if gate.dim() != 2 or gate.shape[0] < 1 or m % gate.shape[0] != 0:
+            raise ValueError("gate: [G][%d], G a divisor of the rows" % d)
+        gate_at, gate_rows = _vector(gate, gate.shape[0] * d, kin, "gate"), max(1, m // gate.shape[0])
+    _call_on(h.get_device(), "sjd_block_norm", lib().sjd_block_norm, m, d, kind, eps, dtype, h_dtype, h_at, h_stride, y_at, y_stride,
+             _vector(post_gain, d, kin, "post_gain"), _vector(post_bias, d, kin, "post_bias"), gate_at, gate_rows, int(bool(gate_tanh)), scale,
+             out_at, out_stride, _vector(pre_gain, d, kin, "pre_gain"), _vector(pre_bias, d, kin, "pre_bias"), z_at, z_stride)
+    return h_out, z
 
 
 def _pool_rows(x, heads, pool, rows, where):

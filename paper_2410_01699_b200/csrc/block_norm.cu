@@ -1,0 +1,204 @@
+// The norm after a block, its gate, the residual and the norm before the next block, in one pass over the rows:
+//   t = N(y) g1 + b1    h' = h + scale * gate * t    z = N(h') g2 + b2        N(x) = x / sqrt(mean(x^2) + eps), or of x - mean(x)
+//
+// A row is a block's (a warp's, up to 1024 entries): its entries stay in registers between the sums, which are in 32 bits; the mean goes
+// off before the squares are summed (squares of the entries less the mean's square would lose what a large mean leaves of them).  z is
+// taken of h' before that is rounded to its type.  A thread has N vectors of VEC entries, T threads apart.
+#include "common.cuh"
+
+namespace sjd {
+namespace {
+
+constexpr int kMaxD = 32768;
+constexpr int kWarpRows = 4;   // rows of a block whose warps have one each
+
+struct NormParams {
+  const void *h, *y, *post_gain, *post_bias, *gate, *pre_gain, *pre_bias;
+  void *h_out, *z;
+  long h_stride, y_stride, h_out_stride, z_stride;
+  int rows, d, layer, gate_rows, gate_tanh;
+  float eps, scale, inv_d;
+};
+
+template <typename T, int VEC>
+__device__ __forceinline__ void load_vec(const T *p, float *v) {
+  if constexpr (VEC == 1) {
+    v[0] = (float)*p;
+  } else if constexpr (sizeof(T) == 4) {
+    const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
+    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+  } else {
+    const uint4 a = *reinterpret_cast<const uint4 *>(p);
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(w[i] << 16), v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+  }
+}
+template <typename T, int VEC>
+__device__ __forceinline__ void store_vec(T *p, const float *v) {
+  if constexpr (VEC == 1) {
+    *p = (T)v[0];   // (to the nearest)
+  } else if constexpr (sizeof(T) == 4) {
+    reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+  } else {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t *>(&b);
+    }
+    *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+
+// Y: type of y, gains, biases, gate and z; H: of h and h_out.  ROW: threads of a row are the block (else a warp).
+template <typename Y, typename H, int VEC, int N, bool ROW>
+__global__ void __launch_bounds__(ROW ? 1024 : 32 * kWarpRows) block_norm_kernel(const __grid_constant__ NormParams p) {
+  __shared__ float red[2][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int T = ROW ? blockDim.x : 32, t = ROW ? threadIdx.x : lane;
+  const long row = ROW ? blockIdx.x : (long)blockIdx.x * kWarpRows + warp;
+  pdl_wait();
+  pdl_trigger();
+  if (!ROW && row >= p.rows) return;
+  int sums = 0;
+  auto sum_of_row = [&](float v) {
+    v = warp_sum(v);
+    if constexpr (ROW) {
+      float *r = red[sums++ & 1];   // (the one before may still be read)
+      if (lane == 0) r[warp] = v;
+      __syncthreads();
+      v = warp_sum(lane < T >> 5 ? r[lane] : 0.0f);
+    }
+    return v;
+  };
+  auto at = [&](int i) { return (i * T + t) * VEC; };
+  auto each = [&](auto f) {   // vectors that there are (d is a multiple of VEC)
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (at(i) < p.d) f(i, at(i));
+  };
+  // x = N(x) gain + bias
+  auto normalise = [&](float (&x)[N][VEC], const Y *gain, const Y *bias) {
+    float mean = 0.0f;
+    if (p.layer) {
+      float s = 0.0f;
+      each([&](int i, int) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) s += x[i][e];
+      });
+      mean = sum_of_row(s) * p.inv_d;
+    }
+    float s = 0.0f;
+    each([&](int i, int) {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        x[i][e] -= mean;
+        s = fmaf(x[i][e], x[i][e], s);
+      }
+    });
+    const float f = 1.0f / sqrtf(fmaf(sum_of_row(s), p.inv_d, p.eps));
+    each([&](int i, int k) {
+      float g[VEC], b[VEC];
+      load_vec<Y, VEC>(gain + k, g);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) b[e] = 0.0f;
+      if (bias) load_vec<Y, VEC>(bias + k, b);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) x[i][e] = fmaf(x[i][e] * f, g[e], b[e]);
+    });
+  };
+
+  // With up to 16 entries a thread both loads are under way at once; with 32, h comes when it is needed (64 registers of 1024 threads).
+  constexpr bool EARLY = N * VEC <= 16;
+  float x[N][VEC], h[EARLY ? N : 1][VEC];
+  const H *hp = (const H *)p.h + row * p.h_stride;
+  if (p.y) {
+    const Y *y = (const Y *)p.y + row * p.y_stride;
+    each([&](int i, int k) { load_vec<Y, VEC>(y + k, x[i]); });
+    if constexpr (EARLY) each([&](int i, int k) { load_vec<H, VEC>(hp + k, h[i]); });
+    if (p.post_gain) normalise(x, (const Y *)p.post_gain, (const Y *)p.post_bias);
+    const Y *gate = (const Y *)p.gate + (p.gate ? row / p.gate_rows * p.d : 0);
+    each([&](int i, int k) {
+      if (p.gate) {
+        float g[VEC];
+        load_vec<Y, VEC>(gate + k, g);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) x[i][e] *= p.gate_tanh ? tanhf(g[e]) : g[e];
+      }
+      if constexpr (!EARLY) load_vec<H, VEC>(hp + k, h[0]);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) x[i][e] = fmaf(p.scale, x[i][e], h[EARLY ? i : 0][e]);
+      store_vec<H, VEC>((H *)p.h_out + row * p.h_out_stride + k, x[i]);
+    });
+  } else {
+    each([&](int i, int k) { load_vec<H, VEC>(hp + k, x[i]); });
+  }
+  if (p.z) {
+    normalise(x, (const Y *)p.pre_gain, (const Y *)p.pre_bias);
+    each([&](int i, int k) { store_vec<Y, VEC>((Y *)p.z + row * p.z_stride + k, x[i]); });
+  }
+}
+
+template <typename Y, typename H>
+int launch_norm(const NormParams &p, bool vec, cudaStream_t stream) {
+  auto launch = [&](auto kernel, int rows_of_block, int threads) -> int {
+    g_pdl = true;   // (waits for the launch before it itself)
+    const cudaError_t e = launch_kernel(kernel, dim3((unsigned)((p.rows + (long)rows_of_block - 1) / rows_of_block)), dim3(threads), 0, stream, p);
+    g_pdl = false;
+    SJD_CUDA(e);
+    SJD_CHECK_LAUNCH();
+    return SJD_OK;
+  };
+  auto threads = [&](int per_thread) { return (p.d + 32 * per_thread - 1) / (32 * per_thread) * 32; };
+  if (vec) {
+    if (p.d <= 256) return launch(block_norm_kernel<Y, H, 8, 1, false>, kWarpRows, 32 * kWarpRows);
+    if (p.d <= 512) return launch(block_norm_kernel<Y, H, 8, 2, false>, kWarpRows, 32 * kWarpRows);
+    if (p.d <= 1024) return launch(block_norm_kernel<Y, H, 8, 4, false>, kWarpRows, 32 * kWarpRows);
+    if (p.d <= 8192 && p.rows <= 512) return launch(block_norm_kernel<Y, H, 8, 1, true>, 1, threads(8));
+    if (p.d <= 16384) return launch(block_norm_kernel<Y, H, 8, 2, true>, 1, threads(16));
+    return launch(block_norm_kernel<Y, H, 8, 4, true>, 1, threads(32));
+  }
+  if (p.d <= 256) return launch(block_norm_kernel<Y, H, 1, 8, false>, kWarpRows, 32 * kWarpRows);
+  if (p.d <= 8192) return launch(block_norm_kernel<Y, H, 1, 8, true>, 1, threads(8));
+  return launch(block_norm_kernel<Y, H, 1, 32, true>, 1, threads(32));
+}
+
+}  // namespace
+}  // namespace sjd
+
+using namespace sjd;
+
+extern "C" int sjd_block_norm(int rows, int d, int kind, float eps, int dtype, int h_dtype, const void *h, int64_t h_stride, const void *y,
+                              int64_t y_stride, const void *post_gain, const void *post_bias, const void *gate, int gate_rows,
+                              int gate_tanh, float scale, void *h_out, int64_t h_out_stride, const void *pre_gain, const void *pre_bias,
+                              void *z, int64_t z_stride, void *cuda_stream) {
+  if ((dtype != SJD_F32 && dtype != SJD_BF16) || (h_dtype != SJD_F32 && h_dtype != SJD_BF16)) return SJD_ERR_UNSUPPORTED;
+  if (kind != SJD_NORM_RMS && kind != SJD_NORM_LAYER) return SJD_ERR_UNSUPPORTED;
+  if (rows < 0 || d < 1 || !(eps >= 0.0f) || eps > 1e30f) return SJD_ERR_BAD_ARG;
+  if (rows == 0 && d <= kMaxD) return SJD_OK;
+  if (!h) return SJD_ERR_BAD_ARG;
+  if (!y != !h_out || !pre_gain != !z || (!y && !z)) return SJD_ERR_BAD_ARG;
+  if ((!y && (post_gain || gate)) || (post_bias && !post_gain) || (pre_bias && !pre_gain) || (gate && gate_rows < 1)) return SJD_ERR_BAD_ARG;
+  if (h_stride < d || (y && (y_stride < d || h_out_stride < d)) || (z && z_stride < d)) return SJD_ERR_BAD_ARG;
+  const int size = dtype == SJD_F32 ? 4 : 2, h_size = h_dtype == SJD_F32 ? 4 : 2;
+  const uintptr_t of_y = (uintptr_t)y | (uintptr_t)post_gain | (uintptr_t)post_bias | (uintptr_t)gate | (uintptr_t)pre_gain | (uintptr_t)pre_bias | (uintptr_t)z;
+  const uintptr_t of_h = (uintptr_t)h | (uintptr_t)h_out;
+  if ((of_y & (size - 1)) != 0 || (of_h & (h_size - 1)) != 0) return SJD_ERR_BAD_ARG;
+  if (d > kMaxD) return SJD_ERR_UNSUPPORTED;
+  NormParams p;
+  memset(&p, 0, sizeof(p));
+  p.h = h, p.y = y, p.post_gain = post_gain, p.post_bias = post_bias, p.gate = gate, p.pre_gain = pre_gain, p.pre_bias = pre_bias;
+  p.h_out = h_out, p.z = z;
+  p.h_stride = h_stride, p.y_stride = y_stride, p.h_out_stride = h_out_stride, p.z_stride = z_stride;
+  p.rows = rows, p.d = d, p.layer = kind == SJD_NORM_LAYER, p.gate_rows = gate_rows, p.gate_tanh = gate_tanh != 0;
+  p.eps = eps, p.scale = scale, p.inv_d = 1.0f / (float)d;
+  // vectors of eight entries where all rows start on 16 bytes
+  const int64_t strides = (y ? y_stride | h_out_stride : 0) | (z ? z_stride : 0) | h_stride;
+  const bool vec = d % 8 == 0 && (strides & 7) == 0 && ((of_y | of_h) & 15) == 0;
+  cudaStream_t stream = (cudaStream_t)cuda_stream;
+  if (dtype == SJD_F32)
+    return h_dtype == SJD_F32 ? launch_norm<float, float>(p, vec, stream) : launch_norm<float, __nv_bfloat16>(p, vec, stream);
+  return h_dtype == SJD_F32 ? launch_norm<__nv_bfloat16, float>(p, vec, stream) : launch_norm<__nv_bfloat16, __nv_bfloat16>(p, vec, stream);
+}
