@@ -384,27 +384,21 @@ def _call_on(index, where, function, *args):
         raise SJDError(status, where)
 
 
-def _rows(x, rows, d, like, where, dtype=None):
-    """(address, row stride) of x [rows][d] on the device of `like`, of `dtype` if that is given; entries of a row are contiguous."""
-    if x.dim() != 2 or x.shape[0] != rows or x.shape[1] != d or (x.stride(1) != 1 and d > 1) or (rows > 1 and x.stride(0) < d):
-        raise ValueError("%s: [%d][%d], entries of a row contiguous" % (where, rows, d))
-    _same_place(x, like, where, dtype)
-    return x.data_ptr(), x.stride(0) if rows > 1 else max(d, x.stride(0))
+def _rows(x, rows, d, dtype, index, where):
+    """(address, row stride) of x [rows][d] of `dtype` on device `index`; entries of a row are contiguous."""
+    stride = x.stride()
+    if x.dtype is not dtype or x.get_device() != index or x.shape != (rows, d) or (stride[1] != 1 and d > 1) or (stride[0] < d and rows > 1):
+        raise ValueError("%s: [%d][%d] of %s on the device of the other tensors, entries of a row contiguous" % (where, rows, d, dtype))
+    return x.data_ptr(), stride[0] if rows > 1 else d
 
 
-def _vector(x, d, like, where):
-    """Address of d contiguous entries of `like`'s type and device; None for None."""
+def _vector(x, d, dtype, index, where):
+    """Address of d contiguous entries of `dtype` on device `index`; None for None."""
     if x is None:
         return None
-    if x.numel() != d or not x.is_contiguous():
-        raise ValueError("%s: %d contiguous entries" % (where, d))
-    _same_place(x, like, where, like.dtype)
+    if x.dtype is not dtype or x.get_device() != index or x.numel() != d or not x.is_contiguous():
+        raise ValueError("%s: %d contiguous entries of %s on the device of the other tensors" % (where, d, dtype))
     return x.data_ptr()
-
-
-def _same_place(x, like, where, dtype):
-    if x.get_device() != like.get_device() or (dtype is not None and x.dtype is not dtype):
-        raise ValueError("%s: on the device of the other tensors, of their type" % where)
 
 
 def sjd_block_norm(h, y=None, post_gain=None, post_bias=None, gate=None, gate_tanh=False, scale=1.0, pre_gain=None, pre_bias=None,
@@ -413,32 +407,32 @@ def sjd_block_norm(h, y=None, post_gain=None, post_bias=None, gate=None, gate_ta
     [M][d], and what the next block reads is its norm (pre_gain).  What is None is left out (see sjd_block_norm in include/sjd.h); without
     y the norm of h alone.  gate [G][d], one row for each M / G rows; y, gains, biases, gate and z are of one type, h and h_out of one.
     Returns (h_out, z), new tensors unless given; None for what is not asked for."""
-    if h.dim() != 2 or not h.is_cuda:
+    index, kin = h.get_device(), y if y is not None else pre_gain
+    if index < 0 or h.dim() != 2:
         raise ValueError("sjd_block_norm: h [M][d] on a cuda device")
-    m, d = h.shape
-    kin = y if y is not None else pre_gain
     if kin is None or (y is None and h_out is not None) or (pre_gain is None and z is not None):
         raise ValueError("sjd_block_norm: y, pre_gain or both, and outputs of what is asked for")
+    m, d = h.shape
+    t, ht = kin.dtype, h.dtype
     dtype, h_dtype = _pool_dtype(kin, "sjd_block_norm"), _pool_dtype(h, "sjd_block_norm")
-    h_at, h_stride = _rows(h, m, d, h, "h")
+    h_at, h_stride = _rows(h, m, d, ht, index, "h")
     y_at, y_stride, out_at, out_stride, z_at, z_stride, gate_at, gate_rows = None, 0, None, 0, None, 0, None, 0
     if y is not None:
-        y_at, y_stride = _rows(y, m, d, h, "y")
+        y_at, y_stride = _rows(y, m, d, t, index, "y")
         if h_out is None:
             h_out = torch.empty_like(h, memory_format=torch.contiguous_format)
-        out_at, out_stride = _rows(h_out, m, d, h, "h_out", h.dtype)
+        out_at, out_stride = _rows(h_out, m, d, ht, index, "h_out")
     if pre_gain is not None:
-        _same_place(kin, h, "pre_gain", None)
         if z is None:
-            z = torch.empty((m, d), dtype=kin.dtype, device=h.device)
-        z_at, z_stride = _rows(z, m, d, h, "z", kin.dtype)
+            z = torch.empty((m, d), dtype=t, device=h.device)
+        z_at, z_stride = _rows(z, m, d, t, index, "z")
     if gate is not None:
         if gate.dim() != 2 or gate.shape[0] < 1 or m % gate.shape[0] != 0:
             raise ValueError("gate: [G][%d], G a divisor of the rows" % d)
-        gate_at, gate_rows = _vector(gate, gate.shape[0] * d, kin, "gate"), max(1, m // gate.shape[0])
-    _call_on(h.get_device(), "sjd_block_norm", lib().sjd_block_norm, m, d, kind, eps, dtype, h_dtype, h_at, h_stride, y_at, y_stride,
-             _vector(post_gain, d, kin, "post_gain"), _vector(post_bias, d, kin, "post_bias"), gate_at, gate_rows, int(bool(gate_tanh)), scale,
-             out_at, out_stride, _vector(pre_gain, d, kin, "pre_gain"), _vector(pre_bias, d, kin, "pre_bias"), z_at, z_stride)
+        gate_at, gate_rows = _vector(gate, gate.shape[0] * d, t, index, "gate"), max(1, m // gate.shape[0])
+    _call_on(index, "sjd_block_norm", lib().sjd_block_norm, m, d, kind, eps, dtype, h_dtype, h_at, h_stride, y_at, y_stride,
+             _vector(post_gain, d, t, index, "post_gain"), _vector(post_bias, d, t, index, "post_bias"), gate_at, gate_rows, gate_tanh, scale,
+             out_at, out_stride, _vector(pre_gain, d, t, index, "pre_gain"), _vector(pre_bias, d, t, index, "pre_bias"), z_at, z_stride)
     return h_out, z
 
 

@@ -4,6 +4,8 @@
 // A row is a block's (a warp's, up to 1024 entries): its entries stay in registers between the sums, which are in 32 bits; the mean goes
 // off before the squares are summed (squares of the entries less the mean's square would lose what a large mean leaves of them).  z is
 // taken of h' before that is rounded to its type.  A thread has N vectors of VEC entries, T threads apart.
+#include <algorithm>
+
 #include "common.cuh"
 
 namespace sjd {
@@ -98,7 +100,7 @@ __global__ void __launch_bounds__(ROW ? 1024 : 32 * kWarpRows) block_norm_kernel
         s = fmaf(x[i][e], x[i][e], s);
       }
     });
-    const float f = 1.0f / sqrtf(fmaf(sum_of_row(s), p.inv_d, p.eps));
+    const float f = rsqrtf(fmaf(sum_of_row(s), p.inv_d, p.eps));
     each([&](int i, int k) {
       float g[VEC], b[VEC];
       load_vec<Y, VEC>(gain + k, g);
@@ -141,8 +143,200 @@ __global__ void __launch_bounds__(ROW ? 1024 : 32 * kWarpRows) block_norm_kernel
   }
 }
 
+// ---- many rows: persistent blocks, the next row's entries on their way to shared memory
+// A group of T threads has a row, four vectors of eight entries each thread (fewer entries, and what a warp does once a row, the sums
+// and the root, is most of its instructions: 512 threads a row of 4096 took 235 us for what a block of 128 threads for each row did in 140).  Gains and biases
+// stay in shared memory, the same for all groups of a block; a slot of a group is filled with the next row as soon as its thread has read it.
+// two fp32 operations an instruction
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\tfma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+constexpr int kN = 4, kMaxGroups = 32, kMaxWarps = 8, kRowsThreads = 1024;
+
+// 16 bytes to shared memory, and the groups of such copies of this thread
+__device__ __forceinline__ void copy_async(void *dst, const void *src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+
+// eight entries, as pairs, from the units of a vector `step` units apart
+template <typename T>
+__device__ __forceinline__ void load_pairs(const uint4 *from, int step, float2 *v) {
+  if constexpr (sizeof(T) == 4) {
+    const float4 a = *reinterpret_cast<const float4 *>(from), b = *reinterpret_cast<const float4 *>(from + step);
+    v[0] = make_float2(a.x, a.y), v[1] = make_float2(a.z, a.w), v[2] = make_float2(b.x, b.y), v[3] = make_float2(b.z, b.w);
+  } else {
+    const uint4 a = *from;
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
+  }
+}
+
+// FULL: a row has an entry for every thread's every vector
+template <typename Y, typename H, bool FULL>
+__global__ void __launch_bounds__(kRowsThreads, 1) block_norm_rows_kernel(const __grid_constant__ NormParams p, int T) {
+  constexpr int YU = sizeof(Y) / 2, HU = sizeof(H) / 2;   // 16-byte units of a vector
+  __shared__ alignas(16) float red[kMaxGroups][2][kMaxWarps];
+  extern __shared__ __align__(16) uint4 shared[];   // gains [4][kN YU][T], slots [group][kN (YU + HU)][T]
+  const int g = threadIdx.x / T, t = threadIdx.x - g * T, lane = threadIdx.x & 31, groups = blockDim.x / T, warps = T >> 5;
+  uint4 *kept = shared + t, *slot = shared + (4 * kN * YU + g * kN * (YU + HU)) * T + t;
+  pdl_wait();
+  pdl_trigger();
+  auto each = [&](auto f) {
+#pragma unroll
+    for (int i = 0; i < kN; ++i)
+      if (FULL || (i * T + t) * 8 < p.d) f(i, (i * T + t) * 8);
+  };
+  auto fetch = [&](const void *base, auto type, long stride, long row, uint4 *to) {   // a row's vectors to the slot
+    constexpr int U = sizeof(type) / 2;
+    const uint4 *from = (const uint4 *)((const decltype(type) *)base + row * stride);
+    if (row < p.rows)
+      each([&](int i, int k) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) copy_async(to + (i * U + u) * T, from + k / 8 * U + u);
+      });
+    copies_commit();
+  };
+  const long first = (long)blockIdx.x * groups + g, step = (long)gridDim.x * groups;
+  uint4 *y_slot = slot, *h_slot = slot + kN * YU * T;
+  if (p.y) fetch(p.y, Y(), p.y_stride, first, y_slot);
+  fetch(p.h, H(), p.h_stride, first, h_slot);
+  if (g == 0) {
+    const void *from[4] = {p.post_gain, p.post_bias, p.pre_gain, p.pre_bias};
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (from[j])
+        each([&](int i, int k) {
+#pragma unroll
+          for (int u = 0; u < YU; ++u) kept[(j * kN * YU + i * YU + u) * T] = ((const uint4 *)from[j])[k / 8 * YU + u];
+        });
+  }
+  __syncthreads();
+  int sums = 0;
+  auto sum_of_row = [&](float v) {
+    v = warp_sum(v);
+    if (warps > 1) {
+      float *r = red[g][sums++ & 1];   // (the one before may still be read)
+      if (lane == 0) r[t >> 5] = v;
+      asm volatile("bar.sync %0, %1;" ::"r"(g), "r"(T) : "memory");
+      v = r[0];
+      for (int w = 1; w < warps; ++w) v += r[w];
+    }
+    return v;
+  };
+  auto normalise = [&](float2 (&x)[kN][4], int j, bool bias) {   // x = N(x) gain j + bias j + 1
+    if (p.layer) {
+      float2 s = make_float2(0.0f, 0.0f);
+      each([&](int i, int) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s = add2(s, x[i][e]);
+      });
+      const float mean = sum_of_row(s.x + s.y) * p.inv_d;
+      each([&](int i, int) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[i][e] = add2(x[i][e], make_float2(-mean, -mean));
+      });
+    }
+    float2 s = make_float2(0.0f, 0.0f);
+    each([&](int i, int) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s = fma2(x[i][e], x[i][e], s);
+    });
+    const float f = rsqrtf(fmaf(sum_of_row(s.x + s.y), p.inv_d, p.eps));
+    each([&](int i, int) {
+      float2 w[4];
+      load_pairs<Y>(kept + (j * kN * YU + i * YU) * T, T, w);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[i][e] = mul2(x[i][e], make_float2(f, f));
+      if (bias) {
+        float2 b[4];
+        load_pairs<Y>(kept + ((j + 1) * kN * YU + i * YU) * T, T, b);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[i][e] = fma2(x[i][e], w[e], b[e]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[i][e] = mul2(x[i][e], w[e]);
+      }
+    });
+  };
+  for (long row = first; row < p.rows; row += step) {
+    float2 x[kN][4];
+    if (p.y) {
+      copies_wait<1>();   // (h may be under way)
+      each([&](int i, int) { load_pairs<Y>(y_slot + i * YU * T, T, x[i]); });
+      fetch(p.y, Y(), p.y_stride, row + step, y_slot);
+      if (p.post_gain) normalise(x, 0, p.post_bias);
+      if (p.gate) {
+        const Y *gate = (const Y *)p.gate + row / p.gate_rows * p.d;
+        each([&](int i, int k) {
+          float2 w[4];
+          load_pairs<Y>((const uint4 *)(gate + k), 1, w);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[i][e] = mul2(x[i][e], p.gate_tanh ? make_float2(tanhf(w[e].x), tanhf(w[e].y)) : w[e]);
+        });
+      }
+      copies_wait<1>();   // (y of the next row may be)
+      each([&](int i, int k) {
+        float2 h[4];
+        load_pairs<H>(h_slot + i * HU * T, T, h);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[i][e] = fma2(x[i][e], make_float2(p.scale, p.scale), h[e]);
+        store_vec<H, 8>((H *)p.h_out + row * p.h_out_stride + k, &x[i][0].x);
+      });
+    } else {
+      copies_wait<0>();
+      each([&](int i, int) { load_pairs<H>(h_slot + i * HU * T, T, x[i]); });
+    }
+    fetch(p.h, H(), p.h_stride, row + step, h_slot);
+    if (p.z) {
+      normalise(x, 2, p.pre_bias);
+      each([&](int i, int k) { store_vec<Y, 8>((Y *)p.z + row * p.z_stride + k, &x[i][0].x); });
+    }
+  }
+  copies_wait<0>();
+}
+
 template <typename Y, typename H>
-int launch_norm(const NormParams &p, bool vec, cudaStream_t stream) {
+int launch_rows(const NormParams &p, int sms, cudaStream_t stream) {
+  const int T = (p.d + kN * 256 - 1) / (kN * 256) * 32;
+  const size_t kept = 4ull * kN * sizeof(Y) / 2 * 16 * T, slot = (size_t)kN * (sizeof(Y) + sizeof(H)) / 2 * 16 * T, most = 232448 - 3072;
+  const int groups = std::min(std::min(kRowsThreads / T, kMaxGroups), (int)((most - kept) / slot));
+  auto launch = [&](auto kernel) -> int {
+    const int rc = allow_smem(kernel, most);
+    if (rc != SJD_OK) return rc;
+    g_pdl = true;   // (waits for the launch before it itself)
+    const cudaError_t e = launch_kernel(kernel, dim3((unsigned)std::min<long>(sms, (p.rows + groups - 1) / groups)), dim3(groups * T), kept + groups * slot, stream, p, T);
+    g_pdl = false;
+    SJD_CUDA(e);
+    SJD_CHECK_LAUNCH();
+    return SJD_OK;
+  };
+  return p.d == T * 8 * kN ? launch(block_norm_rows_kernel<Y, H, true>) : launch(block_norm_rows_kernel<Y, H, false>);
+}
+
+template <typename Y, typename H>
+int launch_norm(const NormParams &p, bool vec, int sms, cudaStream_t stream) {
   auto launch = [&](auto kernel, int rows_of_block, int threads) -> int {
     g_pdl = true;   // (waits for the launch before it itself)
     const cudaError_t e = launch_kernel(kernel, dim3((unsigned)((p.rows + (long)rows_of_block - 1) / rows_of_block)), dim3(threads), 0, stream, p);
@@ -152,6 +346,7 @@ int launch_norm(const NormParams &p, bool vec, cudaStream_t stream) {
     return SJD_OK;
   };
   auto threads = [&](int per_thread) { return (p.d + 32 * per_thread - 1) / (32 * per_thread) * 32; };
+  if (vec && p.d <= kMaxWarps * 32 * 8 * kN && (long)p.rows * p.d > 4l * sms * 4096) return launch_rows<Y, H>(p, sms, stream);
   if (vec) {
     if (p.d <= 256) return launch(block_norm_kernel<Y, H, 8, 1, false>, kWarpRows, 32 * kWarpRows);
     if (p.d <= 512) return launch(block_norm_kernel<Y, H, 8, 2, false>, kWarpRows, 32 * kWarpRows);
@@ -197,8 +392,11 @@ extern "C" int sjd_block_norm(int rows, int d, int kind, float eps, int dtype, i
   // vectors of eight entries where all rows start on 16 bytes
   const int64_t strides = (y ? y_stride | h_out_stride : 0) | (z ? z_stride : 0) | h_stride;
   const bool vec = d % 8 == 0 && (strides & 7) == 0 && ((of_y | of_h) & 15) == 0;
+  int dev = 0, sms = 0;
+  SJD_CUDA(cudaGetDevice(&dev));
+  SJD_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
   cudaStream_t stream = (cudaStream_t)cuda_stream;
   if (dtype == SJD_F32)
-    return h_dtype == SJD_F32 ? launch_norm<float, float>(p, vec, stream) : launch_norm<float, __nv_bfloat16>(p, vec, stream);
-  return h_dtype == SJD_F32 ? launch_norm<__nv_bfloat16, float>(p, vec, stream) : launch_norm<__nv_bfloat16, __nv_bfloat16>(p, vec, stream);
+    return h_dtype == SJD_F32 ? launch_norm<float, float>(p, vec, sms, stream) : launch_norm<float, __nv_bfloat16>(p, vec, sms, stream);
+  return h_dtype == SJD_F32 ? launch_norm<__nv_bfloat16, float>(p, vec, sms, stream) : launch_norm<__nv_bfloat16, __nv_bfloat16>(p, vec, sms, stream);
 }
