@@ -350,6 +350,27 @@ int sjd_block_norm(int rows, int d, int kind, float eps, int dtype, int h_dtype,
                    void *cuda_stream);
 
 /*
+ * One projection with its epilogue, for rows m and features f:
+ *     out[m][f] = residual[m][f] + act(sum_i x[m][i] w[f][i] + bias[f]) * (sum_i x[m][i] w_up[f][i] + bias_up[f])
+ * w_up null: no second factor (then no bias_up); bias, bias_up, residual null: 0; act: an sjd_act.  Everything is bf16: x [rows][k], w and w_up
+ * [n][k] (rows w_stride entries apart in both), bias, bias_up [n], residual and out [rows][n]; sums and the epilogue are in 32 bits, rounded once.
+ * x, w and w_up start on 16 bytes and their strides are multiples of 8 (what lies behind k in a row is not read into the sums); any rows, n and k.
+ * out may be residual (same stride); no other overlap.  rows 0: nothing.
+ * status: device int32 or null: DEVICE_TIMEOUT is left there if a bounded wait ran out (and it was 0); the outputs concerned are NaN.
+ * Errors: BAD_ARG, UNSUPPORTED (act, a device other than sm_100's), CAPACITY (n above 2^21, rows or k above 2^28), CUDA.
+ */
+typedef enum {
+  SJD_ACT_NONE = 0,
+  SJD_ACT_RELU = 1,
+  SJD_ACT_SILU = 2,     /* v / (1 + exp(-v))                                       */
+  SJD_ACT_GELU = 3,     /* v (1 + erf(v / sqrt(2))) / 2                            */
+  SJD_ACT_GELU_TANH = 4 /* v (1 + tanh(sqrt(2 / pi) (v + 0.044715 v^3))) / 2       */
+} sjd_act;
+int sjd_linear(int rows, int n, int k, const void *x, int64_t x_stride, const void *w, const void *w_up, int64_t w_stride, const void *bias,
+               const void *bias_up, int act, const void *residual, int64_t residual_stride, void *out, int64_t out_stride, int32_t *status,
+               void *cuda_stream);
+
+/*
  * A cache in 8 bits for serving (the paper has none): a pool of pages of SJD_KV_PAGE positions, all layers of a position range in one
  * page, shared by sequences through a table of pages.  An entry is an e4m3 number times 2^e, one exponent e for each SJD_POOL_BLOCK
  * positions of a head's keys or values (e is read as the nearest of -100 .. 100).  The sjd_pool functions write, read and manage it:

@@ -21,6 +21,7 @@ SJD_F32, SJD_BF16 = 0, 1
 SJD_INIT_RANDOM, SJD_INIT_COPY_ABOVE, SJD_INIT_COPY_LEFT, SJD_INIT_RESAMPLE_LEFT, SJD_INIT_RESAMPLE_ABOVE = 0, 1, 2, 3, 4
 SJD_Q_ROW, SJD_Q_UNIFORM, SJD_Q_ONEHOT, SJD_Q_RING = 0, 1, 2, 3
 SJD_NORM_RMS, SJD_NORM_LAYER = 0, 1
+SJD_ACT_NONE, SJD_ACT_RELU, SJD_ACT_SILU, SJD_ACT_GELU, SJD_ACT_GELU_TANH = 0, 1, 2, 3, 4
 SJD_SCHEDULE_SJD, SJD_SCHEDULE_JACOBI, SJD_SCHEDULE_NO_REFINE = 0, 1, 2
 SJD_FLAG_NEAR_TIE_ACCEPT, SJD_FLAG_RESIDUAL_EMPTY, SJD_FLAG_NONFINITE, SJD_FLAG_DONE = 1, 4, 8, 16
 
@@ -33,7 +34,7 @@ EXPORTS = ["sjd_workspace_bytes", "sjd_init", "sjd_prefill", "sjd_step", "sjd_ge
            "sjd_gemm_workspace_bytes", "sjd_gemm", "sjd_attention_workspace_bytes", "sjd_attention", "sjd_get_info",
            "sjd_prefill_ragged", "sjd_get_tokens", "sjd_pool_append", "sjd_pool_attention_workspace_bytes",
            "sjd_pool_attention", "sjd_pool_workspace_bytes", "sjd_pool_reserve", "sjd_pool_fork", "sjd_pool_free",
-           "sjd_pool_compact", "sjd_block_norm"]
+           "sjd_pool_compact", "sjd_block_norm", "sjd_linear"]
 SJD_KV_PAGE, SJD_POOL_BLOCK, SJD_POOL_MAX_LIST = 64, 16, 1024
 
 
@@ -142,6 +143,9 @@ def lib():
     L.sjd_attention.restype = C.c_int
     L.sjd_attention.argtypes = [C.c_int] * 6 + [C.c_void_p] * 5 + [C.c_size_t, C.c_void_p]
     _pool, _i64 = C.POINTER(sjd_pool), C.c_int64
+    L.sjd_linear.restype = C.c_int
+    L.sjd_linear.argtypes = [C.c_int] * 3 + [C.c_void_p, _i64, C.c_void_p, C.c_void_p, _i64, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, _i64,
+                                             C.c_void_p, _i64, C.c_void_p, C.c_void_p]
     L.sjd_block_norm.restype = C.c_int
     L.sjd_block_norm.argtypes = [C.c_int, C.c_int, C.c_int, C.c_float, C.c_int, C.c_int, C.c_void_p, _i64, C.c_void_p, _i64, C.c_void_p,
                                  C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_float, C.c_void_p, _i64, C.c_void_p, C.c_void_p,
@@ -434,6 +438,37 @@ def sjd_block_norm(h, y=None, post_gain=None, post_bias=None, gate=None, gate_ta
              _vector(post_gain, d, t, index, "post_gain"), _vector(post_bias, d, t, index, "post_bias"), gate_at, gate_rows, gate_tanh, scale,
              out_at, out_stride, _vector(pre_gain, d, t, index, "pre_gain"), _vector(pre_bias, d, t, index, "pre_bias"), z_at, z_stride)
     return h_out, z
+
+
+def sjd_linear(x, w, w_up=None, bias=None, bias_up=None, act=SJD_ACT_NONE, residual=None, out=None, status=None):
+    """residual + act(x w^T + bias) * (x w_up^T + bias_up) of bf16 cuda tensors: x [M][K], w and w_up [N][K], biases [N], residual and out
+    [M][N]; what is None is left out (see sjd_linear in include/sjd.h).  Rows may be parts of longer ones; those of x, w and w_up start on
+    16 bytes.  status: an int32 tensor in which a kernel leaves SJD_ERR_DEVICE_TIMEOUT if a wait ran out.  Returns out."""
+    index = x.get_device()
+    if index < 0 or x.dim() != 2 or w.dim() != 2:
+        raise ValueError("sjd_linear: x [M][K] and w [N][K] on a cuda device")
+    m, k = x.shape
+    n = w.shape[0]
+    bf16 = torch.bfloat16
+    if x.dtype is not bf16:
+        raise SJDError(SJD_ERR_UNSUPPORTED, "sjd_linear")
+    x_at, x_stride = _rows(x, m, k, bf16, index, "x")
+    w_at, w_stride = _rows(w, n, k, bf16, index, "w")
+    up_at, r_at, r_stride = None, None, 0
+    if w_up is not None:
+        up_at, up_stride = _rows(w_up, n, k, bf16, index, "w_up")
+        if up_stride != w_stride:
+            raise ValueError("w_up: rows as far apart as those of w")
+    if residual is not None:
+        r_at, r_stride = _rows(residual, m, n, bf16, index, "residual")
+    if out is None:
+        out = torch.empty((m, n), dtype=bf16, device=x.device)
+    out_at, out_stride = _rows(out, m, n, bf16, index, "out")
+    if status is not None and (status.dtype is not torch.int32 or status.get_device() != index or status.numel() < 1):
+        raise ValueError("status: int32 on the device of the other tensors")
+    _call_on(index, "sjd_linear", lib().sjd_linear, m, n, k, x_at, x_stride, w_at, up_at, w_stride, _vector(bias, n, bf16, index, "bias"),
+             _vector(bias_up, n, bf16, index, "bias_up"), act, r_at, r_stride, out_at, out_stride, None if status is None else status.data_ptr())
+    return out
 
 
 def _pool_rows(x, heads, pool, rows, where):
