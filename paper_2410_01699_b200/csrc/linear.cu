@@ -10,6 +10,7 @@
 // Many rows (linear_tiles_kernel): the time is that of the products, or of the operands from L2.  CTA pairs with 256 features by up to 256
 // tokens, persistent, two accumulators, so that a unit's epilogue runs under the next unit's products.
 #include <algorithm>
+#include <atomic>
 
 #include "tcgen05.cuh"
 
@@ -32,16 +33,32 @@ struct LinearParams {
   const __nv_bfloat16 *bias, *bias_up, *residual;
   __nv_bfloat16 *out;
   long residual_stride, out_stride;
+  int by_four;          // rows of residual and out start on 8 bytes
   int32_t *status;
 };
 
-__device__ __forceinline__ float activate(int act, float v) {
+template <int ACT>
+__device__ __forceinline__ float activate(float v) {
   // (divisions and exponentials with errors of 2^-21: the result is rounded to 2^-9)
-  if (act == SJD_ACT_NONE) return v;
-  if (act == SJD_ACT_RELU) return v < 0.0f ? 0.0f : v;   // (a NaN stays)
-  if (act == SJD_ACT_SILU) return v * __fdividef(1.0f, 1.0f + __expf(-v));
-  if (act == SJD_ACT_GELU) return 0.5f * v * (1.0f + erff(v * 0.70710678f));
-  return 0.5f * v * (1.0f + tanhf(0.79788456f * fmaf(0.044715f * v * v, v, v)));
+  if constexpr (ACT == SJD_ACT_RELU) return v < 0.0f ? 0.0f : v;   // (a NaN stays)
+  if constexpr (ACT == SJD_ACT_SILU) return v * __fdividef(1.0f, 1.0f + __expf(-v));
+  if constexpr (ACT == SJD_ACT_GELU) return 0.5f * v * (1.0f + erff(v * 0.70710678f));
+  if constexpr (ACT == SJD_ACT_GELU_TANH) return 0.5f * v * (1.0f + tanhf(0.79788456f * fmaf(0.044715f * v * v, v, v)));
+  return v;
+}
+template <int ACT>
+struct Act {
+  static constexpr int kind = ACT;
+};
+template <typename F>
+__device__ __forceinline__ void with_act(int act, F f) {
+  switch (act) {
+    case SJD_ACT_RELU: f(Act<SJD_ACT_RELU>()); break;
+    case SJD_ACT_SILU: f(Act<SJD_ACT_SILU>()); break;
+    case SJD_ACT_GELU: f(Act<SJD_ACT_GELU>()); break;
+    case SJD_ACT_GELU_TANH: f(Act<SJD_ACT_GELU_TANH>()); break;
+    default: f(Act<SJD_ACT_NONE>());
+  }
 }
 
 // AND over the epilogue threads (named barrier 1): keeps their control flow uniform
@@ -58,9 +75,9 @@ __device__ __forceinline__ bool all_of(bool pred) {
 __device__ __forceinline__ void fault(int32_t *status) {
   if (status) atomicCAS(status, 0, SJD_ERR_DEVICE_TIMEOUT);
 }
-__device__ __forceinline__ float ld_cluster(uint32_t addr) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr));
+__device__ __forceinline__ float4 ld_cluster(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
   return v;
 }
 template <int CG>
@@ -223,38 +240,56 @@ __global__ void __launch_bounds__(64 + 128 * CG, CG == 1 ? 2 : 1)
   cluster_sync();
   if (warp >= 2) {
     // ------------------------------------------------------------------ a share of the tokens: the sums of all ranges, and the epilogue
-    constexpr int LANES = EPI / FT;   // tokens at a time
-    const int e = tid - 64, f = e % FT, first = e / FT, feature = feature0 + f;
+    // A lane has four features of a token; with U, 16 lanes have the features of one token and the other 16 those of the next.
+    constexpr int WARPS = EPI / 32, AT_ONCE = GATED ? 2 : 1;
+    const int f = (GATED ? lane & 15 : lane) * 4, feature = feature0 + f;
     const int have = min(p.tokens, p.M - token0), per = (have + p.splits - 1) / p.splits;
     const int m0 = split * per, m1 = min(have, m0 + per);
-    if (feature < p.N) {
-      const float b = p.bias ? __bfloat162float(p.bias[feature]) : 0.0f, c = GATED && p.bias_up ? __bfloat162float(p.bias_up[feature]) : 0.0f;
-      constexpr int U = 4;   // tokens whose loads are under way together
-      for (int m = m0 + first; m < m1; m += U * LANES) {
-        float v[U], u[U], r[U];
+    float b[4], c[4];
 #pragma unroll
-        for (int i = 0; i < U; ++i) {
-          v[i] = u[i] = r[i] = 0.0f;
-          if (p.residual && m + i * LANES < m1) r[i] = __bfloat162float(p.residual[(long)(token0 + m + i * LANES) * p.residual_stride + feature]);
-        }
-        for (int s = 0; s < p.splits; ++s) {
+    for (int j = 0; j < 4; ++j) {
+      b[j] = p.bias && feature + j < p.N ? __bfloat162float(p.bias[feature + j]) : 0.0f;
+      c[j] = GATED && p.bias_up && feature + j < p.N ? __bfloat162float(p.bias_up[feature + j]) : 0.0f;
+    }
+    with_act(p.act, [&](auto act) {
+      for (int m = m0 + (warp - 2) * AT_ONCE + (GATED ? lane >> 4 : 0); m < m1 && feature < p.N; m += WARPS * AT_ONCE) {
+        float4 v[kMaxSplits], u[GATED ? kMaxSplits : 1];
+#pragma unroll
+        for (int s = 0; s < kMaxSplits; ++s) {   // (all loads under way together)
+          if (s >= p.splits) break;
           const uint32_t from = cluster_addr(smem, s * CG + half) + (uint32_t)(m * kRows + f) * 4;
-#pragma unroll
-          for (int i = 0; i < U; ++i) {
-            if (m + i * LANES >= m1) break;
-            v[i] += ld_cluster(from + i * LANES * kRows * 4);
-            if (GATED) u[i] += ld_cluster(from + i * LANES * kRows * 4 + FT * 4);
-          }
+          v[s] = ld_cluster(from);
+          if (GATED) u[s] = ld_cluster(from + FT * 4);
         }
 #pragma unroll
-        for (int i = 0; i < U; ++i) {
-          if (m + i * LANES >= m1) break;
-          float y = activate(p.act, v[i] + b);
-          if (GATED) y *= u[i] + c;
-          p.out[(long)(token0 + m + i * LANES) * p.out_stride + feature] = __float2bfloat16_rn(r[i] + y);
+        for (int s = 1; s < kMaxSplits; ++s) {
+          if (s >= p.splits) break;
+          v[0].x += v[s].x, v[0].y += v[s].y, v[0].z += v[s].z, v[0].w += v[s].w;
+          if (GATED) u[0].x += u[s].x, u[0].y += u[s].y, u[0].z += u[s].z, u[0].w += u[s].w;
+        }
+        const float *g = &v[0].x, *h = &u[0].x;
+        float y[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          y[j] = activate<decltype(act)::kind>(g[j] + b[j]);
+          if (GATED) y[j] *= h[j] + c[j];
+        }
+        const __nv_bfloat16 *res = p.residual + (long)(token0 + m) * p.residual_stride + feature;
+        __nv_bfloat16 *out = p.out + (long)(token0 + m) * p.out_stride + feature;
+        if (p.by_four && feature + 4 <= p.N) {
+          if (p.residual) {
+            const uint2 r = *reinterpret_cast<const uint2 *>(res);
+            y[0] += __uint_as_float(r.x << 16), y[1] += __uint_as_float(r.x & 0xFFFF0000u), y[2] += __uint_as_float(r.y << 16), y[3] += __uint_as_float(r.y & 0xFFFF0000u);
+          }
+          const __nv_bfloat162 lo = __floats2bfloat162_rn(y[0], y[1]), hi = __floats2bfloat162_rn(y[2], y[3]);
+          *reinterpret_cast<uint2 *>(out) = make_uint2(*reinterpret_cast<const uint32_t *>(&lo), *reinterpret_cast<const uint32_t *>(&hi));
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (feature + j < p.N) out[j] = __float2bfloat16_rn(p.residual ? y[j] + __bfloat162float(res[j]) : y[j]);
         }
       }
-    }
+    });
   }
   __syncwarp();
   cluster_sync();   // (nobody leaves while its sums may be read)
@@ -265,7 +300,8 @@ __global__ void __launch_bounds__(64 + 128 * CG, CG == 1 ? 2 : 1)
 }
 
 // Persistent CTA pairs; unit u: tile of 256 weight rows u / token_tiles, tile of tokens u % token_tiles.
-constexpr int kTilesThreads = 64 + 256;
+constexpr int kGroups = 4;                                // of four epilogue warps
+constexpr int kTilesThreads = 64 + kGroups * 128;
 template <bool GATED>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTilesThreads, 1)
     linear_tiles_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap u_map,
@@ -290,7 +326,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTilesThreads, 1)
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&acc_full[i], 1);
-      mbar_init(&acc_empty[i], 16);   // the epilogue warps of both CTAs
+      mbar_init(&acc_empty[i], 2 * 4 * kGroups);   // the epilogue warps of both CTAs
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -353,7 +389,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTilesThreads, 1)
       }
     }
   } else {
-    // ------------------------------------------------------------------ epilogue warps (2..9): two groups of four, 16 tokens in turn
+    // ------------------------------------------------------------------ epilogue warps (from 2 on): groups of four, 16 tokens in turn
     const int quarter = warp & 3, row = quarter * 32 + lane, grp = (warp - 2) >> 2, e = (tid - 64) & 127;
     float *ex = reinterpret_cast<float *>(smem + p.stages * stage_bytes) + grp * kRows * (kExTokens + 1);   // GATED: [128][kExTokens + 1]
     // with U, thread e finishes feature e % 64 for every second token
@@ -365,45 +401,58 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTilesThreads, 1)
       const int m_left = min(p.tokens, p.M - m_base);
       const bool live = feature < p.N;
       const float b = live && p.bias ? __bfloat162float(p.bias[feature]) : 0.0f, c = GATED && live && p.bias_up ? __bfloat162float(p.bias_up[feature]) : 0.0f;
-      if (ok && !all_of<256>(warp_wait(&acc_full[buf], (n >> 1) & 1))) {   // (once it ran out no unit is waited for: all are NaN)
+      if (ok && !all_of<kGroups * 128>(warp_wait(&acc_full[buf], (n >> 1) & 1))) {   // (once it ran out no unit is waited for: all are NaN)
         ok = false;
         if (tid == 64) fault(p.status);
       }
       tc_fence_after();
       const uint32_t at = tmem + ((uint32_t)(quarter * 32) << 16) + buf * p.tokens;
-      for (int m0 = grp * 16; m0 < p.tokens; m0 += 32) {
+      with_act(p.act, [&](auto act) {
         constexpr int PER = GATED ? kExTokens / 2 : kExTokens, STEP = GATED ? 2 : 1;
-        float r[PER];
-        const long first = m_base + m0 + odd;
+        const long first = m_base + grp * 16 + odd;
+        const __nv_bfloat16 *res = p.residual + first * p.residual_stride + feature;
+        __nv_bfloat16 *out = p.out + first * p.out_stride + feature;
+        for (int m0 = grp * 16; m0 < p.tokens; m0 += 16 * kGroups) {
+          const int left = live ? (m_left - m0 - odd + STEP - 1) / STEP : 0;   // outputs of this thread, if below PER
+          float r[PER], y[PER];
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-          r[i] = 0.0f;
-          if (p.residual && live && m0 + odd + STEP * i < m_left) r[i] = __bfloat162float(p.residual[(first + STEP * i) * p.residual_stride + feature]);
-        }
-        uint32_t v[16];
-        tmem_ld16_issue(at + m0, v);
-        tmem_ld_wait();
-        float y[PER];
-        if constexpr (GATED) {
+          for (int i = 0; i < PER; ++i) r[i] = 0.0f;
+          if (p.residual) {
 #pragma unroll
-          for (int i = 0; i < 16; ++i) ex[row * (kExTokens + 1) + i] = __uint_as_float(v[i]);
-          asm volatile("bar.sync %0, 128;" ::"r"(grp + 2) : "memory");
-#pragma unroll
-          for (int i = 0; i < PER; ++i)
-            y[i] = activate(p.act, ex[f * (kExTokens + 1) + 2 * i + odd] + b) * (ex[(64 + f) * (kExTokens + 1) + 2 * i + odd] + c);
-          asm volatile("bar.sync %0, 128;" ::"r"(grp + 2) : "memory");
-        } else {
-#pragma unroll
-          for (int i = 0; i < PER; ++i) y[i] = activate(p.act, __uint_as_float(v[i]) + b);
-        }
-        if (live) {
-#pragma unroll
-          for (int i = 0; i < PER; ++i) {
-            if (m0 + odd + STEP * i >= m_left) break;
-            p.out[(first + STEP * i) * p.out_stride + feature] = __float2bfloat16_rn(ok ? r[i] + y[i] : __int_as_float(0x7FFFFFFF));
+            for (int i = 0; i < PER; ++i)
+              if (i < left) r[i] = __bfloat162float(res[i * STEP * p.residual_stride]);
           }
+          uint32_t v[16];
+          tmem_ld16_issue(at + m0, v);
+          tmem_ld_wait();
+          if constexpr (GATED) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) ex[row * (kExTokens + 1) + i] = __uint_as_float(v[i]);
+            asm volatile("bar.sync %0, 128;" ::"r"(grp + 2) : "memory");
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+              y[i] = activate<decltype(act)::kind>(ex[f * (kExTokens + 1) + 2 * i + odd] + b) * (ex[(64 + f) * (kExTokens + 1) + 2 * i + odd] + c);
+            asm volatile("bar.sync %0, 128;" ::"r"(grp + 2) : "memory");
+          } else {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) y[i] = activate<decltype(act)::kind>(__uint_as_float(v[i]) + b);
+          }
+          if (__builtin_expect(!ok, 0)) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) y[i] = __int_as_float(0x7FFFFFFF);
+          }
+          if (left >= PER) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) out[i * STEP * p.out_stride] = __float2bfloat16_rn(r[i] + y[i]);
+          } else {
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+              if (i < left) out[i * STEP * p.out_stride] = __float2bfloat16_rn(r[i] + y[i]);
+          }
+          res += 16l * kGroups * p.residual_stride;
+          out += 16l * kGroups * p.out_stride;
         }
-      }
+      });
       tc_fence_before();
       __syncwarp();
       if (lane == 0)   // the accumulator is free (the first CTA issues into both CTAs' tensor memory)
@@ -434,6 +483,26 @@ int make_map(TensorMap *out, const void *base, long rows, long cols, long stride
 
 int round16(int n) { return (n + 15) / 16 * 16; }
 
+// Clusters of `size` CTAs with an SM each that the current device holds at a time: its SMs come in groups, and a cluster is in one of
+// them (33 of four, 22 of six and 15 of eight on 148 SMs; a sixteenth cluster of eight doubles the time of a launch).
+int clusters_of(int dev, int size, int *out) {
+  constexpr int kDevices = 64;
+  static std::atomic<int> known[kDevices][kMaxSplits + 1];   // (0: not asked yet)
+  if (dev < kDevices && (*out = known[dev][size].load(std::memory_order_relaxed)) > 0) return SJD_OK;
+  const int rc = allow_smem(linear_split_kernel<2, false>, kSmem);
+  if (rc != SJD_OK) return rc;
+  cudaLaunchConfig_t cfg;
+  memset(&cfg, 0, sizeof(cfg));
+  cfg.gridDim = dim3(size), cfg.blockDim = dim3(64 + 256), cfg.dynamicSmemBytes = kSmem;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = size, attr[0].val.clusterDim.y = 1, attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr, cfg.numAttrs = 1;
+  SJD_CUDA(cudaOccupancyMaxActiveClusters(out, (const void *)linear_split_kernel<2, false>, &cfg));
+  if (dev < kDevices) known[dev][size].store(*out, std::memory_order_relaxed);
+  return SJD_OK;
+}
+
 }  // namespace
 }  // namespace sjd
 
@@ -462,29 +531,45 @@ extern "C" int sjd_linear(int rows, int n, int k, const void *x, int64_t x_strid
   memset(&p, 0, sizeof(p));
   p.M = rows, p.N = n, p.k_blocks = (k + kTileK - 1) / kTileK, p.act = act;
   p.bias = (const __nv_bfloat16 *)bias, p.bias_up = (const __nv_bfloat16 *)bias_up, p.residual = (const __nv_bfloat16 *)residual;
+  p.by_four = (((uintptr_t)residual | (uintptr_t)out) & 7u) == 0 && ((out_stride | (residual ? residual_stride : 0)) & 3) == 0;
   p.residual_stride = residual_stride, p.out = (__nv_bfloat16 *)out, p.out_stride = out_stride, p.status = status;
   // ---- which kernel, and how the work is cut
   const int pairs = sms / 2, kb = p.k_blocks;
   int cg = 1, splits = 1;
   bool tiles = false;
   if (rows <= 64) {
+    // as many ranges of K as all fit at two CTAs per SM
     const int features = (n + ft - 1) / ft;
     p.tokens = round16(rows), p.token_tiles = 1;
-    splits = std::max(1, std::min(std::min(2 * sms / features, kMaxSplits), kb / 2));
+    for (int s : {2, 3, 4, 6, 8}) {
+      if (s * 2 > kb || features * s > 2 * sms) break;
+      int fit = 0;
+      const int rc = clusters_of(dev, s, &fit);
+      if (rc != SJD_OK) return rc;
+      if (features <= 2 * fit) splits = s;
+    }
   } else {
+    // clocks of a launch: a k-block takes a pair its products (8192 a clock), or its 256 + tokens rows from L2, of which an SM takes 64 bytes
+    // and all together 6600 a clock
     const long features = (n + 2 * ft - 1) / (2 * ft);
     double best = 1e300;
     cg = 2;
-    for (int t = (rows + kMaxTokens - 1) / kMaxTokens; t <= (rows + 63) / 64; ++t) {
+    auto consider = [&](int t, int s) {
       const int tokens = round16((rows + t - 1) / t);
-      const double block = 2.0 * tokens + 64;
-      const double whole = (double)((features * t + pairs - 1) / pairs) * (kb * block + 800) + 8.0 * tokens;
-      if (whole < best) best = whole, tiles = true, splits = 1, p.tokens = tokens, p.token_tiles = t;
-      for (int s = 2; s <= 4 && features * t * s <= pairs && s <= kb / 2; ++s) {
-        const double part = (kb + s - 1) / s * block + 800 + 8.0 * tokens;
-        if (part < best) best = part, tiles = false, splits = s, p.tokens = tokens, p.token_tiles = t;
+      const long units = features * t * s, active = std::min<long>(units, pairs);
+      const double bytes = (256.0 + tokens) * kTileK * 2, block = std::max(2.0 * tokens, bytes * std::max(1.0 / 128, active / 6600.0));
+      const double clocks = (double)((units + pairs - 1) / pairs) * ((kb + s - 1) / s * block + 800) + 11.0 * tokens + (s > 1 ? 2500 : 0);
+      if (clocks < best) best = clocks, tiles = s == 1, splits = s, p.tokens = tokens, p.token_tiles = t;
+    };
+    const int t0 = (rows + kMaxTokens - 1) / kMaxTokens;
+    for (int t = t0; t <= (rows + 31) / 32 && t <= t0 + 16; ++t) {
+      consider(t, 1);
+      for (int s = 2; s <= 4 && s * 2 <= kb && features * t * s <= pairs; ++s) {
+        int fit = 0;
+        const int rc = clusters_of(dev, 2 * s, &fit);
+        if (rc != SJD_OK) return rc;
+        if (features * t <= fit) consider(t, s);
       }
-      if (t > (rows + kMaxTokens - 1) / kMaxTokens + 16) break;
     }
   }
   p.splits = splits;
@@ -497,7 +582,7 @@ extern "C" int sjd_linear(int rows, int n, int k, const void *x, int64_t x_strid
   if (rc == SJD_OK) rc = make_map(&xm, x, rows, k, x_stride, p.tokens / cg);
   if (rc != SJD_OK) return rc;
   const CUtensorMap &W = reinterpret_cast<const CUtensorMap &>(wm), &U = reinterpret_cast<const CUtensorMap &>(um), &X = reinterpret_cast<const CUtensorMap &>(xm);
-  const int stage = kWBytes + p.tokens / cg * kTileK * 2, exchange = tiles && gated ? 2 * kRows * (kExTokens + 1) * 4 : 0;
+  const int stage = kWBytes + p.tokens / cg * kTileK * 2, exchange = tiles && gated ? kGroups * kRows * (kExTokens + 1) * 4 : 0;
   const int room = (cg == 1 ? kSmemOfTwo : kSmem) - 1024 - exchange;
   p.stages = std::min(kStages, room / stage);
   const size_t smem = 1024 + std::max((size_t)p.stages * stage + exchange, tiles ? (size_t)0 : (size_t)p.tokens * kRows * 4);
