@@ -451,6 +451,24 @@ int sjd_pool_attention(const sjd_pool *pool, int layer, int batch, int window, i
                        void *ws, size_t ws_bytes, void *cuda_stream);
 
 /*
+ * Attention over the pool for sequences that share pages (sjd_pool_fork): the same rows, positions and result as sjd_pool_attention without
+ * a sliding window, for bf16 queries, but the pages that the tables of a group's sequences begin with, as far as they lie before all of the group's rows,
+ * are read and multiplied once for all of its rows.  Group g is the sequences b = group_begin[g] .. group_begin[g + 1] - 1 of the call (device
+ * int32, n_groups + 1 entries that rise from 0 to batch; null: one group of all; n_groups is not read then).  What a group really shares is found in the tables: sequences
+ * that share nothing are only attended one by one.  out may not overlap q.  Scores and sums are held in 32 bits; a weight is rounded by up to 2^-8 of
+ * itself.  What rows behind a sequence or masked places hold (NaN included) does not matter; a visible NaN shows.
+ * status: as sjd_pool_attention; BAD_ARG for a group_begin that is not as above (no pages are shared then).
+ * ws: device scratch of sjd_pool_attention_shared_workspace_bytes(...) bytes, 256-byte aligned, contents without meaning between calls; one
+ * call at a time on a workspace (captured graphs that may run at the same time have their own).
+ * Errors: BAD_ARG, UNSUPPORTED (head_dim, dtype, a device other than sm_100's), CAPACITY (ws too small, batch above SJD_POOL_MAX_LIST, n_groups
+ * above batch, more than 2^30 rows times heads, tables too long for the call's places to be counted in 32 bits), CUDA.
+ */
+size_t sjd_pool_attention_shared_workspace_bytes(const sjd_pool *pool, int batch, int window, int n_heads);
+int sjd_pool_attention_shared(const sjd_pool *pool, int layer, int batch, int window, int n_heads, int dtype, const void *q, int64_t q_stride,
+                              const int32_t *seqs, const int32_t *in_pos, int n_groups, const int32_t *group_begin, float scale, void *out,
+                              int64_t out_stride, void *ws, size_t ws_bytes, void *cuda_stream);
+
+/*
  * Pages for positions begin[i] .. end[i] - 1 of sequence seqs[i], i = 0 .. n - 1 (device int32 arrays, n <= SJD_POOL_MAX_LIST): absent
  * pages are given; a page that other table entries hold as well is replaced by a page of its own, with a copy of its contents where
  * positions before begin[i] lie in it, except that the last holder keeps it.  Claims count in the order of i, then of positions.

@@ -34,7 +34,8 @@ EXPORTS = ["sjd_workspace_bytes", "sjd_init", "sjd_prefill", "sjd_step", "sjd_ge
            "sjd_gemm_workspace_bytes", "sjd_gemm", "sjd_attention_workspace_bytes", "sjd_attention", "sjd_get_info",
            "sjd_prefill_ragged", "sjd_get_tokens", "sjd_pool_append", "sjd_pool_attention_workspace_bytes",
            "sjd_pool_attention", "sjd_pool_workspace_bytes", "sjd_pool_reserve", "sjd_pool_fork", "sjd_pool_free",
-           "sjd_pool_compact", "sjd_block_norm", "sjd_linear"]
+           "sjd_pool_compact", "sjd_block_norm", "sjd_linear",
+           "sjd_pool_attention_shared_workspace_bytes", "sjd_pool_attention_shared"]
 SJD_KV_PAGE, SJD_POOL_BLOCK, SJD_POOL_MAX_LIST = 64, 16, 1024
 
 
@@ -158,6 +159,11 @@ def lib():
     L.sjd_pool_attention.restype = C.c_int
     L.sjd_pool_attention.argtypes = [_pool] + [C.c_int] * 5 + [C.c_void_p, _i64, C.c_void_p, C.c_void_p, C.c_int, C.c_int,
                                                                C.c_float, C.c_void_p, _i64, C.c_void_p, C.c_size_t, C.c_void_p]
+    L.sjd_pool_attention_shared_workspace_bytes.restype = C.c_size_t
+    L.sjd_pool_attention_shared_workspace_bytes.argtypes = [_pool, C.c_int, C.c_int, C.c_int]
+    L.sjd_pool_attention_shared.restype = C.c_int
+    L.sjd_pool_attention_shared.argtypes = [_pool] + [C.c_int] * 5 + [C.c_void_p, _i64, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_float,
+                                                                      C.c_void_p, _i64, C.c_void_p, C.c_size_t, C.c_void_p]
     L.sjd_pool_workspace_bytes.restype = C.c_size_t
     L.sjd_pool_workspace_bytes.argtypes = [_pool]
     L.sjd_pool_reserve.restype = C.c_int
@@ -332,6 +338,7 @@ class CachePool:
         self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.device)
         self.ws_at = self.ws.data_ptr()
         self._attention_ws = None
+        self._shared_ws, self._shared_bytes = [], {}
 
     @classmethod
     def empty(cls, n_pages, n_seqs, pages_per_seq, n_layers, n_kv_heads, head_dim, device="cuda"):
@@ -347,6 +354,17 @@ class CachePool:
             nbytes = int(lib().sjd_pool_attention_workspace_bytes(self.ref, 64, self.n_kv_heads))   # (tiles have at most 64 rows)
             self._attention_ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         return self._attention_ws
+
+    def shared_ws(self, batch, window, heads):
+        """The pool's workspace for attention over shared pages: the last of those so far if it is large enough for such a call, else another
+        one (the others stay: a captured graph keeps the address that it was given)."""
+        nbytes = self._shared_bytes.get((batch, window, heads))
+        if nbytes is None:
+            nbytes = int(lib().sjd_pool_attention_shared_workspace_bytes(self.ref, batch, window, heads))
+            self._shared_bytes[batch, window, heads] = nbytes
+        if not self._shared_ws or self._shared_ws[-1].nbytes < nbytes:
+            self._shared_ws.append(torch.empty(max(nbytes, 1), dtype=torch.uint8, device=self.device))
+        return self._shared_ws[-1]
 
     def fault(self) -> int:
         """The first fault that a kernel found since the start or clear() (an SJD_ERR_* value, 0: none).  Synchronises."""
@@ -543,6 +561,33 @@ def sjd_pool_attention(pool: CachePool, layer: int, q, in_pos, window: int, slid
     _pool_call(pool, "sjd_pool_attention", lib().sjd_pool_attention, layer, m // window, window, heads, dtype, q.data_ptr(),
                _pool_rows(q, heads, pool, m, "q"), _ints(seqs, m // window, pool, "seqs"), _ints(in_pos, m, pool, "in_pos"), sliding, sinks,
                scale, out.data_ptr(), _pool_rows(out, heads, pool, m, "out"), ws.data_ptr(), ws.nbytes)
+    return out
+
+
+def sjd_pool_attention_shared(pool: CachePool, layer: int, q, in_pos, window: int, group_begin=None, scale=0.0, out=None, ws=None, seqs=None):
+    """Attention of q [B*W][H][hd] (bfloat16) at positions in_pos over the pool, where the sequences group_begin[g] .. group_begin[g + 1] - 1
+    of the call (int32, rising from 0 to B; None: all are one group) may share the pages that their tables begin with: those are attended once
+    for all rows of the group.  ws: as for sjd_pool_attention."""
+    m, heads = in_pos.numel(), q.shape[1]
+    if q.dtype is not torch.bfloat16:
+        raise SJDError(SJD_ERR_UNSUPPORTED, "sjd_pool_attention_shared")
+    if window < 1 or m % window != 0:
+        raise ValueError("sjd_pool_attention_shared: whole windows")
+    if out is None:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    if out.dtype != q.dtype:
+        raise ValueError("out: of q's type")
+    if ws is None:
+        ws = pool.shared_ws(m // window, window, heads)
+    elif ws.get_device() != pool.index or not ws.is_contiguous():
+        raise ValueError("ws: contiguous, on the pool's device")
+    groups = group_begin.numel() - 1 if group_begin is not None else 1
+    if groups < 1:
+        raise ValueError("group_begin: one entry more than groups")
+    _pool_call(pool, "sjd_pool_attention_shared", lib().sjd_pool_attention_shared, layer, m // window, window, heads, SJD_BF16, q.data_ptr(),
+               _pool_rows(q, heads, pool, m, "q"), _ints(seqs, m // window, pool, "seqs"), _ints(in_pos, m, pool, "in_pos"), groups,
+               _ints(group_begin, groups + 1, pool, "group_begin"), scale, out.data_ptr(), _pool_rows(out, heads, pool, m, "out"), ws.data_ptr(),
+               ws.nbytes)
     return out
 
 
