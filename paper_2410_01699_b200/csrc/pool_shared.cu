@@ -1,18 +1,22 @@
 // Attention over the 8-bit paged cache for sequences that share pages: the pages that all tables of a group begin with are attended once,
-// with the rows of all its sequences, the rest of each sequence with its own rows, and the parts are joined.
+// with the rows of all its sequences.
 //
 // Queries are the rows of both products (128 of a stream), keys and dims the columns:
 //   S [128 rows x 128 keys]  =  Q . K^T          O [128 rows x HD]  +=  P . V          (tcgen05, bf16, sums in 32 bits in tensor memory)
-// A shared prefix meets many rows, so that the products and exponentials of a tile decide and its keys may be prepared once for all of them: eight
+// Shared pages meet many rows, so that the products and exponentials of a tile decide and its keys may be prepared once for all of them: four
 // warps turn e4m3 entries times 2^exponent into bf16, which holds them exactly (four bits and any exponent), as they lay them out for
 // the tensor cores.  P goes to the second product through tensor memory, in the columns of the scores that it was.
-// Two streams of four softmax warps, a row a thread: units of more than 128 rows give them 128 rows each of every tile of keys, others every
-// other tile of keys with the same rows, so that one stream's softmax runs under the other's products either way.
+// The rows of all sequences of a call follow one another (per kv head), 256 are a unit.  A unit's keys are segments: a group's common pages,
+// seen by all of its rows among the unit's, and every sequence's own pages, seen by its rows; the weights of the other rows are zeros.  So a
+// unit begins and ends once for many sequences, however short what is theirs alone.
+// Two streams of four softmax warps, a row a thread, have 128 rows each: a tile of keys is for both streams, or (a sequence's own) for the one that
+// has the rows, and those of the two streams take turns, so that one stream's softmax runs under the other's products.  A unit of up to
+// 128 rows gives both streams the same rows and every other tile.
 // A weight is taken under a reference that follows the row's maximum only when that has grown by 2^8 (the sums in tensor memory
 // then need no factor in nearly all tiles), and rounded to bf16, by up to 2^-8 of itself.
 //
-// Three launches: a plan (positions, what tables share, the line of units), the tiles, the joining of parts.  A unit is (group or sequence,
-// up to 256 rows, kv head); the line of all units' tiles is cut into equal ranges, a CTA each.
+// Three launches: a plan (positions, what tables share, the line of units), the tiles, the joining of parts.  The line of all units' tiles is cut into
+// equal ranges, a CTA each; a unit that is within one is written by its CTA, the parts of the others are joined in the order of the ranges.
 #include "tcgen05.cuh"
 
 namespace sjd {
@@ -20,49 +24,44 @@ namespace {
 
 constexpr int kKeys = 128;              // of a tile
 constexpr int kTileRows = 256;          // of a unit
-constexpr int kUnit = 4;                // what a unit's begin and end take, in tiles of one stream
-constexpr int kLeast = 2;               // pages that are worth a unit of their own
+constexpr int kUnit = 6;                // what a unit's begin and end take, in tiles of one stream
+constexpr int kLeast = 2;               // common pages that are worth a tile of their own
 constexpr int kMaxCtas = 192;
 constexpr int kMaxSeqs = SJD_POOL_MAX_LIST;
-constexpr int kBefore = 2048;           // entries whose places are kept in shared memory
+constexpr int kBefore = 1024;           // units of a kv head whose places are kept in shared memory
+constexpr int kMaxSegs = 2 * kTileRows + 2;   // of a unit
 constexpr int kInfo = 4;                // tiles whose notes are kept
-constexpr int kConv = 256, kSoft = 256, kThreads = kSoft + kConv + 32;
+constexpr int kConv = 128, kSoft = 256, kThreads = kSoft + kConv + 32;
 constexpr int kPlanThreads = 1024;
 constexpr float kGrow = 8.0f;           // log2 of what a maximum may grow before its reference follows
 
-struct Entry {   // (group or sequence, tile of rows)
-  int b0, r0, rows;    // first sequence of its rows; row of the first one, counted from there; how many
-  int seq;             // whose table (-1: none)
-  int k0, k1;          // keys
-  int row_base;        // rows of the parts of a kv head in the entries before
-  int prefix;          // keys are before every row's position
+struct Segment {       // keys k0 .. k1 - 1 of a sequence's table, for rows ra .. rb - 1 of a unit
+  int seq, k0, k1, ra, rb, base;   // base: tiles of the unit's segments for the same streams before it
 };
-struct Plan {          // in the workspace
-  int n_entries, all, rows;   // places and rows of the parts of a kv head
+struct Entry {         // 256 rows of a kv head
+  int segs;            // first of its segments: those for both streams, for the first, for the second
+  int n_segs[3], tiles[3];
+  int rows;
 };
-
 struct SharedParams {
   sjd_pool pool;
-  int layer, batch, window, n_heads, group, rows, row_tiles, n_groups;   // rows: window * group
+  int layer, batch, window, n_heads, group, rows, n_entries, n_groups;   // rows: window * group
   float scale;         // times log2(e)
   const __nv_bfloat16 *q;
   long q_stride, out_stride;
   const int32_t *seqs, *in_pos, *group_begin;
   __nv_bfloat16 *out;
   int by_eight;        // queries start on 16 bytes
-  Plan *plan;
-  int *before;         // [max entries + 1]: places of a kv head in the entries before
-  Entry *entry;        // [max entries]
-  int *group_of;       // [batch]
-  int *prefix_of;      // [batch]: first entry of a group's shared keys, -1: none
-  float2 *stats;       // (reference, sum) of a row's parts
+  int *before;         // [n_entries + 1]: places of a kv head in the units before
+  Entry *entry;        // [n_entries]
+  Segment *segs;
+  float2 *stats;       // (reference, sum) of a row's part
   float *parts;        // [HD / 4][rows of the part][4]
-  int max_entries, ctas;
+  int ctas;
 };
 
 __device__ __forceinline__ int padded(int rows) { return (rows + 7) & ~7; }
-// places of a tile: both streams work on it, or one does
-__device__ __forceinline__ int weight_of(int rows) { return rows > 128 ? 2 : 1; }
+__device__ __forceinline__ bool one_stream(int rows) { return rows <= 128; }
 
 __device__ __forceinline__ int row_position(const SharedParams &p, int b, int k, bool tell) {
   int at = p.in_pos[(long)b * p.window + k];
@@ -76,198 +75,240 @@ __device__ __forceinline__ int row_position(const SharedParams &p, int b, int k,
 
 // ---------------------------------------------------------------------------------------------------------------- plan
 __global__ void __launch_bounds__(kPlanThreads) shared_plan_kernel(const __grid_constant__ SharedParams p) {
-  __shared__ int lo[kMaxSeqs], hi[kMaxSeqs], share[kMaxSeqs], leader[kMaxSeqs], first[kMaxSeqs + 1];   // by sequence, and by group
-  __shared__ int bad, sums[2][32];
+  __shared__ int lo[kMaxSeqs], hi[kMaxSeqs], group_of[kMaxSeqs], seq_of[kMaxSeqs];              // by sequence of the call
+  __shared__ int share[kMaxSeqs], leader[kMaxSeqs], live[kMaxSeqs], begin[kMaxSeqs + 1];         // by group
+  __shared__ int bad, sums[32];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = kPlanThreads / 32;
   pdl_wait();
   pdl_trigger();
-  if (tid == 0) bad = 0;
-  for (int b = tid; b < p.batch; b += kPlanThreads) lo[b] = 0x7FFFFFFF, hi[b] = -1;
-  __syncthreads();
-  // positions of every (sequence, tile of rows)
-  const int own = p.batch * p.row_tiles;
-  for (int e = warp; e < own; e += warps) {
-    const int b = e / p.row_tiles, r0 = (e - b * p.row_tiles) * kTileRows, r1 = min(p.rows, r0 + kTileRows);
-    int l = 0x7FFFFFFF, h = -1;
-    for (int k = r0 / p.group + lane; k <= (r1 - 1) / p.group; k += 32) {
-      const int at = row_position(p, b, k, true);
-      if (at >= 0) l = min(l, at), h = max(h, at);
-    }
-    l = __reduce_min_sync(0xffffffffu, l);
-    h = __reduce_max_sync(0xffffffffu, h);
-    if (lane == 0) {
-      if (h >= 0) atomicMin(&lo[b], l), atomicMax(&hi[b], h);
-      Entry n;
-      n.b0 = b, n.r0 = r0, n.rows = r1 - r0, n.seq = h < 0 ? -1 : p.seqs ? p.seqs[b] : b, n.k0 = 0, n.k1 = h + 1, n.row_base = 0, n.prefix = 0;
-      p.entry[e] = n;
-    }
-  }
-  // groups: ranges of sequences that follow one another
   const int groups = p.group_begin ? p.n_groups : 1;
-  auto begin_of = [&](int g) { return p.group_begin ? p.group_begin[g] : g * p.batch; };
-  for (int g = tid; g < groups; g += kPlanThreads) {
-    const int b0 = begin_of(g), b1 = begin_of(g + 1);
-    if (b0 < 0 || b1 < b0 || b1 > p.batch || (g == 0 && b0 != 0) || (g == groups - 1 && b1 != p.batch)) bad = 1;
+  if (tid == 0) bad = 0;
+  for (int g = tid; g <= groups; g += kPlanThreads) {
+    begin[g] = p.group_begin ? p.group_begin[g] : g * p.batch;
+    if (g < groups) share[g] = leader[g] = 0x7FFFFFFF, live[g] = 0;
+  }
+  // positions of every sequence, a group of lanes each
+  int lanes = 1;
+  while (lanes < 32 && lanes < p.window) lanes <<= 1;
+  for (int b0 = 0; b0 < p.batch; b0 += kPlanThreads / lanes) {
+    const int b = b0 + tid / lanes;
+    int l = 0x7FFFFFFF, h = -1;
+    if (b < p.batch)
+      for (int k = tid % lanes; k < p.window; k += lanes) {
+        const int at = row_position(p, b, k, true);
+        if (at >= 0) l = min(l, at), h = max(h, at);
+      }
+    for (int o = lanes >> 1; o > 0; o >>= 1) {
+      l = min(l, __shfl_xor_sync(0xffffffffu, l, o));
+      h = max(h, __shfl_xor_sync(0xffffffffu, h, o));
+    }
+    if (b < p.batch && tid % lanes == 0) lo[b] = l, hi[b] = h, seq_of[b] = p.seqs ? p.seqs[b] : b;
   }
   __syncthreads();
-  if (bad) {
-    if (tid == 0) pool_fault(p.pool.status, SJD_ERR_BAD_ARG);
-    for (int b = tid; b < p.batch; b += kPlanThreads) p.prefix_of[b] = -1;   // (every sequence for itself)
-  } else {
-    for (int g = tid; g < groups; g += kPlanThreads) {
-      const int b0 = begin_of(g), b1 = begin_of(g + 1);
-      int pages = 0x7FFFFFFF, lead = -1, live = 0;
-      for (int b = b0; b < b1; ++b) {
-        p.group_of[b] = g;
-        if (hi[b] < 0) continue;
-        pages = min(pages, (lo[b] + 1) / KV_PAGE);
-        if (lead < 0) lead = b;
-        ++live;
+  // groups: ranges of sequences that follow one another
+  for (int g = tid; g < groups; g += kPlanThreads)
+    if (begin[g] < 0 || begin[g + 1] < begin[g] || begin[g + 1] > p.batch || (g == 0 && begin[g] != 0) || (g == groups - 1 && begin[g + 1] != p.batch)) bad = 1;
+  __syncthreads();
+  if (bad && tid == 0) pool_fault(p.pool.status, SJD_ERR_BAD_ARG);   // (every sequence for itself)
+  if (!bad) {
+    for (int b = tid; b < p.batch; b += kPlanThreads) {
+      int l = 0, h = groups - 1;   // last group that begins at b or before
+      while (l < h) {
+        const int mid = (l + h + 1) >> 1;
+        if (begin[mid] <= b) l = mid; else h = mid - 1;
       }
-      share[g] = live > 1 ? pages : 0;
-      leader[g] = lead;
+      group_of[b] = l;
+      if (hi[b] < 0) continue;
+      atomicMin(&share[l], (lo[b] + 1) / KV_PAGE);
+      atomicMin(&leader[l], b);
+      atomicAdd(&live[l], 1);
     }
+    __syncthreads();
+    for (int g = tid; g < groups; g += kPlanThreads)
+      if (live[g] < 2) share[g] = 0;
     __syncthreads();
     // pages that the tables of a group begin with: up to the first that differs or is absent
     for (int b = warp; b < p.batch; b += warps) {
-      const int g = p.group_of[b];
+      const int g = group_of[b];
       if (hi[b] < 0) continue;
-      const int sa = p.seqs ? p.seqs[leader[g]] : leader[g], sb = p.seqs ? p.seqs[b] : b;
-      const int *ta = p.pool.table + (long)sa * p.pool.pages_per_seq, *tb = p.pool.table + (long)sb * p.pool.pages_per_seq;
+      const int *ta = p.pool.table + (long)seq_of[leader[g]] * p.pool.pages_per_seq, *tb = p.pool.table + (long)seq_of[b] * p.pool.pages_per_seq;
       constexpr int U = 8;
       for (int at = 0; at < *(volatile int *)&share[g]; at += 32 * U) {
+        const int end = *(volatile int *)&share[g];
         int x[U], y[U], least = 0x7FFFFFFF;
 #pragma unroll
         for (int j = 0; j < U; ++j) {
           const int i = at + 32 * j + lane;
-          x[j] = i < share[g] ? ta[i] : -1;
-          y[j] = i < share[g] ? tb[i] : -1;
+          x[j] = y[j] = 0;
+          if (i < end) x[j] = ta[i], y[j] = tb[i];
         }
 #pragma unroll
         for (int j = U - 1; j >= 0; --j)
           if (x[j] != y[j] || x[j] < 0 || x[j] >= p.pool.n_pages) least = at + 32 * j + lane;
         least = __reduce_min_sync(0xffffffffu, least);
+        if (least == 0x7FFFFFFF) continue;
         if (lane == 0) atomicMin(&share[g], least);
-        if (least != 0x7FFFFFFF) break;
+        break;
       }
     }
     __syncthreads();
-    // entries of the groups' rows behind those of the sequences
-    if (warp == 0) {
-      int at = 0;
-      for (int g0 = 0; g0 < groups; g0 += 32) {
-        const int g = g0 + lane;
-        int n = 0;
-        if (g < groups) {
-          if (share[g] < kLeast) share[g] = 0;
-          if (share[g] > 0) n = (int)(((long)(begin_of(g + 1) - begin_of(g)) * p.rows + kTileRows - 1) / kTileRows);
+    for (int g = tid; g < groups; g += kPlanThreads)
+      if (share[g] < kLeast) share[g] = 0;
+    __syncthreads();
+  }
+  // ---- units: their segments, a warp each
+  const int all_rows = p.batch * p.rows;
+  for (int e = warp; e < p.n_entries; e += warps) {
+    const int r0 = e * kTileRows, rows = min(kTileRows, all_rows - r0), b0 = r0 / p.rows, b1 = (r0 + rows - 1) / p.rows;
+    const int g0 = bad ? 0 : group_of[b0], n_groups = bad ? 0 : group_of[b1] - g0 + 1, n = n_groups + b1 - b0 + 1;
+    int hi0 = -1;   // of the unit's rows of its first sequence, if that has more than a unit's
+    if (p.rows > kTileRows) {
+      for (int k = (r0 - b0 * p.rows) / p.group + lane; k <= min(p.rows - 1, r0 + rows - 1 - b0 * p.rows) / p.group; k += 32)
+        hi0 = max(hi0, row_position(p, b0, k, false));
+      hi0 = __reduce_max_sync(0xffffffffu, hi0);
+    }
+    Entry en;
+    en.rows = rows;
+    en.segs = b0 + 2 * e + (bad ? 0 : g0);   // (a unit's sequences and groups are those from its first on to the next unit's first, and one each beside)
+    int made = 0;
+#pragma unroll
+    for (int c = 0; c < 3; ++c) {   // for both streams, the first, the second
+      en.n_segs[c] = en.tiles[c] = 0;
+      if (one_stream(rows) && c != 1) continue;
+      for (int i0 = 0; i0 < n; i0 += 32) {
+        const int i = i0 + lane;
+        Segment s;
+        s.k0 = s.k1 = s.ra = s.rb = s.seq = 0;
+        if (i < n_groups) {
+          const int g = g0 + i;
+          if (live[g] > 0) s.seq = seq_of[leader[g]], s.k1 = share[g] * KV_PAGE;
+          s.ra = max(0, begin[g] * p.rows - r0), s.rb = min(rows, begin[g + 1] * p.rows - r0);
+        } else if (i < n) {
+          const int b = b0 + i - n_groups;
+          s.seq = seq_of[b], s.k0 = bad ? 0 : share[group_of[b]] * KV_PAGE, s.k1 = (b == b0 && p.rows > kTileRows ? hi0 : hi[b]) + 1;
+          if (hi[b] < 0) s.k0 = s.k1 = 0;
+          s.ra = max(0, b * p.rows - r0), s.rb = min(rows, (b + 1) * p.rows - r0);
         }
-        int x = n;
+        const int cls = one_stream(rows) || s.rb <= 128 ? 1 : s.ra >= 128 ? 2 : 0;
+        const int tiles = s.k1 > s.k0 && s.rb > s.ra && cls == c ? (s.k1 - s.k0 + kKeys - 1) / kKeys : 0;
+        int x = tiles;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
           const int y = __shfl_up_sync(0xffffffffu, x, o);
           if (lane >= o) x += y;
         }
-        if (g < groups) first[g] = at + x - n;
-        at += __shfl_sync(0xffffffffu, x, 31);
-      }
-      if (lane == 0) first[groups] = at;
-    }
-    __syncthreads();
-    for (int g = warp; g < groups; g += warps) {
-      const int b0 = begin_of(g), all = (begin_of(g + 1) - b0) * p.rows;
-      for (int i = lane; i < first[g + 1] - first[g]; i += 32) {
-        Entry n;
-        n.b0 = b0, n.r0 = i * kTileRows, n.rows = min(all - n.r0, kTileRows), n.seq = p.seqs ? p.seqs[leader[g]] : leader[g];
-        n.k0 = 0, n.k1 = share[g] * KV_PAGE, n.row_base = 0, n.prefix = 1;
-        p.entry[own + first[g] + i] = n;
+        const unsigned have = __ballot_sync(0xffffffffu, tiles > 0);
+        s.base = en.tiles[c] + x - tiles;
+        if (tiles > 0) p.segs[en.segs + made + __popc(have & ((1u << lane) - 1))] = s;
+        made += __popc(have);
+        en.n_segs[c] += __popc(have);
+        en.tiles[c] += __shfl_sync(0xffffffffu, x, 31);
       }
     }
-    for (int b = tid; b < p.batch; b += kPlanThreads) {
-      const int g = p.group_of[b];
-      p.prefix_of[b] = share[g] > 0 ? own + first[g] : -1;
-      p.group_of[b] = begin_of(g);   // (from here on: its first sequence)
-      lo[b] = share[g] * KV_PAGE;    // (and: its first own key)
+    if (lane == 0) {
+      p.entry[e] = en;
+      const int cost = 2 * en.tiles[0] + en.tiles[1] + en.tiles[2];
+      p.before[e + 1] = cost > 0 ? cost + kUnit : 0;   // (its own so far)
     }
   }
   __syncthreads();
-  // places on the line and rows of the parts, sums over the entries before
-  const int n = own + (bad ? 0 : first[groups]), run = (n + kPlanThreads - 1) / kPlanThreads, e0 = min(n, tid * run), e1 = min(n, e0 + run);
-  int cost = 0, rows = 0;
-  auto cost_of = [&](const Entry &en) { return en.seq < 0 || en.k1 <= en.k0 ? 0 : (en.k1 - en.k0 + kKeys - 1) / kKeys * weight_of(en.rows) + kUnit; };
-  for (int e = e0; e < e1; ++e) {
-    if (e < own && !bad) p.entry[e].k0 = lo[p.entry[e].b0];
-    const Entry en = p.entry[e];
-    const int c = cost_of(en);
-    cost += c;
-    rows += c > 0 ? padded(en.rows) : 0;
-  }
-  int x = cost, y = rows;
+  // places on the line, sums over the units before
+  const int run = (p.n_entries + kPlanThreads - 1) / kPlanThreads, e0 = min(p.n_entries, tid * run), e1 = min(p.n_entries, e0 + run);
+  int cost = 0;
+  for (int e = e0; e < e1; ++e) cost += p.before[e + 1];
+  int x = cost;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int a = __shfl_up_sync(0xffffffffu, x, o), c = __shfl_up_sync(0xffffffffu, y, o);
-    if (lane >= o) x += a, y += c;
+    const int y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
   }
-  if (lane == 31) sums[0][warp] = x, sums[1][warp] = y;
+  if (lane == 31) sums[warp] = x;
   __syncthreads();
-  for (int w = 0; w < warp; ++w) x += sums[0][w], y += sums[1][w];
-  int at = x - cost, row = y - rows;
-  for (int e = e0; e < e1; ++e) {
-    const Entry en = p.entry[e];
-    const int c = cost_of(en);
-    p.before[e] = at;
-    p.entry[e].row_base = row;
-    at += c;
-    row += c > 0 ? padded(en.rows) : 0;
-  }
-  if (tid == kPlanThreads - 1) {
-    p.before[n] = x;
-    p.plan->n_entries = n;
-    p.plan->all = x;
-    p.plan->rows = y;
-  }
+  for (int w = 0; w < warp; ++w) x += sums[w];
+  int at = x - cost;
+  for (int e = e0; e < e1; ++e) p.before[e + 1] = at += p.before[e + 1];
+  if (tid == 0) p.before[0] = 0;
 }
 
 // ---------------------------------------------------------------------------------------------------------------- units
 struct Unit {
-  int e, h, n, w;      // entry, kv head, tiles, places of a tile
-  long first;          // place of the first tile
+  int e, h;
+  long first;          // place of its first tile
 };
 // the unit that place t is in
 template <typename Before>
-__device__ __forceinline__ Unit unit_at(const SharedParams &p, const Before &before, int n_entries, long t) {
-  int lo = 0, hi = n_entries - 1;
+__device__ __forceinline__ Unit unit_at(const SharedParams &p, const Before &before, long t) {
+  int lo = 0, hi = p.n_entries - 1;
   const int heads = p.pool.n_kv_heads;
   while (lo < hi) {   // last entry that begins at t or before
     const int mid = (lo + hi + 1) >> 1;
     if ((long)before(mid) * heads <= t) lo = mid; else hi = mid - 1;
   }
+  const int b = before(lo), cost = before(lo + 1) - b;
   Unit u;
   u.e = lo;
-  const int b = before(lo), cost = before(lo + 1) - b;
-  const long in = t - (long)b * heads;
-  u.h = (int)(in / cost);
-  u.w = weight_of(p.entry[lo].rows);
-  u.n = (cost - kUnit) / u.w;
+  u.h = (int)((t - (long)b * heads) / cost);
   u.first = (long)b * heads + (long)u.h * cost + kUnit;
   return u;
 }
-// tiles of a unit that begin before place t
-__device__ __forceinline__ int tiles_before(const Unit &u, long t) {
-  const long n = t <= u.first ? 0 : (t - u.first + u.w - 1) / u.w;
-  return n < u.n ? (int)n : u.n;
+__device__ __forceinline__ int tiles_of(const Entry &en) { return en.tiles[0] + en.tiles[1] + en.tiles[2]; }
+// tiles of a unit that begin before place t: those for both streams take two places
+__device__ __forceinline__ int tiles_before(const Entry &en, long first, long t) {
+  const long in = t - first;
+  if (in <= 0) return 0;
+  if (in <= 2l * en.tiles[0]) return (int)((in + 1) >> 1);
+  const long n = in - en.tiles[0];
+  return n < tiles_of(en) ? (int)n : tiles_of(en);
 }
-__device__ __forceinline__ long range_of(const Plan &plan, int kv_heads, int ctas) {
-  const long all = (long)plan.all * kv_heads, least = 2 * kUnit;
-  const long chunk = (all + ctas - 1) / ctas;
+__device__ __forceinline__ long range_of(long all, int ctas) {
+  const long least = 2 * kUnit, chunk = (all + ctas - 1) / ctas;
   return chunk < least ? least : chunk;
 }
-// first row of a part: of the unit's first tiles, or of those that CTA c finds begun
-__device__ __forceinline__ long part_row(const SharedParams &p, const Plan &plan, const Entry &en, int h, bool begins, int c) {
-  return begins ? (long)en.row_base * p.pool.n_kv_heads + (long)h * padded(en.rows) : (long)plan.rows * p.pool.n_kv_heads + (long)c * kTileRows;
+// which streams tile i of a unit is for (0, 1, 2: both); `from`: the first tile of the CTA.  The tiles of the two streams take turns.
+__device__ __forceinline__ int stream_of(const Entry &en, int i, int from) {
+  if (one_stream(en.rows)) return (i - from) & 1;
+  const int j = i - en.tiles[0];
+  if (j < 0) return 2;
+  return j < 2 * min(en.tiles[1], en.tiles[2]) ? j & 1 : en.tiles[1] > en.tiles[2] ? 0 : 1;
+}
+// the last of tiles i0 .. i1 - 1 that a stream works on (-1: none)
+__device__ __forceinline__ int last_of(const Entry &en, int st, int i0, int i1) {
+  if (one_stream(en.rows)) {
+    const int i = i1 - 1 - ((i1 - 1 - i0 - st) & 1);
+    return i >= i0 ? i : -1;
+  }
+  const int n = en.tiles[0], turns = 2 * min(en.tiles[1], en.tiles[2]);
+  int j = i1 - 1 - n;
+  if (j >= turns) {
+    if ((en.tiles[1] > en.tiles[2] ? 0 : 1) == st) return i1 - 1;
+    j = turns - 1;
+  }
+  if (j >= 0 && (j & 1) != st) --j;
+  if (j >= 0 && n + j >= i0) return n + j;
+  const int both = min(n, i1) - 1;
+  return both >= i0 ? both : -1;
+}
+// first row of a part: of the unit's first tiles, or of those that CTA c goes on with
+__device__ __forceinline__ long part_row(const SharedParams &p, const Unit &u, bool begins, int c) {
+  return begins ? ((long)u.e * p.pool.n_kv_heads + u.h) * kTileRows : ((long)p.n_entries * p.pool.n_kv_heads + c) * kTileRows;
 }
 
 // ---------------------------------------------------------------------------------------------------------------- tiles
+// two fp32 operations an instruction
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\tfma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t *r) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, "
@@ -312,26 +353,27 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
   asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
-// Two e4m3 bytes, in the high bytes of the halves of t, as bf16: their bits moved into place are the numbers times 2^-120 (a
-// subnormal one stays one), and up (and more, where that is not 1) bring them up by 2^120 and the exponent.  Exact.
-__device__ __forceinline__ uint32_t bf16_of_e4m3(uint32_t t, uint32_t up, uint32_t more, bool twice) {
-  const uint32_t bits = (t & 0x80008000u) | (t >> 4 & 0x07F007F0u);
-  const uint32_t v = mul_bf16x2(bits, up);
-  return twice ? mul_bf16x2(v, more) : v;
-}
+// Two e4m3 bytes, in the high bytes of the halves of t, as bf16 times 2^-120: their bits moved into place (a subnormal number stays one).
+__device__ __forceinline__ uint32_t bf16_bits_of_e4m3(uint32_t t) { return (t & 0x80008000u) | (t >> 4 & 0x07F007F0u); }
 __device__ __forceinline__ uint32_t pair_of(float v) { return bf16_pair(v, v); }
+
+struct Info {          // of a tile
+  int key0, k1, ra, rb;
+  int there;           // bit j: page j of the tile is there
+};
 
 template <int HD>
 struct SharedSmem {
   uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_ready[2], o_full[2], q_ready;
   uint32_t tmem_base;
   int failed;
-  int there[kInfo];                            // bit j: page j of the tile is there
-  uint32_t nan_warps[kInfo][kConv / 32];       // some entry of V that a warp turned was NaN
-  uint16_t nan_dims[kInfo][kKeys][HD / 16];    // which, if so
+  Info info[kInfo];
+  uint32_t nan_warps[2][kConv / 32];           // some entry of V that a warp turned was NaN
+  alignas(16) uint16_t nan_dims[2][kKeys][HD / 16];    // which, if so
   float2 stat[2][128];                         // of both streams' rows
   uint32_t nan_row[2][128][HD / 32];
   int before[kBefore];
+  Segment segs[kMaxSegs];
 };
 
 template <int HD>
@@ -364,17 +406,15 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   pdl_wait();
-  const Plan plan = *p.plan;
-  const int n_entries = plan.n_entries;
-  const bool near = n_entries < kBefore;
+  const bool near = p.n_entries < kBefore;
   if (near)
-    for (int i = tid; i <= n_entries; i += kThreads) sh.before[i] = p.before[i];
+    for (int i = tid; i <= p.n_entries; i += kThreads) sh.before[i] = p.before[i];
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = sh.tmem_base;
   auto before = [&](int e) { return near ? sh.before[e] : p.before[e]; };
-  const long all = (long)plan.all * kv_heads, chunk = range_of(plan, kv_heads, gridDim.x);
+  const long all = (long)before(p.n_entries) * kv_heads, chunk = range_of(all, gridDim.x);
   const long t_begin = min(all, blockIdx.x * chunk), t_end = min(all, t_begin + chunk);
   auto fail = [&]() {
     if (lane == 0) {
@@ -390,14 +430,12 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
   };
   auto next_span = [&](long &t, Span &s) {
     while (t < t_end) {
-      s.u = unit_at(p, before, n_entries, t);
-      s.i0 = tiles_before(s.u, t_begin);
-      s.i1 = tiles_before(s.u, t_end);
-      t = s.u.first + (long)s.u.n * s.u.w;
-      if (s.i1 > s.i0) {
-        s.en = p.entry[s.u.e];
-        return true;
-      }
+      s.u = unit_at(p, before, t);
+      s.en = p.entry[s.u.e];
+      s.i0 = tiles_before(s.en, s.u.first, t_begin);
+      s.i1 = tiles_before(s.en, s.u.first, t_end);
+      t = s.u.first + tiles_of(s.en) + s.en.tiles[0];
+      if (s.i1 > s.i0) return true;
     }
     return false;
   };
@@ -406,124 +444,158 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
     // ------------------------------------------------------------------ keys and values: e4m3 to bf16
     constexpr int SEG = HD / 16, ROWS = kConv / SEG, N = kKeys / ROWS;   // lanes of a row, rows at a time, 16-byte loads of a thread
     const int ct = tid - kSoft, seg = ct % SEG, row0 = ct / SEG, cw = ct >> 5;
-    const uint32_t at0 = (uint32_t)(seg >> 2) * (128 * 128) + row0 * 128, unit0 = (seg & 3) * 2;   // (ROWS is a multiple of 8: the swizzle is the same)
+    // (ROWS is a multiple of 8: a thread's rows have one swizzle)
+    const uint32_t at0 = (uint32_t)(seg >> 2) * (128 * 128) + row0 * 128 + ((((seg & 3) * 2) ^ (row0 & 7)) << 4);
     const long plane = (long)KV_PAGE * HD, head_planes = 2l * kv_heads, page_planes = head_planes * p.pool.n_layers;
-    struct Raw {
-      uint4 k[N], v[N];
-      int k_exp[2], v_exp[2], there, left;   // left: keys of the tile
+    struct Tile {
+      Info info;
+      int h, page[2];
     };
+    auto sync = [&]() { asm volatile("bar.sync 2, %0;" ::"n"(kConv) : "memory"); };
     long t = t_begin;
     Span s;
-    bool more = next_span(t, s);
-    int i = more ? s.i0 : 0;
-    auto load = [&](Raw &r) {   // the next tile's bytes; false: none left
+    bool more = false;
+    int i = 0, at[3] = {0, 0, 0};   // next tile; segments of each kind that it and the tiles before it are in
+    auto begin_span = [&]() {
+      more = next_span(t, s);
+      if (!more) return;
+      sync();   // (nobody looks at the segments of the span before)
+      const int n = s.en.n_segs[0] + s.en.n_segs[1] + s.en.n_segs[2];
+      const int *from = reinterpret_cast<const int *>(p.segs + s.en.segs);
+      int *to = reinterpret_cast<int *>(sh.segs);
+      for (int j = ct; j < n * (int)(sizeof(Segment) / 4); j += kConv) to[j] = from[j];
+      sync();
+      i = s.i0;
+      at[0] = 0, at[1] = s.en.n_segs[0], at[2] = at[1] + s.en.n_segs[1];
+    };
+    auto look_up = [&](Tile &d) {   // what there is to know of the next tile; false: none left
       if (!more) return false;
-      const int key0 = s.en.k0 + i * kKeys;
-      r.left = s.en.k1 - key0;
-      r.there = 0;
-      int page[2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int at = key0 / KV_PAGE + j;
-        page[j] = j * KV_PAGE < r.left && at < p.pool.pages_per_seq ? p.pool.table[(long)s.en.seq * p.pool.pages_per_seq + at] : -1;
-        if (page[j] >= p.pool.n_pages) page[j] = -1;
-        if (page[j] >= 0) r.there |= 1 << j;
+      // its kind, and its number among that kind's
+      int c = one_stream(s.en.rows) ? 1 : stream_of(s.en, i, s.i0) == 2 ? 0 : stream_of(s.en, i, s.i0) + 1, j = i;
+      if (c > 0 && !one_stream(s.en.rows)) {
+        const int both = min(s.en.tiles[1], s.en.tiles[2]);
+        j = i - s.en.tiles[0];
+        j = j < 2 * both ? j >> 1 : j - both;
       }
+      int a = c == 0 ? at[0] : c == 1 ? at[1] : at[2];
+      const int end = (c == 0 ? 0 : c == 1 ? s.en.n_segs[0] : s.en.n_segs[0] + s.en.n_segs[1]) + (c == 0 ? s.en.n_segs[0] : c == 1 ? s.en.n_segs[1] : s.en.n_segs[2]);
+      while (a + 1 < end && sh.segs[a + 1].base <= j) ++a;
+      if (c == 0) at[0] = a;
+      if (c == 1) at[1] = a;
+      if (c == 2) at[2] = a;
+      const Segment g = sh.segs[a];
+      d.info.key0 = g.k0 + (j - g.base) * kKeys;
+      d.info.k1 = g.k1, d.info.ra = g.ra, d.info.rb = g.rb, d.info.there = 0;
+      d.h = s.u.h;
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        r.k_exp[j] = r.v_exp[j] = 0;
-        if (page[j] < 0) continue;
-        const long at = (long)page[j] * page_planes + head_planes * p.layer + s.u.h;
-        r.k_exp[j] = *reinterpret_cast<const int *>(p.pool.exps + at * kPoolBlocks);
-        r.v_exp[j] = *reinterpret_cast<const int *>(p.pool.exps + (at + kv_heads) * kPoolBlocks);
-        const uint8_t *base = (const uint8_t *)p.pool.pages + at * plane + seg * 16;
-#pragma unroll
-        for (int n = 0; n < N; ++n) {
-          const int row = row0 + n * ROWS;
-          if (row >> 6 != j) continue;
-          r.k[n] = *reinterpret_cast<const uint4 *>(base + (row & 63) * HD);
-          r.v[n] = *reinterpret_cast<const uint4 *>(base + (row & 63) * HD + plane * kv_heads);
-        }
+      for (int k = 0; k < 2; ++k) {
+        const int page = d.info.key0 / KV_PAGE + k;
+        d.page[k] = d.info.key0 + k * KV_PAGE < g.k1 ? p.pool.table[(long)g.seq * p.pool.pages_per_seq + page] : -1;
       }
-      if (++i == s.i1) {
-        more = next_span(t, s);
-        i = s.i0;
-      }
+      if (++i == s.i1) begin_span();
       return true;
     };
-    uint32_t made = 0;
-    bool ok = true;
-    // one operand of a tile; nan: told of NaN entries, which become zeros (null: they become NaN)
-    auto turn = [&](const Raw &r, const uint4 (&x)[N], const int (&exps)[2], uint8_t *to, uint32_t *dims) {
+    uint4 raw[2][N];         // a tile's keys and values of this thread
+    int exps[2][2];          // exponents of its pages' blocks
+    auto fetch = [&](const Tile &d, int which) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const bool there = (unsigned)d.page[k] < (unsigned)p.pool.n_pages;
+        const long at = (long)(there ? d.page[k] : 0) * page_planes + head_planes * p.layer + (which ? kv_heads : 0) + d.h;
+        exps[which][k] = 0;
+        if (there) exps[which][k] = *reinterpret_cast<const int *>(p.pool.exps + at * kPoolBlocks);
+        const uint8_t *base = (const uint8_t *)p.pool.pages + at * plane + seg * 16;
+#pragma unroll
+        for (int n = k * N / 2; n < (k + 1) * N / 2; ++n) {
+          const int row = row0 + n * ROWS;
+          raw[which][n] = make_uint4(0, 0, 0, 0);
+          if (there && d.info.key0 + row < d.info.k1) raw[which][n] = *reinterpret_cast<const uint4 *>(base + (row & 63) * HD);
+        }
+      }
+    };
+    // an operand of a tile; returns the loads that had NaN entries, which become NaN (of V: zeros, told in nan_dims)
+    auto turn = [&](int which, uint8_t *to, int stage) {
+      auto exp_of = [&](int n) {
+        const int row = row0 + n * ROWS;
+        return pool_exp((int8_t)(exps[which][n / (N / 2)] >> (8 * (row >> 4 & 3))));
+      };
+      bool large = false;   // an exponent above 0: in two steps
+#pragma unroll
+      for (int n = 0; n < N; ++n) large |= exp_of(n) > 0;
+      uint32_t nan = 0;
 #pragma unroll
       for (int n = 0; n < N; ++n) {
-        const int row = row0 + n * ROWS, j = row >> 6;
+        const uint32_t w[4] = {raw[which][n].x, raw[which][n].y, raw[which][n].z, raw[which][n].w};
+        const int e = exp_of(n);
+        // times 2^120, and the exponent: exact
+        const uint32_t up = pair_of(two_to(min(e, 0) + 120));
         uint32_t out[8];
-        if (row < r.left && (r.there >> j & 1)) {
-          const int e = pool_exp((int8_t)(exps[j] >> (8 * (row >> 4 & 3))));
-          const uint32_t up = pair_of(two_to(min(e, 0) + 120)), over = pair_of(two_to(max(e, 0)));
-          const uint32_t w[4] = {x[n].x, x[n].y, x[n].z, x[n].w};
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            out[2 * c] = bf16_of_e4m3(__byte_perm(w[c], 0, 0x1404), up, over, e > 0);
-            out[2 * c + 1] = bf16_of_e4m3(__byte_perm(w[c], 0, 0x3424), up, over, e > 0);
-          }
-          if (__builtin_expect(has_nan(w[0]) || has_nan(w[1]) || has_nan(w[2]) || has_nan(w[3]), 0)) {
-#pragma unroll
-            for (int c = 0; c < 16; ++c) {
-              if ((w[c >> 2] >> (8 * (c & 3)) & 0x7Fu) != 0x7Fu) continue;
-              const uint32_t half = 0xFFFFu << (16 * (c & 1));
-              out[c >> 1] = dims ? out[c >> 1] & ~half : out[c >> 1] | half;
-              if (dims) dims[n] |= 1u << c;
-            }
-          }
-        } else {
-#pragma unroll
-          for (int c = 0; c < 8; ++c) out[c] = 0;
+        for (int c = 0; c < 4; ++c) {
+          out[2 * c] = mul_bf16x2(bf16_bits_of_e4m3(__byte_perm(w[c], 0, 0x1404)), up);
+          out[2 * c + 1] = mul_bf16x2(bf16_bits_of_e4m3(__byte_perm(w[c], 0, 0x3424)), up);
         }
+        if (__builtin_expect(large, 0)) {
+          const uint32_t over = pair_of(two_to(max(e, 0)));
+#pragma unroll
+          for (int c = 0; c < 8; ++c) out[c] = mul_bf16x2(out[c], over);
+        }
+        uint32_t any = 0;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) any |= (w[c] & 0x7F7F7F7Fu) + 0x01010101u;
+        nan |= (any & 0x80808080u) != 0 ? 1u << n : 0u;
         uint8_t *dst = to + at0 + n * ROWS * 128;
-        *reinterpret_cast<uint4 *>(dst + ((unit0 ^ (row & 7)) << 4)) = make_uint4(out[0], out[1], out[2], out[3]);
-        *reinterpret_cast<uint4 *>(dst + (((unit0 + 1) ^ (row & 7)) << 4)) = make_uint4(out[4], out[5], out[6], out[7]);
+        *reinterpret_cast<uint4 *>(dst) = make_uint4(out[0], out[1], out[2], out[3]);
+        *reinterpret_cast<uint4 *>((uint8_t *)((uintptr_t)dst ^ 16)) = make_uint4(out[4], out[5], out[6], out[7]);
       }
+      const bool found = __any_sync(0xffffffffu, nan != 0);
+      if (__builtin_expect(found, 0)) {
+#pragma unroll 1
+        for (int n = 0; n < N; ++n) {
+          uint32_t dims = 0;
+          uint4 x = raw[which][0];
+#pragma unroll
+          for (int k = 1; k < N; ++k) x = k == n ? raw[which][k] : x;
+          uint16_t *dst = reinterpret_cast<uint16_t *>(to + at0 + n * ROWS * 128);
+#pragma unroll 1
+          for (int c = 0; c < 16; ++c) {
+            const uint32_t w = c < 4 ? x.x : c < 8 ? x.y : c < 12 ? x.z : x.w;
+            if ((w >> (8 * (c & 3)) & 0x7Fu) != 0x7Fu) continue;
+            dims |= 1u << c;
+            *reinterpret_cast<uint16_t *>((uintptr_t)(dst + (c & 7)) ^ (c < 8 ? 0 : 16)) = which ? 0 : 0x7FFF;
+          }
+          if (which) sh.nan_dims[stage][row0 + n * ROWS][seg] = (uint16_t)dims;
+        }
+      }
+      if (which && lane == 0) sh.nan_warps[stage][cw] = found;
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
     };
-    auto make = [&](const Raw &r) {
+    // One tile is turned while the next one's bytes, and the pages of the one after, are on their way.
+    Tile d0, d1, d2;
+    begin_span();
+    bool have0 = look_up(d0), have1 = have0 && look_up(d1), ok = true;
+    if (have0) fetch(d0, 0), fetch(d0, 1);
+    for (uint32_t made = 0; have0 && ok; ++made) {
       const int stage = made & 1, slot = made % kInfo;
       const uint32_t ph = (made >> 1 & 1) ^ 1u;
-      ok = ok && !*(volatile int *)&sh.failed && (made < 2 || warp_wait(&sh.k_empty[stage], ph));
-      if (!ok) return;
-      if (ct == 0) sh.there[slot] = r.there;
-      turn(r, r.k, r.k_exp, Ks + stage * OP, nullptr);
-      if (lane == 0) arrive(&sh.k_full[stage]);
-      ok = made < 2 || warp_wait(&sh.v_empty[stage], ph);
-      if (!ok) return;
-      uint32_t dims[N];
-#pragma unroll
-      for (int n = 0; n < N; ++n) dims[n] = 0;
-      turn(r, r.v, r.v_exp, Vs + stage * OP, dims);
-      uint32_t any = 0;
-#pragma unroll
-      for (int n = 0; n < N; ++n) any |= dims[n];
-      any = __any_sync(0xffffffffu, any != 0);
-      if (__builtin_expect(any, 0)) {
-#pragma unroll
-        for (int n = 0; n < N; ++n) sh.nan_dims[slot][row0 + n * ROWS][seg] = (uint16_t)dims[n];
+      const bool have2 = have1 && look_up(d2);
+      ok = !*(volatile int *)&sh.failed && (made < 2 || warp_wait(&sh.k_empty[stage], ph));
+      if (!ok) break;
+      if (ct == 0) {
+        d0.info.there = ((unsigned)d0.page[0] < (unsigned)p.pool.n_pages ? 1 : 0) | ((unsigned)d0.page[1] < (unsigned)p.pool.n_pages ? 2 : 0);
+        sh.info[slot] = d0.info;
       }
-      if (lane == 0) sh.nan_warps[slot][cw] = any;
-      __syncwarp();
+      turn(0, Ks + stage * OP, stage);
+      if (lane == 0) arrive(&sh.k_full[stage]);
+      if (have1) fetch(d1, 0);
+      ok = made < 2 || warp_wait(&sh.v_empty[stage], ph);
+      if (!ok) break;
+      turn(1, Vs + stage * OP, stage);
       if (lane == 0) arrive(&sh.v_full[stage]);
-      ++made;
-    };
-    // two tiles' bytes in registers: one is turned while the other is on its way
-    Raw a, b;
-    bool have_a = load(a), have_b = false;
-    while (have_a && ok) {
-      have_b = load(b);
-      make(a);
-      if (!have_b || !ok) break;
-      have_a = load(a);
-      make(b);
+      if (have1) fetch(d1, 1);
+      d0 = d1, d1 = d2;
+      have0 = have1, have1 = have2;
     }
     if (!ok) fail();
   } else if (warp == ISSUE) {
@@ -536,46 +608,62 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
     long t = t_begin;
     Span s;
     bool ok = true;
-    uint32_t q_ph = 0, p_ph[2] = {0, 0}, tile0 = 0;   // tile0: tiles of the units before
+    uint32_t q_ph = 0, p_ph0 = 0, p_ph1 = 0, tile0 = 0;   // tile0: tiles of the units before, less this one's first
     while (ok && next_span(t, s)) {
-      const int n = s.i1 - s.i0, both = s.u.w == 2, jobs = both ? 2 * n : n;
+      tile0 -= s.i0;
       ok = warp_wait(&sh.q_ready, q_ph);
       q_ph ^= 1u;
-      auto scores = [&](int j) {
-        const int st = j & 1, tile = both ? j >> 1 : j;
-        const uint32_t use = tile0 + tile, stage = use & 1;
-        ok = ok && !*(volatile int *)&sh.failed && warp_wait(&sh.k_full[stage], use >> 1 & 1);
-        if (!ok) return;
-        tc_fence_after();
-        if (elect_one()) {
-          const uint64_t a = desc | (uint64_t)((q_at + (both ? st * OP : 0)) >> 4), b = desc | (uint64_t)((k_at + stage * OP) >> 4);
-#pragma unroll
-          for (int k = 0; k < HD / 16; ++k) umma_bf16(tmem + st * 128, a + (k >> 2) * (128 * 128 >> 4) + (k & 3) * 2, b + (k >> 2) * (128 * 128 >> 4) + (k & 3) * 2, idesc_s, k > 0);
-          umma_commit(&sh.s_full[st]);
-          if (!both || st == 1) umma_commit(&sh.k_empty[stage]);
-        }
-        __syncwarp();
+      const bool alone = one_stream(s.en.rows);
+      // a product of a tile and a stream; those of tiles for both: the first stream's, then the second's
+      struct Job {
+        int i, st;
+        bool last;   // of its tile
       };
-      scores(0);
-      if (jobs > 1) scores(1);
-      for (int j = 0; j < jobs && ok; ++j) {
-        const int st = j & 1, tile = both ? j >> 1 : j;
-        const uint32_t use = tile0 + tile, stage = use & 1;
-        ok = !*(volatile int *)&sh.failed && warp_wait_both(&sh.p_ready[st], p_ph[st], &sh.v_full[stage], use >> 1 & 1);
-        p_ph[st] ^= 1u;
+      auto first_of = [&](int i) {
+        const int c = i < s.i1 ? stream_of(s.en, i, s.i0) : 0;
+        return Job{i, c == 1 ? 1 : 0, c != 2};
+      };
+      auto next_of = [&](const Job &j) { return j.last ? first_of(j.i + 1) : Job{j.i, 1, true}; };
+      const int end0 = last_of(s.en, 0, s.i0, s.i1), end1 = last_of(s.en, 1, s.i0, s.i1);
+      bool open0 = false, open1 = false, begun0 = false, begun1 = false;   // scores whose weights have not been multiplied; O has been written
+      Job js = first_of(s.i0), jv = js;
+      while (jv.i < s.i1 && ok) {
+        while (js.i < s.i1 && !(js.st ? open1 : open0)) {
+          const uint32_t use = tile0 + js.i, stage = use & 1;
+          ok = !*(volatile int *)&sh.failed && warp_wait(&sh.k_full[stage], use >> 1 & 1);
+          if (!ok) break;
+          tc_fence_after();
+          if (elect_one()) {
+            const uint64_t a = desc | (uint64_t)((q_at + (alone ? 0 : js.st * OP)) >> 4), b = desc | (uint64_t)((k_at + stage * OP) >> 4);
+#pragma unroll
+            for (int k = 0; k < HD / 16; ++k) umma_bf16(tmem + js.st * 128, a + (k >> 2) * (128 * 128 >> 4) + (k & 3) * 2, b + (k >> 2) * (128 * 128 >> 4) + (k & 3) * 2, idesc_s, k > 0);
+            umma_commit(&sh.s_full[js.st]);
+            if (js.last) umma_commit(&sh.k_empty[stage]);
+          }
+          __syncwarp();
+          (js.st ? open1 : open0) = true;
+          js = next_of(js);
+        }
+        if (!ok) break;
+        const uint32_t use = tile0 + jv.i, stage = use & 1;
+        ok = !*(volatile int *)&sh.failed && warp_wait_both(&sh.p_ready[jv.st], jv.st ? p_ph1 : p_ph0, &sh.v_full[stage], use >> 1 & 1);
+        (jv.st ? p_ph1 : p_ph0) ^= 1u;
         if (!ok) break;
         tc_fence_after();
         if (elect_one()) {
           const uint64_t b = desc_v | (uint64_t)((v_at + stage * OP) >> 4);
+          const bool more = jv.st ? begun1 : begun0;
 #pragma unroll
-          for (int k = 0; k < kKeys / 16; ++k) umma_bf16_ts(tmem + 256 + st * 128, tmem + st * 128 + k * 8, b + k * (16 * 128 >> 4), idesc_o, j >= 2 || k > 0);
-          if (!both || st == 1) umma_commit(&sh.v_empty[stage]);
-          if (j + 2 >= jobs) umma_commit(&sh.o_full[st]);
+          for (int k = 0; k < kKeys / 16; ++k) umma_bf16_ts(tmem + 256 + jv.st * 128, tmem + jv.st * 128 + k * 8, b + k * (16 * 128 >> 4), idesc_o, more || k > 0);
+          if (jv.last) umma_commit(&sh.v_empty[stage]);
+          if (jv.i == (jv.st ? end1 : end0)) umma_commit(&sh.o_full[jv.st]);
         }
         __syncwarp();
-        if (j + 2 < jobs) scores(j + 2);
+        (jv.st ? open1 : open0) = false;
+        (jv.st ? begun1 : begun0) = true;
+        jv = next_of(jv);
       }
-      tile0 += n;
+      tile0 += s.i1;
     }
     if (!ok) fail();
   } else {
@@ -588,164 +676,185 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
     bool ok = true;
     uint32_t s_ph = 0, o_ph = 0, tile0 = 0;
     while (next_span(t, s)) {
-      const int n = s.i1 - s.i0, both = s.u.w == 2, mine = both ? n : (n + 1 - st) / 2, rows = s.en.rows;
+      tile0 -= s.i0;
+      const int rows = s.en.rows, row_first = s.u.e * kTileRows;
+      const bool alone = one_stream(rows);
+      const int r = r_in + (alone ? 0 : st * 128);
+      int pos = -1;   // of this thread's row
       // ---- queries of the unit's rows
       {
         const int per_lane = p.by_eight ? 8 : 4, row_lanes = HD / per_lane, each = 32 / row_lanes;   // rows of a warp's load
         const int sub = lane / row_lanes, dim = lane % row_lanes * per_lane;
-        const int count = both ? 256 : 128;
-        auto source = [&](int r) {
-          const int x = s.en.r0 + r, m = x / p.group;
-          return p.q + ((long)s.en.b0 * p.window + m) * p.q_stride + ((long)s.u.h * p.group + (x - m * p.group)) * HD + dim;
+        auto source = [&](int x) {
+          const int m = x / p.group;
+          return p.q + (long)m * p.q_stride + ((long)s.u.h * p.group + (x - m * p.group)) * HD + dim;
         };
-        auto place = [&](int r) {
-          return Qs + (r >> 7) * OP + (dim >> 6) * (128 * 128) + (r & 127) * 128 + ((((dim & 63) >> 3) ^ (r & 7)) << 4) + (dim & 7) * 2;
+        auto place = [&](int x) {
+          return Qs + (x >> 7) * OP + (dim >> 6) * (128 * 128) + (x & 127) * 128 + ((((dim & 63) >> 3) ^ (x & 7)) << 4) + (dim & 7) * 2;
         };
         constexpr int U = 8;
-        for (int r0 = warp * each; r0 < min(count, rows); r0 += kSoft / 32 * each * U) {
+        for (int r0 = warp * each; r0 < rows; r0 += kSoft / 32 * each * U) {
           uint4 v[U];
 #pragma unroll
           for (int j = 0; j < U; ++j) {
-            const int r = r0 + j * (kSoft / 32) * each + sub;
+            const int x = r0 + j * (kSoft / 32) * each + sub;
             v[j] = make_uint4(0, 0, 0, 0);
-            if (r >= rows) continue;
+            if (x >= rows) continue;
             if (p.by_eight) {
-              v[j] = *reinterpret_cast<const uint4 *>(source(r));
+              v[j] = *reinterpret_cast<const uint4 *>(source(row_first + x));
             } else {
-              const uint2 x = *reinterpret_cast<const uint2 *>(source(r));
-              v[j].x = x.x, v[j].y = x.y;
+              const uint2 y = *reinterpret_cast<const uint2 *>(source(row_first + x));
+              v[j].x = y.x, v[j].y = y.y;
             }
           }
 #pragma unroll
           for (int j = 0; j < U; ++j) {
-            const int r = r0 + j * (kSoft / 32) * each + sub;
-            if (r >= rows) continue;
-            if (p.by_eight) *reinterpret_cast<uint4 *>(place(r)) = v[j];
-            else *reinterpret_cast<uint2 *>(place(r)) = make_uint2(v[j].x, v[j].y);
+            const int x = r0 + j * (kSoft / 32) * each + sub;
+            if (x >= rows) continue;
+            if (p.by_eight) *reinterpret_cast<uint4 *>(place(x)) = v[j];
+            else *reinterpret_cast<uint2 *>(place(x)) = make_uint2(v[j].x, v[j].y);
           }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) arrive(&sh.q_ready);
+        if (r < rows) {
+          const int m = (row_first + r) / p.group, b = m / p.window;
+          pos = row_position(p, b, m - b * p.window, false);
+        }
       }
-      const int r = r_in + (both ? st * 128 : 0);
-      const bool warp_live = quarter * 32 + (both ? st * 128 : 0) < rows;
-      int limit = 0x3FFFFFFF;   // the last key that this thread's row sees (no row: any)
-      if (r < rows) {
-        const int m = (s.en.r0 + r) / p.group, b = s.en.b0 + m / p.window;
-        const int at = row_position(p, b, m % p.window, false);
-        limit = at < 0 ? -1 : s.en.prefix ? s.en.k1 - 1 : min(at, s.en.k1 - 1);
-      }
-      const int least = __reduce_min_sync(0xffffffffu, limit);
+      const bool warp_rows = quarter * 32 + (alone ? 0 : st * 128) < rows;   // this warp has any
       float m_ref = -INFINITY, l = 0.0f;
       uint32_t nan[HD / 32];
 #pragma unroll
       for (int j = 0; j < HD / 32; ++j) nan[j] = 0;
-      auto note_nans = [&](int tile) {   // entries of V that are NaN, of a tile whose second product is done
-        const uint32_t slot = (tile0 + tile) % kInfo;
-        uint32_t any = 0;
-#pragma unroll
-        for (int w = 0; w < kConv / 32; ++w) any |= sh.nan_warps[slot][w];
-        if (__builtin_expect(any, 0)) {
-          constexpr int ROWS = kConv / (HD / 16), WARP = 32 / (HD / 16);
-          const int key0 = s.en.k0 + (s.i0 + tile) * kKeys;
-#pragma unroll 1
-          for (int k = 0; k < kKeys; ++k) {
-            if (!sh.nan_warps[slot][k % ROWS / WARP] || key0 + k > limit) continue;
-#pragma unroll
-            for (int j = 0; j < HD / 32; ++j) nan[j] |= *reinterpret_cast<const uint32_t *>(&sh.nan_dims[slot][k][2 * j]);
-          }
-        }
-      };
-      for (int j = 0; j < mine; ++j) {
-        const int tile = both ? j : 2 * j + st, key0 = s.en.k0 + (s.i0 + tile) * kKeys;
+      int mine = 0;
+      for (int i = s.i0; i < s.i1; ++i) {
+        const int c = stream_of(s.en, i, s.i0);
+        if (c != 2 && c != st) continue;
+        ++mine;
+        const uint32_t use = tile0 + i, stage = use & 1;
         ok = ok && !*(volatile int *)&sh.failed;
         if (ok && !warp_wait(&sh.s_full[st], s_ph)) {
           ok = false;
           fail();
         }
         s_ph ^= 1u;
-        if (!warp_live) {   // (what its rows of P hold does not matter)
+        tc_fence_after();
+        const Info f = sh.info[use % kInfo];
+        const int limit = r >= f.ra && r < f.rb ? min(pos, f.k1 - 1) : -1;   // the last key that this row sees
+        if (!__any_sync(0xffffffffu, limit >= f.key0)) {   // (a warp without rows of the segment: no weights)
+          if (warp_rows) {
+            uint32_t w[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) w[k] = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) tmem_st16(t_s + k * 16, w);
+            tmem_st_wait();
+            tc_fence_before();
+          }
           __syncwarp();
           if (lane == 0) arrive(&sh.p_ready[st]);
           continue;
         }
-        tc_fence_after();
-        if (j > 0) note_nans(both ? tile - 1 : tile - 2);
-        const int there = sh.there[(tile0 + tile) % kInfo];
-        const bool whole = key0 + kKeys - 1 <= least && there == 3;
+        const bool whole = __all_sync(0xffffffffu, limit >= f.key0 + kKeys - 1) && f.there == 3;
         // which of 32 keys this row sees
-        auto seen = [&](int c) {
-          const int n_seen = limit - (key0 + c * 32) + 1;
+        auto seen = [&](int k) {
+          const int n_seen = limit - (f.key0 + k * 32) + 1;
           const uint32_t bits = n_seen >= 32 ? 0xFFFFFFFFu : n_seen <= 0 ? 0u : (1u << n_seen) - 1;
-          return there >> (c >> 1) & 1 ? bits : 0u;
+          return f.there >> (k >> 1) & 1 ? bits : 0u;
         };
         float top = -INFINITY;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          uint32_t v[32];
-          tmem_ld32(t_s + c * 32, v);
+        for (int k = 0; k < 4; k += 2) {
+          uint32_t v[64];
+          tmem_ld32(t_s + k * 32, v);
+          tmem_ld32(t_s + k * 32 + 32, v + 32);
           tmem_ld_wait();
           if (!whole) {
-            const uint32_t bits = seen(c);
+            const uint32_t bits = seen(k), more = seen(k + 1);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = bits >> i & 1u ? v[i] : 0xFF800000u;
+            for (int j = 0; j < 32; ++j) {
+              v[j] = bits >> j & 1u ? v[j] : 0xFF800000u;
+              v[32 + j] = more >> j & 1u ? v[32 + j] : 0xFF800000u;
+            }
           }
           float a[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-          for (int i = 0; i < 32; ++i) a[i & 3] = fmaxf(a[i & 3], __uint_as_float(v[i]));
+          for (int j = 0; j < 64; j += 2) a[j >> 1 & 3] = fmaxf(fmaxf(a[j >> 1 & 3], __uint_as_float(v[j])), __uint_as_float(v[j + 1]));
           top = fmaxf(top, fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])));
         }
-        if (!whole && there != 3 && r < rows) {   // (no page where the row sees a key)
-          const int miss = there & 1 ? key0 + KV_PAGE : key0;
+        if (!whole && f.there != 3) {   // (no page where the row sees a key)
+          const int miss = f.there & 1 ? f.key0 + KV_PAGE : f.key0;
           if (limit >= miss) pool_fault(p.pool.status, SJD_ERR_BAD_ARG);
         }
         top *= p.scale;
-        if (j == 0) {
-          m_ref = top;
-        } else if (__any_sync(0xffffffffu, top > m_ref + kGrow)) {
-          const float now = fmaxf(m_ref, top), f = now == -INFINITY ? 1.0f : exp2_fast(m_ref - now);
+        if (m_ref == -INFINITY) m_ref = top;   // (nothing so far: O is zero, or has not been written)
+        if (__any_sync(0xffffffffu, top > m_ref + kGrow)) {
+          const float now = fmaxf(m_ref, top), g = now == -INFINITY ? 1.0f : exp2_fast(m_ref - now);
           m_ref = now;
-          l *= f;
+          l *= g;
 #pragma unroll 1
-          for (int c = 0; c < HD / 32; ++c) {
+          for (int k = 0; k < HD / 32; ++k) {
             uint32_t v[32];
-            tmem_ld32(t_o + st * 128 + c * 32, v);
+            tmem_ld32(t_o + st * 128 + k * 32, v);
             tmem_ld_wait();
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
-            tmem_st16(t_o + st * 128 + c * 32, v);
-            tmem_st16(t_o + st * 128 + c * 32 + 16, v + 16);
+            for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * g);
+            tmem_st16(t_o + st * 128 + k * 32, v);
+            tmem_st16(t_o + st * 128 + k * 32 + 16, v + 16);
           }
           tmem_st_wait();
         }
         const float ref = m_ref == -INFINITY ? 0.0f : m_ref;
-        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        const float2 scale2 = make_float2(p.scale, p.scale), ref2 = make_float2(-ref, -ref);
+        float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+        uint32_t v[2][32];
+        tmem_ld32(t_s, v[0]);
+        tmem_ld_wait();
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          uint32_t v[32], w[16];
-          tmem_ld32(t_s + c * 32, v);
-          tmem_ld_wait();
+        for (int k = 0; k < 4; ++k) {
+          if (k < 3) tmem_ld32(t_s + k * 32 + 32, v[(k + 1) & 1]);   // (under way while this one is worked on)
+          uint32_t *x = v[k & 1], w[16];
           if (!whole) {
-            const uint32_t bits = seen(c);
+            const uint32_t bits = seen(k);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = bits >> i & 1u ? v[i] : 0xFF800000u;
+            for (int j = 0; j < 32; ++j) x[j] = bits >> j & 1u ? x[j] : 0xFF800000u;
           }
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const float x = exp2_fast(fmaf(__uint_as_float(v[2 * i]), p.scale, -ref)), y = exp2_fast(fmaf(__uint_as_float(v[2 * i + 1]), p.scale, -ref));
-            sum[i & 3] += x + y;
-            w[i] = bf16_pair(x, y);
+          for (int j = 0; j < 16; ++j) {
+            float2 y = fma2(make_float2(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1])), scale2, ref2);
+            y.x = exp2_fast(y.x), y.y = exp2_fast(y.y);
+            sum[j & 1] = add2(sum[j & 1], y);
+            w[j] = bf16_pair(y.x, y.y);
           }
-          tmem_st16(t_s + c * 16, w);   // (over scores that have been read)
+          if (k < 3) tmem_ld_wait();
+          tmem_st16(t_s + k * 16, w);   // (over scores that have been read)
         }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
         tmem_st_wait();
         tc_fence_before();
+        // NaN entries of V, which are zeros there, and the rows that see them
+        if (ok && !warp_wait(&sh.v_full[stage], use >> 1 & 1)) {
+          ok = false;
+          fail();
+        }
+        uint32_t any = 0;
+#pragma unroll
+        for (int w = 0; w < kConv / 32; ++w) any |= sh.nan_warps[stage][w];
+        if (__builtin_expect(any, 0)) {
+          constexpr int ROWS = kConv / (HD / 16), WARP = 32 / (HD / 16);
+#pragma unroll 1
+          for (int k = 0; k < kKeys; ++k) {
+            if (!sh.nan_warps[stage][k % ROWS / WARP] || f.key0 + k > limit) continue;
+#pragma unroll
+            for (int j = 0; j < HD / 32; ++j) nan[j] |= *reinterpret_cast<const uint32_t *>(&sh.nan_dims[stage][k][2 * j]);
+          }
+        }
         __syncwarp();
         if (lane == 0) arrive(&sh.p_ready[st]);
       }
-      // ---- this unit's part: references, sums and O
+      // ---- what this CTA has of the unit: references, sums and O
       if (mine > 0) {
         if (ok && !warp_wait(&sh.o_full[st], o_ph)) {
           ok = false;
@@ -753,68 +862,73 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
         }
         o_ph ^= 1u;
         tc_fence_after();
-        if (warp_live) note_nans(both ? mine - 1 : 2 * (mine - 1) + st);
       }
-      const long row = part_row(p, plan, s.en, s.u.h, s.i0 == 0, blockIdx.x);
+      const bool complete = s.i0 == 0 && s.i1 == tiles_of(s.en);
+      const long row = part_row(p, s.u, s.i0 == 0, blockIdx.x);
       const int stride = padded(rows);
       float4 *parts = reinterpret_cast<float4 *>(p.parts + row * HD) + r;   // [HD / 4][padded rows]
-      if (both) {
-        if (warp_live) {
-#pragma unroll 1
-          for (int c = 0; c < HD / 32; ++c) {
-            uint32_t v[32];
-            tmem_ld32(t_o + st * 128 + c * 32, v);
-            tmem_ld_wait();
-            uint32_t bad = nan[0];
+      __nv_bfloat16 *out = p.out;
+      if (r < rows) {
+        const int m = (row_first + r) / p.group;
+        out += (long)m * p.out_stride + ((long)s.u.h * p.group + (row_first + r - m * p.group)) * HD;
+      }
+      // 32 dims of this row, times f (the whole unit: outputs)
+      auto store = [&](int k, const float *v, float f) {
+        if (r >= rows) return;
+        if (complete) {
 #pragma unroll
-            for (int j = 1; j < HD / 32; ++j) bad = c == j ? nan[j] : bad;
-            if (__builtin_expect(bad != 0, 0)) {
+          for (int j = 0; j < 8; ++j)
+            *reinterpret_cast<uint2 *>(out + k * 32 + j * 4) = f == 0.0f ? make_uint2(0u, 0u) : make_uint2(bf16_pair(v[4 * j] * f, v[4 * j + 1] * f), bf16_pair(v[4 * j + 2] * f, v[4 * j + 3] * f));
+        } else {
 #pragma unroll
-              for (int i = 0; i < 32; ++i) v[i] = bad >> i & 1u ? 0x7FFFFFFFu : v[i];
-            }
-            if (r < rows) {
-#pragma unroll
-              for (int i = 0; i < 8; ++i)
-                parts[(c * 8 + i) * stride] = make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]), __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]));
-            }
-          }
-          if (r < rows) p.stats[row + r] = make_float2(m_ref, l);
+          for (int j = 0; j < 8; ++j) parts[(k * 8 + j) * stride] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
         }
-      } else {
-        // both streams have sums of the same rows: each joins half of the dims
-        sh.stat[st][r_in] = make_float2(m_ref, l);
+      };
+      float2 a = make_float2(m_ref, l), b = make_float2(-INFINITY, 0.0f);
+      bool second = false;
+      if (alone) {   // both streams have sums of the same rows: each joins half of the dims
+        sh.stat[st][r_in] = a;
 #pragma unroll
         for (int j = 0; j < HD / 32; ++j) sh.nan_row[st][r_in][j] = nan[j];
         sync();
-        if (warp_live) {
-          const float2 a = sh.stat[0][r_in], b = n > 1 ? sh.stat[1][r_in] : make_float2(-INFINITY, 0.0f);
-          const float best = fmaxf(a.x, b.x), f0 = a.x == -INFINITY ? 0.0f : exp2_fast(a.x - best), f1 = b.x == -INFINITY ? 0.0f : exp2_fast(b.x - best);
+        second = s.i1 - s.i0 > 1;
+        a = sh.stat[0][r_in];
+        if (second) b = sh.stat[1][r_in];
+#pragma unroll
+        for (int j = 0; j < HD / 32; ++j) nan[j] = sh.nan_row[0][r_in][j] | (second ? sh.nan_row[1][r_in][j] : 0u);
+      }
+      if (warp_rows) {
+        const float best = fmaxf(a.x, b.x), f0 = a.x == -INFINITY ? (a.y == 0.0f ? 0.0f : 1.0f) : exp2_fast(a.x - best);   // (scores that are all NaN leave no maximum)
+        const float f1 = b.x == -INFINITY ? (b.y == 0.0f ? 0.0f : 1.0f) : exp2_fast(b.x - best), sum = a.y * f0 + b.y * f1, inv = sum != 0.0f ? 1.0f / sum : 0.0f;
+        if (r < rows && !complete && (!alone || st == 0)) p.stats[row + r] = make_float2(best, sum);
+        const int k0 = alone ? st * (HD / 64) : 0, k1 = alone ? k0 + HD / 64 : HD / 32, o0 = alone ? 0 : st * 128;
 #pragma unroll 1
-          for (int c = st * (HD / 64); c < (st + 1) * (HD / 64); ++c) {
-            uint32_t v[32], w[32];
-            tmem_ld32(t_o + c * 32, v);
-            if (n > 1) tmem_ld32(t_o + 128 + c * 32, w);
+        for (int k = k0; k < k1; ++k) {
+          float v[32];
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] = 0.0f;
+          if (mine > 0 || alone) {
+            uint32_t x[32], y[32];
+            tmem_ld32(t_o + o0 + k * 32, x);
+            if (second) tmem_ld32(t_o + 128 + k * 32, y);
             tmem_ld_wait();
-            const uint32_t bad = sh.nan_row[0][r_in][c] | (n > 1 ? sh.nan_row[1][r_in][c] : 0u);
+            uint32_t bad = nan[0];
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-              float x = __uint_as_float(v[i]) * f0;
-              if (n > 1) x = fmaf(__uint_as_float(w[i]), f1, x);
-              v[i] = bad >> i & 1u ? 0x7FFFFFFFu : __float_as_uint(x);
-            }
-            if (r < rows) {
+            for (int j = 1; j < HD / 32; ++j) bad = k == j ? nan[j] : bad;
 #pragma unroll
-              for (int i = 0; i < 8; ++i)
-                parts[(c * 8 + i) * stride] = make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]), __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]));
+            for (int j = 0; j < 32; ++j) {
+              v[j] = __uint_as_float(x[j]) * f0;
+              if (second) v[j] = fmaf(__uint_as_float(y[j]), f1, v[j]);
+              if (bad >> j & 1u) v[j] = __int_as_float(0x7FFFFFFF);
             }
           }
-          if (st == 0 && r < rows) p.stats[row + r] = make_float2(best, a.y * f0 + b.y * f1);
+          store(k, v, inv);
         }
       }
       tc_fence_before();
       sync();   // (queries, statistics and sums may be written again)
       tc_fence_after();
-      tile0 += n;
+      tile0 += s.i1;
     }
   }
   tc_fence_before();
@@ -826,43 +940,41 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
 }
 
 // ---------------------------------------------------------------------------------------------------------------- joining
-// Eight rows of a sequence and kv head a warp: lane = row + 8 * (dims / 4 % 4).  Parts in the order of their keys.
+// Eight rows of a unit that is cut a warp: lane = row + 8 * (dims / 4 % 4).  Parts in the order of their keys.
 constexpr int kJoinWarps = 4;
 template <int HD>
 __global__ void __launch_bounds__(kJoinWarps * 32) shared_join_kernel(const __grid_constant__ SharedParams p) {
   constexpr int D = HD / 16;
   pdl_wait();
   pdl_trigger();
-  const Plan plan = *p.plan;
-  const int lane = threadIdx.x & 31, kv_heads = p.pool.n_kv_heads, eights = (p.rows + 7) / 8;
+  const int lane = threadIdx.x & 31, kv_heads = p.pool.n_kv_heads, all_rows = p.batch * p.rows, eights = (all_rows + 7) / 8;
   const long job = (long)blockIdx.x * kJoinWarps + (threadIdx.x >> 5);
-  if (job >= (long)p.batch * eights * kv_heads) return;
-  const int h = (int)(job % kv_heads), b = (int)(job / kv_heads / eights), r = (int)(job / kv_heads % eights) * 8 + (lane & 7), d0 = lane >> 3;
-  if (r >= p.rows) return;
-  const int k = r / p.group;
-  const bool live = row_position(p, b, k, false) >= 0;
-  const long chunk = range_of(plan, kv_heads, p.ctas);
+  if (job >= (long)eights * kv_heads) return;
+  const int h = (int)(job / eights), r = (int)(job - (long)h * eights) * 8 + (lane & 7), d0 = lane >> 3;
+  const int e = r / kTileRows, in = r % kTileRows;   // (the eight rows are of one unit)
+  if (r >= all_rows) return;
+  const int b0 = p.before[e], cost = p.before[e + 1] - b0;
+  const long chunk = range_of((long)p.before[p.n_entries] * kv_heads, p.ctas);
   float4 acc[D];
 #pragma unroll
   for (int i = 0; i < D; ++i) acc[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   float ref = -INFINITY, sum = 0.0f;
-  auto add_unit = [&](int e, int in) {   // the parts of row `in` of an entry's rows
-    const int cost = p.before[e + 1] - p.before[e];
-    if (cost == 0) return;
+  if (cost > 0) {
     const Entry en = p.entry[e];
     Unit u;
-    u.e = e, u.h = h, u.w = weight_of(en.rows), u.n = (cost - kUnit) / u.w, u.first = (long)p.before[e] * kv_heads + (long)h * cost + kUnit;
-    const int c1 = (int)((u.first + (long)(u.n - 1) * u.w) / chunk);
-    for (int c = (int)(u.first / chunk); c <= c1; ++c) {
-      const int i0 = tiles_before(u, c * chunk), i1 = tiles_before(u, (c + 1) * chunk);
+    u.e = e, u.h = h, u.first = (long)b0 * kv_heads + (long)h * cost + kUnit;
+    const int n = tiles_of(en), c0 = (int)(u.first / chunk), c1 = (int)((u.first + cost - kUnit - 1) / chunk);
+    for (int c = c0; c <= c1; ++c) {
+      const int i0 = tiles_before(en, u.first, c * chunk), i1 = tiles_before(en, u.first, (c + 1) * chunk);
       if (i0 == i1) continue;
-      const long row = part_row(p, plan, en, h, i0 == 0, c);
+      if (i0 == 0 && i1 == n) return;   // (written by its CTA)
+      const long row = part_row(p, u, i0 == 0, c);
       const float2 s = p.stats[row + in];
       const float4 *from = reinterpret_cast<const float4 *>(p.parts + row * HD) + in;
       float4 x[D];
 #pragma unroll
       for (int i = 0; i < D; ++i) x[i] = from[(d0 + 4 * i) * padded(en.rows)];
-      const float now = fmaxf(ref, s.x), f = ref == -INFINITY ? 0.0f : exp2_fast(ref - now), g = s.x == -INFINITY ? 0.0f : exp2_fast(s.x - now);
+      const float now = fmaxf(ref, s.x), f = ref == -INFINITY ? (sum == 0.0f ? 0.0f : 1.0f) : exp2_fast(ref - now), g = s.x == -INFINITY ? (s.y == 0.0f ? 0.0f : 1.0f) : exp2_fast(s.x - now);
       ref = now;
       sum = sum * f + s.y * g;
 #pragma unroll
@@ -871,17 +983,10 @@ __global__ void __launch_bounds__(kJoinWarps * 32) shared_join_kernel(const __gr
         acc[i].z = fmaf(x[i].z, g, acc[i].z * f), acc[i].w = fmaf(x[i].w, g, acc[i].w * f);
       }
     }
-  };
-  if (live) {
-    const int e = p.prefix_of[b];
-    if (e >= 0) {
-      const int in = (b - p.group_of[b]) * p.rows + r;
-      add_unit(e + in / kTileRows, in % kTileRows);
-    }
-    add_unit(b * p.row_tiles + r / kTileRows, r % kTileRows);
   }
-  const float inv = live && sum != 0.0f ? 1.0f / sum : 0.0f;
-  __nv_bfloat16 *out = p.out + ((long)b * p.window + k) * p.out_stride + ((long)h * p.group + r - k * p.group) * HD;
+  const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
+  const int m = r / p.group;
+  __nv_bfloat16 *out = p.out + (long)m * p.out_stride + ((long)h * p.group + r - m * p.group) * HD;
 #pragma unroll
   for (int i = 0; i < D; ++i) {
     const uint2 v = inv == 0.0f ? make_uint2(0u, 0u) : make_uint2(bf16_pair(acc[i].x * inv, acc[i].y * inv), bf16_pair(acc[i].z * inv, acc[i].w * inv));
@@ -891,20 +996,18 @@ __global__ void __launch_bounds__(kJoinWarps * 32) shared_join_kernel(const __gr
 
 // ---------------------------------------------------------------------------------------------------------------- host
 struct SharedLayout {
-  int64_t entries, rows;          // most entries; most rows of parts
-  size_t before, entry, group_of, prefix_of, stats, parts, bytes;
+  int64_t entries, rows;          // units of a kv head; rows of parts
+  size_t entry, segs, stats, parts, bytes;
 };
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 SharedLayout layout_of(const sjd_pool &pool, int64_t batch, int64_t window, int64_t n_heads) {
   SharedLayout l;
-  const int64_t rows = window * (n_heads / pool.n_kv_heads), own = batch * ((rows + kTileRows - 1) / kTileRows);
-  l.entries = own + (batch * rows + kTileRows - 1) / kTileRows + batch;
-  l.rows = pool.n_kv_heads * (2 * batch * rows + 8 * l.entries) + (int64_t)kMaxCtas * kTileRows;
-  l.before = 256;
-  l.entry = l.before + up256((l.entries + 1) * sizeof(int));
-  l.group_of = l.entry + up256(l.entries * sizeof(Entry));
-  l.prefix_of = l.group_of + up256(batch * sizeof(int));
-  l.stats = l.prefix_of + up256(batch * sizeof(int));
+  const int64_t rows = batch * window * (n_heads / pool.n_kv_heads);
+  l.entries = (rows + kTileRows - 1) / kTileRows;
+  l.rows = (l.entries * pool.n_kv_heads + kMaxCtas) * kTileRows;
+  l.entry = up256((l.entries + 1) * sizeof(int));
+  l.segs = l.entry + up256(l.entries * sizeof(Entry));
+  l.stats = l.segs + up256((2 * batch + 2 * l.entries) * sizeof(Segment));
   l.parts = l.stats + up256(l.rows * sizeof(float2));
   l.bytes = l.parts + up256((size_t)l.rows * pool.head_dim * sizeof(float));
   return l;
@@ -937,8 +1040,10 @@ extern "C" int sjd_pool_attention_shared(const sjd_pool *pool, int layer, int ba
   if (batch > kMaxSeqs || (group_begin && n_groups > batch) || (int64_t)batch * window * n_heads > 1ll << 30) return SJD_ERR_CAPACITY;
   const SharedLayout l = layout_of(*pool, batch, window, n_heads);
   if (ws_bytes < l.bytes) return SJD_ERR_CAPACITY;
-  // (places of a kv head are counted in 32 bits)
-  if (l.entries * (((int64_t)pool->pages_per_seq + 1) + kUnit) >= 1ll << 31) return SJD_ERR_CAPACITY;
+  // (places of a kv head are counted in 32 bits: a sequence's keys count once in each of the units that it has rows in, twice where those are
+  // for both streams)
+  const int64_t most = ((int64_t)pool->pages_per_seq + 1) / 2 + 1;
+  if (2 * most * (2 * (int64_t)batch + 2 * l.entries) + kUnit * l.entries >= 1ll << 31) return SJD_ERR_CAPACITY;
   int dev = 0, cc_major = 0, sms = 0;
   SJD_CUDA(cudaGetDevice(&dev));
   SJD_CUDA(cudaDeviceGetAttribute(&cc_major, cudaDevAttrComputeCapabilityMajor, dev));
@@ -949,15 +1054,14 @@ extern "C" int sjd_pool_attention_shared(const sjd_pool *pool, int layer, int ba
   memset(&p, 0, sizeof(p));
   p.pool = *pool;
   p.layer = layer, p.batch = batch, p.window = window, p.n_heads = n_heads, p.group = n_heads / pool->n_kv_heads;
-  p.rows = window * p.group, p.row_tiles = (p.rows + kTileRows - 1) / kTileRows, p.n_groups = n_groups;
+  p.rows = window * p.group, p.n_entries = (int)l.entries, p.n_groups = n_groups;
   p.scale = (scale > 0.0f ? scale : 1.0f / sqrtf((float)hd)) * 1.4426950408889634f;
   p.q = (const __nv_bfloat16 *)q, p.q_stride = q_stride, p.out = (__nv_bfloat16 *)out, p.out_stride = out_stride;
   p.by_eight = ((uintptr_t)q & 15u) == 0 && (q_stride & 7) == 0;
   p.seqs = seqs, p.in_pos = in_pos, p.group_begin = group_begin;
   char *at = (char *)ws;
-  p.plan = (Plan *)at, p.before = (int *)(at + l.before), p.entry = (Entry *)(at + l.entry), p.group_of = (int *)(at + l.group_of);
-  p.prefix_of = (int *)(at + l.prefix_of), p.stats = (float2 *)(at + l.stats), p.parts = (float *)(at + l.parts);
-  p.max_entries = (int)l.entries;
+  p.before = (int *)at, p.entry = (Entry *)(at + l.entry), p.segs = (Segment *)(at + l.segs);
+  p.stats = (float2 *)(at + l.stats), p.parts = (float *)(at + l.parts);
   p.ctas = sms < kMaxCtas ? sms : kMaxCtas;
   const size_t smem = 1024 + 6ull * 128 * hd * 2 + (hd == 128 ? sizeof(SharedSmem<128>) : sizeof(SharedSmem<64>));
   auto tiles = hd == 128 ? shared_tiles_kernel<128> : shared_tiles_kernel<64>;
@@ -974,6 +1078,6 @@ extern "C" int sjd_pool_attention_shared(const sjd_pool *pool, int layer, int ba
   };
   int s = launch(shared_plan_kernel, 1, kPlanThreads, 0);
   if (s == SJD_OK) s = launch(tiles, (unsigned)p.ctas, kThreads, smem);
-  if (s == SJD_OK) s = launch(join, (unsigned)(((int64_t)batch * ((p.rows + 7) / 8) * pool->n_kv_heads + kJoinWarps - 1) / kJoinWarps), kJoinWarps * 32, 0);
+  if (s == SJD_OK) s = launch(join, (unsigned)((((int64_t)batch * p.rows + 7) / 8 * pool->n_kv_heads + kJoinWarps - 1) / kJoinWarps), kJoinWarps * 32, 0);
   return s;
 }
