@@ -1203,22 +1203,6 @@ __global__ void __launch_bounds__(kJoinRows * 32) pool_attention_join_kernel(con
   else store1(dst, acc[0]), store1(dst + 1, acc[1]);
 }
 
-// the layer's pages as boxes of 64 rows of a plane
-int make_pool_map(TensorMap *out, const sjd_pool &p, int layer) {
-  EncodeTiledFn fn = encode_fn();
-  if (!fn) return SJD_ERR_UNSUPPORTED;
-  const cuuint64_t plane = (cuuint64_t)KV_PAGE * p.head_dim, planes = 2ull * p.n_kv_heads;
-  cuuint64_t dims[4] = {(cuuint64_t)p.head_dim, (cuuint64_t)KV_PAGE, planes, (cuuint64_t)p.n_pages};
-  cuuint64_t strides[3] = {(cuuint64_t)p.head_dim, plane, plane * planes * p.n_layers};
-  cuuint32_t box[4] = {(cuuint32_t)p.head_dim, (cuuint32_t)KV_PAGE, 1, 1};
-  cuuint32_t estr[4] = {1, 1, 1, 1};
-  const CUresult r = fn(reinterpret_cast<CUtensorMap *>(out), CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, (uint8_t *)p.pages + plane * planes * layer,
-                        dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                        p.head_dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  return r == CUDA_SUCCESS ? SJD_OK : SJD_ERR_UNSUPPORTED;
-}
-
 // rows of a unit's tile
 int tile_rows(int64_t rows, int dtype) {
   const int least = dtype == SJD_F32 ? 8 : 16;

@@ -2,10 +2,12 @@
 // with the rows of all its sequences.
 //
 // Queries are the rows of both products (128 of a stream), keys and dims the columns:
-//   S [128 rows x 128 keys]  =  Q . K^T          O [128 rows x HD]  +=  P . V          (tcgen05, bf16, sums in 32 bits in tensor memory)
-// Shared pages meet many rows, so that the products and exponentials of a tile decide and its keys may be prepared once for all of them: four
-// warps turn e4m3 entries times 2^exponent into bf16, which holds them exactly (four bits and any exponent), as they lay them out for
-// the tensor cores.  P goes to the second product through tensor memory, in the columns of the scores that it was.
+//   S [128 rows x 128 keys]  =  Q . K^T          O [128 rows x HD]  +=  P . V          (tcgen05, sums in 32 bits in tensor memory)
+// Keys stay e4m3, as TMA left them; a query is two e4m3 numbers, x1 = e4m3(x) and x2 = e4m3(x - x1) of its entries times a power of two, which hold
+// the eight bits of bf16, and both meet the keys in one sum; a block's exponent is a factor of 16 columns of scores.  Values become bf16, entry times
+// 2^exponent, which holds it exactly (four bits and any exponent; with exponents left to the weights, as sjd_pool_attention has them, a block's largest
+// entry would take places from other blocks' weights): four warps turn a tile for all rows that meet it.  P goes to the second product
+// through tensor memory, in the columns of the scores that it was.
 // The rows of all sequences of a call follow one another (per kv head), 256 are a unit.  A unit's keys are segments: a group's common pages,
 // seen by all of its rows among the unit's, and every sequence's own pages, seen by its rows; the weights of the other rows are zeros.  So a
 // unit begins and ends once for many sequences, however short what is theirs alone.
@@ -28,10 +30,11 @@ constexpr int kUnit = 6;                // what a unit's begin and end take, in 
 constexpr int kLeast = 2;               // common pages that are worth a tile of their own
 constexpr int kMaxCtas = 192;
 constexpr int kMaxSeqs = SJD_POOL_MAX_LIST;
-constexpr int kBefore = 1024;           // units of a kv head whose places are kept in shared memory
-constexpr int kMaxSegs = 2 * kTileRows + 2;   // of a unit
-constexpr int kInfo = 4;                // tiles whose notes are kept
-constexpr int kConv = 128, kSoft = 256, kThreads = kSoft + kConv + 32;
+constexpr int kBefore = 512;            // units of a kv head whose places are kept in shared memory
+constexpr int kSegs = 128;              // segments of a unit that are kept there
+constexpr int kInfo = 8;                // tiles whose notes are kept: more than copies are ahead of weights
+constexpr int kKStages = 3;
+constexpr int kConv = 128, kSoft = 256, kThreads = kSoft + kConv + 64;
 constexpr int kPlanThreads = 1024;
 constexpr float kGrow = 8.0f;           // log2 of what a maximum may grow before its reference follows
 
@@ -51,7 +54,6 @@ struct SharedParams {
   long q_stride, out_stride;
   const int32_t *seqs, *in_pos, *group_begin;
   __nv_bfloat16 *out;
-  int by_eight;        // queries start on 16 bytes
   int *before;         // [n_entries + 1]: places of a kv head in the units before
   Entry *entry;        // [n_entries]
   Segment *segs;
@@ -357,14 +359,56 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
 __device__ __forceinline__ uint32_t bf16_bits_of_e4m3(uint32_t t) { return (t & 0x80008000u) | (t >> 4 & 0x07F007F0u); }
 __device__ __forceinline__ uint32_t pair_of(float v) { return bf16_pair(v, v); }
 
-struct Info {          // of a tile
+struct alignas(16) Info {   // of a tile
   int key0, k1, ra, rb;
-  int there;           // bit j: page j of the tile is there
+  int k_exp[2], v_exp[2];   // exponents of its pages' blocks
+  int there;                // bit j: page j of the tile is there
 };
+__device__ __forceinline__ uint32_t e4m3_of_floats(const float *v) {   // four, the first one in the low byte
+  uint32_t r;
+  asm("{\n\t.reg .b16 x, y;\n\tcvt.rn.satfinite.e4m3x2.f32 x, %2, %1;\n\tcvt.rn.satfinite.e4m3x2.f32 y, %4, %3;\n\tmov.b32 %0, {x, y};\n\t}"
+      : "=r"(r)
+      : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]));
+  return r;
+}
+__device__ __forceinline__ void floats_of_e4m3(uint32_t v, float *f) {   // four
+  uint32_t a, b;
+  asm("{\n\t.reg .b16 x, y;\n\tmov.b32 {x, y}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, x;\n\tcvt.rn.f16x2.e4m3x2 %1, y;\n\t}" : "=r"(a), "=r"(b) : "r"(v));
+  asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %2;\n\tcvt.f32.f16 %0, lo;\n\tcvt.f32.f16 %1, hi;\n\t}" : "=f"(f[0]), "=f"(f[1]) : "r"(a));
+  asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %2;\n\tcvt.f32.f16 %0, lo;\n\tcvt.f32.f16 %1, hi;\n\t}" : "=f"(f[2]), "=f"(f[3]) : "r"(b));
+}
+__device__ __forceinline__ void umma_e4m3(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, bool accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.u32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"((uint32_t)accumulate)
+      : "memory");
+}
+// 64 rows of a plane of a page, swizzled; and a plane of a page as it lies
+__device__ __forceinline__ void copy_box(uint32_t dst, const CUtensorMap *map, int plane, int page, uint64_t *bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %2, %3, %4}], [%5];"
+      ::"r"(dst), "l"(map), "r"(0), "r"(plane), "r"(page), "r"(smem_u32(bar))
+      : "memory");
+}
+__device__ __forceinline__ void copy_plane(uint32_t dst, const void *src, uint32_t bytes, uint64_t *bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(smem_u32(bar))
+               : "memory");
+}
+// K-major operand of rows of BYTES (64 or 128) under the swizzle of that width
+template <int BYTES>
+__device__ __forceinline__ uint64_t rows_desc() {
+  return (uint64_t)1 << 16 | (uint64_t)(8 * BYTES >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)(BYTES == 128 ? 2 : 4) << 61;
+}
+template <int BYTES>
+__device__ __forceinline__ uint32_t swizzled(uint32_t row, uint32_t col) {
+  return row * BYTES + (BYTES == 128 ? col ^ (row & 7) << 4 : col ^ (row >> 1 & 3) << 4);
+}
 
 template <int HD>
 struct SharedSmem {
-  uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_ready[2], o_full[2], q_ready;
+  uint64_t k_full[kKStages], k_empty[kKStages], raw_full[2], raw_empty[2], v_full[2], v_empty[2], s_full[2], p_ready[2], o_full[2], q_ready;
   uint32_t tmem_base;
   int failed;
   Info info[kInfo];
@@ -372,24 +416,30 @@ struct SharedSmem {
   alignas(16) uint16_t nan_dims[2][kKeys][HD / 16];    // which, if so
   float2 stat[2][128];                         // of both streams' rows
   uint32_t nan_row[2][128][HD / 32];
+  float factor[2][128];                        // of the scores of a row: the scale, and what its query was multiplied by
   int before[kBefore];
-  Segment segs[kMaxSegs];
+  Segment segs[kSegs];
 };
 
 template <int HD>
-__global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_constant__ SharedParams p) {
-  constexpr int OP = 128 * HD * 2;          // bytes of an operand: [HD / 64][128 rows][128 bytes], 128-byte swizzle
+__global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ SharedParams p) {
+  constexpr int OP = 128 * HD;              // bytes of 128 rows of e4m3
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t *smem = reinterpret_cast<uint8_t *>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-  uint8_t *Qs = smem, *Ks = smem + 2 * OP, *Vs = smem + 4 * OP;
-  SharedSmem<HD> &sh = *reinterpret_cast<SharedSmem<HD> *>(smem + 6 * OP);
+  // queries [stream][plane], keys [stage], values as they come [stage]; values in bf16 [stage][HD / 64][128 rows][128 bytes], 128-byte swizzle
+  uint8_t *Qs = smem, *Ks = Qs + 4 * OP, *Rs = Ks + kKStages * OP, *Vs = Rs + 2 * OP;
+  SharedSmem<HD> &sh = *reinterpret_cast<SharedSmem<HD> *>(Vs + 4 * OP);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, kv_heads = p.pool.n_kv_heads;
-  constexpr int ISSUE = (kSoft + kConv) / 32;
+  constexpr int ISSUE = (kSoft + kConv) / 32, COPY = ISSUE + 1;
   pdl_trigger();
   if (tid == 0) {
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(&sh.k_full[i], kConv / 32);
+    for (int i = 0; i < kKStages; ++i) {
+      mbar_init(&sh.k_full[i], 1);
       mbar_init(&sh.k_empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&sh.raw_full[i], 1);
+      mbar_init(&sh.raw_empty[i], kConv / 32);
       mbar_init(&sh.v_full[i], kConv / 32);
       mbar_init(&sh.v_empty[i], 1);
       mbar_init(&sh.s_full[i], 1);
@@ -398,6 +448,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
     }
     mbar_init(&sh.q_ready, kSoft / 32);
     sh.failed = 0;
+    tma_prefetch_desc(&map);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -440,169 +491,200 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
     return false;
   };
 
-  if (warp >= kSoft / 32 && warp < ISSUE) {
-    // ------------------------------------------------------------------ keys and values: e4m3 to bf16
+  if (warp == COPY) {
+    // ------------------------------------------------------------------ copies: what 32 tiles are is looked up together, a lane each
+    const long plane = (long)KV_PAGE * HD, head_planes = 2l * kv_heads, page_planes = head_planes * p.pool.n_layers;
+    struct Batch {
+      int n, h;                                   // tiles, kv head
+      int key0, k1, ra, rb, page[2], k_exp[2], v_exp[2];   // of this lane's
+    };
+    long t = t_begin;
+    Span s;
+    bool more = false, kept = false;
+    int i = 0;
+    auto begin_span = [&]() {
+      more = next_span(t, s);
+      if (!more) return;
+      i = s.i0;
+      const int n = s.en.n_segs[0] + s.en.n_segs[1] + s.en.n_segs[2];
+      kept = n <= kSegs;
+      __syncwarp();
+      if (kept)
+        for (int j = lane; j < n * (int)(sizeof(Segment) / 4); j += 32) reinterpret_cast<int *>(sh.segs)[j] = reinterpret_cast<const int *>(p.segs + s.en.segs)[j];
+      __syncwarp();
+    };
+    auto look_up = [&](Batch &b) {
+      b.n = 0;
+      if (!more) return;
+      b.n = min(32, s.i1 - i);
+      b.h = s.u.h;
+      const int x = min(i + lane, s.i1 - 1);
+      // its kind, its number among that kind's, its segment: the last of them that begins there or before
+      const int st = stream_of(s.en, x, s.i0), kind = one_stream(s.en.rows) ? 1 : st == 2 ? 0 : st + 1;
+      int j = x;
+      if (kind > 0) {
+        const int turns = min(s.en.tiles[1], s.en.tiles[2]);
+        j = x - s.en.tiles[0];
+        j = j < 2 * turns ? j >> 1 : j - turns;
+      }
+      const int from = kind == 0 ? 0 : kind == 1 ? s.en.n_segs[0] : s.en.n_segs[0] + s.en.n_segs[1];
+      int lo = from, hi = from + (kind == 0 ? s.en.n_segs[0] : kind == 1 ? s.en.n_segs[1] : s.en.n_segs[2]) - 1;
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if ((kept ? sh.segs[mid].base : p.segs[s.en.segs + mid].base) <= j) lo = mid; else hi = mid - 1;
+      }
+      const Segment g = kept ? sh.segs[lo] : p.segs[s.en.segs + lo];
+      b.key0 = g.k0 + (j - g.base) * kKeys;
+      b.k1 = g.k1, b.ra = g.ra, b.rb = g.rb;
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        b.page[k] = b.key0 + k * KV_PAGE < g.k1 ? p.pool.table[(long)g.seq * p.pool.pages_per_seq + b.key0 / KV_PAGE + k] : -1;
+      i += b.n;
+      if (i == s.i1) begin_span();
+    };
+    auto look_up_exps = [&](Batch &b) {
+      if (b.n == 0) return;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        b.k_exp[k] = b.v_exp[k] = 0;
+        if ((unsigned)b.page[k] >= (unsigned)p.pool.n_pages) b.page[k] = -1;
+        if (b.page[k] < 0) continue;
+        const long at = (long)b.page[k] * page_planes + head_planes * p.layer + b.h;
+        b.k_exp[k] = *reinterpret_cast<const int *>(p.pool.exps + at * kPoolBlocks);
+        b.v_exp[k] = *reinterpret_cast<const int *>(p.pool.exps + (at + kv_heads) * kPoolBlocks);
+      }
+    };
+    Batch now, next;
+    begin_span();
+    look_up(now);
+    look_up_exps(now);
+    bool ok = true;
+    uint32_t made = 0;
+    int stage = 0;
+    uint32_t ph = 1;
+    while (now.n > 0 && ok) {
+      look_up(next);
+#pragma unroll 1
+      for (int k = 0; k < now.n && ok; ++k, ++made) {
+        if (k == now.n / 2) look_up_exps(next);
+        const int page0 = __shfl_sync(0xffffffffu, now.page[0], k), page1 = __shfl_sync(0xffffffffu, now.page[1], k);
+        const int boxes = (page0 >= 0) + (page1 >= 0);
+        ok = !*(volatile int *)&sh.failed && (made < kKStages || warp_wait(&sh.k_empty[stage], ph));
+        if (!ok) break;
+        if (lane == k) {   // (its notes are read by those who wait for the copies)
+          Info f;
+          f.key0 = now.key0, f.k1 = now.k1, f.ra = now.ra, f.rb = now.rb;
+          f.k_exp[0] = now.k_exp[0], f.k_exp[1] = now.k_exp[1], f.v_exp[0] = now.v_exp[0], f.v_exp[1] = now.v_exp[1];
+          f.there = (page0 >= 0 ? 1 : 0) | (page1 >= 0 ? 2 : 0);
+          sh.info[made % kInfo] = f;
+          __threadfence_block();
+        }
+        __syncwarp();
+        if (elect_one()) {
+          const uint32_t dst = smem_u32(Ks) + stage * OP;
+          if (boxes > 0) mbar_expect_tx(&sh.k_full[stage], boxes * (OP / 2)); else arrive(&sh.k_full[stage]);
+          if (page0 >= 0) copy_box(dst, &map, now.h, page0, &sh.k_full[stage]);
+          if (page1 >= 0) copy_box(dst + OP / 2, &map, now.h, page1, &sh.k_full[stage]);
+        }
+        __syncwarp();
+        const int raw = made & 1;
+        ok = made < 2 || warp_wait(&sh.raw_empty[raw], (made >> 1 & 1) ^ 1u);
+        if (!ok) break;
+        if (elect_one()) {
+          const uint32_t dst = smem_u32(Rs) + raw * OP;
+          const uint8_t *from = (const uint8_t *)p.pool.pages + (head_planes * p.layer + kv_heads + now.h) * plane;
+          if (boxes > 0) mbar_expect_tx(&sh.raw_full[raw], boxes * (OP / 2)); else arrive(&sh.raw_full[raw]);
+          if (page0 >= 0) copy_plane(dst, from + page0 * page_planes * plane, OP / 2, &sh.raw_full[raw]);
+          if (page1 >= 0) copy_plane(dst + OP / 2, from + page1 * page_planes * plane, OP / 2, &sh.raw_full[raw]);
+        }
+        __syncwarp();
+        if (++stage == kKStages) { stage = 0; ph ^= 1u; }
+      }
+      now = next;
+    }
+    if (!ok) fail();
+    // leave no copy in flight
+    for (uint32_t j = made > kKStages ? made - kKStages : 0; j < made; ++j) warp_wait(&sh.k_full[j % kKStages], j / kKStages & 1);
+    for (uint32_t j = made > 2 ? made - 2 : 0; j < made; ++j) warp_wait(&sh.raw_full[j & 1], j >> 1 & 1);
+  } else if (warp >= kSoft / 32 && warp < ISSUE) {
+    // ------------------------------------------------------------------ values: e4m3 to bf16
     constexpr int SEG = HD / 16, ROWS = kConv / SEG, N = kKeys / ROWS;   // lanes of a row, rows at a time, 16-byte loads of a thread
     const int ct = tid - kSoft, seg = ct % SEG, row0 = ct / SEG, cw = ct >> 5;
     // (ROWS is a multiple of 8: a thread's rows have one swizzle)
     const uint32_t at0 = (uint32_t)(seg >> 2) * (128 * 128) + row0 * 128 + ((((seg & 3) * 2) ^ (row0 & 7)) << 4);
-    const long plane = (long)KV_PAGE * HD, head_planes = 2l * kv_heads, page_planes = head_planes * p.pool.n_layers;
-    struct Tile {
-      Info info;
-      int h, page[2];
-    };
-    auto sync = [&]() { asm volatile("bar.sync 2, %0;" ::"n"(kConv) : "memory"); };
-    long t = t_begin;
-    Span s;
-    bool more = false;
-    int i = 0, at[3] = {0, 0, 0};   // next tile; segments of each kind that it and the tiles before it are in
-    auto begin_span = [&]() {
-      more = next_span(t, s);
-      if (!more) return;
-      sync();   // (nobody looks at the segments of the span before)
-      const int n = s.en.n_segs[0] + s.en.n_segs[1] + s.en.n_segs[2];
-      const int *from = reinterpret_cast<const int *>(p.segs + s.en.segs);
-      int *to = reinterpret_cast<int *>(sh.segs);
-      for (int j = ct; j < n * (int)(sizeof(Segment) / 4); j += kConv) to[j] = from[j];
-      sync();
-      i = s.i0;
-      at[0] = 0, at[1] = s.en.n_segs[0], at[2] = at[1] + s.en.n_segs[1];
-    };
-    auto look_up = [&](Tile &d) {   // what there is to know of the next tile; false: none left
-      if (!more) return false;
-      // its kind, and its number among that kind's
-      int c = one_stream(s.en.rows) ? 1 : stream_of(s.en, i, s.i0) == 2 ? 0 : stream_of(s.en, i, s.i0) + 1, j = i;
-      if (c > 0 && !one_stream(s.en.rows)) {
-        const int both = min(s.en.tiles[1], s.en.tiles[2]);
-        j = i - s.en.tiles[0];
-        j = j < 2 * both ? j >> 1 : j - both;
-      }
-      int a = c == 0 ? at[0] : c == 1 ? at[1] : at[2];
-      const int end = (c == 0 ? 0 : c == 1 ? s.en.n_segs[0] : s.en.n_segs[0] + s.en.n_segs[1]) + (c == 0 ? s.en.n_segs[0] : c == 1 ? s.en.n_segs[1] : s.en.n_segs[2]);
-      while (a + 1 < end && sh.segs[a + 1].base <= j) ++a;
-      if (c == 0) at[0] = a;
-      if (c == 1) at[1] = a;
-      if (c == 2) at[2] = a;
-      const Segment g = sh.segs[a];
-      d.info.key0 = g.k0 + (j - g.base) * kKeys;
-      d.info.k1 = g.k1, d.info.ra = g.ra, d.info.rb = g.rb, d.info.there = 0;
-      d.h = s.u.h;
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const int page = d.info.key0 / KV_PAGE + k;
-        d.page[k] = d.info.key0 + k * KV_PAGE < g.k1 ? p.pool.table[(long)g.seq * p.pool.pages_per_seq + page] : -1;
-      }
-      if (++i == s.i1) begin_span();
-      return true;
-    };
-    uint4 raw[2][N];         // a tile's keys and values of this thread
-    int exps[2][2];          // exponents of its pages' blocks
-    auto fetch = [&](const Tile &d, int which) {
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const bool there = (unsigned)d.page[k] < (unsigned)p.pool.n_pages;
-        const long at = (long)(there ? d.page[k] : 0) * page_planes + head_planes * p.layer + (which ? kv_heads : 0) + d.h;
-        exps[which][k] = 0;
-        if (there) exps[which][k] = *reinterpret_cast<const int *>(p.pool.exps + at * kPoolBlocks);
-        const uint8_t *base = (const uint8_t *)p.pool.pages + at * plane + seg * 16;
-#pragma unroll
-        for (int n = k * N / 2; n < (k + 1) * N / 2; ++n) {
-          const int row = row0 + n * ROWS;
-          raw[which][n] = make_uint4(0, 0, 0, 0);
-          if (there && d.info.key0 + row < d.info.k1) raw[which][n] = *reinterpret_cast<const uint4 *>(base + (row & 63) * HD);
-        }
-      }
-    };
-    // an operand of a tile; returns the loads that had NaN entries, which become NaN (of V: zeros, told in nan_dims)
-    auto turn = [&](int which, uint8_t *to, int stage) {
-      auto exp_of = [&](int n) {
-        const int row = row0 + n * ROWS;
-        return pool_exp((int8_t)(exps[which][n / (N / 2)] >> (8 * (row >> 4 & 3))));
-      };
-      bool large = false;   // an exponent above 0: in two steps
-#pragma unroll
-      for (int n = 0; n < N; ++n) large |= exp_of(n) > 0;
-      uint32_t nan = 0;
+    long tiles = 0;
+    {
+      long t = t_begin;
+      Span s;
+      while (next_span(t, s)) tiles += s.i1 - s.i0;
+    }
+    bool ok = true;
+    for (uint32_t made = 0; made < tiles && ok; ++made) {
+      const int stage = made & 1;
+      ok = !*(volatile int *)&sh.failed && warp_wait(&sh.raw_full[stage], made >> 1 & 1) && (made < 2 || warp_wait(&sh.v_empty[stage], (made >> 1 & 1) ^ 1u));
+      if (!ok) break;
+      const Info f = sh.info[made % kInfo];
+      const uint8_t *from = Rs + stage * OP + row0 * HD + seg * 16;
+      uint8_t *to = Vs + stage * 2 * OP + at0;
+      uint4 raw[N];
+      uint32_t large = 0, nan = 0;   // exponents above 0: in two steps
 #pragma unroll
       for (int n = 0; n < N; ++n) {
-        const uint32_t w[4] = {raw[which][n].x, raw[which][n].y, raw[which][n].z, raw[which][n].w};
+        raw[n] = *reinterpret_cast<const uint4 *>(from + n * ROWS * HD);
+        if (!(f.there >> (n / (N / 2)) & 1) || f.key0 + row0 + n * ROWS >= f.k1) raw[n] = make_uint4(0, 0, 0, 0);
+      }
+      auto exp_of = [&](int n) { return pool_exp((int8_t)(f.v_exp[n / (N / 2)] >> (8 * ((row0 + n * ROWS) >> 4 & 3)))); };
+#pragma unroll
+      for (int n = 0; n < N; ++n) large |= exp_of(n) > 0 ? 1u : 0u;
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        const uint32_t w[4] = {raw[n].x, raw[n].y, raw[n].z, raw[n].w};
         const int e = exp_of(n);
-        // times 2^120, and the exponent: exact
-        const uint32_t up = pair_of(two_to(min(e, 0) + 120));
-        uint32_t out[8];
+        const uint32_t up = pair_of(two_to(min(e, 0) + 120));   // times 2^120, and the exponent: exact
+        uint32_t out[8], any = 0;
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           out[2 * c] = mul_bf16x2(bf16_bits_of_e4m3(__byte_perm(w[c], 0, 0x1404)), up);
           out[2 * c + 1] = mul_bf16x2(bf16_bits_of_e4m3(__byte_perm(w[c], 0, 0x3424)), up);
+          any |= (w[c] & 0x7F7F7F7Fu) + 0x01010101u;
         }
+        nan |= any & 0x80808080u;
         if (__builtin_expect(large, 0)) {
           const uint32_t over = pair_of(two_to(max(e, 0)));
 #pragma unroll
           for (int c = 0; c < 8; ++c) out[c] = mul_bf16x2(out[c], over);
         }
-        uint32_t any = 0;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) any |= (w[c] & 0x7F7F7F7Fu) + 0x01010101u;
-        nan |= (any & 0x80808080u) != 0 ? 1u << n : 0u;
-        uint8_t *dst = to + at0 + n * ROWS * 128;
+        uint8_t *dst = to + n * ROWS * 128;
         *reinterpret_cast<uint4 *>(dst) = make_uint4(out[0], out[1], out[2], out[3]);
         *reinterpret_cast<uint4 *>((uint8_t *)((uintptr_t)dst ^ 16)) = make_uint4(out[4], out[5], out[6], out[7]);
       }
       const bool found = __any_sync(0xffffffffu, nan != 0);
-      if (__builtin_expect(found, 0)) {
+      if (__builtin_expect(found, 0)) {   // NaN entries become zeros, and are told
 #pragma unroll 1
         for (int n = 0; n < N; ++n) {
           uint32_t dims = 0;
-          uint4 x = raw[which][0];
-#pragma unroll
-          for (int k = 1; k < N; ++k) x = k == n ? raw[which][k] : x;
-          uint16_t *dst = reinterpret_cast<uint16_t *>(to + at0 + n * ROWS * 128);
+          uint16_t *dst = reinterpret_cast<uint16_t *>(to + n * ROWS * 128);
+          const bool there = (f.there >> (n / (N / 2)) & 1) && f.key0 + row0 + n * ROWS < f.k1;
 #pragma unroll 1
           for (int c = 0; c < 16; ++c) {
-            const uint32_t w = c < 4 ? x.x : c < 8 ? x.y : c < 12 ? x.z : x.w;
-            if ((w >> (8 * (c & 3)) & 0x7Fu) != 0x7Fu) continue;
+            if (!there || (from[n * ROWS * HD + c] & 0x7F) != 0x7F) continue;
             dims |= 1u << c;
-            *reinterpret_cast<uint16_t *>((uintptr_t)(dst + (c & 7)) ^ (c < 8 ? 0 : 16)) = which ? 0 : 0x7FFF;
+            *reinterpret_cast<uint16_t *>((uintptr_t)(dst + (c & 7)) ^ (c < 8 ? 0 : 16)) = 0;
           }
-          if (which) sh.nan_dims[stage][row0 + n * ROWS][seg] = (uint16_t)dims;
+          sh.nan_dims[stage][row0 + n * ROWS][seg] = (uint16_t)dims;
         }
       }
-      if (which && lane == 0) sh.nan_warps[stage][cw] = found;
+      if (lane == 0) sh.nan_warps[stage][cw] = found;
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
-    };
-    // One tile is turned while the next one's bytes, and the pages of the one after, are on their way.
-    Tile d0, d1, d2;
-    begin_span();
-    bool have0 = look_up(d0), have1 = have0 && look_up(d1), ok = true;
-    if (have0) fetch(d0, 0), fetch(d0, 1);
-    for (uint32_t made = 0; have0 && ok; ++made) {
-      const int stage = made & 1, slot = made % kInfo;
-      const uint32_t ph = (made >> 1 & 1) ^ 1u;
-      const bool have2 = have1 && look_up(d2);
-      ok = !*(volatile int *)&sh.failed && (made < 2 || warp_wait(&sh.k_empty[stage], ph));
-      if (!ok) break;
-      if (ct == 0) {
-        d0.info.there = ((unsigned)d0.page[0] < (unsigned)p.pool.n_pages ? 1 : 0) | ((unsigned)d0.page[1] < (unsigned)p.pool.n_pages ? 2 : 0);
-        sh.info[slot] = d0.info;
-      }
-      turn(0, Ks + stage * OP, stage);
-      if (lane == 0) arrive(&sh.k_full[stage]);
-      if (have1) fetch(d1, 0);
-      ok = made < 2 || warp_wait(&sh.v_empty[stage], ph);
-      if (!ok) break;
-      turn(1, Vs + stage * OP, stage);
-      if (lane == 0) arrive(&sh.v_full[stage]);
-      if (have1) fetch(d1, 1);
-      d0 = d1, d1 = d2;
-      have0 = have1, have1 = have2;
+      if (lane == 0) arrive(&sh.raw_empty[stage]), arrive(&sh.v_full[stage]);
     }
     if (!ok) fail();
   } else if (warp == ISSUE) {
     // ------------------------------------------------------------------ products
-    constexpr uint32_t idesc_s = (1u << 4) | (1u << 7) | (1u << 10) | (uint32_t)(kKeys >> 3) << 17 | (uint32_t)(128 >> 4) << 24;
+    constexpr uint32_t idesc_s = (1u << 4) | (uint32_t)(kKeys >> 3) << 17 | (uint32_t)(128 >> 4) << 24;   // e4m3 both
     constexpr uint32_t idesc_o = (1u << 4) | (1u << 7) | (1u << 10) | 1u << 16 | (uint32_t)(HD >> 3) << 17 | (uint32_t)(128 >> 4) << 24;   // V: dims follow one another
-    const uint64_t desc = umma_desc_sw128(0);
+    const uint64_t desc = rows_desc<HD>();
     const uint64_t desc_v = (uint64_t)(128 * 128 >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
     const uint32_t q_at = smem_u32(Qs), k_at = smem_u32(Ks), v_at = smem_u32(Vs);
     long t = t_begin;
@@ -629,14 +711,16 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
       Job js = first_of(s.i0), jv = js;
       while (jv.i < s.i1 && ok) {
         while (js.i < s.i1 && !(js.st ? open1 : open0)) {
-          const uint32_t use = tile0 + js.i, stage = use & 1;
-          ok = !*(volatile int *)&sh.failed && warp_wait(&sh.k_full[stage], use >> 1 & 1);
+          const uint32_t use = tile0 + js.i, stage = use % kKStages;
+          ok = !*(volatile int *)&sh.failed && warp_wait(&sh.k_full[stage], use / kKStages & 1);
           if (!ok) break;
           tc_fence_after();
           if (elect_one()) {
-            const uint64_t a = desc | (uint64_t)((q_at + (alone ? 0 : js.st * OP)) >> 4), b = desc | (uint64_t)((k_at + stage * OP) >> 4);
+            const uint64_t a = desc | (uint64_t)((q_at + (alone ? 0 : js.st * 2 * OP)) >> 4), b = desc | (uint64_t)((k_at + stage * OP) >> 4);
 #pragma unroll
-            for (int k = 0; k < HD / 16; ++k) umma_bf16(tmem + js.st * 128, a + (k >> 2) * (128 * 128 >> 4) + (k & 3) * 2, b + (k >> 2) * (128 * 128 >> 4) + (k & 3) * 2, idesc_s, k > 0);
+            for (int k = 0; k < HD / 32; ++k) umma_e4m3(tmem + js.st * 128, a + k * 2, b + k * 2, idesc_s, k > 0);
+#pragma unroll
+            for (int k = 0; k < HD / 32; ++k) umma_e4m3(tmem + js.st * 128, a + (OP >> 4) + k * 2, b + k * 2, idesc_s, true);
             umma_commit(&sh.s_full[js.st]);
             if (js.last) umma_commit(&sh.k_empty[stage]);
           }
@@ -651,7 +735,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
         if (!ok) break;
         tc_fence_after();
         if (elect_one()) {
-          const uint64_t b = desc_v | (uint64_t)((v_at + stage * OP) >> 4);
+          const uint64_t b = desc_v | (uint64_t)((v_at + stage * 2 * OP) >> 4);
           const bool more = jv.st ? begun1 : begun0;
 #pragma unroll
           for (int k = 0; k < kKeys / 16; ++k) umma_bf16_ts(tmem + 256 + jv.st * 128, tmem + jv.st * 128 + k * 8, b + k * (16 * 128 >> 4), idesc_o, more || k > 0);
@@ -681,38 +765,46 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
       const bool alone = one_stream(rows);
       const int r = r_in + (alone ? 0 : st * 128);
       int pos = -1;   // of this thread's row
-      // ---- queries of the unit's rows
+      // ---- queries of the unit's rows: a power of two brings a row's largest entry to 128 .. 256, then its two numbers; a row is HD / 4 lanes
       {
-        const int per_lane = p.by_eight ? 8 : 4, row_lanes = HD / per_lane, each = 32 / row_lanes;   // rows of a warp's load
-        const int sub = lane / row_lanes, dim = lane % row_lanes * per_lane;
-        auto source = [&](int x) {
-          const int m = x / p.group;
-          return p.q + (long)m * p.q_stride + ((long)s.u.h * p.group + (x - m * p.group)) * HD + dim;
-        };
-        auto place = [&](int x) {
-          return Qs + (x >> 7) * OP + (dim >> 6) * (128 * 128) + (x & 127) * 128 + ((((dim & 63) >> 3) ^ (x & 7)) << 4) + (dim & 7) * 2;
-        };
-        constexpr int U = 8;
-        for (int r0 = warp * each; r0 < rows; r0 += kSoft / 32 * each * U) {
-          uint4 v[U];
+        constexpr int LANES = HD / 4, PER = 32 / LANES, U = 4;
+        const int sub = lane / LANES, dim = lane % LANES * 4;
+#pragma unroll 1
+        for (int r0 = warp * PER; r0 < rows; r0 += kSoft / 32 * PER * U) {
+          uint2 x[U];
 #pragma unroll
           for (int j = 0; j < U; ++j) {
-            const int x = r0 + j * (kSoft / 32) * each + sub;
-            v[j] = make_uint4(0, 0, 0, 0);
-            if (x >= rows) continue;
-            if (p.by_eight) {
-              v[j] = *reinterpret_cast<const uint4 *>(source(row_first + x));
-            } else {
-              const uint2 y = *reinterpret_cast<const uint2 *>(source(row_first + x));
-              v[j].x = y.x, v[j].y = y.y;
-            }
+            const int y = row_first + min(r0 + j * (kSoft / 32) * PER + sub, rows - 1), m = y / p.group;
+            x[j] = *reinterpret_cast<const uint2 *>(p.q + (long)m * p.q_stride + ((long)s.u.h * p.group + (y - m * p.group)) * HD + dim);
           }
 #pragma unroll
           for (int j = 0; j < U; ++j) {
-            const int x = r0 + j * (kSoft / 32) * each + sub;
-            if (x >= rows) continue;
-            if (p.by_eight) *reinterpret_cast<uint4 *>(place(x)) = v[j];
-            else *reinterpret_cast<uint2 *>(place(x)) = make_uint2(v[j].x, v[j].y);
+            const int y = r0 + j * (kSoft / 32) * PER + sub;
+            float v[4] = {__uint_as_float(x[j].x << 16), __uint_as_float(x[j].x & 0xFFFF0000u), __uint_as_float(x[j].y << 16), __uint_as_float(x[j].y & 0xFFFF0000u)};
+            float top = 0.0f;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              if (fabsf(v[c]) == INFINITY) v[c] = __int_as_float(0x7FFFFFFF);   // (e4m3 has no infinity: its row is NaN, as it would be)
+              top = fmaxf(top, fabsf(v[c]));
+            }
+#pragma unroll
+            for (int o = LANES / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            int e = top > 0.0f ? 7 - (int)((__float_as_uint(top) >> 23) - 127) : 0;
+            e = max(min(e, 126), -126);   // (entries below 2^-119 lose places)
+            const float up = two_to(e);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) v[c] *= up;
+            if (y < rows) {
+              uint8_t *to = Qs + (y >> 7) * 2 * OP + swizzled<HD>(y & 127, dim);
+              const uint32_t first = e4m3_of_floats(v);
+              float w[4];
+              floats_of_e4m3(first, w);
+#pragma unroll
+              for (int c = 0; c < 4; ++c) v[c] -= w[c];
+              *reinterpret_cast<uint32_t *>(to) = first;
+              *reinterpret_cast<uint32_t *>(to + OP) = e4m3_of_floats(v);
+              if (dim == 0) sh.factor[y >> 7][y & 127] = p.scale * two_to(-e);
+            }
           }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -722,7 +814,9 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
           const int m = (row_first + r) / p.group, b = m / p.window;
           pos = row_position(p, b, m - b * p.window, false);
         }
+        sync();   // (the factors are there)
       }
+      const float factor = r < rows ? sh.factor[r >> 7][r & 127] : 0.0f;
       const bool warp_rows = quarter * 32 + (alone ? 0 : st * 128) < rows;   // this warp has any
       float m_ref = -INFINITY, l = 0.0f;
       uint32_t nan[HD / 32];
@@ -764,6 +858,8 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
           const uint32_t bits = n_seen >= 32 ? 0xFFFFFFFFu : n_seen <= 0 ? 0u : (1u << n_seen) - 1;
           return f.there >> (k >> 1) & 1 ? bits : 0u;
         };
+        // of 16 columns: with the factor of their keys' block
+        auto factor_of = [&](int block) { return factor * two_to(pool_exp((int8_t)(f.k_exp[block >> 2] >> (8 * (block & 3))))); };
         float top = -INFINITY;
 #pragma unroll
         for (int k = 0; k < 4; k += 2) {
@@ -779,16 +875,21 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
               v[32 + j] = more >> j & 1u ? v[32 + j] : 0xFF800000u;
             }
           }
-          float a[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-          for (int j = 0; j < 64; j += 2) a[j >> 1 & 3] = fmaxf(fmaxf(a[j >> 1 & 3], __uint_as_float(v[j])), __uint_as_float(v[j + 1]));
-          top = fmaxf(top, fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])));
+          for (int c = 0; c < 4; ++c) {
+            float a = fmaxf(__uint_as_float(v[16 * c]), __uint_as_float(v[16 * c + 1])), b = fmaxf(__uint_as_float(v[16 * c + 2]), __uint_as_float(v[16 * c + 3]));
+#pragma unroll
+            for (int j = 4; j < 16; j += 4) {
+              a = fmaxf(fmaxf(a, __uint_as_float(v[16 * c + j])), __uint_as_float(v[16 * c + j + 1]));
+              b = fmaxf(fmaxf(b, __uint_as_float(v[16 * c + j + 2])), __uint_as_float(v[16 * c + j + 3]));
+            }
+            top = fmaxf(top, fmaxf(a, b) * factor_of(2 * k + c));
+          }
         }
         if (!whole && f.there != 3) {   // (no page where the row sees a key)
           const int miss = f.there & 1 ? f.key0 + KV_PAGE : f.key0;
           if (limit >= miss) pool_fault(p.pool.status, SJD_ERR_BAD_ARG);
         }
-        top *= p.scale;
         if (m_ref == -INFINITY) m_ref = top;   // (nothing so far: O is zero, or has not been written)
         if (__any_sync(0xffffffffu, top > m_ref + kGrow)) {
           const float now = fmaxf(m_ref, top), g = now == -INFINITY ? 1.0f : exp2_fast(m_ref - now);
@@ -807,7 +908,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
           tmem_st_wait();
         }
         const float ref = m_ref == -INFINITY ? 0.0f : m_ref;
-        const float2 scale2 = make_float2(p.scale, p.scale), ref2 = make_float2(-ref, -ref);
+        const float2 ref2 = make_float2(-ref, -ref);
         float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
         uint32_t v[2][32];
         tmem_ld32(t_s, v[0]);
@@ -821,9 +922,10 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
 #pragma unroll
             for (int j = 0; j < 32; ++j) x[j] = bits >> j & 1u ? x[j] : 0xFF800000u;
           }
+          const float f0 = factor_of(2 * k), f1 = factor_of(2 * k + 1);
 #pragma unroll
           for (int j = 0; j < 16; ++j) {
-            float2 y = fma2(make_float2(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1])), scale2, ref2);
+            float2 y = fma2(make_float2(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1])), j < 8 ? make_float2(f0, f0) : make_float2(f1, f1), ref2);
             y.x = exp2_fast(y.x), y.y = exp2_fast(y.y);
             sum[j & 1] = add2(sum[j & 1], y);
             w[j] = bf16_pair(y.x, y.y);
@@ -1057,27 +1159,30 @@ extern "C" int sjd_pool_attention_shared(const sjd_pool *pool, int layer, int ba
   p.rows = window * p.group, p.n_entries = (int)l.entries, p.n_groups = n_groups;
   p.scale = (scale > 0.0f ? scale : 1.0f / sqrtf((float)hd)) * 1.4426950408889634f;
   p.q = (const __nv_bfloat16 *)q, p.q_stride = q_stride, p.out = (__nv_bfloat16 *)out, p.out_stride = out_stride;
-  p.by_eight = ((uintptr_t)q & 15u) == 0 && (q_stride & 7) == 0;
   p.seqs = seqs, p.in_pos = in_pos, p.group_begin = group_begin;
   char *at = (char *)ws;
   p.before = (int *)at, p.entry = (Entry *)(at + l.entry), p.segs = (Segment *)(at + l.segs);
   p.stats = (float2 *)(at + l.stats), p.parts = (float *)(at + l.parts);
   p.ctas = sms < kMaxCtas ? sms : kMaxCtas;
-  const size_t smem = 1024 + 6ull * 128 * hd * 2 + (hd == 128 ? sizeof(SharedSmem<128>) : sizeof(SharedSmem<64>));
+  TensorMap tm;
+  const int made = make_pool_map(&tm, *pool, layer);
+  if (made != SJD_OK) return made;
+  const CUtensorMap &map = reinterpret_cast<const CUtensorMap &>(tm);
+  const size_t smem = 1024 + (4ull + kKStages + 2 + 4) * 128 * hd + (hd == 128 ? sizeof(SharedSmem<128>) : sizeof(SharedSmem<64>));
   auto tiles = hd == 128 ? shared_tiles_kernel<128> : shared_tiles_kernel<64>;
   auto join = hd == 128 ? shared_join_kernel<128> : shared_join_kernel<64>;
   const int r = allow_smem(tiles, smem);   // (the size follows from the kernel's type)
   if (r != SJD_OK) return r;
-  auto launch = [&](auto kernel, unsigned blocks, int threads, size_t shared) -> int {
+  auto launch = [&](auto kernel, unsigned blocks, int threads, size_t shared, const auto &...args) -> int {
     g_pdl = true;   // (each waits for the launch before it itself)
-    const cudaError_t e = launch_kernel(kernel, dim3(blocks), dim3(threads), shared, (cudaStream_t)cuda_stream, p);
+    const cudaError_t e = launch_kernel(kernel, dim3(blocks), dim3(threads), shared, (cudaStream_t)cuda_stream, args...);
     g_pdl = false;
     SJD_CUDA(e);
     SJD_CHECK_LAUNCH();
     return SJD_OK;
   };
-  int s = launch(shared_plan_kernel, 1, kPlanThreads, 0);
-  if (s == SJD_OK) s = launch(tiles, (unsigned)p.ctas, kThreads, smem);
-  if (s == SJD_OK) s = launch(join, (unsigned)((((int64_t)batch * p.rows + 7) / 8 * pool->n_kv_heads + kJoinWarps - 1) / kJoinWarps), kJoinWarps * 32, 0);
+  int s = launch(shared_plan_kernel, 1, kPlanThreads, 0, p);
+  if (s == SJD_OK) s = launch(tiles, (unsigned)p.ctas, kThreads, smem, map, p);
+  if (s == SJD_OK) s = launch(join, (unsigned)((((int64_t)batch * p.rows + 7) / 8 * pool->n_kv_heads + kJoinWarps - 1) / kJoinWarps), kJoinWarps * 32, 0, p);
   return s;
 }

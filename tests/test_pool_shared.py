@@ -97,12 +97,14 @@ def _queries(m, heads, hd, seed, spread=1.3):
 
 
 def _bound(want, n):
-    """Most that an output may be off.  A weight is rounded to bf16: 2^-8 of itself.  A score's products are exact; tensor memory adds 16 of them a
-    step and rounds towards zero, eight steps, and the product with the scale, the reference and the exponential's argument are rounded: 2^-19 of its
-    magnitudes (reach) covers them; it counts twice, in the numerator and in the sum.  The sums over n keys: n / 16 steps of 2^-23, factors and joints of
+    """Most that an output may be off.  A weight is rounded to bf16: 2^-8 of itself.  A query's two e4m3 numbers hold the eight bits of its entries but
+    for half of the smallest step, 2^-10 where the row's largest is 2^7 or more (flat).  Products are exact; tensor memory adds some of them a
+    step and rounds towards zero, up to eight steps, and the products with the factors, the reference and the exponential's argument are rounded:
+    2^-19 of a score's magnitudes (reach) covers them; a score counts twice, in the numerator and in the sum.  The sums over n keys: n / 16 steps of 2^-23, factors and joints of
     parts 2^-15.  The output's own rounding: half a step, 2^-8."""
-    out, mass, _, reach, _ = want
-    return 1.02 * ((2.0 ** -8 + 2 * reach[..., None] * 2.0 ** -19 + 2.0 ** -15 + n / 16 * 2.0 ** -23) * mass) + 2.0 ** -8 * np.abs(out) + 1e-35
+    out, mass, _, reach, flat = want
+    score = reach * 2.0 ** -19 + flat * 2.0 ** -17
+    return 1.02 * ((2.0 ** -8 + 2 * score[..., None] + 2.0 ** -15 + n / 16 * 2.0 ** -23) * mass) + 2.0 ** -8 * np.abs(out) + 1e-35
 
 
 def _check(pool, q, in_pos, window, begin, scale=0.0, seqs=None, layer=0, out=None):
