@@ -19,6 +19,8 @@
 //
 // Three launches: a plan (positions, what tables share, the line of units), the tiles, the joining of parts.  The line of all units' tiles is cut into
 // equal ranges, a CTA each; a unit that is within one is written by its CTA, the parts of the others are joined in the order of the ranges.
+#include <type_traits>
+
 #include "tcgen05.cuh"
 
 namespace sjd {
@@ -327,6 +329,16 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t *r) {
         "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
 }
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t *r) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t *r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // the first operand in tensor memory
 __device__ __forceinline__ void umma_bf16_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, bool accumulate) {
@@ -626,37 +638,50 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
       const Info f = sh.info[made % kInfo];
       const uint8_t *from = Rs + stage * OP + row0 * HD + seg * 16;
       uint8_t *to = Vs + stage * 2 * OP + at0;
-      uint4 raw[N];
-      uint32_t large = 0, nan = 0;   // exponents above 0: in two steps
+      const int left = f.k1 - f.key0 - row0;   // rows of this thread that there are
+      uint32_t nan = 0;
+      const int v_exp0 = f.v_exp[0], v_exp1 = f.v_exp[1];
+      auto exp_of = [&](int n) { return pool_exp((int8_t)((n < N / 2 ? v_exp0 : v_exp1) >> (8 * ((row0 + n * ROWS) >> 4 & 3)))); };
+      // two loads at a time: as many independent numbers as it takes, and a loop that is short to fetch
+#pragma unroll 1
+      for (int n0 = 0; n0 < N; n0 += 2) {
+        uint4 x[2];
+        uint32_t out[2][8], up[2];
+        bool large = false;   // an exponent above 0: in two steps
 #pragma unroll
-      for (int n = 0; n < N; ++n) {
-        raw[n] = *reinterpret_cast<const uint4 *>(from + n * ROWS * HD);
-        if (!(f.there >> (n / (N / 2)) & 1) || f.key0 + row0 + n * ROWS >= f.k1) raw[n] = make_uint4(0, 0, 0, 0);
-      }
-      auto exp_of = [&](int n) { return pool_exp((int8_t)(f.v_exp[n / (N / 2)] >> (8 * ((row0 + n * ROWS) >> 4 & 3)))); };
-#pragma unroll
-      for (int n = 0; n < N; ++n) large |= exp_of(n) > 0 ? 1u : 0u;
-#pragma unroll
-      for (int n = 0; n < N; ++n) {
-        const uint32_t w[4] = {raw[n].x, raw[n].y, raw[n].z, raw[n].w};
-        const int e = exp_of(n);
-        const uint32_t up = pair_of(two_to(min(e, 0) + 120));   // times 2^120, and the exponent: exact
-        uint32_t out[8], any = 0;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          out[2 * c] = mul_bf16x2(bf16_bits_of_e4m3(__byte_perm(w[c], 0, 0x1404)), up);
-          out[2 * c + 1] = mul_bf16x2(bf16_bits_of_e4m3(__byte_perm(w[c], 0, 0x3424)), up);
-          any |= (w[c] & 0x7F7F7F7Fu) + 0x01010101u;
+        for (int j = 0; j < 2; ++j) {
+          const int n = n0 + j, e = exp_of(n);
+          x[j] = *reinterpret_cast<const uint4 *>(from + n * ROWS * HD);
+          if (!(f.there >> (n / (N / 2)) & 1) || n * ROWS >= left) x[j] = make_uint4(0, 0, 0, 0);
+          up[j] = pair_of(two_to(min(e, 0) + 120));   // times 2^120, and the exponent: exact
+          large |= e > 0;
         }
-        nan |= any & 0x80808080u;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const uint32_t w[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
+          uint32_t any = 0;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            out[j][2 * c] = mul_bf16x2(bf16_bits_of_e4m3(__byte_perm(w[c], 0, 0x1404)), up[j]);
+            out[j][2 * c + 1] = mul_bf16x2(bf16_bits_of_e4m3(__byte_perm(w[c], 0, 0x3424)), up[j]);
+            any |= (w[c] & 0x7F7F7F7Fu) + 0x01010101u;
+          }
+          nan |= any & 0x80808080u;
+        }
         if (__builtin_expect(large, 0)) {
-          const uint32_t over = pair_of(two_to(max(e, 0)));
 #pragma unroll
-          for (int c = 0; c < 8; ++c) out[c] = mul_bf16x2(out[c], over);
+          for (int j = 0; j < 2; ++j) {
+            const uint32_t over = pair_of(two_to(max(exp_of(n0 + j), 0)));
+#pragma unroll
+            for (int c = 0; c < 8; ++c) out[j][c] = mul_bf16x2(out[j][c], over);
+          }
         }
-        uint8_t *dst = to + n * ROWS * 128;
-        *reinterpret_cast<uint4 *>(dst) = make_uint4(out[0], out[1], out[2], out[3]);
-        *reinterpret_cast<uint4 *>((uint8_t *)((uintptr_t)dst ^ 16)) = make_uint4(out[4], out[5], out[6], out[7]);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          uint8_t *dst = to + (n0 + j) * ROWS * 128;
+          *reinterpret_cast<uint4 *>(dst) = make_uint4(out[j][0], out[j][1], out[j][2], out[j][3]);
+          *reinterpret_cast<uint4 *>((uint8_t *)((uintptr_t)dst ^ 16)) = make_uint4(out[j][4], out[j][5], out[j][6], out[j][7]);
+        }
       }
       const bool found = __any_sync(0xffffffffu, nan != 0);
       if (__builtin_expect(found, 0)) {   // NaN entries become zeros, and are told
@@ -664,7 +689,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
         for (int n = 0; n < N; ++n) {
           uint32_t dims = 0;
           uint16_t *dst = reinterpret_cast<uint16_t *>(to + n * ROWS * 128);
-          const bool there = (f.there >> (n / (N / 2)) & 1) && f.key0 + row0 + n * ROWS < f.k1;
+          const bool there = (f.there >> (n / (N / 2)) & 1) && n * ROWS < left;
 #pragma unroll 1
           for (int c = 0; c < 16; ++c) {
             if (!there || (from[n * ROWS * HD + c] & 0x7F) != 0x7F) continue;
@@ -767,23 +792,28 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
       int pos = -1;   // of this thread's row
       // ---- queries of the unit's rows: a power of two brings a row's largest entry to 128 .. 256, then its two numbers; a row is HD / 4 lanes
       {
-        constexpr int LANES = HD / 4, PER = 32 / LANES, U = 4;
-        const int sub = lane / LANES, dim = lane % LANES * 4;
+        constexpr int LANES = HD / 8, PER = 32 / LANES, U = 4;   // lanes of a row, rows of a warp's load, loads under way
+        const int sub = lane / LANES, dim = lane % LANES * 8;
 #pragma unroll 1
         for (int r0 = warp * PER; r0 < rows; r0 += kSoft / 32 * PER * U) {
-          uint2 x[U];
+          uint2 x[U][2];
 #pragma unroll
           for (int j = 0; j < U; ++j) {
             const int y = row_first + min(r0 + j * (kSoft / 32) * PER + sub, rows - 1), m = y / p.group;
-            x[j] = *reinterpret_cast<const uint2 *>(p.q + (long)m * p.q_stride + ((long)s.u.h * p.group + (y - m * p.group)) * HD + dim);
+            const uint2 *from = reinterpret_cast<const uint2 *>(p.q + (long)m * p.q_stride + ((long)s.u.h * p.group + (y - m * p.group)) * HD + dim);
+            x[j][0] = from[0], x[j][1] = from[1];
           }
 #pragma unroll
           for (int j = 0; j < U; ++j) {
             const int y = r0 + j * (kSoft / 32) * PER + sub;
-            float v[4] = {__uint_as_float(x[j].x << 16), __uint_as_float(x[j].x & 0xFFFF0000u), __uint_as_float(x[j].y << 16), __uint_as_float(x[j].y & 0xFFFF0000u)};
-            float top = 0.0f;
+            float v[8], top = 0.0f;
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
+            for (int c = 0; c < 2; ++c) {
+              v[4 * c] = __uint_as_float(x[j][c].x << 16), v[4 * c + 1] = __uint_as_float(x[j][c].x & 0xFFFF0000u);
+              v[4 * c + 2] = __uint_as_float(x[j][c].y << 16), v[4 * c + 3] = __uint_as_float(x[j][c].y & 0xFFFF0000u);
+            }
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
               if (fabsf(v[c]) == INFINITY) v[c] = __int_as_float(0x7FFFFFFF);   // (e4m3 has no infinity: its row is NaN, as it would be)
               top = fmaxf(top, fabsf(v[c]));
             }
@@ -793,16 +823,19 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
             e = max(min(e, 126), -126);   // (entries below 2^-119 lose places)
             const float up = two_to(e);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) v[c] *= up;
+            for (int c = 0; c < 8; ++c) v[c] *= up;
             if (y < rows) {
-              uint8_t *to = Qs + (y >> 7) * 2 * OP + swizzled<HD>(y & 127, dim);
-              const uint32_t first = e4m3_of_floats(v);
-              float w[4];
-              floats_of_e4m3(first, w);
+              uint8_t *to = Qs + (y >> 7) * 2 * OP + swizzled<HD>(y & 127, dim);   // (eight bytes stay together)
 #pragma unroll
-              for (int c = 0; c < 4; ++c) v[c] -= w[c];
-              *reinterpret_cast<uint32_t *>(to) = first;
-              *reinterpret_cast<uint32_t *>(to + OP) = e4m3_of_floats(v);
+              for (int l = 0; l < 2; ++l) {
+                const uint32_t a = e4m3_of_floats(v), b = e4m3_of_floats(v + 4);
+                *reinterpret_cast<uint2 *>(to + l * OP) = make_uint2(a, b);
+                float w[8];
+                floats_of_e4m3(a, w);
+                floats_of_e4m3(b, w + 4);
+#pragma unroll
+                for (int c = 0; c < 8; ++c) v[c] -= w[c];
+              }
               if (dim == 0) sh.factor[y >> 7][y & 127] = p.scale * two_to(-e);
             }
           }
@@ -851,89 +884,94 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
           if (lane == 0) arrive(&sh.p_ready[st]);
           continue;
         }
-        const bool whole = __all_sync(0xffffffffu, limit >= f.key0 + kKeys - 1) && f.there == 3;
-        // which of 32 keys this row sees
-        auto seen = [&](int k) {
-          const int n_seen = limit - (f.key0 + k * 32) + 1;
-          const uint32_t bits = n_seen >= 32 ? 0xFFFFFFFFu : n_seen <= 0 ? 0u : (1u << n_seen) - 1;
-          return f.there >> (k >> 1) & 1 ? bits : 0u;
-        };
         // of 16 columns: with the factor of their keys' block
-        auto factor_of = [&](int block) { return factor * two_to(pool_exp((int8_t)(f.k_exp[block >> 2] >> (8 * (block & 3))))); };
-        float top = -INFINITY;
+        const int k_exp0 = f.k_exp[0], k_exp1 = f.k_exp[1];
+        auto factor_of = [&](int block) { return factor * two_to(pool_exp((int8_t)((block < 4 ? k_exp0 : k_exp1) >> (8 * (block & 3))))); };
+        // Weights of 32 keys after 32 keys, under the reference so far.  Where a score has outgrown it, the weights of this tile so far, O and the
+        // sum follow a new one; references are whole numbers, so that the weights' factor is exact.
+        const bool all = limit >= f.key0 + kKeys - 1;
+        auto weigh = [&](auto some) {   // some: rows that see some of the tile's keys (else all of them or none)
+          constexpr bool SOME = decltype(some)::value;
+          uint32_t x[32];
+          float2 y[16], sum = make_float2(0.0f, 0.0f);
+          tmem_ld32(t_s, x);
 #pragma unroll
-        for (int k = 0; k < 4; k += 2) {
-          uint32_t v[64];
-          tmem_ld32(t_s + k * 32, v);
-          tmem_ld32(t_s + k * 32 + 32, v + 32);
-          tmem_ld_wait();
-          if (!whole) {
-            const uint32_t bits = seen(k), more = seen(k + 1);
-#pragma unroll
-            for (int j = 0; j < 32; ++j) {
-              v[j] = bits >> j & 1u ? v[j] : 0xFF800000u;
-              v[32 + j] = more >> j & 1u ? v[32 + j] : 0xFF800000u;
+          for (int k = 0; k < 4; ++k) {
+            const float f0 = factor_of(2 * k), f1 = factor_of(2 * k + 1), ref = m_ref == -INFINITY ? 0.0f : m_ref;
+            uint32_t bits = 0xFFFFFFFFu;   // which of the 32 keys this row sees
+            if (SOME) {
+              const int n_seen = limit - (f.key0 + k * 32) + 1;
+              bits = n_seen >= 32 ? 0xFFFFFFFFu : n_seen <= 0 ? 0u : (1u << n_seen) - 1;
+              bits = f.there >> (k >> 1) & 1 ? bits : 0u;
             }
-          }
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            float a = fmaxf(__uint_as_float(v[16 * c]), __uint_as_float(v[16 * c + 1])), b = fmaxf(__uint_as_float(v[16 * c + 2]), __uint_as_float(v[16 * c + 3]));
-#pragma unroll
-            for (int j = 4; j < 16; j += 4) {
-              a = fmaxf(fmaxf(a, __uint_as_float(v[16 * c + j])), __uint_as_float(v[16 * c + j + 1]));
-              b = fmaxf(fmaxf(b, __uint_as_float(v[16 * c + j + 2])), __uint_as_float(v[16 * c + j + 3]));
-            }
-            top = fmaxf(top, fmaxf(a, b) * factor_of(2 * k + c));
-          }
-        }
-        if (!whole && f.there != 3) {   // (no page where the row sees a key)
-          const int miss = f.there & 1 ? f.key0 + KV_PAGE : f.key0;
-          if (limit >= miss) pool_fault(p.pool.status, SJD_ERR_BAD_ARG);
-        }
-        if (m_ref == -INFINITY) m_ref = top;   // (nothing so far: O is zero, or has not been written)
-        if (__any_sync(0xffffffffu, top > m_ref + kGrow)) {
-          const float now = fmaxf(m_ref, top), g = now == -INFINITY ? 1.0f : exp2_fast(m_ref - now);
-          m_ref = now;
-          l *= g;
-#pragma unroll 1
-          for (int k = 0; k < HD / 32; ++k) {
-            uint32_t v[32];
-            tmem_ld32(t_o + st * 128 + k * 32, v);
             tmem_ld_wait();
 #pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * g);
-            tmem_st16(t_o + st * 128 + k * 32, v);
-            tmem_st16(t_o + st * 128 + k * 32 + 16, v + 16);
+            for (int j = 0; j < 16; ++j) {
+              y[j] = fma2(make_float2(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1])), j < 8 ? make_float2(f0, f0) : make_float2(f1, f1), make_float2(-ref, -ref));
+              if (SOME) {
+                y[j].x = bits >> (2 * j) & 1u ? y[j].x : -INFINITY;
+                y[j].y = bits >> (2 * j + 1) & 1u ? y[j].y : -INFINITY;
+              }
+            }
+            if (k < 3) tmem_ld32(t_s + k * 32 + 32, x);   // (under way while these are worked on)
+            float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+            for (int j = 0; j < 16; ++j) top[j & 1] = fmaxf(fmaxf(top[j & 1], y[j].x), y[j].y);
+            float most = fmaxf(top[0], top[1]);
+            if (!SOME && !all) most = -INFINITY;
+            const bool need = most > (m_ref == -INFINITY ? -INFINITY : kGrow);
+            if (__builtin_expect(__any_sync(0xffffffffu, need), 0)) {
+              const float now = need ? ceilf(most + ref) : m_ref, g = need ? exp2_fast(m_ref - now) : 1.0f, less = need ? ref - now : 0.0f;
+              m_ref = now;
+              l *= g;
+              sum.x *= g, sum.y *= g;
+#pragma unroll
+              for (int j = 0; j < 16; ++j) y[j].x += less, y[j].y += less;
+              const uint32_t g2 = pair_of(g);
+              tmem_ld_wait();
+#pragma unroll 1
+              for (int c = 0; c < 2 * k; ++c) {
+                uint32_t v[8];
+                tmem_ld8(t_s + c * 8, v);
+                tmem_ld_wait();
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = mul_bf16x2(v[j], g2);
+                tmem_st8(t_s + c * 8, v);
+              }
+              if (mine > 1) {   // (O has been written)
+#pragma unroll 1
+                for (int c = 0; c < HD / 8; ++c) {
+                  uint32_t v[8];
+                  tmem_ld8(t_o + st * 128 + c * 8, v);
+                  tmem_ld_wait();
+#pragma unroll
+                  for (int j = 0; j < 8; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * g);
+                  tmem_st8(t_o + st * 128 + c * 8, v);
+                }
+              }
+              tmem_st_wait();
+            }
+            uint32_t w[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              y[j].x = exp2_fast(y[j].x), y[j].y = exp2_fast(y[j].y);
+              sum = add2(sum, y[j]);
+              w[j] = bf16_pair(y[j].x, y[j].y);
+              if (!SOME) w[j] = all ? w[j] : 0u;
+            }
+            tmem_st16(t_s + k * 16, w);   // (over scores that have been read)
           }
-          tmem_st_wait();
+          if (SOME || all) l += sum.x + sum.y;
+        };
+        if (f.there == 3 && __all_sync(0xffffffffu, all || limit < f.key0)) {
+          weigh(std::false_type());
+        } else {
+          if (f.there != 3) {   // (no page where the row sees a key)
+            const int miss = f.there & 1 ? f.key0 + KV_PAGE : f.key0;
+            if (limit >= miss) pool_fault(p.pool.status, SJD_ERR_BAD_ARG);
+          }
+          weigh(std::true_type());
         }
-        const float ref = m_ref == -INFINITY ? 0.0f : m_ref;
-        const float2 ref2 = make_float2(-ref, -ref);
-        float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
-        uint32_t v[2][32];
-        tmem_ld32(t_s, v[0]);
-        tmem_ld_wait();
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          if (k < 3) tmem_ld32(t_s + k * 32 + 32, v[(k + 1) & 1]);   // (under way while this one is worked on)
-          uint32_t *x = v[k & 1], w[16];
-          if (!whole) {
-            const uint32_t bits = seen(k);
-#pragma unroll
-            for (int j = 0; j < 32; ++j) x[j] = bits >> j & 1u ? x[j] : 0xFF800000u;
-          }
-          const float f0 = factor_of(2 * k), f1 = factor_of(2 * k + 1);
-#pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            float2 y = fma2(make_float2(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1])), j < 8 ? make_float2(f0, f0) : make_float2(f1, f1), ref2);
-            y.x = exp2_fast(y.x), y.y = exp2_fast(y.y);
-            sum[j & 1] = add2(sum[j & 1], y);
-            w[j] = bf16_pair(y.x, y.y);
-          }
-          if (k < 3) tmem_ld_wait();
-          tmem_st16(t_s + k * 16, w);   // (over scores that have been read)
-        }
-        l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
         tmem_st_wait();
         tc_fence_before();
         // NaN entries of V, which are zeros there, and the rows that see them
@@ -1042,49 +1080,76 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
 }
 
 // ---------------------------------------------------------------------------------------------------------------- joining
-// Eight rows of a unit that is cut a warp: lane = row + 8 * (dims / 4 % 4).  Parts in the order of their keys.
+// Eight rows of a unit that is cut a block: lane = row + 8 * (dims / 4 % 4), every kJoinWarps-th of the parts a warp, two parts' loads at a time.
 constexpr int kJoinWarps = 4;
 template <int HD>
 __global__ void __launch_bounds__(kJoinWarps * 32) shared_join_kernel(const __grid_constant__ SharedParams p) {
   constexpr int D = HD / 16;
+  __shared__ float4 of_warp[kJoinWarps - 1][D][32];
+  __shared__ float2 stat_of_warp[kJoinWarps - 1][32];
   pdl_wait();
   pdl_trigger();
-  const int lane = threadIdx.x & 31, kv_heads = p.pool.n_kv_heads, all_rows = p.batch * p.rows, eights = (all_rows + 7) / 8;
-  const long job = (long)blockIdx.x * kJoinWarps + (threadIdx.x >> 5);
-  if (job >= (long)eights * kv_heads) return;
-  const int h = (int)(job / eights), r = (int)(job - (long)h * eights) * 8 + (lane & 7), d0 = lane >> 3;
-  const int e = r / kTileRows, in = r % kTileRows;   // (the eight rows are of one unit)
-  if (r >= all_rows) return;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, kv_heads = p.pool.n_kv_heads, all_rows = p.batch * p.rows;
+  const int h = (int)(blockIdx.x % kv_heads), r0 = (int)(blockIdx.x / kv_heads) * 8, r = min(r0 + (lane & 7), all_rows - 1), d0 = lane >> 3;
+  const int e = r0 / kTileRows, in = r - e * kTileRows;   // (the eight rows are of one unit)
   const int b0 = p.before[e], cost = p.before[e + 1] - b0;
   const long chunk = range_of((long)p.before[p.n_entries] * kv_heads, p.ctas);
   float4 acc[D];
 #pragma unroll
   for (int i = 0; i < D; ++i) acc[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   float ref = -INFINITY, sum = 0.0f;
+  auto add = [&](float2 s, const float4 (&x)[D]) {   // (scores that are all NaN leave no maximum, but a sum)
+    const float now = fmaxf(ref, s.x), f = ref == -INFINITY ? (sum == 0.0f ? 0.0f : 1.0f) : exp2_fast(ref - now), g = s.x == -INFINITY ? (s.y == 0.0f ? 0.0f : 1.0f) : exp2_fast(s.x - now);
+    ref = now;
+    sum = sum * f + s.y * g;
+#pragma unroll
+    for (int i = 0; i < D; ++i) {
+      acc[i].x = fmaf(x[i].x, g, acc[i].x * f), acc[i].y = fmaf(x[i].y, g, acc[i].y * f);
+      acc[i].z = fmaf(x[i].z, g, acc[i].z * f), acc[i].w = fmaf(x[i].w, g, acc[i].w * f);
+    }
+  };
+  int warps = 1;
   if (cost > 0) {
     const Entry en = p.entry[e];
     Unit u;
     u.e = e, u.h = h, u.first = (long)b0 * kv_heads + (long)h * cost + kUnit;
-    const int n = tiles_of(en), c0 = (int)(u.first / chunk), c1 = (int)((u.first + cost - kUnit - 1) / chunk);
-    for (int c = c0; c <= c1; ++c) {
-      const int i0 = tiles_before(en, u.first, c * chunk), i1 = tiles_before(en, u.first, (c + 1) * chunk);
-      if (i0 == i1) continue;
-      if (i0 == 0 && i1 == n) return;   // (written by its CTA)
-      const long row = part_row(p, u, i0 == 0, c);
-      const float2 s = p.stats[row + in];
-      const float4 *from = reinterpret_cast<const float4 *>(p.parts + row * HD) + in;
-      float4 x[D];
+    const int n = tiles_of(en), c0 = (int)(u.first / chunk), c1 = (int)((u.first + cost - kUnit - 1) / chunk), stride = padded(en.rows);
+    if (tiles_before(en, u.first, c0 * chunk) == 0 && tiles_before(en, u.first, (c0 + 1) * chunk) == n) return;   // (written by its CTA)
+    warps = min(kJoinWarps, c1 - c0 + 1);
+    for (int c = c0 + warp; c <= c1; c += 2 * kJoinWarps) {
+      float2 s[2];
+      float4 x[2][D];
 #pragma unroll
-      for (int i = 0; i < D; ++i) x[i] = from[(d0 + 4 * i) * padded(en.rows)];
-      const float now = fmaxf(ref, s.x), f = ref == -INFINITY ? (sum == 0.0f ? 0.0f : 1.0f) : exp2_fast(ref - now), g = s.x == -INFINITY ? (s.y == 0.0f ? 0.0f : 1.0f) : exp2_fast(s.x - now);
-      ref = now;
-      sum = sum * f + s.y * g;
+      for (int j = 0; j < 2; ++j) {
+        const int at = c + j * kJoinWarps;
+        s[j] = make_float2(-INFINITY, 0.0f);
 #pragma unroll
-      for (int i = 0; i < D; ++i) {
-        acc[i].x = fmaf(x[i].x, g, acc[i].x * f), acc[i].y = fmaf(x[i].y, g, acc[i].y * f);
-        acc[i].z = fmaf(x[i].z, g, acc[i].z * f), acc[i].w = fmaf(x[i].w, g, acc[i].w * f);
+        for (int i = 0; i < D; ++i) x[j][i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (at > c1) continue;
+        const int i0 = tiles_before(en, u.first, at * chunk), i1 = tiles_before(en, u.first, (at + 1) * chunk);
+        if (i0 == i1) continue;
+        const long row = part_row(p, u, i0 == 0, at);
+        const float4 *from = reinterpret_cast<const float4 *>(p.parts + row * HD) + in;
+        s[j] = p.stats[row + in];
+#pragma unroll
+        for (int i = 0; i < D; ++i) x[j][i] = from[(d0 + 4 * i) * stride];
       }
+      add(s[0], x[0]);
+      add(s[1], x[1]);
     }
+  }
+  if (warp > 0) {
+    stat_of_warp[warp - 1][lane] = make_float2(ref, sum);
+#pragma unroll
+    for (int i = 0; i < D; ++i) of_warp[warp - 1][i][lane] = acc[i];
+  }
+  __syncthreads();
+  if (warp > 0 || r0 + (lane & 7) >= all_rows) return;
+  for (int w = 1; w < warps; ++w) {
+    float4 x[D];
+#pragma unroll
+    for (int i = 0; i < D; ++i) x[i] = of_warp[w - 1][i][lane];
+    add(stat_of_warp[w - 1][lane], x);
   }
   const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
   const int m = r / p.group;
@@ -1183,6 +1248,6 @@ extern "C" int sjd_pool_attention_shared(const sjd_pool *pool, int layer, int ba
   };
   int s = launch(shared_plan_kernel, 1, kPlanThreads, 0, p);
   if (s == SJD_OK) s = launch(tiles, (unsigned)p.ctas, kThreads, smem, map, p);
-  if (s == SJD_OK) s = launch(join, (unsigned)((((int64_t)batch * p.rows + 7) / 8 * pool->n_kv_heads + kJoinWarps - 1) / kJoinWarps), kJoinWarps * 32, 0, p);
+  if (s == SJD_OK) s = launch(join, (unsigned)(((int64_t)batch * p.rows + 7) / 8 * pool->n_kv_heads), kJoinWarps * 32, 0, p);
   return s;
 }
