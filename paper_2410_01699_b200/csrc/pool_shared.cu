@@ -36,7 +36,7 @@ constexpr int kBefore = 512;            // units of a kv head whose places are k
 constexpr int kSegs = 128;              // segments of a unit that are kept there
 constexpr int kInfo = 8;                // tiles whose notes are kept: more than copies are ahead of weights
 constexpr int kKStages = 3;
-constexpr int kConv = 128, kSoft = 256, kThreads = kSoft + kConv + 64;
+constexpr int kConv = 128, kSoft = 256, kThreads = kSoft + kConv + 96;
 constexpr int kPlanThreads = 1024;
 constexpr float kGrow = 8.0f;           // log2 of what a maximum may grow before its reference follows
 
@@ -422,7 +422,6 @@ template <int HD>
 struct SharedSmem {
   uint64_t k_full[kKStages], k_empty[kKStages], raw_full[2], raw_empty[2], v_full[2], v_empty[2], s_full[2], p_ready[2], o_full[2], q_ready;
   uint32_t tmem_base;
-  int failed;
   Info info[kInfo];
   uint32_t nan_warps[2][kConv / 32];           // some entry of V that a warp turned was NaN
   alignas(16) uint16_t nan_dims[2][kKeys][HD / 16];    // which, if so
@@ -442,24 +441,23 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
   uint8_t *Qs = smem, *Ks = Qs + 4 * OP, *Rs = Ks + kKStages * OP, *Vs = Rs + 2 * OP;
   SharedSmem<HD> &sh = *reinterpret_cast<SharedSmem<HD> *>(Vs + 4 * OP);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, kv_heads = p.pool.n_kv_heads;
-  constexpr int ISSUE = (kSoft + kConv) / 32, COPY = ISSUE + 1;
+  constexpr int ISSUE = (kSoft + kConv) / 32, COPY = ISSUE + 2;   // (a warp issues the products of a stream)
   pdl_trigger();
   if (tid == 0) {
     for (int i = 0; i < kKStages; ++i) {
       mbar_init(&sh.k_full[i], 1);
-      mbar_init(&sh.k_empty[i], 1);
+      mbar_init(&sh.k_empty[i], 2);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sh.raw_full[i], 1);
       mbar_init(&sh.raw_empty[i], kConv / 32);
       mbar_init(&sh.v_full[i], kConv / 32);
-      mbar_init(&sh.v_empty[i], 1);
+      mbar_init(&sh.v_empty[i], 2);
       mbar_init(&sh.s_full[i], 1);
       mbar_init(&sh.p_ready[i], 4);
       mbar_init(&sh.o_full[i], 1);
     }
     mbar_init(&sh.q_ready, kSoft / 32);
-    sh.failed = 0;
     tma_prefetch_desc(&map);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -480,10 +478,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
   const long all = (long)before(p.n_entries) * kv_heads, chunk = range_of(all, gridDim.x);
   const long t_begin = min(all, blockIdx.x * chunk), t_end = min(all, t_begin + chunk);
   auto fail = [&]() {
-    if (lane == 0) {
-      *(volatile int *)&sh.failed = 1;
-      pool_fault(p.pool.status, SJD_ERR_DEVICE_TIMEOUT);
-    }
+    if (lane == 0) pool_fault(p.pool.status, SJD_ERR_DEVICE_TIMEOUT);
   };
   // this CTA's next unit with tiles from place t on: tiles i0 .. i1 - 1 of it; false: no more
   struct Span {
@@ -581,7 +576,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
         if (k == now.n / 2) look_up_exps(next);
         const int page0 = __shfl_sync(0xffffffffu, now.page[0], k), page1 = __shfl_sync(0xffffffffu, now.page[1], k);
         const int boxes = (page0 >= 0) + (page1 >= 0);
-        ok = !*(volatile int *)&sh.failed && (made < kKStages || warp_wait(&sh.k_empty[stage], ph));
+        ok = made < kKStages || warp_wait(&sh.k_empty[stage], ph);
         if (!ok) break;
         if (lane == k) {   // (its notes are read by those who wait for the copies)
           Info f;
@@ -633,7 +628,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
     bool ok = true;
     for (uint32_t made = 0; made < tiles && ok; ++made) {
       const int stage = made & 1;
-      ok = !*(volatile int *)&sh.failed && warp_wait(&sh.raw_full[stage], made >> 1 & 1) && (made < 2 || warp_wait(&sh.v_empty[stage], (made >> 1 & 1) ^ 1u));
+      ok = warp_wait(&sh.raw_full[stage], made >> 1 & 1) && (made < 2 || warp_wait(&sh.v_empty[stage], (made >> 1 & 1) ^ 1u));
       if (!ok) break;
       const Info f = sh.info[made % kInfo];
       const uint8_t *from = Rs + stage * OP + row0 * HD + seg * 16;
@@ -705,74 +700,84 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
       if (lane == 0) arrive(&sh.raw_empty[stage]), arrive(&sh.v_full[stage]);
     }
     if (!ok) fail();
-  } else if (warp == ISSUE) {
-    // ------------------------------------------------------------------ products
+  } else if (warp == ISSUE || warp == ISSUE + 1) {
+    // ------------------------------------------------------------------ products of a stream; of tiles that are the other's alone it only lets go
     constexpr uint32_t idesc_s = (1u << 4) | (uint32_t)(kKeys >> 3) << 17 | (uint32_t)(128 >> 4) << 24;   // e4m3 both
     constexpr uint32_t idesc_o = (1u << 4) | (1u << 7) | (1u << 10) | 1u << 16 | (uint32_t)(HD >> 3) << 17 | (uint32_t)(128 >> 4) << 24;   // V: dims follow one another
-    const uint64_t desc = rows_desc<HD>();
-    const uint64_t desc_v = (uint64_t)(128 * 128 >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
-    const uint32_t q_at = smem_u32(Qs), k_at = smem_u32(Ks), v_at = smem_u32(Vs);
+    const int st = warp - ISSUE;
+    const uint64_t desc_k = rows_desc<HD>() | (uint64_t)(smem_u32(Ks) >> 4);
+    const uint64_t desc_v = (uint64_t)(128 * 128 >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61 | (uint64_t)(smem_u32(Vs) >> 4);
+    const uint32_t t_s = tmem + st * 128, t_o = tmem + 256 + st * 128;
     long t = t_begin;
     Span s;
     bool ok = true;
-    uint32_t q_ph = 0, p_ph0 = 0, p_ph1 = 0, tile0 = 0;   // tile0: tiles of the units before, less this one's first
+    uint32_t q_ph = 0, p_ph = 0;
+    int k_stage = 0, v_stage = 0;
+    uint32_t k_ph = 0, v_ph = 0;
     while (ok && next_span(t, s)) {
-      tile0 -= s.i0;
       ok = warp_wait(&sh.q_ready, q_ph);
       q_ph ^= 1u;
-      const bool alone = one_stream(s.en.rows);
-      // a product of a tile and a stream; those of tiles for both: the first stream's, then the second's
-      struct Job {
-        int i, st;
-        bool last;   // of its tile
-      };
-      auto first_of = [&](int i) {
-        const int c = i < s.i1 ? stream_of(s.en, i, s.i0) : 0;
-        return Job{i, c == 1 ? 1 : 0, c != 2};
-      };
-      auto next_of = [&](const Job &j) { return j.last ? first_of(j.i + 1) : Job{j.i, 1, true}; };
-      const int end0 = last_of(s.en, 0, s.i0, s.i1), end1 = last_of(s.en, 1, s.i0, s.i1);
-      bool open0 = false, open1 = false, begun0 = false, begun1 = false;   // scores whose weights have not been multiplied; O has been written
-      Job js = first_of(s.i0), jv = js;
-      while (jv.i < s.i1 && ok) {
-        while (js.i < s.i1 && !(js.st ? open1 : open0)) {
-          const uint32_t use = tile0 + js.i, stage = use % kKStages;
-          ok = !*(volatile int *)&sh.failed && warp_wait(&sh.k_full[stage], use / kKStages & 1);
-          if (!ok) break;
+      const uint64_t desc_q = rows_desc<HD>() | (uint64_t)((smem_u32(Qs) + (one_stream(s.en.rows) ? 0 : st * 2 * OP)) >> 4);
+      const int last = last_of(s.en, st, s.i0, s.i1);
+      // Scores of the tiles before `end`, up to those of an own tile while the weights of the one before have not been multiplied.  (No further than
+      // two tiles ahead of the values: what the copies wait for is let go of there.)
+      int i = s.i0;
+      bool open = false;
+      auto scores = [&](int end) {
+        for (; i < min(end, s.i1); ++i) {
+          const int c = stream_of(s.en, i, s.i0);
+          const bool own = c == 2 || c == st;
+          if (own && open) return;
+          ok = warp_wait(&sh.k_full[k_stage], k_ph);
+          if (!ok) return;
           tc_fence_after();
           if (elect_one()) {
-            const uint64_t a = desc | (uint64_t)((q_at + (alone ? 0 : js.st * 2 * OP)) >> 4), b = desc | (uint64_t)((k_at + stage * OP) >> 4);
+            if (own) {
+              const uint64_t b = desc_k + k_stage * (OP >> 4);
 #pragma unroll
-            for (int k = 0; k < HD / 32; ++k) umma_e4m3(tmem + js.st * 128, a + k * 2, b + k * 2, idesc_s, k > 0);
+              for (int k = 0; k < HD / 32; ++k) umma_e4m3(t_s, desc_q + k * 2, b + k * 2, idesc_s, k > 0);
 #pragma unroll
-            for (int k = 0; k < HD / 32; ++k) umma_e4m3(tmem + js.st * 128, a + (OP >> 4) + k * 2, b + k * 2, idesc_s, true);
-            umma_commit(&sh.s_full[js.st]);
-            if (js.last) umma_commit(&sh.k_empty[stage]);
+              for (int k = 0; k < HD / 32; ++k) umma_e4m3(t_s, desc_q + (OP >> 4) + k * 2, b + k * 2, idesc_s, true);
+              umma_commit(&sh.s_full[st]);
+              umma_commit(&sh.k_empty[k_stage]);
+            } else {
+              arrive(&sh.k_empty[k_stage]);
+            }
           }
           __syncwarp();
-          (js.st ? open1 : open0) = true;
-          js = next_of(js);
+          if (++k_stage == kKStages) { k_stage = 0; k_ph ^= 1u; }
+          open |= own;
         }
-        if (!ok) break;
-        const uint32_t use = tile0 + jv.i, stage = use & 1;
-        ok = !*(volatile int *)&sh.failed && warp_wait_both(&sh.p_ready[jv.st], jv.st ? p_ph1 : p_ph0, &sh.v_full[stage], use >> 1 & 1);
-        (jv.st ? p_ph1 : p_ph0) ^= 1u;
+      };
+      scores(s.i0 + 2);
+      bool begun = false;
+      for (int j = s.i0; j < s.i1 && ok; ++j) {
+        const int c = stream_of(s.en, j, s.i0);
+        const bool own = c == 2 || c == st;
+        ok = own ? warp_wait_both(&sh.p_ready[st], p_ph, &sh.v_full[v_stage], v_ph) : warp_wait(&sh.v_full[v_stage], v_ph);
         if (!ok) break;
         tc_fence_after();
         if (elect_one()) {
-          const uint64_t b = desc_v | (uint64_t)((v_at + stage * 2 * OP) >> 4);
-          const bool more = jv.st ? begun1 : begun0;
+          if (own) {
+            const uint64_t b = desc_v + v_stage * (2 * OP >> 4);
 #pragma unroll
-          for (int k = 0; k < kKeys / 16; ++k) umma_bf16_ts(tmem + 256 + jv.st * 128, tmem + jv.st * 128 + k * 8, b + k * (16 * 128 >> 4), idesc_o, more || k > 0);
-          if (jv.last) umma_commit(&sh.v_empty[stage]);
-          if (jv.i == (jv.st ? end1 : end0)) umma_commit(&sh.o_full[jv.st]);
+            for (int k = 0; k < kKeys / 16; ++k) umma_bf16_ts(t_o, t_s + k * 8, b + k * (16 * 128 >> 4), idesc_o, begun || k > 0);
+            umma_commit(&sh.v_empty[v_stage]);
+            if (j == last) umma_commit(&sh.o_full[st]);
+          } else {
+            arrive(&sh.v_empty[v_stage]);
+          }
         }
         __syncwarp();
-        (jv.st ? open1 : open0) = false;
-        (jv.st ? begun1 : begun0) = true;
-        jv = next_of(jv);
+        v_stage ^= 1;
+        v_ph ^= v_stage == 0;
+        if (own) {
+          p_ph ^= 1u;
+          begun = true;
+          open = false;
+        }
+        scores(j + 3);
       }
-      tile0 += s.i1;
     }
     if (!ok) fail();
   } else {
@@ -861,7 +866,6 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
         if (c != 2 && c != st) continue;
         ++mine;
         const uint32_t use = tile0 + i, stage = use & 1;
-        ok = ok && !*(volatile int *)&sh.failed;
         if (ok && !warp_wait(&sh.s_full[st], s_ph)) {
           ok = false;
           fail();
