@@ -19,8 +19,6 @@
 //
 // Three launches: a plan (positions, what tables share, the line of units), the tiles, the joining of parts.  The line of all units' tiles is cut into
 // equal ranges, a CTA each; a unit that is within one is written by its CTA, the parts of the others are joined in the order of the ranges.
-#include <type_traits>
-
 #include "tcgen05.cuh"
 
 namespace sjd {
@@ -36,7 +34,7 @@ constexpr int kBefore = 512;            // units of a kv head whose places are k
 constexpr int kSegs = 128;              // segments of a unit that are kept there
 constexpr int kInfo = 8;                // tiles whose notes are kept: more than copies are ahead of weights
 constexpr int kKStages = 3;
-constexpr int kConv = 128, kSoft = 256, kThreads = kSoft + kConv + 96;
+constexpr int kConv = 128, kSoft = 256, kThreads = kSoft + kConv + 128;
 constexpr int kPlanThreads = 1024;
 constexpr float kGrow = 8.0f;           // log2 of what a maximum may grow before its reference follows
 
@@ -361,7 +359,6 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
   return *reinterpret_cast<const uint32_t *>(&v);
 }
-__device__ __forceinline__ bool has_nan(uint32_t bytes) { return (((bytes & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) != 0; }
 __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
   uint32_t r;
   asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
@@ -498,7 +495,10 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
     return false;
   };
 
+  // Registers go to the softmax warps, whose threads hold the 128 scores of a row: of 512 threads' 128 each, 256 x 176 + 256 x 80.  (Every
+  // branch says so for itself: the compiler counts on what a branch begins with.)
   if (warp == COPY) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
     // ------------------------------------------------------------------ copies: what 32 tiles are is looked up together, a lane each
     const long plane = (long)KV_PAGE * HD, head_planes = 2l * kv_heads, page_planes = head_planes * p.pool.n_layers;
     struct Batch {
@@ -614,6 +614,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
     for (uint32_t j = made > kKStages ? made - kKStages : 0; j < made; ++j) warp_wait(&sh.k_full[j % kKStages], j / kKStages & 1);
     for (uint32_t j = made > 2 ? made - 2 : 0; j < made; ++j) warp_wait(&sh.raw_full[j & 1], j >> 1 & 1);
   } else if (warp >= kSoft / 32 && warp < ISSUE) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
     // ------------------------------------------------------------------ values: e4m3 to bf16
     constexpr int SEG = HD / 16, ROWS = kConv / SEG, N = kKeys / ROWS;   // lanes of a row, rows at a time, 16-byte loads of a thread
     const int ct = tid - kSoft, seg = ct % SEG, row0 = ct / SEG, cw = ct >> 5;
@@ -701,6 +702,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
     }
     if (!ok) fail();
   } else if (warp == ISSUE || warp == ISSUE + 1) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
     // ------------------------------------------------------------------ products of a stream; of tiles that are the other's alone it only lets go
     constexpr uint32_t idesc_s = (1u << 4) | (uint32_t)(kKeys >> 3) << 17 | (uint32_t)(128 >> 4) << 24;   // e4m3 both
     constexpr uint32_t idesc_o = (1u << 4) | (1u << 7) | (1u << 10) | 1u << 16 | (uint32_t)(HD >> 3) << 17 | (uint32_t)(128 >> 4) << 24;   // V: dims follow one another
@@ -780,7 +782,8 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
       }
     }
     if (!ok) fail();
-  } else {
+  } else if (warp < kSoft / 32) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
     // ------------------------------------------------------------------ softmax warps: a row a thread
     const int st = warp >> 2, quarter = warp & 3, r_in = quarter * 32 + lane;
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16, t_s = tmem + lanes + st * 128, t_o = tmem + lanes + 256;
@@ -854,7 +857,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
         }
         sync();   // (the factors are there)
       }
-      const float factor = r < rows ? sh.factor[r >> 7][r & 127] : 0.0f;
+      const float factor = fmaxf(r < rows ? sh.factor[r >> 7][r & 127] : 0.0f, 1e-38f);   // (not zero: masked scores stay infinite)
       const bool warp_rows = quarter * 32 + (alone ? 0 : st * 128) < rows;   // this warp has any
       float m_ref = -INFINITY, l = 0.0f;
       uint32_t nan[HD / 32];
@@ -891,90 +894,70 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
         // of 16 columns: with the factor of their keys' block
         const int k_exp0 = f.k_exp[0], k_exp1 = f.k_exp[1];
         auto factor_of = [&](int block) { return factor * two_to(pool_exp((int8_t)((block < 4 ? k_exp0 : k_exp1) >> (8 * (block & 3))))); };
-        // Weights of 32 keys after 32 keys, under the reference so far.  Where a score has outgrown it, the weights of this tile so far, O and the
-        // sum follow a new one; references are whole numbers, so that the weights' factor is exact.
-        const bool all = limit >= f.key0 + kKeys - 1;
-        auto weigh = [&](auto some) {   // some: rows that see some of the tile's keys (else all of them or none)
-          constexpr bool SOME = decltype(some)::value;
-          uint32_t x[32];
-          float2 y[16], sum = make_float2(0.0f, 0.0f);
-          tmem_ld32(t_s, x);
+        uint32_t x[128];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const float f0 = factor_of(2 * k), f1 = factor_of(2 * k + 1), ref = m_ref == -INFINITY ? 0.0f : m_ref;
-            uint32_t bits = 0xFFFFFFFFu;   // which of the 32 keys this row sees
-            if (SOME) {
-              const int n_seen = limit - (f.key0 + k * 32) + 1;
-              bits = n_seen >= 32 ? 0xFFFFFFFFu : n_seen <= 0 ? 0u : (1u << n_seen) - 1;
-              bits = f.there >> (k >> 1) & 1 ? bits : 0u;
-            }
-            tmem_ld_wait();
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-              y[j] = fma2(make_float2(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1])), j < 8 ? make_float2(f0, f0) : make_float2(f1, f1), make_float2(-ref, -ref));
-              if (SOME) {
-                y[j].x = bits >> (2 * j) & 1u ? y[j].x : -INFINITY;
-                y[j].y = bits >> (2 * j + 1) & 1u ? y[j].y : -INFINITY;
-              }
-            }
-            if (k < 3) tmem_ld32(t_s + k * 32 + 32, x);   // (under way while these are worked on)
-            float top[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-            for (int j = 0; j < 16; ++j) top[j & 1] = fmaxf(fmaxf(top[j & 1], y[j].x), y[j].y);
-            float most = fmaxf(top[0], top[1]);
-            if (!SOME && !all) most = -INFINITY;
-            const bool need = most > (m_ref == -INFINITY ? -INFINITY : kGrow);
-            if (__builtin_expect(__any_sync(0xffffffffu, need), 0)) {
-              const float now = need ? ceilf(most + ref) : m_ref, g = need ? exp2_fast(m_ref - now) : 1.0f, less = need ? ref - now : 0.0f;
-              m_ref = now;
-              l *= g;
-              sum.x *= g, sum.y *= g;
-#pragma unroll
-              for (int j = 0; j < 16; ++j) y[j].x += less, y[j].y += less;
-              const uint32_t g2 = pair_of(g);
-              tmem_ld_wait();
-#pragma unroll 1
-              for (int c = 0; c < 2 * k; ++c) {
-                uint32_t v[8];
-                tmem_ld8(t_s + c * 8, v);
-                tmem_ld_wait();
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = mul_bf16x2(v[j], g2);
-                tmem_st8(t_s + c * 8, v);
-              }
-              if (mine > 1) {   // (O has been written)
-#pragma unroll 1
-                for (int c = 0; c < HD / 8; ++c) {
-                  uint32_t v[8];
-                  tmem_ld8(t_o + st * 128 + c * 8, v);
-                  tmem_ld_wait();
-#pragma unroll
-                  for (int j = 0; j < 8; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * g);
-                  tmem_st8(t_o + st * 128 + c * 8, v);
-                }
-              }
-              tmem_st_wait();
-            }
-            uint32_t w[16];
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-              y[j].x = exp2_fast(y[j].x), y[j].y = exp2_fast(y[j].y);
-              sum = add2(sum, y[j]);
-              w[j] = bf16_pair(y[j].x, y[j].y);
-              if (!SOME) w[j] = all ? w[j] : 0u;
-            }
-            tmem_st16(t_s + k * 16, w);   // (over scores that have been read)
-          }
-          if (SOME || all) l += sum.x + sum.y;
-        };
-        if (f.there == 3 && __all_sync(0xffffffffu, all || limit < f.key0)) {
-          weigh(std::false_type());
-        } else {
+        for (int k = 0; k < 4; ++k) tmem_ld32(t_s + k * 32, x + k * 32);
+        tmem_ld_wait();
+        if (!__all_sync(0xffffffffu, limit >= f.key0 + kKeys - 1) || f.there != 3) {   // some row does not see some key
           if (f.there != 3) {   // (no page where the row sees a key)
             const int miss = f.there & 1 ? f.key0 + KV_PAGE : f.key0;
             if (limit >= miss) pool_fault(p.pool.status, SJD_ERR_BAD_ARG);
           }
-          weigh(std::true_type());
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int n_seen = limit - (f.key0 + k * 32) + 1;
+            uint32_t bits = n_seen >= 32 ? 0xFFFFFFFFu : n_seen <= 0 ? 0u : (1u << n_seen) - 1;   // which of 32 keys this row sees
+            bits = f.there >> (k >> 1) & 1 ? bits : 0u;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) x[k * 32 + j] = bits >> j & 1u ? x[k * 32 + j] : 0xFF800000u;
+          }
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+          float a = __uint_as_float(x[16 * c]), b = __uint_as_float(x[16 * c + 1]);
+#pragma unroll
+          for (int j = 2; j < 16; j += 4) {
+            a = fmaxf(fmaxf(a, __uint_as_float(x[16 * c + j])), __uint_as_float(x[16 * c + j + 1]));
+            if (j + 2 < 16) b = fmaxf(fmaxf(b, __uint_as_float(x[16 * c + j + 2])), __uint_as_float(x[16 * c + j + 3]));
+          }
+          top = fmaxf(top, fmaxf(a, b) * factor_of(c));
+        }
+        // Where a score has outgrown the reference, that, O and the sum follow.
+        const bool need = top > m_ref + kGrow || (m_ref == -INFINITY && top > -INFINITY);
+        if (__builtin_expect(__any_sync(0xffffffffu, need), 0)) {
+          const float g = need ? exp2_fast(m_ref - top) : 1.0f;
+          m_ref = need ? top : m_ref;
+          l *= g;
+          if (mine > 1) {   // (O has been written)
+#pragma unroll 1
+            for (int c = 0; c < HD / 8; ++c) {
+              uint32_t v[8];
+              tmem_ld8(t_o + st * 128 + c * 8, v);
+              tmem_ld_wait();
+#pragma unroll
+              for (int j = 0; j < 8; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * g);
+              tmem_st8(t_o + st * 128 + c * 8, v);
+            }
+          }
+        }
+        {
+          const float ref = m_ref == -INFINITY ? 0.0f : m_ref;
+          float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const float g = factor_of(k);
+            uint32_t w[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              float2 y = fma2(make_float2(__uint_as_float(x[16 * k + 2 * j]), __uint_as_float(x[16 * k + 2 * j + 1])), make_float2(g, g), make_float2(-ref, -ref));
+              y.x = exp2_fast(y.x), y.y = exp2_fast(y.y);
+              sum[j & 1] = add2(sum[j & 1], y);
+              w[j] = bf16_pair(y.x, y.y);
+            }
+            tmem_st8(t_s + k * 8, w);   // (over the scores)
+          }
+          l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
         }
         tmem_st_wait();
         tc_fence_before();
@@ -1074,6 +1057,8 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
       tc_fence_after();
       tile0 += s.i1;
     }
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
   }
   tc_fence_before();
   __syncthreads();
