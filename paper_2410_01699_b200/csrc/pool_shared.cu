@@ -34,7 +34,7 @@ constexpr int kBefore = 512;            // units of a kv head whose places are k
 constexpr int kSegs = 128;              // segments of a unit that are kept there
 constexpr int kInfo = 8;                // tiles whose notes are kept: more than copies are ahead of weights
 constexpr int kKStages = 3;
-constexpr int kConv = 128, kSoft = 256, kThreads = kSoft + kConv + 128;
+constexpr int kConv = 128, kSoft = 256, kThreads = kSoft + kConv + 96;
 constexpr int kPlanThreads = 1024;
 constexpr float kGrow = 8.0f;           // log2 of what a maximum may grow before its reference follows
 
@@ -273,23 +273,6 @@ __device__ __forceinline__ int stream_of(const Entry &en, int i, int from) {
   if (j < 0) return 2;
   return j < 2 * min(en.tiles[1], en.tiles[2]) ? j & 1 : en.tiles[1] > en.tiles[2] ? 0 : 1;
 }
-// the last of tiles i0 .. i1 - 1 that a stream works on (-1: none)
-__device__ __forceinline__ int last_of(const Entry &en, int st, int i0, int i1) {
-  if (one_stream(en.rows)) {
-    const int i = i1 - 1 - ((i1 - 1 - i0 - st) & 1);
-    return i >= i0 ? i : -1;
-  }
-  const int n = en.tiles[0], turns = 2 * min(en.tiles[1], en.tiles[2]);
-  int j = i1 - 1 - n;
-  if (j >= turns) {
-    if ((en.tiles[1] > en.tiles[2] ? 0 : 1) == st) return i1 - 1;
-    j = turns - 1;
-  }
-  if (j >= 0 && (j & 1) != st) --j;
-  if (j >= 0 && n + j >= i0) return n + j;
-  const int both = min(n, i1) - 1;
-  return both >= i0 ? both : -1;
-}
 // first row of a part: of the unit's first tiles, or of those that CTA c goes on with
 __device__ __forceinline__ long part_row(const SharedParams &p, const Unit &u, bool begins, int c) {
   return begins ? ((long)u.e * p.pool.n_kv_heads + u.h) * kTileRows : ((long)p.n_entries * p.pool.n_kv_heads + c) * kTileRows;
@@ -350,6 +333,11 @@ __device__ __forceinline__ void umma_bf16_ts(uint32_t tmem_d, uint32_t tmem_a, u
 __device__ __forceinline__ void arrive(uint64_t *bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
+__device__ __forceinline__ float max3(uint32_t a, uint32_t b, uint32_t c) {   // (a NaN is no maximum)
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(__uint_as_float(a)), "f"(__uint_as_float(b)), "f"(__uint_as_float(c)));
+  return d;
+}
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -370,8 +358,11 @@ __device__ __forceinline__ uint32_t pair_of(float v) { return bf16_pair(v, v); }
 
 struct alignas(16) Info {   // of a tile
   int key0, k1, ra, rb;
-  int k_exp[2], v_exp[2];   // exponents of its pages' blocks
   int there;                // bit j: page j of the tile is there
+  int v_exp[2];             // exponents of its pages' blocks of values; some are above 0
+  int large;
+  float k_up[8];            // 2^exponent of its blocks of keys
+  uint32_t v_up[8];         // and of values, times 2^120, twice in bf16 (exponents up to 0)
 };
 __device__ __forceinline__ uint32_t e4m3_of_floats(const float *v) {   // four, the first one in the low byte
   uint32_t r;
@@ -417,7 +408,7 @@ __device__ __forceinline__ uint32_t swizzled(uint32_t row, uint32_t col) {
 
 template <int HD>
 struct SharedSmem {
-  uint64_t k_full[kKStages], k_empty[kKStages], raw_full[2], raw_empty[2], v_full[2], v_empty[2], s_full[2], p_ready[2], o_full[2], q_ready;
+  uint64_t k_full[kKStages], k_empty[kKStages], raw_full[2], raw_empty[2], v_full[2], v_empty[2], s_full[2][2], p_ready[2][2], o_done[2][2], q_ready;
   uint32_t tmem_base;
   Info info[kInfo];
   uint32_t nan_warps[2][kConv / 32];           // some entry of V that a warp turned was NaN
@@ -450,9 +441,11 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
       mbar_init(&sh.raw_empty[i], kConv / 32);
       mbar_init(&sh.v_full[i], kConv / 32);
       mbar_init(&sh.v_empty[i], 2);
-      mbar_init(&sh.s_full[i], 1);
-      mbar_init(&sh.p_ready[i], 4);
-      mbar_init(&sh.o_full[i], 1);
+      for (int h = 0; h < 2; ++h) {
+        mbar_init(&sh.s_full[i][h], 1);
+        mbar_init(&sh.p_ready[i][h], 4);
+        mbar_init(&sh.o_done[i][h], 1);
+      }
     }
     mbar_init(&sh.q_ready, kSoft / 32);
     tma_prefetch_desc(&map);
@@ -495,10 +488,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
     return false;
   };
 
-  // Registers go to the softmax warps, whose threads hold the 128 scores of a row: of 512 threads' 128 each, 256 x 176 + 256 x 80.  (Every
-  // branch says so for itself: the compiler counts on what a branch begins with.)
   if (warp == COPY) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
     // ------------------------------------------------------------------ copies: what 32 tiles are is looked up together, a lane each
     const long plane = (long)KV_PAGE * HD, head_planes = 2l * kv_heads, page_planes = head_planes * p.pool.n_layers;
     struct Batch {
@@ -581,8 +571,15 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
         if (lane == k) {   // (its notes are read by those who wait for the copies)
           Info f;
           f.key0 = now.key0, f.k1 = now.k1, f.ra = now.ra, f.rb = now.rb;
-          f.k_exp[0] = now.k_exp[0], f.k_exp[1] = now.k_exp[1], f.v_exp[0] = now.v_exp[0], f.v_exp[1] = now.v_exp[1];
+          f.v_exp[0] = now.v_exp[0], f.v_exp[1] = now.v_exp[1], f.large = 0;
           f.there = (page0 >= 0 ? 1 : 0) | (page1 >= 0 ? 2 : 0);
+#pragma unroll
+          for (int b = 0; b < 8; ++b) {
+            const int e = pool_exp((int8_t)((b < 4 ? now.v_exp[0] : now.v_exp[1]) >> (8 * (b & 3))));
+            f.k_up[b] = two_to(pool_exp((int8_t)((b < 4 ? now.k_exp[0] : now.k_exp[1]) >> (8 * (b & 3)))));
+            f.v_up[b] = pair_of(two_to(min(e, 0) + 120));
+            f.large |= e > 0;
+          }
           sh.info[made % kInfo] = f;
           __threadfence_block();
         }
@@ -614,7 +611,6 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
     for (uint32_t j = made > kKStages ? made - kKStages : 0; j < made; ++j) warp_wait(&sh.k_full[j % kKStages], j / kKStages & 1);
     for (uint32_t j = made > 2 ? made - 2 : 0; j < made; ++j) warp_wait(&sh.raw_full[j & 1], j >> 1 & 1);
   } else if (warp >= kSoft / 32 && warp < ISSUE) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
     // ------------------------------------------------------------------ values: e4m3 to bf16
     constexpr int SEG = HD / 16, ROWS = kConv / SEG, N = kKeys / ROWS;   // lanes of a row, rows at a time, 16-byte loads of a thread
     const int ct = tid - kSoft, seg = ct % SEG, row0 = ct / SEG, cw = ct >> 5;
@@ -631,26 +627,22 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
       const int stage = made & 1;
       ok = warp_wait(&sh.raw_full[stage], made >> 1 & 1) && (made < 2 || warp_wait(&sh.v_empty[stage], (made >> 1 & 1) ^ 1u));
       if (!ok) break;
-      const Info f = sh.info[made % kInfo];
+      const Info &f = sh.info[made % kInfo];
       const uint8_t *from = Rs + stage * OP + row0 * HD + seg * 16;
       uint8_t *to = Vs + stage * 2 * OP + at0;
-      const int left = f.k1 - f.key0 - row0;   // rows of this thread that there are
+      const int left = f.k1 - f.key0 - row0, there = f.there, large = f.large;   // left: rows of this thread that there are
       uint32_t nan = 0;
-      const int v_exp0 = f.v_exp[0], v_exp1 = f.v_exp[1];
-      auto exp_of = [&](int n) { return pool_exp((int8_t)((n < N / 2 ? v_exp0 : v_exp1) >> (8 * ((row0 + n * ROWS) >> 4 & 3)))); };
       // two loads at a time: as many independent numbers as it takes, and a loop that is short to fetch
 #pragma unroll 1
       for (int n0 = 0; n0 < N; n0 += 2) {
         uint4 x[2];
         uint32_t out[2][8], up[2];
-        bool large = false;   // an exponent above 0: in two steps
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const int n = n0 + j, e = exp_of(n);
+          const int n = n0 + j;
           x[j] = *reinterpret_cast<const uint4 *>(from + n * ROWS * HD);
-          if (!(f.there >> (n / (N / 2)) & 1) || n * ROWS >= left) x[j] = make_uint4(0, 0, 0, 0);
-          up[j] = pair_of(two_to(min(e, 0) + 120));   // times 2^120, and the exponent: exact
-          large |= e > 0;
+          if (!(there >> (n / (N / 2)) & 1) || n * ROWS >= left) x[j] = make_uint4(0, 0, 0, 0);
+          up[j] = f.v_up[(row0 + n * ROWS) >> 4];
         }
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -664,10 +656,11 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
           }
           nan |= any & 0x80808080u;
         }
-        if (__builtin_expect(large, 0)) {
+        if (__builtin_expect(large, 0)) {   // (exponents above 0 in a second step)
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            const uint32_t over = pair_of(two_to(max(exp_of(n0 + j), 0)));
+            const int block = (row0 + (n0 + j) * ROWS) >> 4;
+            const uint32_t over = pair_of(two_to(max(pool_exp((int8_t)((block < 4 ? f.v_exp[0] : f.v_exp[1]) >> (8 * (block & 3)))), 0)));
 #pragma unroll
             for (int c = 0; c < 8; ++c) out[j][c] = mul_bf16x2(out[j][c], over);
           }
@@ -685,10 +678,10 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
         for (int n = 0; n < N; ++n) {
           uint32_t dims = 0;
           uint16_t *dst = reinterpret_cast<uint16_t *>(to + n * ROWS * 128);
-          const bool there = (f.there >> (n / (N / 2)) & 1) && n * ROWS < left;
+          const bool row = (there >> (n / (N / 2)) & 1) && n * ROWS < left;
 #pragma unroll 1
           for (int c = 0; c < 16; ++c) {
-            if (!there || (from[n * ROWS * HD + c] & 0x7F) != 0x7F) continue;
+            if (!row || (from[n * ROWS * HD + c] & 0x7F) != 0x7F) continue;
             dims |= 1u << c;
             *reinterpret_cast<uint16_t *>((uintptr_t)(dst + (c & 7)) ^ (c < 8 ? 0 : 16)) = 0;
           }
@@ -702,9 +695,8 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
     }
     if (!ok) fail();
   } else if (warp == ISSUE || warp == ISSUE + 1) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
     // ------------------------------------------------------------------ products of a stream; of tiles that are the other's alone it only lets go
-    constexpr uint32_t idesc_s = (1u << 4) | (uint32_t)(kKeys >> 3) << 17 | (uint32_t)(128 >> 4) << 24;   // e4m3 both
+    constexpr uint32_t idesc_s = (1u << 4) | (uint32_t)(kKeys / 2 >> 3) << 17 | (uint32_t)(128 >> 4) << 24;   // e4m3 both
     constexpr uint32_t idesc_o = (1u << 4) | (1u << 7) | (1u << 10) | 1u << 16 | (uint32_t)(HD >> 3) << 17 | (uint32_t)(128 >> 4) << 24;   // V: dims follow one another
     const int st = warp - ISSUE;
     const uint64_t desc_k = rows_desc<HD>() | (uint64_t)(smem_u32(Ks) >> 4);
@@ -720,35 +712,45 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
       ok = warp_wait(&sh.q_ready, q_ph);
       q_ph ^= 1u;
       const uint64_t desc_q = rows_desc<HD>() | (uint64_t)((smem_u32(Qs) + (one_stream(s.en.rows) ? 0 : st * 2 * OP)) >> 4);
-      const int last = last_of(s.en, st, s.i0, s.i1);
-      // Scores of the tiles before `end`, up to those of an own tile while the weights of the one before have not been multiplied.  (No further than
-      // two tiles ahead of the values: what the copies wait for is let go of there.)
+      // Scores of the halves of the own tiles before `end`, each when the weights in its columns have been multiplied.  (No further than two tiles ahead
+      // of the values: what the copies wait for is let go of there.)
       int i = s.i0;
-      bool open = false;
+      bool half = false, open0 = false, open1 = false;   // the first half of tile i has its scores; weights that have not been multiplied
+      auto products = [&](int h) {
+        const uint64_t b = desc_k + k_stage * (OP >> 4) + h * (OP / 2 >> 4);
+#pragma unroll
+        for (int k = 0; k < HD / 32; ++k) umma_e4m3(t_s + h * 64, desc_q + k * 2, b + k * 2, idesc_s, k > 0);
+#pragma unroll
+        for (int k = 0; k < HD / 32; ++k) umma_e4m3(t_s + h * 64, desc_q + (OP >> 4) + k * 2, b + k * 2, idesc_s, true);
+        umma_commit(&sh.s_full[st][h]);
+      };
       auto scores = [&](int end) {
-        for (; i < min(end, s.i1); ++i) {
+        for (; ok && i < min(end, s.i1); ++i) {
           const int c = stream_of(s.en, i, s.i0);
           const bool own = c == 2 || c == st;
-          if (own && open) return;
-          ok = warp_wait(&sh.k_full[k_stage], k_ph);
-          if (!ok) return;
-          tc_fence_after();
-          if (elect_one()) {
-            if (own) {
-              const uint64_t b = desc_k + k_stage * (OP >> 4);
-#pragma unroll
-              for (int k = 0; k < HD / 32; ++k) umma_e4m3(t_s, desc_q + k * 2, b + k * 2, idesc_s, k > 0);
-#pragma unroll
-              for (int k = 0; k < HD / 32; ++k) umma_e4m3(t_s, desc_q + (OP >> 4) + k * 2, b + k * 2, idesc_s, true);
-              umma_commit(&sh.s_full[st]);
-              umma_commit(&sh.k_empty[k_stage]);
-            } else {
-              arrive(&sh.k_empty[k_stage]);
+          if (!half) {
+            if (own && open0) return;
+            ok = warp_wait(&sh.k_full[k_stage], k_ph);
+            if (!ok) return;
+            tc_fence_after();
+            if (elect_one()) {
+              if (own) products(0);
+              else arrive(&sh.k_empty[k_stage]);
             }
+            __syncwarp();
+            if (own) half = open0 = true;
           }
-          __syncwarp();
+          if (own) {
+            if (open1) return;
+            if (elect_one()) {
+              products(1);
+              umma_commit(&sh.k_empty[k_stage]);
+            }
+            __syncwarp();
+            open1 = true;
+            half = false;
+          }
           if (++k_stage == kKStages) { k_stage = 0; k_ph ^= 1u; }
-          open |= own;
         }
       };
       scores(s.i0 + 2);
@@ -756,34 +758,37 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
       for (int j = s.i0; j < s.i1 && ok; ++j) {
         const int c = stream_of(s.en, j, s.i0);
         const bool own = c == 2 || c == st;
-        ok = own ? warp_wait_both(&sh.p_ready[st], p_ph, &sh.v_full[v_stage], v_ph) : warp_wait(&sh.v_full[v_stage], v_ph);
-        if (!ok) break;
-        tc_fence_after();
-        if (elect_one()) {
-          if (own) {
-            const uint64_t b = desc_v + v_stage * (2 * OP >> 4);
+        if (own) {
 #pragma unroll
-            for (int k = 0; k < kKeys / 16; ++k) umma_bf16_ts(t_o, t_s + k * 8, b + k * (16 * 128 >> 4), idesc_o, begun || k > 0);
-            umma_commit(&sh.v_empty[v_stage]);
-            if (j == last) umma_commit(&sh.o_full[st]);
-          } else {
-            arrive(&sh.v_empty[v_stage]);
+          for (int h = 0; h < 2; ++h) {
+            if (ok) ok = h == 0 ? warp_wait_both(&sh.p_ready[st][h], p_ph, &sh.v_full[v_stage], v_ph) : warp_wait(&sh.p_ready[st][h], p_ph);
+            if (!ok) break;
+            tc_fence_after();
+            if (elect_one()) {
+              const uint64_t b = desc_v + v_stage * (2 * OP >> 4) + h * (64 * 128 >> 4);
+#pragma unroll
+              for (int k = 0; k < kKeys / 32; ++k) umma_bf16_ts(t_o, t_s + h * 64 + k * 8, b + k * (16 * 128 >> 4), idesc_o, begun || h > 0 || k > 0);
+              umma_commit(&sh.o_done[st][h]);
+              if (h == 1) umma_commit(&sh.v_empty[v_stage]);
+            }
+            __syncwarp();
+            (h == 0 ? open0 : open1) = false;
+            scores(j + 3);
           }
+          begun = true;
+          p_ph ^= 1u;
+        } else {
+          ok = warp_wait(&sh.v_full[v_stage], v_ph);
+          if (ok && elect_one()) arrive(&sh.v_empty[v_stage]);
+          __syncwarp();
+          scores(j + 3);
         }
-        __syncwarp();
         v_stage ^= 1;
         v_ph ^= v_stage == 0;
-        if (own) {
-          p_ph ^= 1u;
-          begun = true;
-          open = false;
-        }
-        scores(j + 3);
       }
     }
     if (!ok) fail();
-  } else if (warp < kSoft / 32) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
+  } else {
     // ------------------------------------------------------------------ softmax warps: a row a thread
     const int st = warp >> 2, quarter = warp & 3, r_in = quarter * 32 + lane;
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16, t_s = tmem + lanes + st * 128, t_o = tmem + lanes + 256;
@@ -791,7 +796,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
     long t = t_begin;
     Span s;
     bool ok = true;
-    uint32_t s_ph = 0, o_ph = 0, tile0 = 0;
+    uint32_t tile0 = 0, done = 0;   // done: this stream's tiles so far
     while (next_span(t, s)) {
       tile0 -= s.i0;
       const int rows = s.en.rows, row_first = s.u.e * kTileRows;
@@ -867,127 +872,133 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
       for (int i = s.i0; i < s.i1; ++i) {
         const int c = stream_of(s.en, i, s.i0);
         if (c != 2 && c != st) continue;
-        ++mine;
         const uint32_t use = tile0 + i, stage = use & 1;
-        if (ok && !warp_wait(&sh.s_full[st], s_ph)) {
-          ok = false;
-          fail();
-        }
-        s_ph ^= 1u;
-        tc_fence_after();
-        const Info f = sh.info[use % kInfo];
-        const int limit = r >= f.ra && r < f.rb ? min(pos, f.k1 - 1) : -1;   // the last key that this row sees
-        if (!__any_sync(0xffffffffu, limit >= f.key0)) {   // (a warp without rows of the segment: no weights)
-          if (warp_rows) {
+        const Info &f = sh.info[use % kInfo];
+        int limit = 0, there = 0, key0 = 0;
+        // (the halves of a tile take turns: while one is worked on, the other's weights are multiplied and its next scores come)
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h) {
+          if (ok && !warp_wait(&sh.s_full[st][h], done & 1)) {
+            ok = false;
+            fail();
+          }
+          tc_fence_after();
+          if (h == 0) {
+            const int4 a = *reinterpret_cast<const int4 *>(&f);
+            key0 = a.x, there = f.there;
+            limit = r >= a.z && r < a.w ? min(pos, a.y - 1) : -1;   // the last key that this row sees
+            ++mine;
+          }
+          const uint32_t t_h = t_s + h * 64;
+          int n_seen = min(max(limit - (key0 + h * 64) + 1, 0), 64);   // of the 64 keys (no row: any number)
+          if (!(there >> h & 1)) {
+            if (n_seen > 0) pool_fault(p.pool.status, SJD_ERR_BAD_ARG);   // (no page where the row sees a key)
+            n_seen = 0;
+          }
+          if (__any_sync(0xffffffffu, n_seen > 0)) {
+            uint32_t x[64];
+            tmem_ld32(t_h, x);
+            tmem_ld32(t_h + 32, x + 32);
+            const float4 up = *reinterpret_cast<const float4 *>(&f.k_up[h * 4]);
+            const float by[4] = {factor * up.x, factor * up.y, factor * up.z, factor * up.w};   // of 16 columns
+            tmem_ld_wait();
+            if (!__all_sync(0xffffffffu, n_seen == 64 || r >= rows)) {   // some row does not see some key
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                const int n = n_seen - 32 * k;
+                const uint32_t bits = n >= 32 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << n) - 1;
+#pragma unroll
+                for (int j = 0; j < 32; ++j) x[k * 32 + j] = bits >> j & 1u ? x[k * 32 + j] : 0xFF800000u;
+              }
+            }
+            float top = -INFINITY;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              const uint32_t *v = x + 16 * c;
+              float a = max3(v[0], v[1], v[2]), b = max3(v[3], v[4], v[5]);
+              a = max3(__float_as_uint(a), v[6], v[7]), b = max3(__float_as_uint(b), v[8], v[9]);
+              a = max3(__float_as_uint(a), v[10], v[11]), b = max3(__float_as_uint(b), v[12], v[13]);
+              a = max3(__float_as_uint(a), v[14], v[15]);
+              top = fmaxf(top, fmaxf(a, b) * by[c]);
+            }
+            // Where a score has outgrown the reference, that, O and the sum follow.
+            const bool need = r < rows && (top > m_ref + kGrow || (m_ref == -INFINITY && top > -INFINITY));
+            if (__builtin_expect(__any_sync(0xffffffffu, need), 0)) {
+              const float g = need ? exp2_fast(m_ref - top) : 1.0f;
+              m_ref = need ? top : m_ref;
+              l *= g;
+              if (mine > 1 || h > 0) {   // (O has been written: when the weights so far have been multiplied)
+                if (ok && !warp_wait(&sh.o_done[st][h ^ 1], (done - 1 + h) & 1)) {
+                  ok = false;
+                  fail();
+                }
+                tc_fence_after();
+#pragma unroll 1
+                for (int c = 0; c < HD / 8; ++c) {
+                  uint32_t v[8];
+                  tmem_ld8(t_o + st * 128 + c * 8, v);
+                  tmem_ld_wait();
+#pragma unroll
+                  for (int j = 0; j < 8; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * g);
+                  tmem_st8(t_o + st * 128 + c * 8, v);
+                }
+              }
+            }
+            const float ref = m_ref == -INFINITY ? 0.0f : m_ref;
+            float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              uint32_t w[16];
+#pragma unroll
+              for (int j = 0; j < 16; ++j) {
+                const float g = by[2 * k + (j >> 3)];
+                float2 y = fma2(make_float2(__uint_as_float(x[32 * k + 2 * j]), __uint_as_float(x[32 * k + 2 * j + 1])), make_float2(g, g), make_float2(-ref, -ref));
+                y.x = exp2_fast(y.x), y.y = exp2_fast(y.y);
+                sum[j & 1] = add2(sum[j & 1], y);
+                w[j] = bf16_pair(y.x, y.y);
+              }
+              tmem_st16(t_h + k * 16, w);   // (over the scores)
+            }
+            l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+            tmem_st_wait();
+          } else if (warp_rows) {   // (a warp without rows that see them: no weights)
             uint32_t w[16];
 #pragma unroll
             for (int k = 0; k < 16; ++k) w[k] = 0;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) tmem_st16(t_s + k * 16, w);
+            tmem_st16(t_h, w);
+            tmem_st16(t_h + 16, w);
             tmem_st_wait();
-            tc_fence_before();
+          }
+          tc_fence_before();
+          if (h == 1) {   // NaN entries of V, which are zeros there, and the rows that see them
+            if (ok && !warp_wait(&sh.v_full[stage], use >> 1 & 1)) {
+              ok = false;
+              fail();
+            }
+            uint32_t any = 0;
+#pragma unroll
+            for (int w = 0; w < kConv / 32; ++w) any |= sh.nan_warps[stage][w];
+            if (__builtin_expect(any, 0)) {
+              constexpr int ROWS = kConv / (HD / 16), WARP = 32 / (HD / 16);
+#pragma unroll 1
+              for (int k = 0; k < kKeys; ++k) {
+                if (!sh.nan_warps[stage][k % ROWS / WARP] || key0 + k > limit) continue;
+#pragma unroll
+                for (int j = 0; j < HD / 32; ++j) nan[j] |= *reinterpret_cast<const uint32_t *>(&sh.nan_dims[stage][k][2 * j]);
+              }
+            }
           }
           __syncwarp();
-          if (lane == 0) arrive(&sh.p_ready[st]);
-          continue;
+          if (lane == 0) arrive(&sh.p_ready[st][h]);
         }
-        // of 16 columns: with the factor of their keys' block
-        const int k_exp0 = f.k_exp[0], k_exp1 = f.k_exp[1];
-        auto factor_of = [&](int block) { return factor * two_to(pool_exp((int8_t)((block < 4 ? k_exp0 : k_exp1) >> (8 * (block & 3))))); };
-        uint32_t x[128];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) tmem_ld32(t_s + k * 32, x + k * 32);
-        tmem_ld_wait();
-        if (!__all_sync(0xffffffffu, limit >= f.key0 + kKeys - 1) || f.there != 3) {   // some row does not see some key
-          if (f.there != 3) {   // (no page where the row sees a key)
-            const int miss = f.there & 1 ? f.key0 + KV_PAGE : f.key0;
-            if (limit >= miss) pool_fault(p.pool.status, SJD_ERR_BAD_ARG);
-          }
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const int n_seen = limit - (f.key0 + k * 32) + 1;
-            uint32_t bits = n_seen >= 32 ? 0xFFFFFFFFu : n_seen <= 0 ? 0u : (1u << n_seen) - 1;   // which of 32 keys this row sees
-            bits = f.there >> (k >> 1) & 1 ? bits : 0u;
-#pragma unroll
-            for (int j = 0; j < 32; ++j) x[k * 32 + j] = bits >> j & 1u ? x[k * 32 + j] : 0xFF800000u;
-          }
-        }
-        float top = -INFINITY;
-#pragma unroll
-        for (int c = 0; c < 8; ++c) {
-          float a = __uint_as_float(x[16 * c]), b = __uint_as_float(x[16 * c + 1]);
-#pragma unroll
-          for (int j = 2; j < 16; j += 4) {
-            a = fmaxf(fmaxf(a, __uint_as_float(x[16 * c + j])), __uint_as_float(x[16 * c + j + 1]));
-            if (j + 2 < 16) b = fmaxf(fmaxf(b, __uint_as_float(x[16 * c + j + 2])), __uint_as_float(x[16 * c + j + 3]));
-          }
-          top = fmaxf(top, fmaxf(a, b) * factor_of(c));
-        }
-        // Where a score has outgrown the reference, that, O and the sum follow.
-        const bool need = top > m_ref + kGrow || (m_ref == -INFINITY && top > -INFINITY);
-        if (__builtin_expect(__any_sync(0xffffffffu, need), 0)) {
-          const float g = need ? exp2_fast(m_ref - top) : 1.0f;
-          m_ref = need ? top : m_ref;
-          l *= g;
-          if (mine > 1) {   // (O has been written)
-#pragma unroll 1
-            for (int c = 0; c < HD / 8; ++c) {
-              uint32_t v[8];
-              tmem_ld8(t_o + st * 128 + c * 8, v);
-              tmem_ld_wait();
-#pragma unroll
-              for (int j = 0; j < 8; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * g);
-              tmem_st8(t_o + st * 128 + c * 8, v);
-            }
-          }
-        }
-        {
-          const float ref = m_ref == -INFINITY ? 0.0f : m_ref;
-          float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
-#pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const float g = factor_of(k);
-            uint32_t w[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              float2 y = fma2(make_float2(__uint_as_float(x[16 * k + 2 * j]), __uint_as_float(x[16 * k + 2 * j + 1])), make_float2(g, g), make_float2(-ref, -ref));
-              y.x = exp2_fast(y.x), y.y = exp2_fast(y.y);
-              sum[j & 1] = add2(sum[j & 1], y);
-              w[j] = bf16_pair(y.x, y.y);
-            }
-            tmem_st8(t_s + k * 8, w);   // (over the scores)
-          }
-          l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
-        }
-        tmem_st_wait();
-        tc_fence_before();
-        // NaN entries of V, which are zeros there, and the rows that see them
-        if (ok && !warp_wait(&sh.v_full[stage], use >> 1 & 1)) {
-          ok = false;
-          fail();
-        }
-        uint32_t any = 0;
-#pragma unroll
-        for (int w = 0; w < kConv / 32; ++w) any |= sh.nan_warps[stage][w];
-        if (__builtin_expect(any, 0)) {
-          constexpr int ROWS = kConv / (HD / 16), WARP = 32 / (HD / 16);
-#pragma unroll 1
-          for (int k = 0; k < kKeys; ++k) {
-            if (!sh.nan_warps[stage][k % ROWS / WARP] || f.key0 + k > limit) continue;
-#pragma unroll
-            for (int j = 0; j < HD / 32; ++j) nan[j] |= *reinterpret_cast<const uint32_t *>(&sh.nan_dims[stage][k][2 * j]);
-          }
-        }
-        __syncwarp();
-        if (lane == 0) arrive(&sh.p_ready[st]);
+        ++done;
       }
       // ---- what this CTA has of the unit: references, sums and O
       if (mine > 0) {
-        if (ok && !warp_wait(&sh.o_full[st], o_ph)) {
+        if (ok && !warp_wait_both(&sh.o_done[st][0], (done - 1) & 1, &sh.o_done[st][1], (done - 1) & 1)) {
           ok = false;
           fail();
         }
-        o_ph ^= 1u;
         tc_fence_after();
       }
       const bool complete = s.i0 == 0 && s.i1 == tiles_of(s.en);
@@ -1057,8 +1068,6 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
       tc_fence_after();
       tile0 += s.i1;
     }
-  } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
   }
   tc_fence_before();
   __syncthreads();
