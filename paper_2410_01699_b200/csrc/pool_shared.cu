@@ -36,6 +36,7 @@ constexpr int kInfo = 8;                // tiles whose notes are kept: more than
 constexpr int kKStages = 3;
 constexpr int kConv = 128, kSoft = 256, kThreads = kSoft + kConv + 96;
 constexpr int kPlanThreads = 1024;
+constexpr int kCosts = 1024;            // units of a kv head whose places the plan keeps in shared memory
 constexpr float kGrow = 8.0f;           // log2 of what a maximum may grow before its reference follows
 
 struct Segment {       // keys k0 .. k1 - 1 of a sequence's table, for rows ra .. rb - 1 of a unit
@@ -79,7 +80,7 @@ __device__ __forceinline__ int row_position(const SharedParams &p, int b, int k,
 __global__ void __launch_bounds__(kPlanThreads) shared_plan_kernel(const __grid_constant__ SharedParams p) {
   __shared__ int lo[kMaxSeqs], hi[kMaxSeqs], group_of[kMaxSeqs], seq_of[kMaxSeqs];              // by sequence of the call
   __shared__ int share[kMaxSeqs], leader[kMaxSeqs], live[kMaxSeqs], begin[kMaxSeqs + 1];         // by group
-  __shared__ int bad, sums[32];
+  __shared__ int bad, sums[32], costs[kCosts];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = kPlanThreads / 32;
   pdl_wait();
   pdl_trigger();
@@ -210,14 +211,15 @@ __global__ void __launch_bounds__(kPlanThreads) shared_plan_kernel(const __grid_
     if (lane == 0) {
       p.entry[e] = en;
       const int cost = 2 * en.tiles[0] + en.tiles[1] + en.tiles[2];
-      p.before[e + 1] = cost > 0 ? cost + kUnit : 0;   // (its own so far)
+      (p.n_entries <= kCosts ? costs[e] : p.before[e + 1]) = cost > 0 ? cost + kUnit : 0;   // (its own so far)
     }
   }
   __syncthreads();
   // places on the line, sums over the units before
   const int run = (p.n_entries + kPlanThreads - 1) / kPlanThreads, e0 = min(p.n_entries, tid * run), e1 = min(p.n_entries, e0 + run);
   int cost = 0;
-  for (int e = e0; e < e1; ++e) cost += p.before[e + 1];
+  auto cost_of = [&](int e) { return p.n_entries <= kCosts ? costs[e] : p.before[e + 1]; };
+  for (int e = e0; e < e1; ++e) cost += cost_of(e);
   int x = cost;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -228,7 +230,10 @@ __global__ void __launch_bounds__(kPlanThreads) shared_plan_kernel(const __grid_
   __syncthreads();
   for (int w = 0; w < warp; ++w) x += sums[w];
   int at = x - cost;
-  for (int e = e0; e < e1; ++e) p.before[e + 1] = at += p.before[e + 1];
+  for (int e = e0; e < e1; ++e) {
+    at += cost_of(e);
+    p.before[e + 1] = at;
+  }
   if (tid == 0) p.before[0] = 0;
 }
 
@@ -364,18 +369,24 @@ struct alignas(16) Info {   // of a tile
   float k_up[8];            // 2^exponent of its blocks of keys
   uint32_t v_up[8];         // and of values, times 2^120, twice in bf16 (exponents up to 0)
 };
-__device__ __forceinline__ uint32_t e4m3_of_floats(const float *v) {   // four, the first one in the low byte
+// pairs of fp16, and four e4m3 numbers in a word
+__device__ __forceinline__ uint32_t halves_of_floats(float a, float b) {
+  uint32_t h;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(h) : "f"(b), "f"(a));
+  return h;
+}
+__device__ __forceinline__ uint32_t e4m3_of_halves(uint32_t a, uint32_t b) {
   uint32_t r;
-  asm("{\n\t.reg .b16 x, y;\n\tcvt.rn.satfinite.e4m3x2.f32 x, %2, %1;\n\tcvt.rn.satfinite.e4m3x2.f32 y, %4, %3;\n\tmov.b32 %0, {x, y};\n\t}"
-      : "=r"(r)
-      : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]));
+  asm("{\n\t.reg .b16 x, y;\n\tcvt.rn.satfinite.e4m3x2.f16x2 x, %1;\n\tcvt.rn.satfinite.e4m3x2.f16x2 y, %2;\n\tmov.b32 %0, {x, y};\n\t}" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
-__device__ __forceinline__ void floats_of_e4m3(uint32_t v, float *f) {   // four
-  uint32_t a, b;
+__device__ __forceinline__ void halves_of_e4m3(uint32_t v, uint32_t &a, uint32_t &b) {
   asm("{\n\t.reg .b16 x, y;\n\tmov.b32 {x, y}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, x;\n\tcvt.rn.f16x2.e4m3x2 %1, y;\n\t}" : "=r"(a), "=r"(b) : "r"(v));
-  asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %2;\n\tcvt.f32.f16 %0, lo;\n\tcvt.f32.f16 %1, hi;\n\t}" : "=f"(f[0]), "=f"(f[1]) : "r"(a));
-  asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %2;\n\tcvt.f32.f16 %0, lo;\n\tcvt.f32.f16 %1, hi;\n\t}" : "=f"(f[2]), "=f"(f[3]) : "r"(b));
+}
+__device__ __forceinline__ uint32_t sub_halves(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
 }
 __device__ __forceinline__ void umma_e4m3(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, bool accumulate) {
   asm volatile(
@@ -793,52 +804,53 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
       int pos = -1;   // of this thread's row
       // ---- queries of the unit's rows: a power of two brings a row's largest entry to 128 .. 256, then its two numbers; a row is HD / 4 lanes
       {
-        constexpr int LANES = HD / 8, PER = 32 / LANES, U = 4;   // lanes of a row, rows of a warp's load, loads under way
+        constexpr int LANES = HD / 8, PER = 32 / LANES, U = 4, STEP = kSoft / 32 * PER;   // lanes of a row, rows of a warp's load, loads under way, rows between them
         const int sub = lane / LANES, dim = lane % LANES * 8;
-#pragma unroll 1
-        for (int r0 = warp * PER; r0 < rows; r0 += kSoft / 32 * PER * U) {
-          uint2 x[U][2];
+        const __nv_bfloat16 *q = p.q + (long)s.u.h * p.group * HD + dim;
+        auto load = [&](int r0, uint2 (&x)[U][2]) {
 #pragma unroll
           for (int j = 0; j < U; ++j) {
-            const int y = row_first + min(r0 + j * (kSoft / 32) * PER + sub, rows - 1), m = y / p.group;
-            const uint2 *from = reinterpret_cast<const uint2 *>(p.q + (long)m * p.q_stride + ((long)s.u.h * p.group + (y - m * p.group)) * HD + dim);
+            const int y = row_first + min(r0 + j * STEP + sub, rows - 1), m = y / p.group;
+            const uint2 *from = reinterpret_cast<const uint2 *>(q + (long)m * p.q_stride + (y - m * p.group) * HD);
             x[j][0] = from[0], x[j][1] = from[1];
           }
+        };
+        uint2 x[U][2], next[U][2];
+        load(warp * PER, x);
+#pragma unroll 1
+        for (int r0 = warp * PER; r0 < rows; r0 += STEP * U) {
+          load(r0 + STEP * U, next);   // (behind the last: the last row)
 #pragma unroll
           for (int j = 0; j < U; ++j) {
-            const int y = r0 + j * (kSoft / 32) * PER + sub;
-            float v[8], top = 0.0f;
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-              v[4 * c] = __uint_as_float(x[j][c].x << 16), v[4 * c + 1] = __uint_as_float(x[j][c].x & 0xFFFF0000u);
-              v[4 * c + 2] = __uint_as_float(x[j][c].y << 16), v[4 * c + 3] = __uint_as_float(x[j][c].y & 0xFFFF0000u);
-            }
-#pragma unroll
-            for (int c = 0; c < 8; ++c) {
-              if (fabsf(v[c]) == INFINITY) v[c] = __int_as_float(0x7FFFFFFF);   // (e4m3 has no infinity: its row is NaN, as it would be)
-              top = fmaxf(top, fabsf(v[c]));
-            }
+            const int y = r0 + j * STEP + sub;
+            float v[8];
+            v[0] = __uint_as_float(x[j][0].x << 16), v[1] = __uint_as_float(x[j][0].x & 0xFFFF0000u);
+            v[2] = __uint_as_float(x[j][0].y << 16), v[3] = __uint_as_float(x[j][0].y & 0xFFFF0000u);
+            v[4] = __uint_as_float(x[j][1].x << 16), v[5] = __uint_as_float(x[j][1].x & 0xFFFF0000u);
+            v[6] = __uint_as_float(x[j][1].y << 16), v[7] = __uint_as_float(x[j][1].y & 0xFFFF0000u);
+            float top = fmaxf(fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3]))), fmaxf(fmaxf(fabsf(v[4]), fabsf(v[5])), fmaxf(fabsf(v[6]), fabsf(v[7]))));
 #pragma unroll
             for (int o = LANES / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
             int e = top > 0.0f ? 7 - (int)((__float_as_uint(top) >> 23) - 127) : 0;
             e = max(min(e, 126), -126);   // (entries below 2^-119 lose places)
-            const float up = two_to(e);
+            const float up = top == INFINITY ? __int_as_float(0x7FFFFFFF) : two_to(e);   // (e4m3 has no infinity: its row is NaN, as it would be)
+            uint32_t h[4], first[2], second[2];   // (fp16 holds eight bits of what is 2^-10 or more)
 #pragma unroll
-            for (int c = 0; c < 8; ++c) v[c] *= up;
+            for (int c = 0; c < 4; ++c) h[c] = halves_of_floats(v[2 * c] * up, v[2 * c + 1] * up);
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              first[c] = e4m3_of_halves(h[2 * c], h[2 * c + 1]);
+              uint32_t a, b;
+              halves_of_e4m3(first[c], a, b);
+              second[c] = e4m3_of_halves(sub_halves(h[2 * c], a), sub_halves(h[2 * c + 1], b));
+            }
             if (y < rows) {
               uint8_t *to = Qs + (y >> 7) * 2 * OP + swizzled<HD>(y & 127, dim);   // (eight bytes stay together)
-#pragma unroll
-              for (int l = 0; l < 2; ++l) {
-                const uint32_t a = e4m3_of_floats(v), b = e4m3_of_floats(v + 4);
-                *reinterpret_cast<uint2 *>(to + l * OP) = make_uint2(a, b);
-                float w[8];
-                floats_of_e4m3(a, w);
-                floats_of_e4m3(b, w + 4);
-#pragma unroll
-                for (int c = 0; c < 8; ++c) v[c] -= w[c];
-              }
+              *reinterpret_cast<uint2 *>(to) = make_uint2(first[0], first[1]);
+              *reinterpret_cast<uint2 *>(to + OP) = make_uint2(second[0], second[1]);
               if (dim == 0) sh.factor[y >> 7][y & 127] = p.scale * two_to(-e);
             }
+            x[j][0] = next[j][0], x[j][1] = next[j][1];
           }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
