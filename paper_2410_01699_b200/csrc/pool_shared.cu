@@ -30,7 +30,6 @@ constexpr int kUnit = 6;                // what a unit's begin and end take, in 
 constexpr int kLeast = 2;               // common pages that are worth a tile of their own
 constexpr int kMaxCtas = 192;
 constexpr int kMaxSeqs = SJD_POOL_MAX_LIST;
-constexpr int kBefore = 512;            // units of a kv head whose places are kept in shared memory
 constexpr int kSegs = 128;              // segments of a unit that are kept there
 constexpr int kInfo = 8;                // tiles whose notes are kept: more than copies are ahead of weights
 constexpr int kKStages = 3;
@@ -47,6 +46,14 @@ struct Entry {         // 256 rows of a kv head
   int n_segs[3], tiles[3];
   int rows;
 };
+struct Unit {
+  int e, h;
+  long first;          // place of its first tile
+};
+struct Begin {         // the unit in which a CTA begins
+  Unit u;
+  Entry en;
+};
 struct SharedParams {
   sjd_pool pool;
   int layer, batch, window, n_heads, group, rows, n_entries, n_groups;   // rows: window * group
@@ -55,9 +62,11 @@ struct SharedParams {
   long q_stride, out_stride;
   const int32_t *seqs, *in_pos, *group_begin;
   __nv_bfloat16 *out;
+  long *all;           // places of the call
   int *before;         // [n_entries + 1]: places of a kv head in the units before
   Entry *entry;        // [n_entries]
   Segment *segs;
+  Begin *begin;        // [ctas]
   float2 *stats;       // (reference, sum) of a row's part
   float *parts;        // [HD / 4][rows of the part][4]
   int ctas;
@@ -74,6 +83,20 @@ __device__ __forceinline__ int row_position(const SharedParams &p, int b, int k,
     at = -1;
   }
   return at;
+}
+
+__device__ __forceinline__ int tiles_of(const Entry &en) { return en.tiles[0] + en.tiles[1] + en.tiles[2]; }
+// tiles of a unit that begin before place t: those for both streams take two places
+__device__ __forceinline__ int tiles_before(const Entry &en, long first, long t) {
+  const long in = t - first;
+  if (in <= 0) return 0;
+  if (in <= 2l * en.tiles[0]) return (int)((in + 1) >> 1);
+  const long n = in - en.tiles[0];
+  return n < tiles_of(en) ? (int)n : tiles_of(en);
+}
+__device__ __forceinline__ long range_of(long all, int ctas) {
+  const long least = 2 * kUnit, chunk = (all + ctas - 1) / ctas;
+  return chunk < least ? least : chunk;
 }
 
 // ---------------------------------------------------------------------------------------------------------------- plan
@@ -235,42 +258,31 @@ __global__ void __launch_bounds__(kPlanThreads) shared_plan_kernel(const __grid_
     p.before[e + 1] = at;
   }
   if (tid == 0) p.before[0] = 0;
+  __syncthreads();
+  // where every CTA begins
+  const long all = (long)p.before[p.n_entries] * p.pool.n_kv_heads, chunk = range_of(all, p.ctas);
+  for (int c = tid; c < p.ctas; c += kPlanThreads) {
+    const long t = c * chunk;
+    Begin b;
+    b.u.e = b.u.h = 0, b.u.first = 0;
+    if (t < all) {
+      int lo = 0, hi = p.n_entries - 1;
+      while (lo < hi) {   // last unit that begins at t or before
+        const int mid = (lo + hi + 1) >> 1;
+        if ((long)p.before[mid] * p.pool.n_kv_heads <= t) lo = mid; else hi = mid - 1;
+      }
+      const int b0 = p.before[lo], cost = p.before[lo + 1] - b0;
+      b.u.e = lo;
+      b.u.h = (int)((t - (long)b0 * p.pool.n_kv_heads) / cost);
+      b.u.first = (long)b0 * p.pool.n_kv_heads + (long)b.u.h * cost + kUnit;
+    }
+    b.en = p.entry[b.u.e];
+    p.begin[c] = b;
+  }
+  if (tid == 0) *p.all = all;
 }
 
 // ---------------------------------------------------------------------------------------------------------------- units
-struct Unit {
-  int e, h;
-  long first;          // place of its first tile
-};
-// the unit that place t is in
-template <typename Before>
-__device__ __forceinline__ Unit unit_at(const SharedParams &p, const Before &before, long t) {
-  int lo = 0, hi = p.n_entries - 1;
-  const int heads = p.pool.n_kv_heads;
-  while (lo < hi) {   // last entry that begins at t or before
-    const int mid = (lo + hi + 1) >> 1;
-    if ((long)before(mid) * heads <= t) lo = mid; else hi = mid - 1;
-  }
-  const int b = before(lo), cost = before(lo + 1) - b;
-  Unit u;
-  u.e = lo;
-  u.h = (int)((t - (long)b * heads) / cost);
-  u.first = (long)b * heads + (long)u.h * cost + kUnit;
-  return u;
-}
-__device__ __forceinline__ int tiles_of(const Entry &en) { return en.tiles[0] + en.tiles[1] + en.tiles[2]; }
-// tiles of a unit that begin before place t: those for both streams take two places
-__device__ __forceinline__ int tiles_before(const Entry &en, long first, long t) {
-  const long in = t - first;
-  if (in <= 0) return 0;
-  if (in <= 2l * en.tiles[0]) return (int)((in + 1) >> 1);
-  const long n = in - en.tiles[0];
-  return n < tiles_of(en) ? (int)n : tiles_of(en);
-}
-__device__ __forceinline__ long range_of(long all, int ctas) {
-  const long least = 2 * kUnit, chunk = (all + ctas - 1) / ctas;
-  return chunk < least ? least : chunk;
-}
 // which streams tile i of a unit is for (0, 1, 2: both); `from`: the first tile of the CTA.  The tiles of the two streams take turns.
 __device__ __forceinline__ int stream_of(const Entry &en, int i, int from) {
   if (one_stream(en.rows)) return (i - from) & 1;
@@ -427,7 +439,6 @@ struct SharedSmem {
   float2 stat[2][128];                         // of both streams' rows
   uint32_t nan_row[2][128][HD / 32];
   float factor[2][128];                        // of the scores of a row: the scale, and what its query was multiplied by
-  int before[kBefore];
   Segment segs[kSegs];
 };
 
@@ -468,35 +479,41 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   pdl_wait();
-  const bool near = p.n_entries < kBefore;
-  if (near)
-    for (int i = tid; i <= p.n_entries; i += kThreads) sh.before[i] = p.before[i];
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = sh.tmem_base;
-  auto before = [&](int e) { return near ? sh.before[e] : p.before[e]; };
-  const long all = (long)before(p.n_entries) * kv_heads, chunk = range_of(all, gridDim.x);
+  const long all = *p.all, chunk = range_of(all, gridDim.x);
   const long t_begin = min(all, blockIdx.x * chunk), t_end = min(all, t_begin + chunk);
   auto fail = [&]() {
     if (lane == 0) pool_fault(p.pool.status, SJD_ERR_DEVICE_TIMEOUT);
   };
-  // this CTA's next unit with tiles from place t on: tiles i0 .. i1 - 1 of it; false: no more
+  // This CTA's units that have tiles in its range, one after the other: tiles i0 .. i1 - 1 of one.  (t: the end of the last, 0 before the first.)
   struct Span {
     Unit u;
     Entry en;
     int i0, i1;
   };
   auto next_span = [&](long &t, Span &s) {
-    while (t < t_end) {
-      s.u = unit_at(p, before, t);
-      s.en = p.entry[s.u.e];
+    for (;;) {
+      if (t == 0) {
+        if (t_begin == t_end) return false;
+        const Begin b = p.begin[blockIdx.x];
+        s.u = b.u, s.en = b.en;
+      } else {
+        if (t >= t_end) return false;
+        if (++s.u.h == kv_heads) {
+          s.u.h = 0;
+          do s.en = p.entry[++s.u.e];
+          while (tiles_of(s.en) == 0);   // (t < all: there is one)
+        }
+        s.u.first = t + kUnit;
+      }
       s.i0 = tiles_before(s.en, s.u.first, t_begin);
       s.i1 = tiles_before(s.en, s.u.first, t_end);
       t = s.u.first + tiles_of(s.en) + s.en.tiles[0];
       if (s.i1 > s.i0) return true;
     }
-    return false;
   };
 
   if (warp == COPY) {
@@ -506,7 +523,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
       int n, h;                                   // tiles, kv head
       int key0, k1, ra, rb, page[2], k_exp[2], v_exp[2];   // of this lane's
     };
-    long t = t_begin;
+    long t = 0;
     Span s;
     bool more = false, kept = false;
     int i = 0;
@@ -629,7 +646,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
     const uint32_t at0 = (uint32_t)(seg >> 2) * (128 * 128) + row0 * 128 + ((((seg & 3) * 2) ^ (row0 & 7)) << 4);
     long tiles = 0;
     {
-      long t = t_begin;
+      long t = 0;
       Span s;
       while (next_span(t, s)) tiles += s.i1 - s.i0;
     }
@@ -713,7 +730,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
     const uint64_t desc_k = rows_desc<HD>() | (uint64_t)(smem_u32(Ks) >> 4);
     const uint64_t desc_v = (uint64_t)(128 * 128 >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61 | (uint64_t)(smem_u32(Vs) >> 4);
     const uint32_t t_s = tmem + st * 128, t_o = tmem + 256 + st * 128;
-    long t = t_begin;
+    long t = 0;
     Span s;
     bool ok = true;
     uint32_t q_ph = 0, p_ph = 0;
@@ -792,7 +809,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
     const int st = warp >> 2, quarter = warp & 3, r_in = quarter * 32 + lane;
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16, t_s = tmem + lanes + st * 128, t_o = tmem + lanes + 256;
     auto sync = [&]() { asm volatile("bar.sync 1, %0;" ::"n"(kSoft) : "memory"); };
-    long t = t_begin;
+    long t = 0;
     Span s;
     bool ok = true;
     uint32_t tile0 = 0, done = 0;   // done: this stream's tiles so far
@@ -820,37 +837,59 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
 #pragma unroll 1
         for (int r0 = warp * PER; r0 < rows; r0 += STEP * U) {
           load(r0 + STEP * U, next);   // (behind the last: the last row)
+          // (each step for all of the rows: it takes that many to hide its latency)
+          float v[U][8], top[U], up[U];
+          int e[U];
+#pragma unroll
+          for (int j = 0; j < U; ++j) {
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              v[j][4 * c] = __uint_as_float(x[j][c].x << 16), v[j][4 * c + 1] = __uint_as_float(x[j][c].x & 0xFFFF0000u);
+              v[j][4 * c + 2] = __uint_as_float(x[j][c].y << 16), v[j][4 * c + 3] = __uint_as_float(x[j][c].y & 0xFFFF0000u);
+            }
+            top[j] = fmaxf(fmaxf(fmaxf(fabsf(v[j][0]), fabsf(v[j][1])), fmaxf(fabsf(v[j][2]), fabsf(v[j][3]))),
+                           fmaxf(fmaxf(fabsf(v[j][4]), fabsf(v[j][5])), fmaxf(fabsf(v[j][6]), fabsf(v[j][7]))));
+            x[j][0] = next[j][0], x[j][1] = next[j][1];
+          }
+#pragma unroll
+          for (int o = LANES / 2; o > 0; o >>= 1) {
+            float other[U];
+#pragma unroll
+            for (int j = 0; j < U; ++j) other[j] = __shfl_xor_sync(0xffffffffu, top[j], o);
+#pragma unroll
+            for (int j = 0; j < U; ++j) top[j] = fmaxf(top[j], other[j]);
+          }
+          uint32_t h[U][4], first[U][2];   // (fp16 holds eight bits of what is 2^-10 or more)
+#pragma unroll
+          for (int j = 0; j < U; ++j) {
+            e[j] = top[j] > 0.0f ? 7 - (int)((__float_as_uint(top[j]) >> 23) - 127) : 0;
+            e[j] = max(min(e[j], 126), -126);   // (entries below 2^-119 lose places)
+            up[j] = top[j] == INFINITY ? __int_as_float(0x7FFFFFFF) : two_to(e[j]);   // (e4m3 has no infinity: its row is NaN, as it would be)
+          }
+#pragma unroll
+          for (int j = 0; j < U; ++j)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) h[j][c] = halves_of_floats(v[j][2 * c] * up[j], v[j][2 * c + 1] * up[j]);
+#pragma unroll
+          for (int j = 0; j < U; ++j)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) first[j][c] = e4m3_of_halves(h[j][2 * c], h[j][2 * c + 1]);
 #pragma unroll
           for (int j = 0; j < U; ++j) {
             const int y = r0 + j * STEP + sub;
-            float v[8];
-            v[0] = __uint_as_float(x[j][0].x << 16), v[1] = __uint_as_float(x[j][0].x & 0xFFFF0000u);
-            v[2] = __uint_as_float(x[j][0].y << 16), v[3] = __uint_as_float(x[j][0].y & 0xFFFF0000u);
-            v[4] = __uint_as_float(x[j][1].x << 16), v[5] = __uint_as_float(x[j][1].x & 0xFFFF0000u);
-            v[6] = __uint_as_float(x[j][1].y << 16), v[7] = __uint_as_float(x[j][1].y & 0xFFFF0000u);
-            float top = fmaxf(fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3]))), fmaxf(fmaxf(fabsf(v[4]), fabsf(v[5])), fmaxf(fabsf(v[6]), fabsf(v[7]))));
-#pragma unroll
-            for (int o = LANES / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-            int e = top > 0.0f ? 7 - (int)((__float_as_uint(top) >> 23) - 127) : 0;
-            e = max(min(e, 126), -126);   // (entries below 2^-119 lose places)
-            const float up = top == INFINITY ? __int_as_float(0x7FFFFFFF) : two_to(e);   // (e4m3 has no infinity: its row is NaN, as it would be)
-            uint32_t h[4], first[2], second[2];   // (fp16 holds eight bits of what is 2^-10 or more)
-#pragma unroll
-            for (int c = 0; c < 4; ++c) h[c] = halves_of_floats(v[2 * c] * up, v[2 * c + 1] * up);
+            uint32_t second[2];
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-              first[c] = e4m3_of_halves(h[2 * c], h[2 * c + 1]);
               uint32_t a, b;
-              halves_of_e4m3(first[c], a, b);
-              second[c] = e4m3_of_halves(sub_halves(h[2 * c], a), sub_halves(h[2 * c + 1], b));
+              halves_of_e4m3(first[j][c], a, b);
+              second[c] = e4m3_of_halves(sub_halves(h[j][2 * c], a), sub_halves(h[j][2 * c + 1], b));
             }
             if (y < rows) {
               uint8_t *to = Qs + (y >> 7) * 2 * OP + swizzled<HD>(y & 127, dim);   // (eight bytes stay together)
-              *reinterpret_cast<uint2 *>(to) = make_uint2(first[0], first[1]);
+              *reinterpret_cast<uint2 *>(to) = make_uint2(first[j][0], first[j][1]);
               *reinterpret_cast<uint2 *>(to + OP) = make_uint2(second[0], second[1]);
-              if (dim == 0) sh.factor[y >> 7][y & 127] = p.scale * two_to(-e);
+              if (dim == 0) sh.factor[y >> 7][y & 127] = p.scale * two_to(-e[j]);
             }
-            x[j][0] = next[j][0], x[j][1] = next[j][1];
           }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -1096,7 +1135,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) shared_join_kernel(const __gr
   const int h = (int)(blockIdx.x % kv_heads), r0 = (int)(blockIdx.x / kv_heads) * 8, r = min(r0 + (lane & 7), all_rows - 1), d0 = lane >> 3;
   const int e = r0 / kTileRows, in = r - e * kTileRows;   // (the eight rows are of one unit)
   const int b0 = p.before[e], cost = p.before[e + 1] - b0;
-  const long chunk = range_of((long)p.before[p.n_entries] * kv_heads, p.ctas);
+  const long chunk = range_of(*p.all, p.ctas);
   float4 acc[D];
 #pragma unroll
   for (int i = 0; i < D; ++i) acc[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -1167,7 +1206,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) shared_join_kernel(const __gr
 // ---------------------------------------------------------------------------------------------------------------- host
 struct SharedLayout {
   int64_t entries, rows;          // units of a kv head; rows of parts
-  size_t entry, segs, stats, parts, bytes;
+  size_t before, entry, segs, begin, stats, parts, bytes;
 };
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 SharedLayout layout_of(const sjd_pool &pool, int64_t batch, int64_t window, int64_t n_heads) {
@@ -1175,9 +1214,11 @@ SharedLayout layout_of(const sjd_pool &pool, int64_t batch, int64_t window, int6
   const int64_t rows = batch * window * (n_heads / pool.n_kv_heads);
   l.entries = (rows + kTileRows - 1) / kTileRows;
   l.rows = (l.entries * pool.n_kv_heads + kMaxCtas) * kTileRows;
-  l.entry = up256((l.entries + 1) * sizeof(int));
+  l.before = 256;
+  l.entry = l.before + up256((l.entries + 1) * sizeof(int));
   l.segs = l.entry + up256(l.entries * sizeof(Entry));
-  l.stats = l.segs + up256((2 * batch + 2 * l.entries) * sizeof(Segment));
+  l.begin = l.segs + up256((2 * batch + 2 * l.entries) * sizeof(Segment));
+  l.stats = l.begin + up256(kMaxCtas * sizeof(Begin));
   l.parts = l.stats + up256(l.rows * sizeof(float2));
   l.bytes = l.parts + up256((size_t)l.rows * pool.head_dim * sizeof(float));
   return l;
@@ -1229,7 +1270,7 @@ extern "C" int sjd_pool_attention_shared(const sjd_pool *pool, int layer, int ba
   p.q = (const __nv_bfloat16 *)q, p.q_stride = q_stride, p.out = (__nv_bfloat16 *)out, p.out_stride = out_stride;
   p.seqs = seqs, p.in_pos = in_pos, p.group_begin = group_begin;
   char *at = (char *)ws;
-  p.before = (int *)at, p.entry = (Entry *)(at + l.entry), p.segs = (Segment *)(at + l.segs);
+  p.all = (long *)at, p.before = (int *)(at + l.before), p.begin = (Begin *)(at + l.begin), p.entry = (Entry *)(at + l.entry), p.segs = (Segment *)(at + l.segs);
   p.stats = (float2 *)(at + l.stats), p.parts = (float *)(at + l.parts);
   p.ctas = sms < kMaxCtas ? sms : kMaxCtas;
   TensorMap tm;
