@@ -431,7 +431,7 @@ __device__ __forceinline__ uint32_t swizzled(uint32_t row, uint32_t col) {
 
 template <int HD>
 struct SharedSmem {
-  uint64_t k_full[kKStages], k_empty[kKStages], raw_full[2], raw_empty[2], v_full[2], v_empty[2], s_full[2], p_ready[2][2], o_done[2][2], q_ready;
+  uint64_t k_full[kKStages], k_empty[kKStages], raw_full[2], raw_empty[2], v_full[2], v_empty[2], s_full[2][2], p_ready[2][2], o_done[2][2], q_ready;
   uint32_t tmem_base;
   Info info[kInfo];
   uint32_t nan_warps[2][kConv / 32];           // some entry of V that a warp turned was NaN
@@ -463,8 +463,8 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
       mbar_init(&sh.raw_empty[i], kConv / 32);
       mbar_init(&sh.v_full[i], kConv / 32);
       mbar_init(&sh.v_empty[i], 2);
-      mbar_init(&sh.s_full[i], 1);
       for (int h = 0; h < 2; ++h) {
+        mbar_init(&sh.s_full[i][h], 1);
         mbar_init(&sh.p_ready[i][h], 4);
         mbar_init(&sh.o_done[i][h], 1);
       }
@@ -724,7 +724,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
     if (!ok) fail();
   } else if (warp == ISSUE || warp == ISSUE + 1) {
     // ------------------------------------------------------------------ products of a stream; of tiles that are the other's alone it only lets go
-    constexpr uint32_t idesc_s = (1u << 4) | (uint32_t)(kKeys >> 3) << 17 | (uint32_t)(128 >> 4) << 24;   // e4m3 both
+    constexpr uint32_t idesc_s = (1u << 4) | (uint32_t)(kKeys / 2 >> 3) << 17 | (uint32_t)(128 >> 4) << 24;   // e4m3 both
     constexpr uint32_t idesc_o = (1u << 4) | (1u << 7) | (1u << 10) | 1u << 16 | (uint32_t)(HD >> 3) << 17 | (uint32_t)(128 >> 4) << 24;   // V: dims follow one another
     const int st = warp - ISSUE;
     const uint64_t desc_k = rows_desc<HD>() | (uint64_t)(smem_u32(Ks) >> 4);
@@ -740,34 +740,45 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
       ok = warp_wait(&sh.q_ready, q_ph);
       q_ph ^= 1u;
       const uint64_t desc_q = rows_desc<HD>() | (uint64_t)((smem_u32(Qs) + (one_stream(s.en.rows) ? 0 : st * 2 * OP)) >> 4);
-      // Scores of the tiles before `end`, up to those of an own tile while the weights of the one before have not been multiplied.  (No further than
-      // two tiles ahead of the values: what the copies wait for is let go of there.)
+      // Scores of the halves of the own tiles before `end`, each when the weights in its columns have been multiplied.  (No further than two tiles ahead
+      // of the values: what the copies wait for is let go of there.)
       int i = s.i0;
-      bool open = false;
+      bool half = false, open0 = false, open1 = false;   // the first half of tile i has its scores; weights that have not been multiplied
+      auto products = [&](int h) {
+        const uint64_t b = desc_k + k_stage * (OP >> 4) + h * (OP / 2 >> 4);
+#pragma unroll
+        for (int k = 0; k < HD / 32; ++k) umma_e4m3(t_s + h * 64, desc_q + k * 2, b + k * 2, idesc_s, k > 0);
+#pragma unroll
+        for (int k = 0; k < HD / 32; ++k) umma_e4m3(t_s + h * 64, desc_q + (OP >> 4) + k * 2, b + k * 2, idesc_s, true);
+        umma_commit(&sh.s_full[st][h]);
+      };
       auto scores = [&](int end) {
         for (; i < min(end, s.i1); ++i) {
           const int c = stream_of(s.en, i, s.i0);
           const bool own = c == 2 || c == st;
-          if (own && open) return;
-          ok = warp_wait(&sh.k_full[k_stage], k_ph);
-          if (!ok) return;
-          tc_fence_after();
-          if (elect_one()) {
-            if (own) {
-              const uint64_t b = desc_k + k_stage * (OP >> 4);
-#pragma unroll
-              for (int k = 0; k < HD / 32; ++k) umma_e4m3(t_s, desc_q + k * 2, b + k * 2, idesc_s, k > 0);
-#pragma unroll
-              for (int k = 0; k < HD / 32; ++k) umma_e4m3(t_s, desc_q + (OP >> 4) + k * 2, b + k * 2, idesc_s, true);
-              umma_commit(&sh.s_full[st]);
-              umma_commit(&sh.k_empty[k_stage]);
-            } else {
-              arrive(&sh.k_empty[k_stage]);
+          if (!half) {
+            if (own && open0) return;
+            ok = warp_wait(&sh.k_full[k_stage], k_ph);
+            if (!ok) return;
+            tc_fence_after();
+            if (elect_one()) {
+              if (own) products(0);
+              else arrive(&sh.k_empty[k_stage]);
             }
+            __syncwarp();
+            if (own) half = open0 = true;
           }
-          __syncwarp();
+          if (own) {
+            if (open1) return;
+            if (elect_one()) {
+              products(1);
+              umma_commit(&sh.k_empty[k_stage]);
+            }
+            __syncwarp();
+            open1 = true;
+            half = false;
+          }
           if (++k_stage == kKStages) { k_stage = 0; k_ph ^= 1u; }
-          open |= own;
         }
       };
       scores(s.i0 + 2);
@@ -789,9 +800,10 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
               if (h == 1) umma_commit(&sh.v_empty[v_stage]);
             }
             __syncwarp();
+            (h == 0 ? open0 : open1) = false;
+            if (h == 0) scores(j + 2);
           }
           begun = true;
-          open = false;
           p_ph ^= 1u;
         } else {
           ok = warp_wait(&sh.v_full[v_stage], v_ph);
@@ -914,15 +926,15 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
         const uint32_t use = tile0 + i, stage = use & 1;
         const Info &f = sh.info[use % kInfo];
         int limit = 0, there = 0, key0 = 0;
-        // (in halves: the weights of the first are multiplied while the second is worked on)
+        // (the halves take turns: while one is worked on, the other's weights are multiplied and its next scores come)
 #pragma unroll 1
         for (int h = 0; h < 2; ++h) {
+          if (ok && !warp_wait(&sh.s_full[st][h], done & 1)) {
+            ok = false;
+            fail();
+          }
+          tc_fence_after();
           if (h == 0) {
-            if (ok && !warp_wait(&sh.s_full[st], done & 1)) {
-              ok = false;
-              fail();
-            }
-            tc_fence_after();
             const int4 a = *reinterpret_cast<const int4 *>(&f);
             key0 = a.x, there = f.there;
             limit = r >= a.z && r < a.w ? min(pos, a.y - 1) : -1;   // the last key that this row sees
@@ -967,8 +979,8 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
               m_ref = need ? top : m_ref;
               l *= g;
               if (mine > 1 || h > 0) {   // O has been written
-                // (the scores have waited for the products of the tiles before; those of this tile's first half may be under way)
-                if (h > 0 && ok && !warp_wait(&sh.o_done[st][0], done & 1)) {
+                // (the scores have waited for the products of their half of the tile before; those of the half before this one may be under way)
+                if (ok && !warp_wait(&sh.o_done[st][h ^ 1], (done - 1 + h) & 1)) {
                   ok = false;
                   fail();
                 }
