@@ -26,7 +26,8 @@ namespace {
 
 constexpr int kKeys = 128;              // of a tile
 constexpr int kTileRows = 256;          // of a unit
-constexpr int kUnit = 6;                // what a unit's begin and end take, in tiles of one stream
+// Places on the line: of a unit's begin and end, of a tile for both streams, of one for one of them (about 1 us each: 10, 3.1 and 2.0 to 2.3 measured)
+constexpr int kUnit = 10, kBoth = 3, kSingle = 2;
 constexpr int kLeast = 2;               // common pages that are worth a tile of their own
 constexpr int kMaxCtas = 192;
 constexpr int kMaxSeqs = SJD_POOL_MAX_LIST;
@@ -86,12 +87,13 @@ __device__ __forceinline__ int row_position(const SharedParams &p, int b, int k,
 }
 
 __device__ __forceinline__ int tiles_of(const Entry &en) { return en.tiles[0] + en.tiles[1] + en.tiles[2]; }
-// tiles of a unit that begin before place t: those for both streams take two places
+__device__ __forceinline__ int places_of(const Entry &en) { return kBoth * en.tiles[0] + kSingle * (en.tiles[1] + en.tiles[2]); }
+// tiles of a unit that begin before place t
 __device__ __forceinline__ int tiles_before(const Entry &en, long first, long t) {
   const long in = t - first;
   if (in <= 0) return 0;
-  if (in <= 2l * en.tiles[0]) return (int)((in + 1) >> 1);
-  const long n = in - en.tiles[0];
+  if (in <= (long)kBoth * en.tiles[0]) return (int)((in + kBoth - 1) / kBoth);
+  const long n = en.tiles[0] + (in - (long)kBoth * en.tiles[0] + kSingle - 1) / kSingle;
   return n < tiles_of(en) ? (int)n : tiles_of(en);
 }
 __device__ __forceinline__ long range_of(long all, int ctas) {
@@ -233,7 +235,7 @@ __global__ void __launch_bounds__(kPlanThreads) shared_plan_kernel(const __grid_
     }
     if (lane == 0) {
       p.entry[e] = en;
-      const int cost = 2 * en.tiles[0] + en.tiles[1] + en.tiles[2];
+      const int cost = places_of(en);
       (p.n_entries <= kCosts ? costs[e] : p.before[e + 1]) = cost > 0 ? cost + kUnit : 0;   // (its own so far)
     }
   }
@@ -511,7 +513,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
       }
       s.i0 = tiles_before(s.en, s.u.first, t_begin);
       s.i1 = tiles_before(s.en, s.u.first, t_end);
-      t = s.u.first + tiles_of(s.en) + s.en.tiles[0];
+      t = s.u.first + places_of(s.en);
       if (s.i1 > s.i0) return true;
     }
   };
@@ -1263,10 +1265,9 @@ extern "C" int sjd_pool_attention_shared(const sjd_pool *pool, int layer, int ba
   if (batch > kMaxSeqs || (group_begin && n_groups > batch) || (int64_t)batch * window * n_heads > 1ll << 30) return SJD_ERR_CAPACITY;
   const SharedLayout l = layout_of(*pool, batch, window, n_heads);
   if (ws_bytes < l.bytes) return SJD_ERR_CAPACITY;
-  // (places of a kv head are counted in 32 bits: a sequence's keys count once in each of the units that it has rows in, twice where those are
-  // for both streams)
+  // (places of a kv head are counted in 32 bits: a sequence's keys count in each of the units that it has rows in)
   const int64_t most = ((int64_t)pool->pages_per_seq + 1) / 2 + 1;
-  if (2 * most * (2 * (int64_t)batch + 2 * l.entries) + kUnit * l.entries >= 1ll << 31) return SJD_ERR_CAPACITY;
+  if (kBoth * most * (2 * (int64_t)batch + 2 * l.entries) + kUnit * l.entries >= 1ll << 31) return SJD_ERR_CAPACITY;
   int dev = 0, cc_major = 0, sms = 0;
   SJD_CUDA(cudaGetDevice(&dev));
   SJD_CUDA(cudaDeviceGetAttribute(&cc_major, cudaDevAttrComputeCapabilityMajor, dev));
