@@ -797,7 +797,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
             if (elect_one()) {
               const uint64_t b = desc_v + v_stage * (2 * OP >> 4) + h * (64 * 128 >> 4);
 #pragma unroll
-              for (int k = 0; k < kKeys / 32; ++k) umma_bf16_ts(t_o, t_s + h * 64 + k * 8, b + k * (16 * 128 >> 4), idesc_o, begun || h > 0 || k > 0);
+              for (int k = 0; k < kKeys / 32; ++k) umma_bf16_ts(t_o, t_s + h * 64 + (k >> 1) * 32 + (k & 1) * 8, b + k * (16 * 128 >> 4), idesc_o, begun || h > 0 || k > 0);
               umma_commit(&sh.o_done[st][h]);
               if (h == 1) umma_commit(&sh.v_empty[v_stage]);
             }
@@ -949,30 +949,34 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
             n_seen = 0;
           }
           if (__any_sync(0xffffffffu, n_seen > 0)) {
-            uint32_t x[64];
-            tmem_ld32(t_h, x);
-            tmem_ld32(t_h + 32, x + 32);
+            // 32 scores at a time, the first of them twice: more do not fit beside the rest of the registers, and what the compiler lays aside is far away (shared
+            // memory leaves the cache little room: with 64 at once, 136 bytes laid aside, a tile of two streams took 3.0 us)
+            const bool all = __all_sync(0xffffffffu, n_seen == 64 || r >= rows);
+            uint32_t x[32];
+            auto load = [&](int k) { tmem_ld32(t_h + k * 32, x); };
+            auto hide = [&](int k) {   // scores of keys that the row does not see
+              const int n = n_seen - 32 * k;
+              const uint32_t bits = n >= 32 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << n) - 1;
+#pragma unroll
+              for (int j = 0; j < 32; ++j) x[j] = bits >> j & 1u ? x[j] : 0xFF800000u;
+            };
+            load(0);
             const float4 up = *reinterpret_cast<const float4 *>(&f.k_up[h * 4]);
             const float by[4] = {factor * up.x, factor * up.y, factor * up.z, factor * up.w};   // of 16 columns
-            tmem_ld_wait();
-            if (!__all_sync(0xffffffffu, n_seen == 64 || r >= rows)) {   // some row does not see some key
-#pragma unroll
-              for (int k = 0; k < 2; ++k) {
-                const int n = n_seen - 32 * k;
-                const uint32_t bits = n >= 32 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << n) - 1;
-#pragma unroll
-                for (int j = 0; j < 32; ++j) x[k * 32 + j] = bits >> j & 1u ? x[k * 32 + j] : 0xFF800000u;
-              }
-            }
             float top = -INFINITY;
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              const uint32_t *v = x + 16 * c;
-              float a = max3(v[0], v[1], v[2]), b = max3(v[3], v[4], v[5]);
-              a = max3(__float_as_uint(a), v[6], v[7]), b = max3(__float_as_uint(b), v[8], v[9]);
-              a = max3(__float_as_uint(a), v[10], v[11]), b = max3(__float_as_uint(b), v[12], v[13]);
-              a = max3(__float_as_uint(a), v[14], v[15]);
-              top = fmaxf(top, fmaxf(a, b) * by[c]);
+            for (int k = 0; k < 2; ++k) {
+              tmem_ld_wait();
+              if (!all) hide(k);
+              float tops[2];
+#pragma unroll
+              for (int c = 0; c < 2; ++c) {
+                const uint32_t *v = x + 16 * c;
+                const float a = max3(v[0], v[1], v[2]), b = max3(v[3], v[4], v[5]), d = max3(v[6], v[7], v[8]), e = max3(v[9], v[10], v[11]), g = max3(v[12], v[13], v[14]);
+                tops[c] = max3(__float_as_uint(max3(__float_as_uint(a), __float_as_uint(b), __float_as_uint(d))), __float_as_uint(fmaxf(e, g)), v[15]) * by[2 * k + c];
+              }
+              if (k == 0) load(1);
+              top = max3(__float_as_uint(top), __float_as_uint(tops[0]), __float_as_uint(tops[1]));
             }
             // Where a score has outgrown the reference, that, O and the sum follow.
             const bool need = r < rows && (top > m_ref + kGrow || (m_ref == -INFINITY && top > -INFINITY));
@@ -1001,21 +1005,29 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
             const float ref = m_ref == -INFINITY ? 0.0f : m_ref;
             float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {   // 16 at a time, and each operation for all of them: it takes that many to hide its latency
-              float2 y[8];
-              uint32_t w[8];
+            for (int k = 1; k >= 0; --k) {   // (the second 32 scores are still here)
+              if (k == 0) {
+                load(0);
+                tmem_ld_wait();
+                if (!all) hide(0);
+              }
 #pragma unroll
-              for (int j = 0; j < 8; ++j)
-                y[j] = fma2(make_float2(__uint_as_float(x[16 * k + 2 * j]), __uint_as_float(x[16 * k + 2 * j + 1])), make_float2(by[k], by[k]), make_float2(-ref, -ref));
+              for (int c = 0; c < 2; ++c) {   // 16 at a time, and each operation for all of them: it takes that many to hide its latency
+                float2 y[8];
+                uint32_t w[8];
 #pragma unroll
-              for (int j = 0; j < 8; ++j) y[j].x = exp2_fast(y[j].x), y[j].y = exp2_fast(y[j].y);
+                for (int j = 0; j < 8; ++j)
+                  y[j] = fma2(make_float2(__uint_as_float(x[16 * c + 2 * j]), __uint_as_float(x[16 * c + 2 * j + 1])), make_float2(by[2 * k + c], by[2 * k + c]), make_float2(-ref, -ref));
 #pragma unroll
-              for (int j = 0; j < 8; ++j) w[j] = bf16_pair(y[j].x, y[j].y);
-              tmem_st8(t_h + k * 8, w);   // (over the scores)
+                for (int j = 0; j < 8; ++j) y[j].x = exp2_fast(y[j].x), y[j].y = exp2_fast(y[j].y);
 #pragma unroll
-              for (int j = 0; j < 4; ++j) y[j] = add2(y[j], y[j + 4]);
+                for (int j = 0; j < 8; ++j) w[j] = bf16_pair(y[j].x, y[j].y);
+                tmem_st8(t_h + k * 32 + c * 8, w);   // (over their own scores)
 #pragma unroll
-              for (int j = 0; j < 2; ++j) sum[j] = add2(sum[j], add2(y[j], y[j + 2]));
+                for (int j = 0; j < 4; ++j) y[j] = add2(y[j], y[j + 4]);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) sum[j] = add2(sum[j], add2(y[j], y[j + 2]));
+              }
             }
             l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
             tmem_st_wait();
@@ -1024,7 +1036,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
 #pragma unroll
             for (int k = 0; k < 16; ++k) w[k] = 0;
             tmem_st16(t_h, w);
-            tmem_st16(t_h + 16, w);
+            tmem_st16(t_h + 32, w);
             tmem_st_wait();
           }
           tc_fence_before();
