@@ -47,12 +47,8 @@ struct Entry {         // 256 rows of a kv head
   int n_segs[3], tiles[3];
   int rows;
 };
-struct Unit {
-  int e, h;
-  long first;          // place of its first tile
-};
 struct Begin {         // the unit in which a CTA begins
-  Unit u;
+  int e, h, first;     // first: place of its first tile, counted from where the CTA begins
   Entry en;
 };
 struct SharedParams {
@@ -89,12 +85,13 @@ __device__ __forceinline__ int row_position(const SharedParams &p, int b, int k,
 __device__ __forceinline__ int tiles_of(const Entry &en) { return en.tiles[0] + en.tiles[1] + en.tiles[2]; }
 __device__ __forceinline__ int places_of(const Entry &en) { return kBoth * en.tiles[0] + kSingle * (en.tiles[1] + en.tiles[2]); }
 // tiles of a unit that begin before place t
-__device__ __forceinline__ int tiles_before(const Entry &en, long first, long t) {
-  const long in = t - first;
+template <typename Place>
+__device__ __forceinline__ int tiles_before(const Entry &en, Place first, Place t) {
+  const Place in = t - first;
   if (in <= 0) return 0;
-  if (in <= (long)kBoth * en.tiles[0]) return (int)((in + kBoth - 1) / kBoth);
-  const long n = en.tiles[0] + (in - (long)kBoth * en.tiles[0] + kSingle - 1) / kSingle;
-  return n < tiles_of(en) ? (int)n : tiles_of(en);
+  if (in >= places_of(en)) return tiles_of(en);
+  const int n = (int)in;
+  return n <= kBoth * en.tiles[0] ? (n + kBoth - 1) / kBoth : en.tiles[0] + (n - kBoth * en.tiles[0] + kSingle - 1) / kSingle;
 }
 __device__ __forceinline__ long range_of(long all, int ctas) {
   const long least = 2 * kUnit, chunk = (all + ctas - 1) / ctas;
@@ -266,7 +263,7 @@ __global__ void __launch_bounds__(kPlanThreads) shared_plan_kernel(const __grid_
   for (int c = tid; c < p.ctas; c += kPlanThreads) {
     const long t = c * chunk;
     Begin b;
-    b.u.e = b.u.h = 0, b.u.first = 0;
+    b.e = b.h = b.first = 0;
     if (t < all) {
       int lo = 0, hi = p.n_entries - 1;
       while (lo < hi) {   // last unit that begins at t or before
@@ -274,11 +271,11 @@ __global__ void __launch_bounds__(kPlanThreads) shared_plan_kernel(const __grid_
         if ((long)p.before[mid] * p.pool.n_kv_heads <= t) lo = mid; else hi = mid - 1;
       }
       const int b0 = p.before[lo], cost = p.before[lo + 1] - b0;
-      b.u.e = lo;
-      b.u.h = (int)((t - (long)b0 * p.pool.n_kv_heads) / cost);
-      b.u.first = (long)b0 * p.pool.n_kv_heads + (long)b.u.h * cost + kUnit;
+      b.e = lo;
+      b.h = (int)((t - (long)b0 * p.pool.n_kv_heads) / cost);
+      b.first = (int)((long)b0 * p.pool.n_kv_heads + (long)b.h * cost + kUnit - t);
     }
-    b.en = p.entry[b.u.e];
+    b.en = p.entry[b.e];
     p.begin[c] = b;
   }
   if (tid == 0) *p.all = all;
@@ -293,8 +290,8 @@ __device__ __forceinline__ int stream_of(const Entry &en, int i, int from) {
   return j < 2 * min(en.tiles[1], en.tiles[2]) ? j & 1 : en.tiles[1] > en.tiles[2] ? 0 : 1;
 }
 // first row of a part: of the unit's first tiles, or of those that CTA c goes on with
-__device__ __forceinline__ long part_row(const SharedParams &p, const Unit &u, bool begins, int c) {
-  return begins ? ((long)u.e * p.pool.n_kv_heads + u.h) * kTileRows : ((long)p.n_entries * p.pool.n_kv_heads + c) * kTileRows;
+__device__ __forceinline__ long part_row(const SharedParams &p, int e, int h, bool begins, int c) {
+  return begins ? ((long)e * p.pool.n_kv_heads + h) * kTileRows : ((long)p.n_entries * p.pool.n_kv_heads + c) * kTileRows;
 }
 
 // ---------------------------------------------------------------------------------------------------------------- tiles
@@ -486,34 +483,35 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
   tc_fence_after();
   const uint32_t tmem = sh.tmem_base;
   const long all = *p.all, chunk = range_of(all, gridDim.x);
-  const long t_begin = min(all, blockIdx.x * chunk), t_end = min(all, t_begin + chunk);
+  const int places = (int)max(0l, min(chunk, all - blockIdx.x * chunk));   // of this CTA
   auto fail = [&]() {
     if (lane == 0) pool_fault(p.pool.status, SJD_ERR_DEVICE_TIMEOUT);
   };
-  // This CTA's units that have tiles in its range, one after the other: tiles i0 .. i1 - 1 of one.  (t: the end of the last, 0 before the first.)
+  // This CTA's units that have tiles in its range, one after the other: tiles i0 .. i1 - 1 of one.
   struct Span {
-    Unit u;
+    int e, h, next;    // next: the place behind it (-1: before the first)
     Entry en;
     int i0, i1;
   };
-  auto next_span = [&](long &t, Span &s) {
+  auto next_span = [&](Span &s) {
     for (;;) {
-      if (t == 0) {
-        if (t_begin == t_end) return false;
+      int first;
+      if (s.next < 0) {
+        if (places == 0) return false;
         const Begin b = p.begin[blockIdx.x];
-        s.u = b.u, s.en = b.en;
+        s.e = b.e, s.h = b.h, s.en = b.en, first = b.first;
       } else {
-        if (t >= t_end) return false;
-        if (++s.u.h == kv_heads) {
-          s.u.h = 0;
-          do s.en = p.entry[++s.u.e];
-          while (tiles_of(s.en) == 0);   // (t < all: there is one)
+        if (s.next >= places) return false;
+        if (++s.h == kv_heads) {
+          s.h = 0;
+          do s.en = p.entry[++s.e];
+          while (tiles_of(s.en) == 0);   // (there is one: the line goes on)
         }
-        s.u.first = t + kUnit;
+        first = s.next + kUnit;
       }
-      s.i0 = tiles_before(s.en, s.u.first, t_begin);
-      s.i1 = tiles_before(s.en, s.u.first, t_end);
-      t = s.u.first + places_of(s.en);
+      s.i0 = tiles_before(s.en, first, 0);
+      s.i1 = tiles_before(s.en, first, places);
+      s.next = first + places_of(s.en);
       if (s.i1 > s.i0) return true;
     }
   };
@@ -525,12 +523,12 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
       int n, h;                                   // tiles, kv head
       int key0, k1, ra, rb, page[2], k_exp[2], v_exp[2];   // of this lane's
     };
-    long t = 0;
     Span s;
+    s.next = -1;
     bool more = false, kept = false;
     int i = 0;
     auto begin_span = [&]() {
-      more = next_span(t, s);
+      more = next_span(s);
       if (!more) return;
       i = s.i0;
       const int n = s.en.n_segs[0] + s.en.n_segs[1] + s.en.n_segs[2];
@@ -544,7 +542,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
       b.n = 0;
       if (!more) return;
       b.n = min(32, s.i1 - i);
-      b.h = s.u.h;
+      b.h = s.h;
       const int x = min(i + lane, s.i1 - 1);
       // its kind, its number among that kind's, its segment: the last of them that begins there or before
       const int st = stream_of(s.en, x, s.i0), kind = one_stream(s.en.rows) ? 1 : st == 2 ? 0 : st + 1;
@@ -648,9 +646,9 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
     const uint32_t at0 = (uint32_t)(seg >> 2) * (128 * 128) + row0 * 128 + ((((seg & 3) * 2) ^ (row0 & 7)) << 4);
     long tiles = 0;
     {
-      long t = 0;
       Span s;
-      while (next_span(t, s)) tiles += s.i1 - s.i0;
+      s.next = -1;
+      while (next_span(s)) tiles += s.i1 - s.i0;
     }
     bool ok = true;
     for (uint32_t made = 0; made < tiles && ok; ++made) {
@@ -732,13 +730,13 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
     const uint64_t desc_k = rows_desc<HD>() | (uint64_t)(smem_u32(Ks) >> 4);
     const uint64_t desc_v = (uint64_t)(128 * 128 >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61 | (uint64_t)(smem_u32(Vs) >> 4);
     const uint32_t t_s = tmem + st * 128, t_o = tmem + 256 + st * 128;
-    long t = 0;
     Span s;
+    s.next = -1;
     bool ok = true;
     uint32_t q_ph = 0, p_ph = 0;
     int k_stage = 0, v_stage = 0;
     uint32_t k_ph = 0, v_ph = 0;
-    while (ok && next_span(t, s)) {
+    while (ok && next_span(s)) {
       ok = warp_wait(&sh.q_ready, q_ph);
       q_ph ^= 1u;
       const uint64_t desc_q = rows_desc<HD>() | (uint64_t)((smem_u32(Qs) + (one_stream(s.en.rows) ? 0 : st * 2 * OP)) >> 4);
@@ -823,13 +821,13 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
     const int st = warp >> 2, quarter = warp & 3, r_in = quarter * 32 + lane;
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16, t_s = tmem + lanes + st * 128, t_o = tmem + lanes + 256;
     auto sync = [&]() { asm volatile("bar.sync 1, %0;" ::"n"(kSoft) : "memory"); };
-    long t = 0;
     Span s;
+    s.next = -1;
     bool ok = true;
     uint32_t tile0 = 0, done = 0;   // done: this stream's tiles so far
-    while (next_span(t, s)) {
+    while (next_span(s)) {
       tile0 -= s.i0;
-      const int rows = s.en.rows, row_first = s.u.e * kTileRows;
+      const int rows = s.en.rows, row_first = s.e * kTileRows;
       const bool alone = one_stream(rows);
       const int r = r_in + (alone ? 0 : st * 128);
       int pos = -1;   // of this thread's row
@@ -837,7 +835,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
       {
         constexpr int LANES = HD / 8, PER = 32 / LANES, U = 4, STEP = kSoft / 32 * PER;   // lanes of a row, rows of a warp's load, loads under way, rows between them
         const int sub = lane / LANES, dim = lane % LANES * 8;
-        const __nv_bfloat16 *q = p.q + (long)s.u.h * p.group * HD + dim;
+        const __nv_bfloat16 *q = p.q + (long)s.h * p.group * HD + dim;
         auto load = [&](int r0, uint2 (&x)[U][2]) {
 #pragma unroll
           for (int j = 0; j < U; ++j) {
@@ -918,9 +916,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
       const float factor = fmaxf(r < rows ? sh.factor[r >> 7][r & 127] : 0.0f, 1e-38f);   // (not zero: masked scores stay infinite)
       const bool warp_rows = quarter * 32 + (alone ? 0 : st * 128) < rows;   // this warp has any
       float m_ref = -INFINITY, l = 0.0f;
-      uint32_t nan[HD / 32];
-#pragma unroll
-      for (int j = 0; j < HD / 32; ++j) nan[j] = 0;
+      bool nans = false;   // the row has seen some: sh.nan_row says which dims
       int mine = 0;
       for (int i = s.i0; i < s.i1; ++i) {
         const int c = stream_of(s.en, i, s.i0);
@@ -1054,7 +1050,8 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
               for (int k = 0; k < kKeys; ++k) {
                 if (!sh.nan_warps[stage][k % ROWS / WARP] || key0 + k > limit) continue;
 #pragma unroll
-                for (int j = 0; j < HD / 32; ++j) nan[j] |= *reinterpret_cast<const uint32_t *>(&sh.nan_dims[stage][k][2 * j]);
+                for (int j = 0; j < HD / 32; ++j) sh.nan_row[st][r_in][j] = (nans ? sh.nan_row[st][r_in][j] : 0u) | *reinterpret_cast<const uint32_t *>(&sh.nan_dims[stage][k][2 * j]);
+                nans = true;
               }
             }
           }
@@ -1072,13 +1069,13 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
         tc_fence_after();
       }
       const bool complete = s.i0 == 0 && s.i1 == tiles_of(s.en);
-      const long row = part_row(p, s.u, s.i0 == 0, blockIdx.x);
+      const long row = part_row(p, s.e, s.h, s.i0 == 0, blockIdx.x);
       const int stride = padded(rows);
       float4 *parts = reinterpret_cast<float4 *>(p.parts + row * HD) + r;   // [HD / 4][padded rows]
       __nv_bfloat16 *out = p.out;
       if (r < rows) {
         const int m = (row_first + r) / p.group;
-        out += (long)m * p.out_stride + ((long)s.u.h * p.group + (row_first + r - m * p.group)) * HD;
+        out += (long)m * p.out_stride + ((long)s.h * p.group + (row_first + r - m * p.group)) * HD;
       }
       // 32 dims of this row, times f (the whole unit: outputs)
       auto store = [&](int k, const float *v, float f) {
@@ -1096,14 +1093,15 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
       bool second = false;
       if (alone) {   // both streams have sums of the same rows: each joins half of the dims
         sh.stat[st][r_in] = a;
+        if (!nans) {
 #pragma unroll
-        for (int j = 0; j < HD / 32; ++j) sh.nan_row[st][r_in][j] = nan[j];
+          for (int j = 0; j < HD / 32; ++j) sh.nan_row[st][r_in][j] = 0;
+        }
         sync();
         second = s.i1 - s.i0 > 1;
         a = sh.stat[0][r_in];
         if (second) b = sh.stat[1][r_in];
-#pragma unroll
-        for (int j = 0; j < HD / 32; ++j) nan[j] = sh.nan_row[0][r_in][j] | (second ? sh.nan_row[1][r_in][j] : 0u);
+        nans = true;
       }
       if (warp_rows) {
         const float best = fmaxf(a.x, b.x), f0 = a.x == -INFINITY ? (a.y == 0.0f ? 0.0f : 1.0f) : exp2_fast(a.x - best);   // (scores that are all NaN leave no maximum)
@@ -1120,9 +1118,8 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
             tmem_ld32(t_o + o0 + k * 32, x);
             if (second) tmem_ld32(t_o + 128 + k * 32, y);
             tmem_ld_wait();
-            uint32_t bad = nan[0];
-#pragma unroll
-            for (int j = 1; j < HD / 32; ++j) bad = k == j ? nan[j] : bad;
+            uint32_t bad = 0;
+            if (nans) bad = alone ? sh.nan_row[0][r_in][k] | (second ? sh.nan_row[1][r_in][k] : 0u) : sh.nan_row[st][r_in][k];
 #pragma unroll
             for (int j = 0; j < 32; ++j) {
               v[j] = __uint_as_float(x[j]) * f0;
@@ -1179,10 +1176,9 @@ __global__ void __launch_bounds__(kJoinWarps * 32) shared_join_kernel(const __gr
   int warps = 1;
   if (cost > 0) {
     const Entry en = p.entry[e];
-    Unit u;
-    u.e = e, u.h = h, u.first = (long)b0 * kv_heads + (long)h * cost + kUnit;
-    const int n = tiles_of(en), c0 = (int)(u.first / chunk), c1 = (int)((u.first + cost - kUnit - 1) / chunk), stride = padded(en.rows);
-    if (tiles_before(en, u.first, c0 * chunk) == 0 && tiles_before(en, u.first, (c0 + 1) * chunk) == n) return;   // (written by its CTA)
+    const long first = (long)b0 * kv_heads + (long)h * cost + kUnit;
+    const int n = tiles_of(en), c0 = (int)(first / chunk), c1 = (int)((first + cost - kUnit - 1) / chunk), stride = padded(en.rows);
+    if (tiles_before(en, first, c0 * chunk) == 0 && tiles_before(en, first, (c0 + 1) * chunk) == n) return;   // (written by its CTA)
     warps = min(kJoinWarps, c1 - c0 + 1);
     for (int c = c0 + warp; c <= c1; c += 2 * kJoinWarps) {
       float2 s[2];
@@ -1194,9 +1190,9 @@ __global__ void __launch_bounds__(kJoinWarps * 32) shared_join_kernel(const __gr
 #pragma unroll
         for (int i = 0; i < D; ++i) x[j][i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         if (at > c1) continue;
-        const int i0 = tiles_before(en, u.first, at * chunk), i1 = tiles_before(en, u.first, (at + 1) * chunk);
+        const int i0 = tiles_before(en, first, at * chunk), i1 = tiles_before(en, first, (at + 1) * chunk);
         if (i0 == i1) continue;
-        const long row = part_row(p, u, i0 == 0, at);
+        const long row = part_row(p, e, h, i0 == 0, at);
         const float4 *from = reinterpret_cast<const float4 *>(p.parts + row * HD) + in;
         s[j] = p.stats[row + in];
 #pragma unroll
@@ -1277,9 +1273,11 @@ extern "C" int sjd_pool_attention_shared(const sjd_pool *pool, int layer, int ba
   if (batch > kMaxSeqs || (group_begin && n_groups > batch) || (int64_t)batch * window * n_heads > 1ll << 30) return SJD_ERR_CAPACITY;
   const SharedLayout l = layout_of(*pool, batch, window, n_heads);
   if (ws_bytes < l.bytes) return SJD_ERR_CAPACITY;
-  // (places of a kv head are counted in 32 bits: a sequence's keys count in each of the units that it has rows in)
+  // (places of a kv head are counted in 32 bits: a sequence's keys count in each of the units that it has rows in;
   const int64_t most = ((int64_t)pool->pages_per_seq + 1) / 2 + 1;
-  if (kBoth * most * (2 * (int64_t)batch + 2 * l.entries) + kUnit * l.entries >= 1ll << 31) return SJD_ERR_CAPACITY;
+  // and those of a CTA)
+  const int64_t line = kBoth * most * (2 * (int64_t)batch + 2 * l.entries) + kUnit * l.entries;
+  if (line >= 1ll << 30 || line * pool->n_kv_heads / 64 >= 1ll << 30) return SJD_ERR_CAPACITY;
   int dev = 0, cc_major = 0, sms = 0;
   SJD_CUDA(cudaGetDevice(&dev));
   SJD_CUDA(cudaDeviceGetAttribute(&cc_major, cudaDevAttrComputeCapabilityMajor, dev));
