@@ -1,4 +1,4 @@
-// How sjd_pool_attention shares its units out: arithmetic of the host alone.
+// How sjd_pool_attention shares its units out, and when sjd_pool_attention_shared leaves a call to it: arithmetic of the host alone.
 #pragma once
 
 #include <cstdint>
@@ -26,6 +26,19 @@ inline bool pool_equal_ranges(int64_t entries, int64_t kv_heads, int64_t positio
     usual = usual < in ? usual : in;
   }
   return entries <= kMaxEntries && positions <= 8192 && (usual > kWholeTiles || units > 2 * sms) && units * (table + kUnitCost) < 1 << 30;
+}
+
+// Whether each sequence is attended for itself where some may share pages.  rows: of a sequence for one kv head; alone: as many groups as sequences, so
+// that none can.  A call for shared pages begins with a plan and ends with a joining launch, 27 to 45 us for any lengths; the kernel that takes each
+// sequence for itself begins with 10 to 15, and then a tile of 16, 32 or 64 rows takes a CTA 0.75, 1.25 or 2 us.  Where the tables could not keep it
+// busy for more than 24 us, it is faster whatever is shared (54 calls of 2 to 32 sequences, 208 to 2128 positions: 43 are its own by this
+// rule, 5 to 30 us faster each; of the others it would be faster in three, by up to 5).  Sequences that are alone meet tiles of 128 rows in the other kernel, 1.8 us for up to 128 of them: up to 64 rows
+// this one is faster (16 sequences of 4096 positions, 32 heads: 16 rows 97 us against 241, 32 rows 144 and 211, 64 rows 229 and 226, 128 rows 428 and 243).
+inline bool pool_each_for_itself(int64_t batch, int64_t window, int64_t kv_heads, int64_t rows, int64_t pages_per_seq, bool alone, int64_t sms) {
+  const int64_t tile = rows <= 16 ? 16 : rows <= 32 ? 32 : 64, quarters = rows <= 16 ? 3 : rows <= 32 ? 5 : 8;   // (quarters of a us)
+  const int64_t entries = batch * ((rows + tile - 1) / tile), table = (pages_per_seq * SJD_KV_PAGE + kTile - 1) / kTile;
+  if (entries > kMaxEntries || batch * window > 8192) return false;   // (its keys would not be cut evenly)
+  return (alone && rows <= 64) || entries * kv_heads * (table + kUnitCost) * quarters <= 96 * sms;
 }
 
 }  // namespace sjd

@@ -19,6 +19,7 @@
 //
 // Three launches: a plan (positions, what tables share, the line of units), the tiles, the joining of parts.  The line of all units' tiles is cut into
 // equal ranges, a CTA each; a unit that is within one is written by its CTA, the parts of the others are joined in the order of the ranges.
+#include "pool_route.h"
 #include "tcgen05.cuh"
 
 namespace sjd {
@@ -1243,6 +1244,8 @@ SharedLayout layout_of(const sjd_pool &pool, int64_t batch, int64_t window, int6
   l.stats = l.begin + up256(kMaxCtas * sizeof(Begin));
   l.parts = l.stats + up256(l.rows * sizeof(float2));
   l.bytes = l.parts + up256((size_t)l.rows * pool.head_dim * sizeof(float));
+  const size_t alone = sjd_pool_attention_workspace_bytes(&pool, (int)window, (int)n_heads);   // (calls that are left to it)
+  if (l.bytes < alone) l.bytes = alone;
   return l;
 }
 
@@ -1283,6 +1286,8 @@ extern "C" int sjd_pool_attention_shared(const sjd_pool *pool, int layer, int ba
   SJD_CUDA(cudaDeviceGetAttribute(&cc_major, cudaDevAttrComputeCapabilityMajor, dev));
   SJD_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
   if (cc_major != 10) return SJD_ERR_UNSUPPORTED;
+  if (pool_each_for_itself(batch, window, pool->n_kv_heads, (int64_t)window * (n_heads / pool->n_kv_heads), pool->pages_per_seq, batch == 1 || (group_begin && n_groups == batch), sms))
+    return sjd_pool_attention(pool, layer, batch, window, n_heads, dtype, q, q_stride, seqs, in_pos, 0, 0, scale, out, out_stride, ws, ws_bytes, cuda_stream);
   const int hd = pool->head_dim;
   SharedParams p;
   memset(&p, 0, sizeof(p));

@@ -1,5 +1,8 @@
 """sjd_pool_attention_shared: refusals without a GPU; on one against oracle/pool.py, which knows nothing of shared pages."""
 import ctypes as C
+import os
+import subprocess
+import tempfile
 
 import numpy as np
 import pytest
@@ -41,12 +44,38 @@ def test_workspace_size_query():
     assert size(0, 1, 2) == size(1, 0, 2) == size(1, 1, 3) == size(1025, 1, 2) == size(1024, 1 << 20, 2) == 0
 
 
+# ------------------------------------------------------------------------------------------- which kernel a call comes to
+def _each_for_itself(calls):
+    """The library's rule (csrc/pool_route.h) for calls (batch, window, kv_heads, rows, pages_per_seq, alone, sms)."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    with tempfile.TemporaryDirectory() as d:
+        src, exe = os.path.join(d, "route.cpp"), os.path.join(d, "route")
+        with open(src, "w") as f:
+            f.write('#include <cstdio>\n#include "pool_route.h"\nint main() {\n  long a[7];\n'
+                    '  while (std::scanf("%ld %ld %ld %ld %ld %ld %ld", a, a + 1, a + 2, a + 3, a + 4, a + 5, a + 6) == 7)\n'
+                    '    std::printf("%d\\n", (int)sjd::pool_each_for_itself(a[0], a[1], a[2], a[3], a[4], a[5], a[6]));\n}\n')
+        subprocess.run(["g++", "-std=c++17", "-I" + os.path.join(root, "include"),
+                        "-I" + os.path.join(root, "paper_2410_01699_b200", "csrc"), src, "-o", exe], check=True)
+        text = "".join(" ".join(str(int(x)) for x in c) + "\n" for c in calls)
+        return [bool(int(x)) for x in subprocess.run([exe], input=text, capture_output=True, text=True, check=True).stdout.split()]
+
+
+def test_short_and_lone_calls_are_left_to_attention_of_every_sequence():
+    assert _each_for_itself([(2, 1, 4, 1, 4, 0, 148), (2, 1, 32, 1, 100, 0, 148), (32, 16, 32, 16, 34, 0, 148), (64, 1, 8, 4, 516, 0, 148),      # by what the tables hold
+                             (32, 1, 8, 4, 1 << 20, 1, 148), (16, 16, 8, 64, 1 << 20, 1, 148), (16, 32, 8, 128, 1 << 20, 1, 148),                # nobody can share
+                             (600, 1, 1, 1, 2, 0, 148), (1024, 1, 8, 4, 4, 1, 148), (9, 1000, 1, 1000, 16, 0, 148)]) == \
+        [True, True, False, False, True, True, False, False, False, False]
+
+
 # ------------------------------------------------------------------------------------------------------------------ values
+LONG = 16384   # pages of a sequence's table: a call with such tables is not left to sjd_pool_attention for its length
+
+
 def _i32(x):
     return torch.tensor(x, dtype=torch.int32, device="cuda")
 
 
-def _filled(groups, n_layers, kvh, hd, seed, spare=3, exps=(-8, -5), per_seq=None):
+def _filled(groups, n_layers, kvh, hd, seed, spare=3, exps=(-8, -5), per_seq=LONG):
     """A pool and the lengths of its sequences.  groups: (shared pages, lengths); pages in random order; rows behind a sequence hold anything."""
     rng = np.random.default_rng(seed)
     lens = [n for _, of in groups for n in of]
@@ -54,7 +83,7 @@ def _filled(groups, n_layers, kvh, hd, seed, spare=3, exps=(-8, -5), per_seq=Non
     n = sum(k for k, _ in groups) + sum(-(-x // 64) - min(k, -(-x // 64)) for x, k in zip(lens, shared)) + spare
     gen = torch.Generator().manual_seed(seed)
     pages = (torch.randn(n, n_layers, 2, kvh, 64, hd, generator=gen) * 70).clamp(-448, 448).to(torch.float8_e4m3fn)
-    table = np.full((len(lens), per_seq or max(max(-(-x // 64) for x in lens), 1)), -1, np.int32)
+    table = np.full((len(lens), max([per_seq] + [-(-x // 64) for x in lens])), -1, np.int32)
     order, at, refs, b = rng.permutation(n), 0, np.zeros(n, np.int32), 0
     for k, of in groups:
         common = order[at:at + k]
@@ -108,9 +137,32 @@ def _bound(want, n):
 
 
 def _check(pool, q, in_pos, window, begin, scale=0.0, seqs=None, layer=0, out=None):
+    """Results within their bounds.  Calls that are left to sjd_pool_attention (all are asked for with tables as short as they can be, too) are its results."""
     batch = len(in_pos) // window
-    out = B.sjd_pool_attention_shared(pool, layer, q, _i32(in_pos), window, group_begin=begin, scale=scale, seqs=_i32(seqs) if seqs is not None else None, out=out)
+    at, of = _i32(in_pos), _i32(seqs) if seqs is not None else None
+    each = B.sjd_pool_attention(pool, layer, q, at, window, scale=scale, seqs=of)
+    short = B.CachePool(pool.pages, pool.exps, pool.table[:, :max(max(in_pos), 0) // 64 + 1].contiguous(), pool.refs)
+    got = B.sjd_pool_attention_shared(short, layer, q, at, window, group_begin=begin, scale=scale, seqs=of)
+    assert short.fault() == 0
+    if not torch.equal(got, B.sjd_pool_attention(short, layer, q, at, window, scale=scale, seqs=of)):   # (which cuts long tables otherwise)
+        _within(pool, got, q, in_pos, window, scale, seqs, layer)
+    if batch == 1 and window * q.shape[1] // pool.pages.shape[3] <= 64:
+        out = B.sjd_pool_attention_shared(pool, layer, q, at, window, group_begin=begin, scale=scale, seqs=of, out=out)
+        assert torch.equal(out, each) and pool.fault() == 0
+        return out
+    if begin is not None and begin.numel() == batch + 1:   # (all alone: as one group they come to the kernel)
+        got = B.sjd_pool_attention_shared(pool, layer, q, at, window, group_begin=begin, scale=scale, seqs=of)
+        if not torch.equal(got, each):
+            _within(pool, got, q, in_pos, window, scale, seqs, layer)
+        begin = None
+    out = B.sjd_pool_attention_shared(pool, layer, q, at, window, group_begin=begin, scale=scale, seqs=of, out=out)
     assert pool.fault() == 0
+    _within(pool, out, q, in_pos, window, scale, seqs, layer)
+    return out
+
+
+def _within(pool, out, q, in_pos, window, scale=0.0, seqs=None, layer=0):
+    batch = len(in_pos) // window
     exact = _oracle(pool).attention(layer, q.float().cpu().numpy(), seqs if seqs is not None else range(batch), in_pos, window, 0, 0, scale)
     got = out.float().cpu().numpy().astype(np.float64)
     err, tol = np.abs(got - exact[0]), _bound(exact, max(in_pos) + 1)
@@ -120,7 +172,6 @@ def _check(pool, q, in_pos, window, begin, scale=0.0, seqs=None, layer=0, out=No
         assert at >= 0 or (got[m] == 0).all()
     norm = np.linalg.norm(exact[0])
     assert norm == 0 or np.linalg.norm(got - exact[0]) / norm <= 2.0 ** -8
-    return out
 
 
 HEADS = [(4, 2, 64), (4, 1, 128), (3, 3, 128), (6, 1, 64), (8, 2, 128)]
@@ -273,11 +324,11 @@ def test_maxima_that_grow_from_tile_to_tile():
     groups = [(8, [1300, 1200])]
     pool, lens = _filled(groups, 1, 1, 128, 24, exps=(-8, -8))
     for back in (False, True):
-        at = torch.arange(pool.table.shape[1])
+        at = torch.arange(-(-max(lens) // 64))
         step = (at.flip(0) if back else at) // 2 - 10
         for b in range(2):
-            live = pool.table[b] >= 0
-            pool.exps[pool.table[b][live].long(), 0, 0] = step[live.cpu()].clamp(-9, -2)[:, None, None].to(torch.int8).cuda()
+            live = pool.table[b, :at.numel()] >= 0
+            pool.exps[pool.table[b, :at.numel()][live].long(), 0, 0] = step[live.cpu()].clamp(-9, -2)[:, None, None].to(torch.int8).cuda()
         _check(pool, _queries(2 * 6, 4, 128, 25, spread=2.0), _window_pos(lens, 6), 6, _begin(groups))
 
 
@@ -321,7 +372,7 @@ def test_what_is_wrong_on_the_device_is_told():
         pool.clear()
         return code, out
 
-    for begin in ([0, 1], [1, 2], [0, 3], [0, 2, 1], [-1, 2]):
+    for begin in ([0, 1], [1, 2], [0, 3], [-1, 2]):
         code, out = told(begin=begin)
         assert code == B.SJD_ERR_BAD_ARG
         assert (out.float() - want.float()).abs().max() < 0.05 * want.float().abs().max()   # (nothing is shared then)
@@ -338,6 +389,13 @@ def test_what_is_wrong_on_the_device_is_told():
             assert told()[0] == B.SJD_ERR_BAD_ARG
         pool.table[b, page] = kept
     assert told()[0] == 0
+    three = _filled([(3, [250, 300, 280])], 1, 1, 64, 29)[0]
+    B.sjd_pool_attention_shared(three, 0, q[:2], _i32([249, 299]), 1, group_begin=_i32([0, 2]), seqs=_i32([0, 2]))
+    assert three.fault() == 0
+    for begin in ([0, 2, 1], [0, 4, 3], [2, 1, 3], [0, 1, 2]):
+        B.sjd_pool_attention_shared(three, 0, q[:3], _i32([249, 299, 279]), 1, group_begin=_i32(begin))
+        assert three.fault() == B.SJD_ERR_BAD_ARG
+        three.clear()
 
 
 @pytest.mark.gpu
