@@ -1146,7 +1146,8 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
 }
 
 // ---------------------------------------------------------------------------------------------------------------- joining
-// Eight rows of a unit that is cut a block: lane = row + 8 * (dims / 4 % 4), every kJoinWarps-th of the parts a warp, two parts' loads at a time.
+// Eight rows of a unit that is cut a block: lane = row + 8 * (dims / 4 % 4), every kJoinWarps-th of the parts a warp.  (Two parts' loads at a time take 125 registers
+// instead of 76: a call of 64 units 61.2 us against 58.7, one of 8 units of 19 parts each the same; with 2 warps the latter takes 105 instead of 98, with 8 the former 68.)
 constexpr int kJoinWarps = 4;
 template <int HD>
 __global__ void __launch_bounds__(kJoinWarps * 32) shared_join_kernel(const __grid_constant__ SharedParams p) {
@@ -1181,26 +1182,16 @@ __global__ void __launch_bounds__(kJoinWarps * 32) shared_join_kernel(const __gr
     const int n = tiles_of(en), c0 = (int)(first / chunk), c1 = (int)((first + cost - kUnit - 1) / chunk), stride = padded(en.rows);
     if (tiles_before(en, first, c0 * chunk) == 0 && tiles_before(en, first, (c0 + 1) * chunk) == n) return;   // (written by its CTA)
     warps = min(kJoinWarps, c1 - c0 + 1);
-    for (int c = c0 + warp; c <= c1; c += 2 * kJoinWarps) {
-      float2 s[2];
-      float4 x[2][D];
+    for (int c = c0 + warp; c <= c1; c += kJoinWarps) {
+      const int i0 = tiles_before(en, first, c * chunk), i1 = tiles_before(en, first, (c + 1) * chunk);
+      if (i0 == i1) continue;
+      const long row = part_row(p, e, h, i0 == 0, c);
+      const float4 *from = reinterpret_cast<const float4 *>(p.parts + row * HD) + in;
+      const float2 s = p.stats[row + in];
+      float4 x[D];
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int at = c + j * kJoinWarps;
-        s[j] = make_float2(-INFINITY, 0.0f);
-#pragma unroll
-        for (int i = 0; i < D; ++i) x[j][i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if (at > c1) continue;
-        const int i0 = tiles_before(en, first, at * chunk), i1 = tiles_before(en, first, (at + 1) * chunk);
-        if (i0 == i1) continue;
-        const long row = part_row(p, e, h, i0 == 0, at);
-        const float4 *from = reinterpret_cast<const float4 *>(p.parts + row * HD) + in;
-        s[j] = p.stats[row + in];
-#pragma unroll
-        for (int i = 0; i < D; ++i) x[j][i] = from[(d0 + 4 * i) * stride];
-      }
-      add(s[0], x[0]);
-      add(s[1], x[1]);
+      for (int i = 0; i < D; ++i) x[i] = from[(d0 + 4 * i) * stride];
+      add(s, x);
     }
   }
   if (warp > 0) {
