@@ -132,6 +132,17 @@ def test_alone_in_place_and_no_rows():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows,d", [(6001, 512), (700, 4096), (333, 8192)])
+def test_many_rows_in_place(rows, d):
+    """Enough of them for the kernel that fetches rows ahead: those are read before, or after, nobody writes them."""
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    h, y, w = (torch.randn(*s, generator=g, device="cuda").bfloat16() for s in ((rows, d), (rows, d), (d,)))
+    a, b = B.sjd_block_norm(h, y=y, post_gain=w, pre_gain=w, kind=B.SJD_NORM_LAYER)
+    B.sjd_block_norm(h, y=y, post_gain=w, pre_gain=w, kind=B.SJD_NORM_LAYER, h_out=h, z=y)
+    assert torch.equal(h, a) and torch.equal(y, b)
+
+
+@pytest.mark.gpu
 def test_rows_do_not_touch_one_another():
     """A NaN or an infinity stays in its row; entries beside the rows stay as they are."""
     h = torch.randn(20, 648, device="cuda").bfloat16()
