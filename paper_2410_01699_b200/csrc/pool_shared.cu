@@ -431,7 +431,7 @@ __device__ __forceinline__ uint32_t swizzled(uint32_t row, uint32_t col) {
 
 template <int HD>
 struct SharedSmem {
-  uint64_t k_full[kKStages], k_empty[kKStages], raw_full[2], raw_empty[2], v_full[2], v_empty[2], s_full[2][2], p_ready[2][2], o_done[2][2], q_ready;
+  uint64_t k_full[kKStages], k_empty[kKStages], raw_full[2], raw_empty[2], v_full[2], v_empty[2], s_full[2][2], p_ready[2][2], o_done[2][2], q_ready, q_seen;
   uint32_t tmem_base;
   Info info[kInfo];
   uint32_t nan_warps[2][kConv / 32];           // some entry of V that a warp turned was NaN
@@ -470,6 +470,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
       }
     }
     mbar_init(&sh.q_ready, kSoft / 32);
+    mbar_init(&sh.q_seen, 2);
     tma_prefetch_desc(&map);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -740,6 +741,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
     while (ok && next_span(s)) {
       ok = warp_wait(&sh.q_ready, q_ph);
       q_ph ^= 1u;
+      if (lane == 0) arrive(&sh.q_seen);
       const uint64_t desc_q = rows_desc<HD>() | (uint64_t)((smem_u32(Qs) + (one_stream(s.en.rows) ? 0 : st * 2 * OP)) >> 4);
       // Scores of the halves of the own tiles before `end`, each when the weights in its columns have been multiplied.  (No further than two tiles ahead
       // of the values: what the copies wait for is let go of there.)
@@ -825,13 +827,19 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
     Span s;
     s.next = -1;
     bool ok = true;
-    uint32_t tile0 = 0, done = 0;   // done: this stream's tiles so far
+    uint32_t tile0 = 0, done = 0, q_ph = 1;   // done: this stream's tiles so far
     while (next_span(s)) {
       tile0 -= s.i0;
       const int rows = s.en.rows, row_first = s.e * kTileRows;
       const bool alone = one_stream(rows);
       const int r = r_in + (alone ? 0 : st * 128);
       int pos = -1;   // of this thread's row
+      // (a stream without tiles in the unit before may not have looked for its queries yet, and would miss them behind the next ones)
+      if (ok && !warp_wait(&sh.q_seen, q_ph)) {
+        ok = false;
+        fail();
+      }
+      q_ph ^= 1u;
       // ---- queries of the unit's rows: a power of two brings a row's largest entry to 128 .. 256, then its two numbers; a row is HD / 4 lanes
       {
         constexpr int LANES = HD / 8, PER = 32 / LANES, U = 4, STEP = kSoft / 32 * PER;   // lanes of a row, rows of a warp's load, loads under way, rows between them
