@@ -431,10 +431,10 @@ __device__ __forceinline__ uint32_t swizzled(uint32_t row, uint32_t col) {
 
 template <int HD>
 struct SharedSmem {
-  uint64_t k_full[kKStages], k_empty[kKStages], raw_full[2], raw_empty[2], v_full[2], v_empty[2], s_full[2][2], p_ready[2][2], o_done[2][2], q_ready, q_seen;
+  uint64_t k_full[kKStages], k_empty[kKStages], raw_full[2], raw_empty[2], v_full[2][2], v_empty[2][2], s_full[2][2], p_ready[2][2], o_done[2][2], q_ready, q_seen;
   uint32_t tmem_base;
   Info info[kInfo];
-  uint32_t nan_warps[2][kConv / 32];           // some entry of V that a warp turned was NaN
+  alignas(4) uint8_t nan_warps[2][2][kConv / 32];      // of half a tile: some entry of V that a warp turned was NaN
   alignas(16) uint16_t nan_dims[2][kKeys][HD / 16];    // which, if so
   float2 stat[2][128];                         // of both streams' rows
   uint32_t nan_row[2][128][HD / 32];
@@ -461,9 +461,9 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sh.raw_full[i], 1);
       mbar_init(&sh.raw_empty[i], kConv / 32);
-      mbar_init(&sh.v_full[i], kConv / 32);
-      mbar_init(&sh.v_empty[i], 2);
       for (int h = 0; h < 2; ++h) {
+        mbar_init(&sh.v_full[i][h], kConv / 32);
+        mbar_init(&sh.v_empty[i][h], 2);
         mbar_init(&sh.s_full[i][h], 1);
         mbar_init(&sh.p_ready[i][h], 4);
         mbar_init(&sh.o_done[i][h], 1);
@@ -655,73 +655,82 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
     bool ok = true;
     for (uint32_t made = 0; made < tiles && ok; ++made) {
       const int stage = made & 1;
-      ok = warp_wait(&sh.raw_full[stage], made >> 1 & 1) && (made < 2 || warp_wait(&sh.v_empty[stage], (made >> 1 & 1) ^ 1u));
+      ok = warp_wait(&sh.raw_full[stage], made >> 1 & 1);
       if (!ok) break;
       const Info &f = sh.info[made % kInfo];
       const uint8_t *from = Rs + stage * OP + row0 * HD + seg * 16;
       uint8_t *to = Vs + stage * 2 * OP + at0;
       const int left = f.k1 - f.key0 - row0, there = f.there, large = f.large;   // left: rows of this thread that there are
-      uint32_t nan = 0;
-      // two loads at a time: as many independent numbers as it takes, and a loop that is short to fetch
+      // (a half as soon as the products with the one there are done)
 #pragma unroll 1
-      for (int n0 = 0; n0 < N; n0 += 2) {
-        uint4 x[2];
-        uint32_t out[2][8], up[2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int n = n0 + j;
-          x[j] = *reinterpret_cast<const uint4 *>(from + n * ROWS * HD);
-          if (!(there >> (n / (N / 2)) & 1) || n * ROWS >= left) x[j] = make_uint4(0, 0, 0, 0);
-          up[j] = f.v_up[(row0 + n * ROWS) >> 4];
-        }
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const uint32_t w[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
-          uint32_t any = 0;
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            out[j][2 * c] = mul_bf16x2(bf16_bits_of_e4m3(__byte_perm(w[c], 0, 0x1404)), up[j]);
-            out[j][2 * c + 1] = mul_bf16x2(bf16_bits_of_e4m3(__byte_perm(w[c], 0, 0x3424)), up[j]);
-            any |= (w[c] & 0x7F7F7F7Fu) + 0x01010101u;
-          }
-          nan |= any & 0x80808080u;
-        }
-        if (__builtin_expect(large, 0)) {   // (exponents above 0 in a second step)
+      for (int h = 0; h < 2 && ok; ++h) {
+        ok = made < 2 || warp_wait(&sh.v_empty[stage][h], (made >> 1 & 1) ^ 1u);
+        if (!ok) break;
+        uint32_t nan = 0;
+        // two loads at a time: as many independent numbers as it takes, and a loop that is short to fetch
+#pragma unroll 1
+        for (int n0 = h * (N / 2); n0 < (h + 1) * (N / 2); n0 += 2) {
+          uint4 x[2];
+          uint32_t out[2][8], up[2];
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            const int block = (row0 + (n0 + j) * ROWS) >> 4;
-            const uint32_t over = pair_of(two_to(max(pool_exp((int8_t)((block < 4 ? f.v_exp[0] : f.v_exp[1]) >> (8 * (block & 3)))), 0)));
+            const int n = n0 + j;
+            x[j] = *reinterpret_cast<const uint4 *>(from + n * ROWS * HD);
+            if (!(there >> (n / (N / 2)) & 1) || n * ROWS >= left) x[j] = make_uint4(0, 0, 0, 0);
+            up[j] = f.v_up[(row0 + n * ROWS) >> 4];
+          }
 #pragma unroll
-            for (int c = 0; c < 8; ++c) out[j][c] = mul_bf16x2(out[j][c], over);
+          for (int j = 0; j < 2; ++j) {
+            const uint32_t w[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
+            uint32_t any = 0;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              out[j][2 * c] = mul_bf16x2(bf16_bits_of_e4m3(__byte_perm(w[c], 0, 0x1404)), up[j]);
+              out[j][2 * c + 1] = mul_bf16x2(bf16_bits_of_e4m3(__byte_perm(w[c], 0, 0x3424)), up[j]);
+              any |= (w[c] & 0x7F7F7F7Fu) + 0x01010101u;
+            }
+            nan |= any & 0x80808080u;
+          }
+          if (__builtin_expect(large, 0)) {   // (exponents above 0 in a second step)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              const int block = (row0 + (n0 + j) * ROWS) >> 4;
+              const uint32_t over = pair_of(two_to(max(pool_exp((int8_t)((block < 4 ? f.v_exp[0] : f.v_exp[1]) >> (8 * (block & 3)))), 0)));
+#pragma unroll
+              for (int c = 0; c < 8; ++c) out[j][c] = mul_bf16x2(out[j][c], over);
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            uint8_t *dst = to + (n0 + j) * ROWS * 128;
+            *reinterpret_cast<uint4 *>(dst) = make_uint4(out[j][0], out[j][1], out[j][2], out[j][3]);
+            *reinterpret_cast<uint4 *>((uint8_t *)((uintptr_t)dst ^ 16)) = make_uint4(out[j][4], out[j][5], out[j][6], out[j][7]);
           }
         }
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          uint8_t *dst = to + (n0 + j) * ROWS * 128;
-          *reinterpret_cast<uint4 *>(dst) = make_uint4(out[j][0], out[j][1], out[j][2], out[j][3]);
-          *reinterpret_cast<uint4 *>((uint8_t *)((uintptr_t)dst ^ 16)) = make_uint4(out[j][4], out[j][5], out[j][6], out[j][7]);
-        }
-      }
-      const bool found = __any_sync(0xffffffffu, nan != 0);
-      if (__builtin_expect(found, 0)) {   // NaN entries become zeros, and are told
+        const bool found = __any_sync(0xffffffffu, nan != 0);
+        if (__builtin_expect(found, 0)) {   // NaN entries become zeros, and are told
 #pragma unroll 1
-        for (int n = 0; n < N; ++n) {
-          uint32_t dims = 0;
-          uint16_t *dst = reinterpret_cast<uint16_t *>(to + n * ROWS * 128);
-          const bool row = (there >> (n / (N / 2)) & 1) && n * ROWS < left;
+          for (int n = h * (N / 2); n < (h + 1) * (N / 2); ++n) {
+            uint32_t dims = 0;
+            uint16_t *dst = reinterpret_cast<uint16_t *>(to + n * ROWS * 128);
+            const bool row = (there >> (n / (N / 2)) & 1) && n * ROWS < left;
 #pragma unroll 1
-          for (int c = 0; c < 16; ++c) {
-            if (!row || (from[n * ROWS * HD + c] & 0x7F) != 0x7F) continue;
-            dims |= 1u << c;
-            *reinterpret_cast<uint16_t *>((uintptr_t)(dst + (c & 7)) ^ (c < 8 ? 0 : 16)) = 0;
+            for (int c = 0; c < 16; ++c) {
+              if (!row || (from[n * ROWS * HD + c] & 0x7F) != 0x7F) continue;
+              dims |= 1u << c;
+              *reinterpret_cast<uint16_t *>((uintptr_t)(dst + (c & 7)) ^ (c < 8 ? 0 : 16)) = 0;
+            }
+            sh.nan_dims[stage][row0 + n * ROWS][seg] = (uint16_t)dims;
           }
-          sh.nan_dims[stage][row0 + n * ROWS][seg] = (uint16_t)dims;
+        }
+        if (lane == 0) sh.nan_warps[stage][h][cw] = found;
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+          if (h == 1) arrive(&sh.raw_empty[stage]);
+          arrive(&sh.v_full[stage][h]);
         }
       }
-      if (lane == 0) sh.nan_warps[stage][cw] = found;
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      __syncwarp();
-      if (lane == 0) arrive(&sh.raw_empty[stage]), arrive(&sh.v_full[stage]);
     }
     if (!ok) fail();
   } else if (warp == ISSUE || warp == ISSUE + 1) {
@@ -792,7 +801,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
         if (own) {
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            if (ok) ok = h == 0 ? warp_wait_both(&sh.p_ready[st][h], p_ph, &sh.v_full[v_stage], v_ph) : warp_wait(&sh.p_ready[st][h], p_ph);
+            if (ok) ok = warp_wait_both(&sh.p_ready[st][h], p_ph, &sh.v_full[v_stage][h], v_ph);
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
@@ -800,17 +809,17 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
 #pragma unroll
               for (int k = 0; k < kKeys / 32; ++k) umma_bf16_ts(t_o, t_s + h * 64 + (k >> 1) * 32 + (k & 1) * 8, b + k * (16 * 128 >> 4), idesc_o, begun || h > 0 || k > 0);
               umma_commit(&sh.o_done[st][h]);
-              if (h == 1) umma_commit(&sh.v_empty[v_stage]);
+              umma_commit(&sh.v_empty[v_stage][h]);
             }
             __syncwarp();
             (h == 0 ? open0 : open1) = false;
-            if (h == 0) scores(j + 2);
+            if (h == 0) scores(j + 3);
           }
           begun = true;
           p_ph ^= 1u;
         } else {
-          ok = warp_wait(&sh.v_full[v_stage], v_ph);
-          if (ok && elect_one()) arrive(&sh.v_empty[v_stage]);
+          ok = warp_wait_both(&sh.v_full[v_stage][0], v_ph, &sh.v_full[v_stage][1], v_ph);
+          if (ok && elect_one()) arrive(&sh.v_empty[v_stage][0]), arrive(&sh.v_empty[v_stage][1]);
           __syncwarp();
         }
         if (ok) scores(j + 3);
@@ -1045,23 +1054,19 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
             tmem_st_wait();
           }
           tc_fence_before();
-          if (h == 1) {   // NaN entries of V, which are zeros there, and the rows that see them
-            if (ok && !warp_wait(&sh.v_full[stage], use >> 1 & 1)) {
-              ok = false;
-              fail();
-            }
-            uint32_t any = 0;
-#pragma unroll
-            for (int w = 0; w < kConv / 32; ++w) any |= sh.nan_warps[stage][w];
-            if (__builtin_expect(any, 0)) {
-              constexpr int ROWS = kConv / (HD / 16), WARP = 32 / (HD / 16);
+          // NaN entries of V, which are zeros there, and the rows that see them
+          if (ok && !warp_wait(&sh.v_full[stage][h], use >> 1 & 1)) {
+            ok = false;
+            fail();
+          }
+          if (__builtin_expect(*reinterpret_cast<const uint32_t *>(sh.nan_warps[stage][h]) != 0, 0)) {
+            constexpr int ROWS = kConv / (HD / 16), WARP = 32 / (HD / 16);
 #pragma unroll 1
-              for (int k = 0; k < kKeys; ++k) {
-                if (!sh.nan_warps[stage][k % ROWS / WARP] || key0 + k > limit) continue;
+            for (int k = h * 64; k < h * 64 + 64; ++k) {
+              if (!sh.nan_warps[stage][h][k % ROWS / WARP] || key0 + k > limit) continue;
 #pragma unroll
-                for (int j = 0; j < HD / 32; ++j) sh.nan_row[st][r_in][j] = (nans ? sh.nan_row[st][r_in][j] : 0u) | *reinterpret_cast<const uint32_t *>(&sh.nan_dims[stage][k][2 * j]);
-                nans = true;
-              }
+              for (int j = 0; j < HD / 32; ++j) sh.nan_row[st][r_in][j] = (nans ? sh.nan_row[st][r_in][j] : 0u) | *reinterpret_cast<const uint32_t *>(&sh.nan_dims[stage][k][2 * j]);
+              nans = true;
             }
           }
           __syncwarp();
