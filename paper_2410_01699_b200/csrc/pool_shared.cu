@@ -440,6 +440,7 @@ struct SharedSmem {
   uint32_t nan_row[2][128][HD / 32];
   float factor[2][128];                        // of the scores of a row: the scale, and what its query was multiplied by
   Segment segs[kSegs];
+  Begin begin;                                 // where this CTA begins
 };
 
 template <int HD>
@@ -480,11 +481,13 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   pdl_wait();
+  const long all = *p.all;
+  if (tid < (int)(sizeof(Begin) / 4)) reinterpret_cast<int *>(&sh.begin)[tid] = reinterpret_cast<const int *>(p.begin + blockIdx.x)[tid];
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = sh.tmem_base;
-  const long all = *p.all, chunk = range_of(all, gridDim.x);
+  const long chunk = range_of(all, gridDim.x);
   const int places = (int)max(0l, min(chunk, all - blockIdx.x * chunk));   // of this CTA
   auto fail = [&]() {
     if (lane == 0) pool_fault(p.pool.status, SJD_ERR_DEVICE_TIMEOUT);
@@ -500,8 +503,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
       int first;
       if (s.next < 0) {
         if (places == 0) return false;
-        const Begin b = p.begin[blockIdx.x];
-        s.e = b.e, s.h = b.h, s.en = b.en, first = b.first;
+        s.e = sh.begin.e, s.h = sh.begin.h, s.en = sh.begin.en, first = sh.begin.first;
       } else {
         if (s.next >= places) return false;
         if (++s.h == kv_heads) {
