@@ -4,6 +4,11 @@
 // A row is a block's (a warp's, up to 1024 entries): its entries stay in registers between the sums, which are in 32 bits; the mean goes
 // off before the squares are summed (squares of the entries less the mean's square would lose what a large mean leaves of them).  z is
 // taken of h' before that is rounded to its type.  A thread has N vectors of VEC entries, T threads apart.
+//
+// Few rows are bound by the launch and two or four round trips (256 rows of 4096, gate and residual: 10.6 us).  Many are bound by the bytes, and where
+// a block has one row at a time, by what it waits for between fetching a row and writing it: those of block_norm_rows_kernel keep the
+// next rows coming (16892 rows of 4096, layer norms, gate, bf16: 235 us with a row a block, 140 with two vectors a thread, 113 now,
+// 86 are the bytes; RMS 99; residual stream in fp32 195 and 129).
 #include <algorithm>
 
 #include "common.cuh"
@@ -19,6 +24,7 @@ struct NormParams {
   void *h_out, *z;
   long h_stride, y_stride, h_out_stride, z_stride;
   int rows, d, layer, gate_rows, gate_tanh;
+  int wide_h, wide_z;   // rows of h_out, of z start on 32 bytes (with vectors)
   float eps, scale, inv_d;
 };
 
@@ -36,13 +42,20 @@ __device__ __forceinline__ void load_vec(const T *p, float *v) {
     for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(w[i] << 16), v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
   }
 }
+// wide: p is a multiple of 32 bytes (two stores of half a sector each take 228 us instead of 195 where h is fp32)
 template <typename T, int VEC>
-__device__ __forceinline__ void store_vec(T *p, const float *v) {
+__device__ __forceinline__ void store_vec(T *p, const float *v, bool wide) {
   if constexpr (VEC == 1) {
     *p = (T)v[0];   // (to the nearest)
   } else if constexpr (sizeof(T) == 4) {
-    reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-    reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+    if (wide) {
+      asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                   ::"l"(p), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7])
+                   : "memory");
+    } else {
+      reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+      reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+    }
   } else {
     uint32_t w[4];
 #pragma unroll
@@ -132,14 +145,14 @@ __global__ void __launch_bounds__(ROW ? 1024 : 32 * kWarpRows) block_norm_kernel
       if constexpr (!EARLY) load_vec<H, VEC>(hp + k, h[0]);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) x[i][e] = fmaf(p.scale, x[i][e], h[EARLY ? i : 0][e]);
-      store_vec<H, VEC>((H *)p.h_out + row * p.h_out_stride + k, x[i]);
+      store_vec<H, VEC>((H *)p.h_out + row * p.h_out_stride + k, x[i], p.wide_h);
     });
   } else {
     each([&](int i, int k) { load_vec<H, VEC>(hp + k, x[i]); });
   }
   if (p.z) {
     normalise(x, (const Y *)p.pre_gain, (const Y *)p.pre_bias);
-    each([&](int i, int k) { store_vec<Y, VEC>((Y *)p.z + row * p.z_stride + k, x[i]); });
+    each([&](int i, int k) { store_vec<Y, VEC>((Y *)p.z + row * p.z_stride + k, x[i], p.wide_z); });
   }
 }
 
@@ -169,7 +182,8 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
       : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
   return d;
 }
-constexpr int kN = 4, kMaxGroups = 32, kMaxWarps = 8, kRowsThreads = 1024;
+// Threads of a block: with 1024 (64 registers, of which 40 to 70 bytes are laid aside) the case above takes 120 us, with 640 118, with 512 119.
+constexpr int kN = 4, kMaxGroups = 32, kMaxWarps = 8, kRowsThreads = 768;
 
 // 16 bytes to shared memory, and the groups of such copies of this thread
 __device__ __forceinline__ void copy_async(void *dst, const void *src) {
@@ -302,7 +316,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) block_norm_rows_kernel(const 
         load_pairs<H>(h_slot + i * HU * T, T, h);
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[i][e] = fma2(x[i][e], make_float2(p.scale, p.scale), h[e]);
-        store_vec<H, 8>((H *)p.h_out + row * p.h_out_stride + k, &x[i][0].x);
+        store_vec<H, 8>((H *)p.h_out + row * p.h_out_stride + k, &x[i][0].x, p.wide_h);
       });
     } else {
       copies_wait<0>();
@@ -311,7 +325,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) block_norm_rows_kernel(const 
     fetch(p.h, H(), p.h_stride, row + step, h_slot);
     if (p.z) {
       normalise(x, 2, p.pre_bias);
-      each([&](int i, int k) { store_vec<Y, 8>((Y *)p.z + row * p.z_stride + k, &x[i][0].x); });
+      each([&](int i, int k) { store_vec<Y, 8>((Y *)p.z + row * p.z_stride + k, &x[i][0].x, p.wide_z); });
     }
   }
   copies_wait<0>();
@@ -392,6 +406,7 @@ extern "C" int sjd_block_norm(int rows, int d, int kind, float eps, int dtype, i
   // vectors of eight entries where all rows start on 16 bytes
   const int64_t strides = (y ? y_stride | h_out_stride : 0) | (z ? z_stride : 0) | h_stride;
   const bool vec = d % 8 == 0 && (strides & 7) == 0 && ((of_y | of_h) & 15) == 0;
+  p.wide_h = ((uintptr_t)h_out & 31) == 0, p.wide_z = ((uintptr_t)z & 31) == 0;
   int dev = 0, sms = 0;
   SJD_CUDA(cudaGetDevice(&dev));
   SJD_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));

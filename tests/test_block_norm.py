@@ -143,6 +143,18 @@ def test_many_rows_in_place(rows, d):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows,d", [(9, 264), (9, 2048), (3000, 1024)])
+def test_outputs_that_start_on_16_bytes(rows, d):
+    g = torch.Generator(device="cuda").manual_seed(d)
+    h, y, w = (torch.randn(*s, generator=g, device="cuda") for s in ((rows, d), (rows, d), (d,)))
+    a, b = B.sjd_block_norm(h, y=y, post_gain=w, pre_gain=w)
+    out, z = (torch.full((rows * d + 8,), 7.0, device="cuda") for _ in range(2))
+    B.sjd_block_norm(h, y=y, post_gain=w, pre_gain=w, h_out=out[4:4 + rows * d].view(rows, d), z=z[4:4 + rows * d].view(rows, d))
+    for got, want in ((out, a), (z, b)):
+        assert torch.equal(got[4:-4].view(rows, d), want) and (got[:4] == 7).all() and (got[-4:] == 7).all()
+
+
+@pytest.mark.gpu
 def test_rows_do_not_touch_one_another():
     """A NaN or an infinity stays in its row; entries beside the rows stay as they are."""
     h = torch.randn(20, 648, device="cuda").bfloat16()
