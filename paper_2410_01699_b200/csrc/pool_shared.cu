@@ -19,6 +19,14 @@
 //
 // Three launches: a plan (positions, what tables share, the line of units), the tiles, the joining of parts.  The line of all units' tiles is cut into
 // equal ranges, a CTA each; a unit that is within one is written by its CTA, the parts of the others are joined in the order of the ranges.
+//
+// What bounds it (32 heads of 128): the softmax.  A tile of 128 keys for both streams takes 2.8 us, where its exponentials alone would take 1.07 by their rate.
+// Left out one at a time, the exponentials take 0.8 us with them, half of the maxima 0.2, the turning of the values 0.13, the second numbers of the
+// queries 0.04; without a softmax at all the two products and their barriers take 1.8.  Two softmax warps share a scheduler, 43 % of its slots are used.
+// Slower: 16 softmax warps with 88 registers; 64 scores at once (3.0 us); one pass under the reference that there is, with the maxima behind it (3.4 to
+// 3.6: more of a row is held at a time, and what is laid aside is far away, for shared memory leaves the cache little room).  Around the tiles 40 to 45 us
+// stay the same for any lengths: the plan 7 to 12, queries and first copies 7 to 8, parts 3 to 4, the longest range 6 to 10 beyond the mean, the joining
+// launch 11 to 13.
 #include "pool_route.h"
 #include "tcgen05.cuh"
 
