@@ -334,7 +334,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) block_norm_rows_kernel(const 
 template <typename Y, typename H>
 int launch_rows(const NormParams &p, int sms, cudaStream_t stream) {
   const int T = (p.d + kN * 256 - 1) / (kN * 256) * 32;
-  const size_t kept = 4ull * kN * sizeof(Y) / 2 * 16 * T, slot = (size_t)kN * (sizeof(Y) + sizeof(H)) / 2 * 16 * T, most = 232448 - 3072;
+  const size_t kept = 4ull * kN * sizeof(Y) / 2 * 16 * T, slot = (size_t)kN * (sizeof(Y) + sizeof(H)) / 2 * 16 * T, most = 224 * 1024;   // (of 227 KB; the rest is static)
   const int groups = std::min(std::min(kRowsThreads / T, kMaxGroups), (int)((most - kept) / slot));
   auto launch = [&](auto kernel) -> int {
     const int rc = allow_smem(kernel, most);
