@@ -112,3 +112,30 @@ def test_steps_of_a_decoder(batch, window, pages):
     assert status.item() == 0 and pool.fault() == 0
     shared = pool.table[:, :PROMPT // 64]
     assert (shared == shared[:1]).all() and (pool.table[:, PROMPT // 64].unique().numel() == batch)
+
+
+@pytest.mark.gpu
+def test_calls_on_two_streams_at_once():
+    """Calls of every kernel beside one another, attention with a workspace for each stream: the bits of calls one after the other."""
+    g = torch.Generator(device="cuda").manual_seed(42)
+    rnd = lambda *s: torch.randn(*s, generator=g, device="cuda").bfloat16()
+    pool, lens = S._filled([(6, [600, 500, 430]), (3, [300, 210])], 1, 2, 128, 43)
+    q, at, begin = rnd(len(lens) * 20, 8, 128), S._i32(S._window_pos(lens, 20)), S._i32([0, 3, 5])
+    short = B.CachePool(pool.pages, pool.exps, pool.table[:, :10].contiguous(), pool.refs)
+    x, w, up, gain = rnd(700, 1024), rnd(1024, 1024) / 32, rnd(1024, 1024) / 32, rnd(1024)
+    nbytes = int(B.lib().sjd_pool_attention_shared_workspace_bytes(pool.ref, len(lens), 20, 8))
+
+    def work(ws):
+        return [B.sjd_pool_attention_shared(pool, 0, q, at, 20, group_begin=begin, ws=ws), B.sjd_linear(x, w, w_up=up, act=B.SJD_ACT_SILU),
+                B.sjd_block_norm(x, y=x, pre_gain=gain)[1], B.sjd_linear(x[:33], w, residual=x[:33]), B.sjd_pool_attention_shared(short, 0, q, at, 20, group_begin=begin, ws=ws),
+                B.sjd_linear(x[:200], w), B.sjd_block_norm(x.repeat(6, 1), pre_gain=gain)[1]]
+    spaces = [torch.empty(nbytes, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    want = work(spaces[0])
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in spaces], []
+    for _ in range(5):
+        for stream, ws in zip(streams, spaces):
+            with torch.cuda.stream(stream):
+                got.append(work(ws))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for each in got for a, b in zip(each, want)) and pool.fault() == 0 and short.fault() == 0
