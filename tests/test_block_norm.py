@@ -155,6 +155,20 @@ def test_outputs_that_start_on_16_bytes(rows, d):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows,d", [(300000, 8192), (70000, 32768)])
+def test_rows_behind_four_gigabytes(rows, d):
+    """More than 2^31 numbers: the last rows are those of the first, repeated."""
+    g = torch.Generator(device="cuda").manual_seed(47)
+    part, w = torch.randn(1000, d, generator=g, device="cuda").bfloat16(), torch.randn(d, generator=g, device="cuda").bfloat16()
+    h = part.repeat(rows // 1000, 1)
+    _, z = B.sjd_block_norm(h, y=h, post_gain=w, pre_gain=w, h_out=h)
+    want, off = _norm(part[-50:].double(), torch.zeros(50, d, dtype=torch.float64, device="cuda"), w, None, False, 1e-5)
+    want, off = part[-50:].double() + want, off + E * (part[-50:].double().abs() + 2 * want.abs())
+    assert ((h[-50:].double() - want).abs() <= 1.01 * off + 2.0 ** -8 * want.abs() + 1e-37).all()
+    assert torch.equal(z[:1000], z[-1000:]) and torch.equal(h[:1000], h[-1000:])
+
+
+@pytest.mark.gpu
 def test_rows_do_not_touch_one_another():
     """A NaN or an infinity stays in its row; entries beside the rows stay as they are."""
     h = torch.randn(20, 648, device="cuda").bfloat16()

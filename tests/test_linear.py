@@ -181,6 +181,18 @@ def test_the_same_bits_every_time_in_a_graph_and_on_another_stream(rows, n, k, g
 
 
 @pytest.mark.gpu
+def test_outputs_behind_four_gigabytes():
+    """More than 2^31 numbers: rows from both ends beside a call of their own."""
+    g = torch.Generator(device="cuda").manual_seed(46)
+    x, w = torch.randn(66000, 64, generator=g, device="cuda").bfloat16(), (torch.randn(32768, 64, generator=g, device="cuda") / 8).bfloat16()
+    out = B.sjd_linear(x, w)
+    for rows in (slice(0, 100), slice(65500, 65600), slice(65950, 66000)):
+        v = x[rows].double() @ w.double().t()
+        off = _off(x[rows].double().abs() @ w.double().abs().t(), 64, v, "none")
+        assert ((out[rows].double() - v).abs() <= 1.001 * off + 2.0 ** -8 * v.abs() + 1e-37).all()
+
+
+@pytest.mark.gpu
 def test_no_rows():
     assert B.sjd_linear(torch.zeros(0, 64, device="cuda").bfloat16(), torch.zeros(8, 64, device="cuda").bfloat16()).shape == (0, 8)
 

@@ -424,6 +424,24 @@ def test_in_a_graph_on_another_stream_and_with_a_workspace_of_its_own():
 
 
 @pytest.mark.gpu
+def test_pages_behind_four_gigabytes():
+    groups = [(5, [500, 420, 390]), (2, [200, 300])]
+    pool, lens = _filled(groups, 8, 8, 128, 44)
+    q, at, begin = _queries(5 * 4, 16, 128, 45), _i32(_window_pos(lens, 4)), _begin(groups)
+    n, count = pool.pages.shape[0], 4400   # (a megabyte each)
+    pages = torch.zeros((count, *pool.pages.shape[1:]), dtype=torch.uint8, device="cuda")
+    exps = torch.zeros((count, *pool.exps.shape[1:]), dtype=torch.int8, device="cuda")
+    pages[count - n:], exps[count - n:] = pool.pages.view(torch.uint8).flip(0), pool.exps.flip(0)
+    refs = torch.zeros(count, dtype=torch.int32, device="cuda")
+    refs[count - n:] = pool.refs.flip(0)
+    far = B.CachePool(pages.view(torch.float8_e4m3fn), exps, torch.where(pool.table >= 0, count - 1 - pool.table, pool.table), refs)
+    for layer in (0, 7):
+        want = B.sjd_pool_attention_shared(pool, layer, q, at, 4, group_begin=begin)
+        assert torch.equal(B.sjd_pool_attention_shared(far, layer, q, at, 4, group_begin=begin), want)
+    assert pool.fault() == 0 and far.fault() == 0
+
+
+@pytest.mark.gpu
 def test_the_same_as_attention_of_every_sequence():
     """Beside sjd_pool_attention, whose weights have other roundings (2^-8 as well)."""
     groups = [(10, [900, 801, 1200, 700])]
