@@ -47,6 +47,7 @@ constexpr int kConv = 128, kSoft = 256, kThreads = kSoft + kConv + 96;
 constexpr int kPlanThreads = 1024;
 constexpr int kCosts = 1024;            // units of a kv head whose places the plan keeps in shared memory
 constexpr float kGrow = 8.0f;           // log2 of what a maximum may grow before its reference follows
+constexpr float kLeastFactor = 1.1754944e-38f;   // 2^-126
 
 struct Segment {       // keys k0 .. k1 - 1 of a sequence's table, for rows ra .. rb - 1 of a unit
   int seq, k0, k1, ra, rb, base;   // base: tiles of the unit's segments for the same streams before it
@@ -941,7 +942,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
         }
         sync();   // (the factors are there)
       }
-      const float factor = fmaxf(r < rows ? sh.factor[r >> 7][r & 127] : 0.0f, 1e-38f);   // (not zero: masked scores stay infinite)
+      const float factor = r < rows ? sh.factor[r >> 7][r & 127] : 0.0f;
       const bool warp_rows = quarter * 32 + (alone ? 0 : st * 128) < rows;   // this warp has any
       float m_ref = -INFINITY, l = 0.0f;
       bool nans = false;   // the row has seen some: sh.nan_row says which dims
@@ -986,7 +987,8 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
             };
             load(0);
             const float4 up = *reinterpret_cast<const float4 *>(&f.k_up[h * 4]);
-            const float by[4] = {factor * up.x, factor * up.y, factor * up.z, factor * up.w};   // of 16 columns
+            // of 16 columns; never zero: masked scores stay infinite (others, up to 2^24, are nothing with a factor this small)
+            const float by[4] = {fmaxf(factor * up.x, kLeastFactor), fmaxf(factor * up.y, kLeastFactor), fmaxf(factor * up.z, kLeastFactor), fmaxf(factor * up.w, kLeastFactor)};
             float top = -INFINITY;
 #pragma unroll
             for (int k = 0; k < 2; ++k) {

@@ -319,6 +319,26 @@ def test_exponents_of_any_size():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("heads,kvh,hd,window", [(2, 1, 64, 8), (8, 1, 128, 40)])
+@pytest.mark.parametrize("keys,behind,size,scale", [((-100, -100), None, 2.0 ** -60, 0.0), ((-128, -128), None, 1.3, 1e-20),
+                                                   ((-100, 0), None, 1.3, 1e-30), ((-24, -24), None, 1.3, 0.0), ((-8, -5), -128, 2.0 ** -60, 0.0), ((-8, -5), -100, 1.3, 1e-20)])
+def test_keys_queries_and_scales_of_any_size(heads, kvh, hd, window, keys, behind, size, scale):
+    """A factor of the scores may be as small as it likes, of keys that a row sees and of those that it does not: hidden ones stay hidden.  Rows at -1 hold the
+    smallest number that there is.  behind: exponents of the blocks behind a sequence."""
+    groups = [(2, [150, 330, 129, 200])]
+    pool, lens = _filled(groups, 1, kvh, hd, 48)
+    rng = np.random.default_rng(49)
+    pool.exps[:, :, 0] = torch.from_numpy(rng.integers(keys[0], keys[1] + 1, tuple(pool.exps[:, :, 0].shape)).astype(np.int8)).cuda()
+    if behind is not None:
+        for b, n in enumerate(lens):
+            if n % 64:
+                pool.exps[pool.table[b, n // 64].long(), :, 0, :, -(-n % 64 // 16):] = behind
+    q, at = _queries(len(lens) * window, heads, hd, 50, spread=size), _window_pos(lens, window, (window, window, 1, window - 3))
+    q[torch.tensor(at) < 0] = torch.tensor(1, dtype=torch.int16).view(torch.bfloat16).cuda()
+    _check(pool, q, at, window, _begin(groups), scale=scale)
+
+
+@pytest.mark.gpu
 def test_maxima_that_grow_from_tile_to_tile():
     """Scores that rise by far more than a reference may lag behind, and that fall."""
     groups = [(8, [1300, 1200])]
