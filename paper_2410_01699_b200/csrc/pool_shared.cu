@@ -48,6 +48,7 @@ constexpr int kPlanThreads = 1024;
 constexpr int kCosts = 1024;            // units of a kv head whose places the plan keeps in shared memory
 constexpr float kGrow = 8.0f;           // log2 of what a maximum may grow before its reference follows
 constexpr float kLeastFactor = 1.1754944e-38f;   // 2^-126
+constexpr float kCoarse = 67108864.0f;  // 2^26
 
 struct Segment {       // keys k0 .. k1 - 1 of a sequence's table, for rows ra .. rb - 1 of a unit
   int seq, k0, k1, ra, rb, base;   // base: tiles of the unit's segments for the same streams before it
@@ -372,6 +373,9 @@ __device__ __forceinline__ float exp2_fast(float x) {
 __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
   return *reinterpret_cast<const uint32_t *>(&v);
+}
+__device__ __forceinline__ float power_near(float v) {   // a power of two, 2/3 to 4/3 of v (normal and positive)
+  return __uint_as_float((__float_as_uint(v) + 0x400000u) & 0x7F800000u);
 }
 __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
   uint32_t r;
@@ -942,7 +946,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
         }
         sync();   // (the factors are there)
       }
-      const float factor = r < rows ? sh.factor[r >> 7][r & 127] : 0.0f;
+      float factor = r < rows ? sh.factor[r >> 7][r & 127] : 0.0f;
       const bool warp_rows = quarter * 32 + (alone ? 0 : st * 128) < rows;   // this warp has any
       float m_ref = -INFINITY, l = 0.0f;
       bool nans = false;   // the row has seen some: sh.nan_row says which dims
@@ -988,7 +992,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
             load(0);
             const float4 up = *reinterpret_cast<const float4 *>(&f.k_up[h * 4]);
             // of 16 columns; never zero: masked scores stay infinite (others, up to 2^24, are nothing with a factor this small)
-            const float by[4] = {fmaxf(factor * up.x, kLeastFactor), fmaxf(factor * up.y, kLeastFactor), fmaxf(factor * up.z, kLeastFactor), fmaxf(factor * up.w, kLeastFactor)};
+            float by[4] = {fmaxf(factor * up.x, kLeastFactor), fmaxf(factor * up.y, kLeastFactor), fmaxf(factor * up.z, kLeastFactor), fmaxf(factor * up.w, kLeastFactor)};
             float top = -INFINITY;
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
@@ -1007,6 +1011,24 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
             // Where a score has outgrown the reference, that, O and the sum follow.
             const bool need = r < rows && (top > m_ref + kGrow || (m_ref == -INFINITY && top > -INFINITY));
             if (__builtin_expect(__any_sync(0xffffffffu, need), 0)) {
+              // A weight's argument is the exact product less the reference, a rounded one, which is off from its own exact one by 4 at 2^26 and beyond what an exponential
+              // holds at 2^31. From 2^26 on the row's factor becomes a power of two: products are exact then. (Its scores are off by 2^7 and more as they are, and
+              // smaller differences, in which alone a factor of 2/3 to 4/3 could show, mean nothing.)
+              const bool coarse = need && fabsf(top) >= kCoarse && factor != power_near(factor);
+              if (__builtin_expect(__any_sync(0xffffffffu, coarse), 0)) {
+                if (coarse) m_ref *= power_near(factor) / factor, factor = power_near(factor), top = -INFINITY;
+#pragma unroll 1
+                for (int c = 0; c < 8; ++c) {
+                  uint32_t v[8];
+                  tmem_ld8(t_h + c * 8, v);
+                  tmem_ld_wait();
+#pragma unroll
+                  for (int j = 0; j < 8; ++j)
+                    if (coarse && c * 8 + j < n_seen) top = fmaxf(top, __uint_as_float(v[j]) * fmaxf(factor * f.k_up[h * 4 + c / 2], kLeastFactor));
+                }
+#pragma unroll
+                for (int c = 0; c < 4; ++c) by[c] = fmaxf(factor * f.k_up[h * 4 + c], kLeastFactor);
+              }
               const float g = need ? exp2_fast(m_ref - top) : 1.0f;
               m_ref = need ? top : m_ref;
               l *= g;
@@ -1094,6 +1116,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
         }
         tc_fence_after();
       }
+      if (const float asked = r < rows ? sh.factor[r >> 7][r & 127] : 0.0f; factor != asked) m_ref *= asked / factor;   // (in the unit that all parts have)
       const bool complete = s.i0 == 0 && s.i1 == tiles_of(s.en);
       const long row = part_row(p, s.e, s.h, s.i0 == 0, blockIdx.x);
       const int stride = padded(rows);

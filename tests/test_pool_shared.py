@@ -339,6 +339,18 @@ def test_keys_queries_and_scales_of_any_size(heads, kvh, hd, window, keys, behin
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("heads,kvh,hd,window", [(2, 1, 64, 8), (8, 1, 128, 40)])
+@pytest.mark.parametrize("keys", [(-100, 100), (14, 18), (24, 28), (30, 34), (90, 100)])
+def test_scores_that_32_bits_hold_without_fractions(heads, kvh, hd, window, keys):
+    """Scores of 2^25 and far more, where the key with the largest takes all of the weight (what is next to it is behind by more than scores are off)."""
+    groups = [(2, [150, 330, 129, 200])]
+    pool, lens = _filled(groups, 1, kvh, hd, 48)
+    rng = np.random.default_rng(49)
+    pool.exps[:, :, 0] = torch.from_numpy(rng.integers(keys[0], keys[1] + 1, tuple(pool.exps[:, :, 0].shape)).astype(np.int8)).cuda()
+    _check(pool, _queries(len(lens) * window, heads, hd, 50), _window_pos(lens, window, (window, window, 1, window - 3)), window, _begin(groups))
+
+
+@pytest.mark.gpu
 def test_maxima_that_grow_from_tile_to_tile():
     """Scores that rise by far more than a reference may lag behind, and that fall."""
     groups = [(8, [1300, 1200])]
