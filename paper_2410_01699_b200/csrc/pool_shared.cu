@@ -1012,11 +1012,12 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
             const bool need = r < rows && (top > m_ref + kGrow || (m_ref == -INFINITY && top > -INFINITY));
             if (__builtin_expect(__any_sync(0xffffffffu, need), 0)) {
               // A weight's argument is the exact product less the reference, a rounded one, which is off from its own exact one by 4 at 2^26 and beyond what an exponential
-              // holds at 2^31. From 2^26 on the row's factor becomes a power of two: products are exact then. (Its scores are off by 2^7 and more as they are, and
-              // smaller differences, in which alone a factor of 2/3 to 4/3 could show, mean nothing.)
-              const bool coarse = need && fabsf(top) >= kCoarse && factor != power_near(factor);
-              if (__builtin_expect(__any_sync(0xffffffffu, coarse), 0)) {
-                if (coarse) m_ref *= power_near(factor) / factor, factor = power_near(factor), top = -INFINITY;
+              // holds at 2^31. While it is 2^26 or more, or as far below zero, the row's factor is a power of two: products are exact then. (Its scores are off by 2^7 and more
+              // as they are, and smaller differences, in which alone a factor of 2/3 to 4/3 could show, mean nothing.)
+              const float asked = need ? sh.factor[r >> 7][r & 127] : factor, use = need && fabsf(top) >= kCoarse ? power_near(asked) : asked;
+              const bool other = factor != use;
+              if (__builtin_expect(__any_sync(0xffffffffu, other), 0)) {
+                if (other) m_ref *= use / factor, factor = use, top = -INFINITY;
 #pragma unroll 1
                 for (int c = 0; c < 8; ++c) {
                   uint32_t v[8];
@@ -1024,7 +1025,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
                   tmem_ld_wait();
 #pragma unroll
                   for (int j = 0; j < 8; ++j)
-                    if (coarse && c * 8 + j < n_seen) top = fmaxf(top, __uint_as_float(v[j]) * fmaxf(factor * f.k_up[h * 4 + c / 2], kLeastFactor));
+                    if (other && c * 8 + j < n_seen) top = fmaxf(top, __uint_as_float(v[j]) * fmaxf(factor * f.k_up[h * 4 + c / 2], kLeastFactor));
                 }
 #pragma unroll
                 for (int c = 0; c < 4; ++c) by[c] = fmaxf(factor * f.k_up[h * 4 + c], kLeastFactor);

@@ -351,6 +351,24 @@ def test_scores_that_32_bits_hold_without_fractions(heads, kvh, hd, window, keys
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("heads,kvh,hd,window", [(2, 1, 64, 8), (8, 1, 128, 40)])
+@pytest.mark.parametrize("far", [17, 30, 60])
+@pytest.mark.parametrize("pages", [[0, 1], [0], [1, 2], [3, 4], [0, 1, 2, 3, 4, 5]])
+def test_scores_far_below_zero_do_not_change_those_of_other_keys(heads, kvh, hd, window, far, pages):
+    """Some of the pages hold keys whose scores are -2^27 and far less: tiles of only such, or of such and others; at last all tiles."""
+    groups = [(3, [250, 330, 229, 300])]
+    pool, lens = _filled(groups, 1, kvh, hd, 51)
+    q, at = _queries(len(lens) * window, heads, hd, 52).abs(), _window_pos(lens, window, (window, window, 1, window - 3))
+    for page in pages:
+        of = pool.table[:, page][pool.table[:, page] >= 0].long()
+        raw = pool.pages.view(torch.uint8)[of, :, 0]
+        pool.pages.view(torch.uint8)[of, :, 0] = raw & 0x7F | 0x80
+        pool.exps[of, :, 0] = far
+    pool.pages.view(torch.uint8)[:, :, 0][(pool.pages.view(torch.uint8)[:, :, 0] & 0x7F) == 0x7F] = 0x10   # (behind the sequences)
+    _check(pool, q, at, window, _begin(groups))
+
+
+@pytest.mark.gpu
 def test_maxima_that_grow_from_tile_to_tile():
     """Scores that rise by far more than a reference may lag behind, and that fall."""
     groups = [(8, [1300, 1200])]
