@@ -44,11 +44,20 @@ struct LinearParams {
 
 template <int ACT>
 __device__ __forceinline__ float activate(float v) {
-  // (divisions and exponentials with errors of 2^-21: the result is rounded to 2^-9)
+  // Forms in which nothing cancels: 1 + erf and 1 + tanh of -5 have lost what bf16 holds.  The exponential is off by up to 2 + 1.2 |argument| units in the last place,
+  // 2^-16 at 87; from there on the quotient is 0, where v is left with less than 2^-119.  The result is rounded to 2^-9.
   if constexpr (ACT == SJD_ACT_RELU) return v < 0.0f ? 0.0f : v;   // (a NaN stays)
   if constexpr (ACT == SJD_ACT_SILU) return v * __fdividef(1.0f, 1.0f + __expf(-v));
-  if constexpr (ACT == SJD_ACT_GELU) return 0.5f * v * (1.0f + erff(v * 0.70710678f));
-  if constexpr (ACT == SJD_ACT_GELU_TANH) return 0.5f * v * (1.0f + tanhf(0.79788456f * fmaf(0.044715f * v * v, v, v)));
+  if constexpr (ACT == SJD_ACT_GELU) {
+    // half of erfc(|v| / sqrt(2)): t P(t) exp(-v^2 / 2), t = 1 / (1 + 0.55 |v| / sqrt(2)), P fitted for the least relative error, 2^-17.8.  (erfcf in its place, 1063 x 6144 x 4096:
+    // 48.9 us instead of 45.4)
+    const float t = __fdividef(1.0f, fmaf(0.388908744f, fabsf(v), 1.0f));
+    float q = fmaf(0.0494243689f, t, -0.15092659f);
+    q = fmaf(q, t, 0.0885907039f), q = fmaf(q, t, 0.0693082735f), q = fmaf(q, t, 0.133359432f), q = fmaf(q, t, 0.155093849f), q = fmaf(q, t, 0.155152082f);
+    q *= t * __expf(-0.5f * v * v);
+    return v * (v > 0.0f ? 1.0f - q : q);
+  }
+  if constexpr (ACT == SJD_ACT_GELU_TANH) return v * __fdividef(1.0f, 1.0f + __expf(-1.5957691f * fmaf(0.044715f * v * v, v, v)));   // (1 + tanh(u)) / 2 = 1 / (1 + exp(-2 u))
   return v;
 }
 template <int ACT>

@@ -112,6 +112,25 @@ def test_epilogues(rows, n, k, act, gated, bias, residual):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows", [3, 200])
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
+@pytest.mark.parametrize("gated", [False, True])
+def test_tails_of_activations(rows, act, gated):
+    """Sums that are exact (one product, by 1), where 1 + erf and 1 + tanh have cancelled: the error is the activation's own, relative to it.  Arguments of
+    the exponentials are up to 2 u = 87 with up to 8 roundings, 87 * 8 * 2^-24, and exponentials off by 2 + 1.2 * 87 units of 2^-23; in GELU the argument is v^2 / 2 = 50
+    and the rest of the complementary error function off by 2^-17; quotients and products 2^-18.  So 2^-14, and the output's rounding."""
+    v = torch.cat((torch.linspace(-10, -3, 701), torch.linspace(-3, 10, 400))).bfloat16().cuda()
+    x, w = torch.zeros(rows, 8, device="cuda").bfloat16(), torch.zeros(v.numel(), 8, device="cuda").bfloat16()
+    x[:, 3], w[:, 3] = 1, v
+    out = B.sjd_linear(x, w, w_up=torch.where(w == 0, w, torch.full_like(w, 1024.0)) if gated else None, act=ACTS[act])
+    e = v.double()
+    want = e * torch.special.erfc(-e * 0.5 ** 0.5) / 2 if act == "gelu" else _act(e, act)
+    want = want * torch.where(v == 0, 0.0, 1024.0) if gated else want
+    err = (out.double() - want).abs()
+    assert (err <= (2.0 ** -8 + 2.0 ** -14) * want.abs()).all(), "%.3g of it" % (err / want.abs().clamp(min=1e-300)).max()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("rows,n,k", [(1, 40, 24), (9, 100, 120), (70, 100, 120), (600, 300, 64)])
 def test_strides_and_in_place(rows, n, k):
     _check(rows, n, k, pad=3, out_pad=5, residual=True)
