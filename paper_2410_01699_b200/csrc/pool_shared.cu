@@ -169,8 +169,10 @@ __global__ void __launch_bounds__(kPlanThreads) shared_plan_kernel(const __grid_
       if (hi[b] < 0) continue;
       const int *ta = p.pool.table + (long)seq_of[leader[g]] * p.pool.pages_per_seq, *tb = p.pool.table + (long)seq_of[b] * p.pool.pages_per_seq;
       constexpr int U = 8;
-      for (int at = 0; at < *(volatile int *)&share[g]; at += 32 * U) {
-        const int end = *(volatile int *)&share[g];
+      for (int at = 0;; at += 32 * U) {
+        // (other warps lower it meanwhile: one lane looks, and all go by what it saw)
+        const int end = __shfl_sync(0xffffffffu, lane == 0 ? *(volatile int *)&share[g] : 0, 0);
+        if (at >= end) break;
         int x[U], y[U], least = 0x7FFFFFFF;
 #pragma unroll
         for (int j = 0; j < U; ++j) {

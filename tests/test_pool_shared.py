@@ -226,6 +226,23 @@ def test_sequences_of_a_group_that_share_less_or_nothing(hd):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("least", [3, 40])
+def test_many_sequences_that_part_at_pages_of_their_own(least):
+    """Hundreds of a group, more than warps that compare their tables: what they share is lowered by many at a time.  Nothing depends on which comes first."""
+    groups = [(44, [44 * 64 + 1 + 7 * i % 90 for i in range(300)]), (44, [44 * 64 + 3 + 5 * i % 70 for i in range(40)])]
+    pool, lens = _filled(groups, 1, 1, 64, 53, spare=700)
+    rng, own = np.random.default_rng(54), torch.nonzero(pool.refs == 0)[:, 0].to(torch.int32)
+    where = rng.integers(least, 44, len(lens))
+    where[0], where[-1] = 43, least
+    pool.table[torch.arange(len(lens)), torch.from_numpy(where)] = own[:len(lens)]   # (pages with other contents)
+    q, at = _queries(len(lens), 2, 64, 55), _window_pos(lens, 1)
+    a = _check(pool, q, at, 1, _begin(groups))
+    for _ in range(10):
+        assert torch.equal(a, B.sjd_pool_attention_shared(pool, 0, q, _i32(at), 1, group_begin=_begin(groups)))
+    assert pool.fault() == 0
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("heads,kvh,hd,window", [(2, 1, 128, 9), (4, 4, 64, 40), (8, 1, 128, 40)])
 def test_rows_and_sequences_that_see_nothing(heads, kvh, hd, window):
     groups = [(3, [200, 260, 300, 250]), (2, [150, 0, 170]), (0, [0, 0])]
