@@ -866,7 +866,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
         fail();
       }
       q_ph ^= 1u;
-      // ---- queries of the unit's rows: a power of two brings a row's largest entry to 128 .. 256, then its two numbers; a row is HD / 4 lanes
+      // ---- queries of the unit's rows: a power of two brings a row's largest entry to 128 .. 256, then its two numbers; a row is HD / 8 lanes
       {
         constexpr int LANES = HD / 8, PER = 32 / LANES, U = 4, STEP = kSoft / 32 * PER;   // lanes of a row, rows of a warp's load, loads under way, rows between them
         const int sub = lane / LANES, dim = lane % LANES * 8;
@@ -1149,7 +1149,9 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
 #pragma unroll
           for (int j = 0; j < HD / 32; ++j) sh.nan_row[st][r_in][j] = 0;
         }
+        tc_fence_before();
         sync();
+        tc_fence_after();   // (the other stream's products, which its warps have waited for)
         second = s.i1 - s.i0 > 1;
         a = sh.stat[0][r_in];
         if (second) b = sh.stat[1][r_in];

@@ -266,6 +266,18 @@ def test_long_sequences_are_spread_over_the_device(window, heads, kvh, hd, group
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("window,groups", [(1, [(5, [400, 390])]), (8, [(9, [700, 641])]), (8, [(9, [700, 641]), (2, [300, 290])]), (16, [(20, [1400, 1390])])])
+def test_units_whose_rows_both_streams_have(hd, window, groups):
+    """Up to 128 rows: every other tile is a stream's, and each reads the sums of both.  (The last case has more rows: beside them.)"""
+    pool, lens = _filled(groups, 1, 2, hd, 56)
+    q, at, begin = _queries(len(lens) * window, 16, hd, 57), _window_pos(lens, window), _begin(groups)
+    a = _check(pool, q, at, window, begin)
+    for _ in range(20):
+        assert torch.equal(a, B.sjd_pool_attention_shared(pool, 0, q, _i32(at), window, group_begin=begin))
+
+
+@pytest.mark.gpu
 def test_many_sequences():
     """1024 sequences in groups of 1 to 40, more units than places kept in shared memory."""
     rng, groups, left = np.random.default_rng(13), [], 1024
