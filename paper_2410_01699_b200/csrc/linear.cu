@@ -165,7 +165,6 @@ __global__ void __launch_bounds__(64 + 128 * CG, CG == 1 ? 2 : 1)
   const int stage_bytes = kWBytes + x_rows * kTileK * 2;
   const int kb0 = (int)((long)split * p.k_blocks / p.splits), kb1 = (int)((long)(split + 1) * p.k_blocks / p.splits);
   const uint32_t cols = tmem_columns(p.tokens), smem0 = smem_u32(smem);
-  pdl_trigger();
   if (tid == 0) {
     tma_prefetch_desc(&w_map);
     tma_prefetch_desc(&x_map);
@@ -181,6 +180,7 @@ __global__ void __launch_bounds__(64 + 128 * CG, CG == 1 ? 2 : 1)
   tc_fence_before();
   cluster_sync();   // (barriers of a pair's other CTA)
   tc_fence_after();
+  pdl_trigger();   // (not before the allocation: a CTA of a later kernel that holds tensor memory waits for this one)
   const uint32_t tmem = s_tmem;
   pdl_wait();
 
@@ -330,7 +330,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTilesThreads, 1)
   const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1, x_rows = p.tokens / 2;
   const int stage_bytes = kWBytes + x_rows * kTileK * 2;
   const uint32_t cols = tmem_columns(2 * p.tokens), smem0 = smem_u32(smem);
-  pdl_trigger();
   if (tid == 0) {
     tma_prefetch_desc(&w_map);
     tma_prefetch_desc(&x_map);
@@ -349,6 +348,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTilesThreads, 1)
   tc_fence_before();
   cluster_sync();
   tc_fence_after();
+  pdl_trigger();   // (not before the allocation: a CTA of a later kernel that holds tensor memory waits for this one)
   const uint32_t tmem = s_tmem;
   pdl_wait();
 

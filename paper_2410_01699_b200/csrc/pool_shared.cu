@@ -468,7 +468,6 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
   SharedSmem<HD> &sh = *reinterpret_cast<SharedSmem<HD> *>(Vs + 4 * OP);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, kv_heads = p.pool.n_kv_heads;
   constexpr int ISSUE = (kSoft + kConv) / 32, COPY = ISSUE + 2;   // (a warp issues the products of a stream)
-  pdl_trigger();
   if (tid == 0) {
     for (int i = 0; i < kKStages; ++i) {
       mbar_init(&sh.k_full[i], 1);
@@ -501,6 +500,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  pdl_trigger();   // (not before the allocation: a CTA of a later kernel that holds tensor memory waits for this one)
   const uint32_t tmem = sh.tmem_base;
   const long chunk = range_of(all, gridDim.x);
   const int places = (int)max(0l, min(chunk, all - blockIdx.x * chunk));   // of this CTA
