@@ -357,13 +357,15 @@ class CachePool:
 
     def shared_ws(self, batch, window, heads):
         """The pool's workspace for attention over shared pages: the last of those so far if it is large enough for such a call, else another
-        one (the others stay: a captured graph keeps the address that it was given)."""
+        one (the others stay: a captured graph keeps the address that it was given).  Each is at least twice the one before, so that all of them
+        are less than four times what the largest call needs."""
         nbytes = self._shared_bytes.get((batch, window, heads))
         if nbytes is None:
             nbytes = int(lib().sjd_pool_attention_shared_workspace_bytes(self.ref, batch, window, heads))
             self._shared_bytes[batch, window, heads] = nbytes
-        if not self._shared_ws or self._shared_ws[-1].nbytes < nbytes:
-            self._shared_ws.append(torch.empty(max(nbytes, 1), dtype=torch.uint8, device=self.device))
+        have = self._shared_ws[-1].nbytes if self._shared_ws else 0
+        if have < max(nbytes, 1):
+            self._shared_ws.append(torch.empty(max(nbytes, 2 * have, 1), dtype=torch.uint8, device=self.device))
         return self._shared_ws[-1]
 
     def fault(self) -> int:

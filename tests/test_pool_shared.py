@@ -44,6 +44,20 @@ def test_workspace_size_query():
     assert size(0, 1, 2) == size(1, 0, 2) == size(1, 1, 3) == size(1025, 1, 2) == size(1024, 1 << 20, 2) == 0
 
 
+def test_workspaces_of_a_pool_whose_calls_grow():
+    """Those that were too small stay, for graphs that hold them, but do not add up."""
+    pool = B.CachePool.empty(4, 2, 4, 1, 2, 64, device="cpu")
+    need, kept = [], []
+    for batch in range(1, 400):
+        need.append(int(B.lib().sjd_pool_attention_shared_workspace_bytes(pool.ref, batch, 40, 16)))
+        ws = pool.shared_ws(batch, 40, 16)
+        kept += [ws] if not kept or ws is not kept[-1] else []
+        assert ws.nbytes >= need[-1]
+    assert need[-1] > 2 * need[0] and len(kept) <= 4 and all(a is b for a, b in zip(pool._shared_ws, kept))
+    assert sum(x.nbytes for x in pool._shared_ws) < 4 * need[-1]
+    assert pool.shared_ws(1, 40, 16) is kept[-1] and pool.shared_ws(399, 40, 16) is kept[-1]
+
+
 # ------------------------------------------------------------------------------------------- which kernel a call comes to
 def _each_for_itself(calls):
     """The library's rule (csrc/pool_route.h) for calls (batch, window, kv_heads, rows, pages_per_seq, alone, sms)."""
