@@ -339,7 +339,7 @@ int sjd_attention(int batch, int window, int n_heads, int n_kv_heads, int head_d
  * Null: post_gain (no norm after the block), either bias (0), gate (1), pre_gain with z (no norm after the residual), y with h_out (z is the
  * norm of h; then no post_gain and no gate).  y, gains and biases [d], gate [.][d], z are of dtype, h and h_out of h_dtype, SJD_F32 or SJD_BF16
  * each; rows are *_stride elements apart.  All arithmetic is in 32 bits, rounded once for each output; z is of h_out before it is rounded.
- * h_out may be h and z may be y (same stride); no other overlap.  d <= 32768.  Where d and the strides are multiples of 8 and all
+ * y may be h, h_out may be h, z may be y (same strides; the two outputs apart); no other overlap.  d <= 32768.  Where d and the strides are multiples of 8 and all
  * addresses of 16 bytes, rows are read and written in vectors.  rows 0: nothing.
  * Errors: BAD_ARG (also an address that is not a multiple of its type's size), UNSUPPORTED (types, kind, d), CUDA.
  */

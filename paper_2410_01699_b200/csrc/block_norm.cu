@@ -3,7 +3,8 @@
 //
 // A row is a block's (a warp's, up to 1024 entries): its entries stay in registers between the sums, which are in 32 bits; the mean goes
 // off before the squares are summed (squares of the entries less the mean's square would lose what a large mean leaves of them).  z is
-// taken of h' before that is rounded to its type.  A thread has N vectors of VEC entries, T threads apart.
+// taken of h' before that is rounded to its type.  A thread has N vectors of VEC entries, T threads apart.  A row's
+// entries are read by the thread that writes them, before it does: that is why outputs may lie where inputs do.
 //
 // Few rows are bound by the launch and two or four round trips (256 rows of 4096, gate and residual: 10.6 us).  Many are bound by the bytes, and where
 // a block has one row at a time, by what it waits for between fetching a row and writing it: those of block_norm_rows_kernel keep the

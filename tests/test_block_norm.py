@@ -143,6 +143,22 @@ def test_many_rows_in_place(rows, d):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows,d", [(5, 200), (5, 203), (7, 1000), (9, 683), (9, 2048), (600, 8192), (9, 10007), (9, 16384), (9, 32768), (6001, 512), (700, 4096)])
+@pytest.mark.parametrize("dtype", list(DT))
+def test_a_block_whose_output_is_the_residual_stream_itself(rows, d, dtype):
+    """y is h, and both outputs go where it was, one of them each time: rows of warps and of blocks, in vectors and one by one, and rows fetched ahead."""
+    g = torch.Generator(device="cuda").manual_seed(d)
+    h, w = torch.randn(rows, d, generator=g, device="cuda").to(DT[dtype]), torch.randn(d, generator=g, device="cuda").to(DT[dtype])
+    kw = dict(post_gain=w, pre_gain=w, kind=B.SJD_NORM_LAYER, scale=0.5)
+    a, b = B.sjd_block_norm(h, y=h.clone(), **kw)
+    x, y = h.clone(), h.clone()
+    _, z = B.sjd_block_norm(x, y=x, h_out=x, **kw)
+    assert torch.equal(x, a) and torch.equal(z, b)
+    out, _ = B.sjd_block_norm(y, y=y, z=y, **kw)
+    assert torch.equal(out, a) and torch.equal(y, b)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("rows,d", [(9, 264), (9, 2048), (3000, 1024)])
 def test_outputs_that_start_on_16_bytes(rows, d):
     g = torch.Generator(device="cuda").manual_seed(d)
