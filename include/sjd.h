@@ -455,8 +455,10 @@ int sjd_pool_attention(const sjd_pool *pool, int layer, int batch, int window, i
  * a sliding window, for bf16 queries, but the pages that the tables of a group's sequences begin with, as far as they lie before all of the group's rows,
  * are read and multiplied once for all of its rows.  Group g is the sequences b = group_begin[g] .. group_begin[g + 1] - 1 of the call (device
  * int32, n_groups + 1 entries that rise from 0 to batch; null: one group of all; n_groups is not read then).  What a group really shares is found in the tables: sequences
- * that share nothing are only attended one by one.  Where nothing could be won (tables too short for the call's size, or as many groups as sequences and
- * few rows), sjd_pool_attention's kernel takes the call, and group_begin is not read.  out may not overlap q.  Scores and sums are held in 32 bits; a weight is rounded as in
+ * that share nothing are only attended one by one, which takes longer than sjd_pool_attention where they have few rows (32 tokens 2.4 times as long): a batch that shares nothing is
+ * better told as groups of one, or given to that.  What a group shares ends where the first of its sequences parts.  Where nothing could be won (tables too short for the call's size, or
+ * as many groups as sequences and few rows), sjd_pool_attention's kernel takes the call, and group_begin is not read.  That goes by the width of the tables, pages_per_seq, and so do
+ * the roundings: the same call may give other bits in a pool with other tables.  out may not overlap q.  Scores and sums are held in 32 bits; a weight is rounded as in
  * sjd_pool_attention or by up to 2^-8 of itself.  What rows behind a sequence or masked places hold (NaN included) does not matter; a visible NaN shows.
  * status: as sjd_pool_attention; BAD_ARG for a group_begin that is not as above (no pages are shared then).
  * ws: device scratch of sjd_pool_attention_shared_workspace_bytes(...) bytes, 256-byte aligned, contents without meaning between calls; one

@@ -10,9 +10,9 @@
 // Many rows (linear_tiles_kernel): the time is that of the products, or of the operands from L2.  CTA pairs with 256 features by up to 256
 // tokens, persistent, two accumulators, so that a unit's epilogue runs under the next unit's products.
 //
-// Measured (bf16, in brackets a library's product of the same sizes, without an epilogue; replayed from a graph): 1 x 4096 x 4096 9.1 us (13.3), 64 x 4096 x 4096
-// 11.2 (9.5), 32 x 14336 x 4096 with U 41.6 (38.5, 36.6 are the bytes: 90 %), 256 x 4096 x 11008 26.7 (24.2), 1063 x 6144 x 4096 40 to 41 (38), 4223 x 14336 x 4096
-// with U 632 to 655 (624 to 673; 1500 TFLOP/s).  With four epilogue warps instead of sixteen 4223 x 1408 x 512 with U took 52 us, now 31; with the
+// Measured (bf16, in brackets a library's product of the same sizes, or two of them for U, without an epilogue; 20 calls with the same operands replayed from a graph, so that up
+// to 100 MB of them stay in L2): 1 x 4096 x 4096 7.4 us (12.6), 64 x 4096 x 4096 9.4 (7.6), 32 x 14336 x 4096 with U 40.9 (42.2; 36.6 are the bytes: 90 %), 256 x 4096 x 11008 28 to
+// 30 (23.3), 1063 x 6144 x 4096 41.3 (38.0), 4223 x 14336 x 4096 with U 650 to 660 (645 to 655; 1500 TFLOP/s).  With four epilogue warps instead of sixteen 4223 x 1408 x 512 with U took 52 us, now 31; with the
 // sums of ranges read a number at a time, in more clusters than the device holds at once, 256 x 4096 x 11008 took 64.
 #include <algorithm>
 #include <atomic>

@@ -34,6 +34,8 @@ inline bool pool_equal_ranges(int64_t entries, int64_t kv_heads, int64_t positio
 // busy for more than 24 us, it is faster whatever is shared (54 calls of 2 to 32 sequences, 208 to 2128 positions: 43 are its own by this
 // rule, 5 to 30 us faster each; of the others it would be faster in three, by up to 5).  Sequences that are alone meet tiles of 128 rows in the other kernel, 1.8 us for up to 128 of them: up to 64 rows
 // this one is faster (16 sequences of 4096 positions, 32 heads: 16 rows 97 us against 241, 32 rows 144 and 211, 64 rows 229 and 226, 128 rows 428 and 243).
+// All of these had tables as wide as their longest sequence.  The width is what the host knows, and a short call of a pool with wide tables is not left to the other kernel by it: two
+// tokens of 217 positions take 9.7 us with tables of 4 pages, and 19.3 with tables of 16,384, where that would take 12.2.
 inline bool pool_each_for_itself(int64_t batch, int64_t window, int64_t kv_heads, int64_t rows, int64_t pages_per_seq, bool alone, int64_t sms) {
   const int64_t tile = rows <= 16 ? 16 : rows <= 32 ? 32 : 64, quarters = rows <= 16 ? 3 : rows <= 32 ? 5 : 8;   // (quarters of a us)
   const int64_t entries = batch * ((rows + tile - 1) / tile), table = (pages_per_seq * SJD_KV_PAGE + kTile - 1) / kTile;

@@ -20,11 +20,12 @@
 // Three launches: a plan (positions, what tables share, the line of units), the tiles, the joining of parts.  The line of all units' tiles is cut into
 // equal ranges, a CTA each; a unit that is within one is written by its CTA, the parts of the others are joined in the order of the ranges.
 //
-// What bounds it (32 heads of 128): the softmax.  A tile of 128 keys for both streams takes 2.8 us, where its exponentials alone would take 1.07 by their rate.
+// What bounds it (32 heads of 128): the softmax.  A tile of 128 keys for both streams takes 3.0 us (2.9 before a row's factor could change, which is 1 to 2 % of a call),
+// where its exponentials alone would take 1.07 by their rate.
 // Left out one at a time, the exponentials take 0.8 us with them, half of the maxima 0.2, the turning of the values 0.13, the second numbers of the
 // queries 0.04; without a softmax at all the two products and their barriers take 1.8.  Two softmax warps share a scheduler, 43 % of its slots are used.
-// Slower: 16 softmax warps with 88 registers; 64 scores at once (3.0 us); one pass under the reference that there is, with the maxima behind it (3.4 to
-// 3.6: more of a row is held at a time, and what is laid aside is far away, for shared memory leaves the cache little room).  Around the tiles 40 to 45 us
+// Slower: 16 softmax warps with 88 registers; 64 scores at once (by 0.2 us a tile); one pass under the reference that there is, with the maxima behind it (by 0.6 to
+// 0.8: more of a row is held at a time, and what is laid aside is far away, for shared memory leaves the cache little room).  Around the tiles 40 to 45 us
 // stay the same for any lengths: the plan 7 to 12, queries and first copies 7 to 8, parts 3 to 4, the longest range 6 to 10 beyond the mean, the joining
 // launch 11 to 13.
 #include "pool_route.h"
@@ -41,7 +42,7 @@ constexpr int kLeast = 2;               // common pages that are worth a tile of
 constexpr int kMaxCtas = 192;
 constexpr int kMaxSeqs = SJD_POOL_MAX_LIST;
 constexpr int kSegs = 128;              // segments of a unit that are kept there
-constexpr int kInfo = 8;                // tiles whose notes are kept: more than copies are ahead of weights
+constexpr int kInfo = 8;                // tiles whose notes are kept: more than copies are ahead of weights (five would do by tests/test_pool_shared_barriers.py)
 constexpr int kKStages = 3;
 constexpr int kConv = 128, kSoft = 256, kThreads = kSoft + kConv + 96;
 constexpr int kPlanThreads = 1024;
@@ -770,7 +771,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
       if (lane == 0) arrive(&sh.q_seen);
       const uint64_t desc_q = rows_desc<HD>() | (uint64_t)((smem_u32(Qs) + (one_stream(s.en.rows) ? 0 : st * 2 * OP)) >> 4);
       // Scores of the halves of the own tiles before `end`, each when the weights in its columns have been multiplied.  (No further than two tiles ahead
-      // of the values: what the copies wait for is let go of there.)
+      // of the values: what the copies wait for is let go of there.  Three meet parities that have come round: tests/test_pool_shared_barriers.py.)
       int i = s.i0;
       bool half = false, open0 = false, open1 = false;   // the first half of tile i has its scores; weights that have not been multiplied
       auto products = [&](int h) {
@@ -981,7 +982,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
           }
           if (__any_sync(0xffffffffu, n_seen > 0)) {
             // 32 scores at a time, the first of them twice: more do not fit beside the rest of the registers, and what the compiler lays aside is far away (shared
-            // memory leaves the cache little room: with 64 at once, 136 bytes laid aside, a tile of two streams took 3.0 us)
+            // memory leaves the cache little room: with 64 at once, 136 bytes laid aside, a tile of two streams took 0.2 us more)
             const bool all = __all_sync(0xffffffffu, n_seen == 64 || r >= rows);
             uint32_t x[32];
             auto load = [&](int k) { tmem_ld32(t_h + k * 32, x); };
@@ -1199,8 +1200,8 @@ __global__ void __launch_bounds__(kThreads, 1) shared_tiles_kernel(const __grid_
 }
 
 // ---------------------------------------------------------------------------------------------------------------- joining
-// Eight rows of a unit that is cut a block: lane = row + 8 * (dims / 4 % 4), every kJoinWarps-th of the parts a warp.  (Two parts' loads at a time take 125 registers
-// instead of 76: a call of 64 units 61.2 us against 58.7, one of 8 units of 19 parts each the same; with 2 warps the latter takes 105 instead of 98, with 8 the former 68.)
+// Eight rows of a unit that is cut a block: lane = row + 8 * (dims / 4 % 4), every kJoinWarps-th of the parts a warp.  96 registers of a thread for 128 dims, 72 for 64.  (Two
+// parts' loads at a time: a call of 64 units 61.2 us against 58.7, one of 8 units of 19 parts each the same; with 2 warps the latter takes 105 instead of 98, with 8 the former 68.)
 constexpr int kJoinWarps = 4;
 template <int HD>
 __global__ void __launch_bounds__(kJoinWarps * 32) shared_join_kernel(const __grid_constant__ SharedParams p) {
